@@ -59,6 +59,7 @@ typedef enum {
 #define DS_DEV_INDEX 1u   /* an entry of idx (or of a sequence list) was out of range and was clamped, or idx was not
                              strictly ascending (its rows are then fetched one by one, in the order given) */
 #define DS_DEV_TIMEOUT 2u /* a bounded mbarrier wait expired; outputs of that CTA are invalid */
+#define DS_DEV_PAGES 4u   /* ds_page_update only: a sequence was refused its new rows (no free page, no room in the row arrays) */
 
 typedef enum { DS_F32 = 0, DS_BF16 = 1 } ds_dtype;
 
@@ -395,6 +396,189 @@ typedef struct {
 
 /* `p` is a HOST pointer; the pointers inside it are device pointers. */
 DS_API int ds_block_begin(const ds_block_params *p, void *stream);
+
+/* ------------------------------------------------------------------------
+ * The paged key/value cache (no counterpart in the paper, whose prefix cache
+ * is one dense buffer with one length for the batch): sequences of different
+ * lengths share a pool of pages.
+ *   ds_page_update   block tables and slot maps, from the lengths, on the GPU
+ *   ds_qk_norm_rope  per-head norm + rotary position, K/V into the pages
+ *   ds_attn_paged    attention of the new rows over the pages
+ *
+ * A page holds page_size rows of every KV head.  block_table[b][j] is the page
+ * that holds rows j * page_size .. of sequence b; the slot of a row is
+ * page * page_size + row % page_size.  The caches are described by element
+ * strides for page, head and row, so [pages][Hkv][page_size][D] and
+ * [pages][page_size][Hkv][D] (and slices of either) are both served.  New rows
+ * of all sequences are packed: row_start[b] .. row_start[b + 1] - 1 are those
+ * of sequence b.  Lengths, tables and row numbers live on the device.
+ * ------------------------------------------------------------------------ */
+
+/* ds_page_update: one step's bookkeeping.  With ps = page_size, pages(n) = ceil(n / ps), F = *free_cnt:
+ *   1. the pages of the sequences with done[b] != 0 go back to the pool, in sequence and table order:
+ *      free_list[F ..] = block_table[b][0 .. pages(kv_len[b]) - 1]; F' = F + their number; old_b = 0.
+ *      For the others old_b = kv_len[b].
+ *   2. need_b = pages(old_b + n_new[b]) - pages(old_b).  A sequence gets all of its n_new[b] rows or none: it is
+ *      refused when need_b > 0 and need_0 + .. + need_b > F', or n_new[b] > 0 and n_new[0] + .. + n_new[b] > max_rows.
+ *      (So from the first sequence on that the pool cannot serve, only those that need no page are served.)
+ *      A refusal raises DS_DEV_PAGES.
+ *   3. pages are taken from the top of the pool: the k-th page handed out (k = 0, 1, ..: sequence order, then
+ *      table order) is free_list[F' - 1 - k]; block_table[b][pages(old_b) ..] = the pages of sequence b.
+ *   4. kv_len_out[b] = old_b + rows granted, *free_cnt_out = F' - pages handed out, row_start[0 .. B] = exclusive
+ *      sum of the rows granted; for the i-th new row of sequence b, r = row_start[b] + i:
+ *      positions[r] = old_b + i, slot_map[r] = its slot.  Rows r >= row_start[B]: positions 0, slot_map -1.
+ * kv_len_out may be kv_len and free_cnt_out may be free_cnt; no other two arguments may overlap.  Entries of
+ * block_table and free_list that the rules do not name are left as they are.
+ * A length or count that is negative, and a length or request beyond max_pages pages, raise DS_DEV_INDEX: the length
+ * is clamped to 0 .. max_pages * ps, the request counts as 0 rows.  A page number outside [0, n_pages) raises
+ * DS_DEV_INDEX; it is copied as it is and rows in such a page get slot -1.  A *free_cnt outside [0, n_pages], or more
+ * returned pages than the list has room for, raises DS_DEV_INDEX; the count is clamped and the surplus pages are lost.
+ * Errors: DS_ERR_INVALID_ARG (NULL pointer, misaligned pointer, B, max_rows < 0, page_size, max_pages, n_pages < 1,
+ * table_stride < max_pages); DS_ERR_UNSUPPORTED (B > 8192, max_pages * page_size or n_pages * page_size > 2^31 - 1). */
+typedef struct {
+  int32_t B;
+  int32_t page_size;
+  int32_t max_pages;            /* columns of block_table */
+  int32_t n_pages;              /* pages in the pool */
+  int32_t max_rows;             /* length of positions / slot_map, and the most new rows of one call */
+  const int32_t *kv_len;        /* [B] rows each sequence holds */
+  const int32_t *n_new;         /* [B] rows each sequence adds */
+  const uint8_t *done;          /* optional [B] (e.g. eos_exit of finished sequences): give the pages back first */
+  int32_t *block_table;         /* [B][max_pages] in/out */
+  int64_t table_stride;         /* elements, >= max_pages */
+  int32_t *free_list;           /* [n_pages] in/out, the first *free_cnt entries are the free pages */
+  const int32_t *free_cnt;      /* [1] */
+  int32_t *kv_len_out;          /* [B] */
+  int32_t *free_cnt_out;        /* [1] */
+  int32_t *row_start;           /* [B + 1] out */
+  int32_t *positions;           /* optional [max_rows] out */
+  int64_t *slot_map;            /* optional [max_rows] out */
+  uint32_t *status;             /* optional device word */
+} ds_page_params;
+
+/* `p` is a HOST pointer; the pointers inside it are device pointers. */
+DS_API int ds_page_update(const ds_page_params *p, void *stream);
+
+/* Rotary frequencies, worked out once by ds_rope_table_init (HOST, pure) and passed by value with every call.
+ * Pair d of the rotary_dim / 2 pairs turns by f_d radians per position, f_d = theta^(-2d / rotary_dim) scaled as
+ * `scaling` says:
+ *   DS_ROPE_NONE    f_d
+ *   DS_ROPE_LINEAR  f_d / factor                                                        (position interpolation)
+ *   DS_ROPE_NTK     theta * factor^(rotary_dim / (rotary_dim - 2)) in place of theta
+ *   DS_ROPE_YARN    f_d (1 - r_d) + f_d / factor r_d, r_d = clamp((d - lo) / max(hi - lo, 1e-3), 0, 1),
+ *                   lo = max(floor(c(beta_fast)), 0), hi = min(ceil(c(beta_slow)), rotary_dim - 1),
+ *                   c(t) = rotary_dim ln(orig_len / (2 pi t)) / (2 ln theta): pairs that turn more than beta_fast
+ *                   times in the orig_len positions of the original context keep their frequency, those that turn
+ *                   less than beta_slow times are slowed by factor (Peng et al., "YaRN", 2023); the rotated values
+ *                   are multiplied by 0.1 ln(factor) + 1 when factor > 1
+ * turn[d] is f_d / 2 pi modulo 1 as a 64-bit binary fraction, so that position * turn, in integers modulo 2^64, is
+ * the exact phase for every 32-bit position.  Pairs are (d, d + rotary_dim / 2), or (2d, 2d + 1) when interleaved.
+ * Errors: DS_ERR_INVALID_ARG (NULL, rotary_dim < 2 or odd, theta <= 1, an unknown scaling, factor not a positive
+ * number, and with DS_ROPE_YARN orig_len < 1 or not 0 < beta_slow < beta_fast), DS_ERR_UNSUPPORTED (rotary_dim > 256
+ * or not a multiple of 16). */
+typedef enum { DS_ROPE_NONE = 0, DS_ROPE_LINEAR = 1, DS_ROPE_NTK = 2, DS_ROPE_YARN = 3 } ds_rope_scaling;
+typedef struct {
+  int32_t rotary_dim;
+  int32_t interleaved;
+  float mscale;                 /* factor on the rotated values */
+  int32_t reserved;
+  uint64_t turn[128];
+} ds_rope_table;
+DS_API int ds_rope_table_init(ds_rope_table *t, int32_t rotary_dim, int32_t interleaved, double theta, int32_t scaling,
+                       double factor, double orig_len, double beta_fast, double beta_slow);
+
+/* ds_qk_norm_rope: for every packed row n (position positions[n], slot s = slot_map[n]) and head
+ *     y    = w .* x * rsqrt(mean(x^2) + eps)        (q with q_weight, k with k_weight; y = x where the weight is NULL)
+ *     z    = y with its first rope.rotary_dim dimensions rotated by the row's position
+ *     q_out[n][h] = z(q);  k_out[n][g] = z(k), v_out[n][g] = v;  k_cache[slot s][g] = z(k), v_cache[slot s][g] = v
+ * in fp32, rounded once to the element type.  k_out/v_out and k_cache/v_cache are optional pairs; q_out, k_out and
+ * v_out may be q, k and v themselves (same strides), other overlaps are not allowed.  Rows n >= *n_rows (optional
+ * device scalar, clamped to [0, N]) are left as they are; a row whose slot is -1 is not written to the cache.
+ * A slot outside [0, n_pages * page_size) other than -1 raises DS_DEV_INDEX and is not written.  The slots of one
+ * call must differ from one another.
+ *
+ * Layout: element strides for row and head (cache: page, head, row), D contiguous; bases 16-byte aligned and strides
+ * multiples of 16 bytes.  Types: DS_F32, DS_BF16.  Errors: DS_ERR_INVALID_ARG; DS_ERR_UNSUPPORTED (D > 256 or not a
+ * multiple of 8, rotary_dim > D). */
+typedef struct {
+  int32_t N;                    /* rows of the packed arrays */
+  int32_t Hq, Hkv, D;
+  int32_t dtype;
+  int32_t page_size, n_pages;   /* used with a cache */
+  float eps;
+  const int32_t *n_rows;        /* optional device scalar, e.g. row_start + B */
+  const void *q;                /* [N][Hq][D] */
+  const void *k, *v;            /* [N][Hkv][D] */
+  int64_t q_stride[2], kv_stride[2];
+  const void *q_weight, *k_weight; /* optional [D], element type */
+  const int32_t *positions;     /* [N] */
+  const ds_rope_table *rope;    /* HOST */
+  void *q_out;                  /* [N][Hq][D] */
+  void *k_out, *v_out;          /* optional [N][Hkv][D] */
+  int64_t q_out_stride[2], kv_out_stride[2];
+  void *k_cache, *v_cache;      /* optional */
+  int64_t cache_stride[3];      /* page, head, row */
+  const int64_t *slot_map;      /* [N], needed with a cache */
+  uint32_t *status;             /* optional device word */
+} ds_qk_params;
+
+/* `p` is a HOST pointer; the pointers inside it, apart from rope, are device pointers. */
+DS_API int ds_qk_norm_rope(const ds_qk_params *p, void *stream);
+
+/* ds_attn_paged: sequence b has L = kv_len[b] rows in the cache, its n_b = row_start[b + 1] - row_start[b] query rows
+ * among them (they are the last n_b; append first, attend then).  With row_start == NULL every sequence has max_q rows
+ * and they start at b * max_q.  Query i of b sees row t of the cache when
+ *     t < e_i   and   (window == 0  or  t < sinks  or  t >= e_i - window),
+ *     e_i = L - n_b + 1 + i if causal, else L         (bidirectional: a decoding block sees itself and the prefix)
+ *     out[r][h] = sum_t softmax_t(scale * <q[r][h], k_t>) v_t,   lse[r][h] = log sum_t exp(scale * <q[r][h], k_t>)
+ * with KV head h / (Hq / Hkv), fp32 accumulation, out in the element type.  A query that sees nothing gets
+ * out = 0, lse = -inf.  Rows of q/out that belong to no sequence are left as they are.  What the cache holds in rows
+ * beyond L, in pages no table names, and in rows the window hides from every query is not used, whatever its bits; K
+ * and V of a row that some query sees and another does not reach only the one that does (a NaN there stays there).
+ *
+ * max_q and max_len are HOST bounds of n_b and L that size the launch; a sequence beyond them raises DS_DEV_INDEX and
+ * is clamped (max_len = 0: the capacity of the block table).  A page number outside [0, n_pages) raises DS_DEV_INDEX
+ * and is clamped, as is a row range outside [0, N].
+ *
+ * Layout as above: q_stride/out_stride row, head; cache_stride page, head, row, the same for K and V; D contiguous,
+ * bases 16-byte aligned, strides multiples of 16 bytes.  Envelope: DS_BF16 with D in {64, 128}, DS_F32 with D in
+ * {32, 64, 128, 256}; any Hq / Hkv, page_size, n_b.
+ *
+ * Workspace: ds_attn_paged_workspace(p) bytes, 256-byte aligned, contents need not be kept between calls.  It holds
+ * the partial results of sequences whose length is split over CTAs.  A call without a (large enough) workspace is
+ * not an error; it runs unsplit.  Calls that may overlap must not share a workspace.
+ * Errors: DS_ERR_INVALID_ARG (NULL or misaligned pointer, misaligned stride, Hq % Hkv != 0, window or sinks < 0, max_q < 1,
+ * scale not finite, row_start == NULL with B * max_q > N, table_stride < max_pages); DS_ERR_UNSUPPORTED (D outside the
+ * envelope, B > 8192, max_pages * page_size or n_pages * page_size > 2^31 - 1). */
+typedef struct {
+  int32_t B, Hq, Hkv, D;
+  int32_t dtype;
+  int32_t N;                    /* rows of q and out */
+  int32_t max_q;                /* most query rows of a sequence */
+  int32_t max_len;              /* most cache rows of a sequence, 0 = max_pages * page_size */
+  int32_t page_size, max_pages, n_pages;
+  int32_t causal, window, sinks;
+  float scale;
+  const int32_t *row_start;     /* optional [B + 1] */
+  const int32_t *kv_len;        /* [B] */
+  const int32_t *block_table;   /* [B][max_pages] */
+  int64_t table_stride;
+  const void *q;                /* [N][Hq][D] */
+  int64_t q_stride[2];
+  const void *k_cache, *v_cache;
+  int64_t cache_stride[3];
+  void *out;                    /* [N][Hq][D] */
+  int64_t out_stride[2];
+  float *lse;                   /* optional [N][Hq], dense */
+  void *workspace;
+  size_t workspace_bytes;
+  uint32_t *status;             /* optional device word */
+} ds_paged_params;
+
+/* HOST, pure: bytes of workspace ds_attn_paged needs for *p (0 when none). */
+DS_API size_t ds_attn_paged_workspace(const ds_paged_params *p);
+/* `p` is a HOST pointer; the pointers inside it are device pointers. */
+DS_API int ds_attn_paged(const ds_paged_params *p, void *stream);
 
 /* ------------------------------------------------------------------------
  * Utilities

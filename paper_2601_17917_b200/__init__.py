@@ -23,12 +23,14 @@ __all__ = [
     "ds_launch_count", "ds_block_begin", "ds_confidence_listed", "AttnPlan", "ds_selftest_bounded_wait",
     "DsError", "DS_F32", "DS_BF16", "DS_DEV_INDEX", "DS_DEV_TIMEOUT",
     "DS_ATTN_KERNEL_AUTO", "DS_ATTN_KERNEL_ONE_TILE", "DS_ATTN_KERNEL_TWO_TILE",
+    "DS_DEV_PAGES", "RopeTable", "ds_page_update", "ds_qk_norm_rope", "ds_attn_paged", "ds_attn_paged_workspace",
+    "PageUpdatePlan", "QkNormRopePlan", "PagedAttnPlan",
 ]
 
 DS_F32, DS_BF16 = 0, 1
 DS_OK, DS_ERR_INVALID_ARG, DS_ERR_UNSUPPORTED, DS_ERR_WORKSPACE, DS_ERR_CUDA, DS_ERR_STATIC_LIMIT = range(6)
 DS_CONFIDENCE_STATIC_MAX_ROWS = 4096
-DS_DEV_INDEX, DS_DEV_TIMEOUT = 1, 2
+DS_DEV_INDEX, DS_DEV_TIMEOUT, DS_DEV_PAGES = 1, 2, 4
 DS_ATTN_KERNEL_AUTO, DS_ATTN_KERNEL_ONE_TILE, DS_ATTN_KERNEL_TWO_TILE = 0, 1, 2
 
 _LIB_PATH = Path(__file__).resolve().parent / "libds_b200.so"
@@ -140,6 +142,14 @@ def lib() -> ctypes.CDLL:
         L.ds_block_begin.argtypes = [ctypes.POINTER(_BlockParams), ctypes.c_void_p]
         L.ds_unmask_select.restype = ctypes.c_int
         L.ds_unmask_select.argtypes = [ctypes.POINTER(_SelectParams), ctypes.c_void_p]
+        for name, struct in paged.ENTRY_POINTS:
+            getattr(L, name).restype = ctypes.c_int
+            getattr(L, name).argtypes = [ctypes.POINTER(struct), ctypes.c_void_p]
+        L.ds_attn_paged_workspace.restype = ctypes.c_size_t
+        L.ds_attn_paged_workspace.argtypes = [ctypes.POINTER(paged.PagedParams)]
+        L.ds_rope_table_init.restype = ctypes.c_int
+        L.ds_rope_table_init.argtypes = [ctypes.POINTER(paged.RopeTableStruct), ctypes.c_int32, ctypes.c_int32,
+                                         ctypes.c_double, ctypes.c_int32] + [ctypes.c_double] * 4
         L.ds_read_status.restype = ctypes.c_int
         L.ds_read_status.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.POINTER(ctypes.c_uint32)]
         L.ds_selftest_bounded_wait.restype = ctypes.c_int
@@ -559,3 +569,8 @@ def ds_read_status(status: torch.Tensor, stream=None) -> int:
     if rc != DS_OK:
         raise DsError(rc, "ds_read_status")
     return int(host.value)
+
+
+from . import paged  # noqa: E402  (needs the helpers above)
+from .paged import (PagedAttnPlan, PageUpdatePlan, QkNormRopePlan, RopeTable, ds_attn_paged,  # noqa: E402
+                    ds_attn_paged_workspace, ds_page_update, ds_qk_norm_rope)

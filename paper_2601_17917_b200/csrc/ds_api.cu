@@ -1,6 +1,7 @@
 // C ABI of the denoising-step library: argument validation and dispatch.
 // Every step of the path runs in the CUDA kernels of the sibling files.
 #include <atomic>
+#include <cmath>
 #include <new>
 
 #include "ds_common.cuh"
@@ -64,6 +65,81 @@ int validate_attn(const ds_attn_params *p) {
   if (p->dtype == DS_BF16) return attn_tc_supported(*p) ? DS_OK : DS_ERR_UNSUPPORTED;
   if (p->D != 32 && p->D != 64 && p->D != 128 && p->D != 256) return DS_ERR_UNSUPPORTED;
   if (!(p->scale > -1e30f && p->scale < 1e30f)) return DS_ERR_UNSUPPORTED;
+  return DS_OK;
+}
+
+// Strides of the paged-cache entry points: non-negative multiples of 16 bytes.
+bool strides_ok(const int64_t *s, int n, int64_t unit) {
+  for (int d = 0; d < n; ++d)
+    if (s[d] < 0 || s[d] % unit != 0) return false;
+  return true;
+}
+
+int validate_pages(const ds_page_params *p) {
+  if (!p) return DS_ERR_INVALID_ARG;
+  if (p->B < 0 || p->max_rows < 0 || p->page_size < 1 || p->max_pages < 1 || p->n_pages < 1) return DS_ERR_INVALID_ARG;
+  if (!p->free_list || !p->free_cnt || !p->free_cnt_out || !p->row_start) return DS_ERR_INVALID_ARG;
+  if (p->B > 0 && (!p->kv_len || !p->n_new || !p->block_table || !p->kv_len_out)) return DS_ERR_INVALID_ARG;
+  if (p->table_stride < p->max_pages) return DS_ERR_INVALID_ARG;
+  const void *words[] = {p->kv_len, p->n_new, p->block_table, p->free_list, p->free_cnt, p->kv_len_out, p->free_cnt_out,
+                         p->row_start, p->positions, p->status};
+  for (const void *w : words)
+    if (!aligned(w, 4)) return DS_ERR_INVALID_ARG;
+  if (!aligned(p->slot_map, 8)) return DS_ERR_INVALID_ARG;
+  if (p->B > 8192 || (int64_t)p->max_pages * p->page_size > 0x7fffffffLL || (int64_t)p->n_pages * p->page_size > 0x7fffffffLL)
+    return DS_ERR_UNSUPPORTED;
+  return DS_OK;
+}
+
+int validate_qk(const ds_qk_params *p) {
+  if (!p || !p->rope) return DS_ERR_INVALID_ARG;
+  if (p->dtype != DS_F32 && p->dtype != DS_BF16) return DS_ERR_INVALID_ARG;
+  if (p->N < 0 || p->Hq <= 0 || p->Hkv <= 0 || p->D <= 0 || !(p->eps >= 0.f)) return DS_ERR_INVALID_ARG;
+  if (p->rope->rotary_dim < 2 || p->rope->rotary_dim % 2 != 0) return DS_ERR_INVALID_ARG;
+  const bool cache = p->k_cache || p->v_cache;
+  if (p->N > 0) {
+    if (!p->q || !p->k || !p->v || !p->positions || !p->q_out) return DS_ERR_INVALID_ARG;
+    if ((p->k_out == nullptr) != (p->v_out == nullptr) || (p->k_cache == nullptr) != (p->v_cache == nullptr))
+      return DS_ERR_INVALID_ARG;
+    if (cache && (!p->slot_map || p->page_size < 1 || p->n_pages < 1)) return DS_ERR_INVALID_ARG;
+  }
+  const void *ptrs[] = {p->q, p->k, p->v, p->q_weight, p->k_weight, p->q_out, p->k_out, p->v_out, p->k_cache, p->v_cache};
+  for (const void *q : ptrs)
+    if (!aligned(q, 16)) return DS_ERR_INVALID_ARG;
+  if (!aligned(p->positions, 4) || !aligned(p->n_rows, 4) || !aligned(p->status, 4) || !aligned(p->slot_map, 8))
+    return DS_ERR_INVALID_ARG;
+  const int64_t unit = p->dtype == DS_BF16 ? 8 : 4;
+  if (!strides_ok(p->q_stride, 2, unit) || !strides_ok(p->kv_stride, 2, unit) || !strides_ok(p->q_out_stride, 2, unit))
+    return DS_ERR_INVALID_ARG;
+  if (p->k_out && !strides_ok(p->kv_out_stride, 2, unit)) return DS_ERR_INVALID_ARG;
+  if (cache && !strides_ok(p->cache_stride, 3, unit)) return DS_ERR_INVALID_ARG;
+  if (p->D % 8 != 0 || p->D > 256 || p->rope->rotary_dim % 16 != 0 || p->rope->rotary_dim > p->D) return DS_ERR_UNSUPPORTED;
+  if (cache && (int64_t)p->n_pages * p->page_size > 0x7fffffffLL) return DS_ERR_UNSUPPORTED;
+  return DS_OK;
+}
+
+int validate_paged(const ds_paged_params *p) {
+  if (!p) return DS_ERR_INVALID_ARG;
+  if (p->dtype != DS_F32 && p->dtype != DS_BF16) return DS_ERR_INVALID_ARG;
+  if (p->B < 0 || p->Hq <= 0 || p->Hkv <= 0 || p->D <= 0 || p->N < 0 || p->max_q < 1 || p->max_len < 0) return DS_ERR_INVALID_ARG;
+  if (p->page_size < 1 || p->max_pages < 1 || p->n_pages < 1 || p->window < 0 || p->sinks < 0) return DS_ERR_INVALID_ARG;
+  if (p->Hq % p->Hkv != 0 || !std::isfinite(p->scale) || p->table_stride < p->max_pages) return DS_ERR_INVALID_ARG;
+  if (!p->row_start && (int64_t)p->B * p->max_q > p->N) return DS_ERR_INVALID_ARG;
+  if (p->B > 0 && p->N > 0 && (!p->kv_len || !p->block_table || !p->q || !p->k_cache || !p->v_cache || !p->out))
+    return DS_ERR_INVALID_ARG;
+  const void *ptrs[] = {p->q, p->k_cache, p->v_cache, p->out};
+  for (const void *q : ptrs)
+    if (!aligned(q, 16)) return DS_ERR_INVALID_ARG;
+  const void *words[] = {p->row_start, p->kv_len, p->block_table, p->lse, p->status};
+  for (const void *w : words)
+    if (!aligned(w, 4)) return DS_ERR_INVALID_ARG;
+  const int64_t unit = p->dtype == DS_BF16 ? 8 : 4;
+  if (!strides_ok(p->q_stride, 2, unit) || !strides_ok(p->cache_stride, 3, unit) || !strides_ok(p->out_stride, 2, unit))
+    return DS_ERR_INVALID_ARG;
+  const bool d_ok = p->dtype == DS_BF16 ? (p->D == 64 || p->D == 128) : (p->D == 32 || p->D == 64 || p->D == 128 || p->D == 256);
+  if (!d_ok || p->B > 8192 || (int64_t)p->max_pages * p->page_size > 0x7fffffffLL ||
+      (int64_t)p->n_pages * p->page_size > 0x7fffffffLL)
+    return DS_ERR_UNSUPPORTED;
   return DS_OK;
 }
 
@@ -273,6 +349,73 @@ int ds_block_begin(const ds_block_params *p, void *stream) {
   if ((long long)p->B * p->K > 0x7fffffffLL) return DS_ERR_UNSUPPORTED;
   if (p->B > 0 && (!p->eos_exit || !p->masked || !p->x_block || !p->active_seq)) return DS_ERR_INVALID_ARG;
   return ds::launch_block_begin(*p, reinterpret_cast<cudaStream_t>(stream));
+}
+
+int ds_page_update(const ds_page_params *p, void *stream) {
+  const int rc = ds::validate_pages(p);
+  if (rc != DS_OK) return rc;
+  return ds::launch_page_update(*p, reinterpret_cast<cudaStream_t>(stream));
+}
+
+int ds_rope_table_init(ds_rope_table *t, int32_t rotary_dim, int32_t interleaved, double theta, int32_t scaling,
+                       double factor, double orig_len, double beta_fast, double beta_slow) {
+  if (!t || rotary_dim < 2 || rotary_dim % 2 != 0 || !(theta > 1.0) || !std::isfinite(theta)) return DS_ERR_INVALID_ARG;
+  if (scaling < DS_ROPE_NONE || scaling > DS_ROPE_YARN) return DS_ERR_INVALID_ARG;
+  if (scaling != DS_ROPE_NONE && (!(factor > 0.0) || !std::isfinite(factor))) return DS_ERR_INVALID_ARG;
+  if (scaling == DS_ROPE_YARN && (!(orig_len >= 1.0) || !std::isfinite(orig_len) || !(beta_slow > 0.0) ||
+                                  !(beta_fast > beta_slow) || !std::isfinite(beta_fast)))
+    return DS_ERR_INVALID_ARG;
+  if (rotary_dim > 256 || rotary_dim % 16 != 0) return DS_ERR_UNSUPPORTED;
+  const long double R = rotary_dim, two_pi = 6.283185307179586476925286766559L;
+  long double base = theta;
+  if (scaling == DS_ROPE_NTK) base *= std::pow((long double)factor, R / (R - 2));
+  long double lo = 0, hi = 0;
+  if (scaling == DS_ROPE_YARN) {
+    const long double per_e = R / (2 * std::log((long double)theta));
+    lo = std::floor(per_e * std::log(orig_len / (beta_fast * two_pi)));
+    hi = std::ceil(per_e * std::log(orig_len / (beta_slow * two_pi)));
+    lo = lo > 0 ? lo : 0;
+    hi = hi < R - 1 ? hi : R - 1;
+  }
+  t->rotary_dim = rotary_dim;
+  t->interleaved = interleaved != 0;
+  t->mscale = scaling == DS_ROPE_YARN && factor > 1.0 ? (float)(0.1L * std::log((long double)factor) + 1.0L) : 1.0f;
+  t->reserved = 0;
+  for (int d = 0; d < 128; ++d) {
+    t->turn[d] = 0;
+    if (d >= rotary_dim / 2) continue;
+    long double f = std::pow(base, -2.0L * d / R);
+    if (scaling == DS_ROPE_LINEAR) f /= factor;
+    if (scaling == DS_ROPE_YARN) {
+      const long double width = hi - lo > 1e-3L ? hi - lo : 1e-3L;
+      long double ramp = (d - lo) / width;
+      ramp = ramp < 0 ? 0 : ramp > 1 ? 1 : ramp;
+      f = f * (1 - ramp) + f / factor * ramp;
+    }
+    long double turn = f / two_pi;
+    turn -= std::floor(turn);
+    // 64 fraction bits; a fraction that rounds up to a whole turn is no turn
+    const long double bits = std::floor(turn * 18446744073709551616.0L + 0.5L);
+    t->turn[d] = bits >= 18446744073709551616.0L ? 0 : (uint64_t)bits;
+  }
+  return DS_OK;
+}
+
+int ds_qk_norm_rope(const ds_qk_params *p, void *stream) {
+  const int rc = ds::validate_qk(p);
+  if (rc != DS_OK) return rc;
+  return p->N == 0 ? (int)DS_OK : ds::launch_qk_norm_rope(*p, reinterpret_cast<cudaStream_t>(stream));
+}
+
+size_t ds_attn_paged_workspace(const ds_paged_params *p) {
+  return ds::validate_paged(p) == DS_OK ? ds::attn_paged_workspace_bytes(*p) : 0;
+}
+
+int ds_attn_paged(const ds_paged_params *p, void *stream) {
+  const int rc = ds::validate_paged(p);
+  if (rc != DS_OK) return rc;
+  if (p->B == 0 || p->N == 0) return DS_OK;
+  return ds::launch_attn_paged(*p, reinterpret_cast<cudaStream_t>(stream));
 }
 
 int ds_selftest_bounded_wait(uint32_t poll_limit, uint32_t *status, int32_t *report, void *stream) {
