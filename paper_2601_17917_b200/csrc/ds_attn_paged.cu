@@ -1,104 +1,797 @@
 // ds_attn_paged: attention of the new rows of every sequence over its pages.
 //
-// One warp owns one query row and head; the lanes split the head dimension, and the keys that the row sees are visited
-// in order with an online softmax in fp32 (base 2).
+// With one or a few query rows per KV head this is a stream over the cache: every byte of K and V is used for
+// G n_b rows at most, so the kernel is built to keep loads in flight.  The (sequence, KV head, row tile, key tile)
+// units of the whole batch are laid end to end and cut into equal ranges, one per resident CTA, from the lengths on the
+// device: uneven lengths cost nothing and one long sequence spreads over the whole GPU.  An item that crosses a range
+// boundary leaves partial results (unnormalised sums with their maximum) in the workspace; a second, small
+// kernel, launched early and waiting for the first, joins them in a fixed order.
+//
+// Inside a CTA the four warps take equal parts of every key tile and share nothing until the item ends: each has its own
+// ring of cp.async stages in shared memory (16-byte chunks, XOR swizzle), its own running maximum, sum and output, so
+// the loop has no CTA-wide barrier.  At the end of an item the four results are joined through shared memory.
+//
+// bf16: mma.sync m16n8k16 (rows = the stacked queries, up to 16 M).  The few rows leave tcgen05's 128-row tile
+// nearly empty and the stream, not the products, bounds the kernel.  The weights enter the second product as two bf16
+// halves (hi + lo), which keeps 16 bits of them: the product is free here, and an output is then rounded once.
+// fp32: CUDA cores, 8 lanes per key.
+#include <type_traits>
+
 #include "ds_common.cuh"
+#include "ds_paged_index.cuh"
+#include "ds_sm100.cuh"
 
 namespace ds {
 namespace {
 
-constexpr int kWarps = 8;
+constexpr int kWarps = 4, kThreads = kWarps * 32, kStages = 3;
+constexpr int kMinTiles = 4;     // a range has at least so many key tiles
+constexpr int kWholeTiles = 8;   // items of at most so many key tiles are not split
 
-__device__ __forceinline__ float to_f32(float x) { return x; }
-__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
-__device__ __forceinline__ void from_f32(float x, float &y) { y = x; }
-__device__ __forceinline__ void from_f32(float x, __nv_bfloat16 &y) { y = __float2bfloat16_rn(x); }
+struct Params {
+  ds_paged_params p;
+  PagedShape s;
+  FastDiv page_div, group_div;
+  int split;
+  PagedJoin *joins;   // [gridDim.x]
+  float2 *part_ml;    // [2 gridDim.x][row_tile]  maximum (base 2, scaled) and sum
+  float *part_o;      // [2 gridDim.x][row_tile][D]
+};
 
-template <typename T, int D>
-__global__ void __launch_bounds__(kWarps * 32) attn_paged_row_kernel(const ds_paged_params p) {
-  constexpr int E = D / 32;
-  const int lane = threadIdx.x & 31, b = blockIdx.y;
-  const long long idx = (long long)blockIdx.x * kWarps + (threadIdx.x >> 5);
-  const int i = (int)(idx / p.Hq), h = (int)(idx % p.Hq), g = h / (p.Hq / p.Hkv);
-  uint32_t flags = 0;
-  int first = b * p.max_q, count = p.max_q;
-  if (p.row_start) {
-    const int lo = p.row_start[b], hi = p.row_start[b + 1];
-    first = min(max(lo, 0), p.N);
-    count = min(max(hi - first, 0), min(p.max_q, p.N - first));
-    if (first != lo || hi - lo != count) flags |= DS_DEV_INDEX;
-  }
-  const int cap = p.max_pages * p.page_size;
-  const int bound = p.max_len > 0 ? min(p.max_len, cap) : cap;
-  int len = p.kv_len[b];
-  if (len < 0 || len > bound) flags |= DS_DEV_INDEX;
-  len = min(max(len, 0), bound);
-  if (i < count) {
-    const long long row = first + i;
-    const int end = p.causal ? len - count + 1 + i : len;
-    float q[E], o[E], m = -INFINITY, l = 0.f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      q[e] = to_f32(reinterpret_cast<const T *>(p.q)[row * p.q_stride[0] + h * p.q_stride[1] + e * 32 + lane]);
-      o[e] = 0.f;
-    }
-    const float scale2 = p.scale * kLog2e;
-    const int lo = p.window ? max(end - p.window, min(p.sinks, end)) : 0;
-    for (int t = 0; t < end; ++t) {
-      if (t < lo && t >= p.sinks) t = lo;
-      int page = p.block_table[b * p.table_stride + t / p.page_size];
-      if (page < 0 || page >= p.n_pages) {
-        flags |= DS_DEV_INDEX;
-        page = page < 0 ? 0 : p.n_pages - 1;
-      }
-      const long long at = page * p.cache_stride[0] + g * p.cache_stride[1] + (long long)(t % p.page_size) * p.cache_stride[2];
-      float z = 0.f;
-#pragma unroll
-      for (int e = 0; e < E; ++e) z = fmaf(q[e], to_f32(reinterpret_cast<const T *>(p.k_cache)[at + e * 32 + lane]), z);
-#pragma unroll
-      for (int x = 16; x > 0; x >>= 1) z += __shfl_xor_sync(0xffffffffu, z, x);
-      z *= scale2;
-      const float nm = fmaxf(m, z);
-      // a score of -inf has no weight, also while nothing else has been seen (-inf - -inf would be NaN)
-      const float keep = m == -INFINITY ? 0.f : ex2_approx(m - nm), w = z == -INFINITY ? 0.f : ex2_approx(z - nm);
-      m = nm;
-      l = fmaf(l, keep, w);
-#pragma unroll
-      for (int e = 0; e < E; ++e)
-        o[e] = fmaf(o[e], keep, w * to_f32(reinterpret_cast<const T *>(p.v_cache)[at + e * 32 + lane]));
-    }
-    const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
-#pragma unroll
-    for (int e = 0; e < E; ++e)
-      from_f32(o[e] * inv, reinterpret_cast<T *>(p.out)[row * p.out_stride[0] + h * p.out_stride[1] + e * 32 + lane]);
-    if (p.lse && lane == 0) p.lse[row * p.Hq + h] = l > 0.f ? (m + log2f(l)) * kLn2 : (l == 0.f ? -INFINITY : l);
-  }
-  if (flags && p.status && lane == 0) atomicOr(p.status, flags);
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, bool there) {
+  // a chunk that is not there is filled with zeros and not read
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void ldmatrix4(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+               "{%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-template <typename T, int D>
+// Byte offset of 16-byte chunk `c` of row `r` in a tile of rows of ROW bytes: chunks are XOR-ed with the row number
+// within groups of eight, which makes ldmatrix and the float4 reads below free of bank conflicts.
+template <int ROW>
+__device__ __forceinline__ uint32_t chunk_at(int r, int c) { return r * ROW + ((c ^ (r & 7)) << 4); }
+
+// The item a CTA works on.
+struct Item {
+  PagedSeq q;
+  int b, g;            // sequence, KV head
+  int row0, rows;      // stacked rows row0 .. row0 + rows - 1 of the sequence
+};
+
+// Stacked row -> query row of the packed arrays, head, and how much of the cache it sees.
+struct Row {
+  long long n;
+  int h, end;
+};
+__device__ __forceinline__ Row row_of(const Params &a, const Item &it, int r) {
+  const int rr = it.row0 + r, i = fast_div(rr, a.group_div);
+  return {(long long)it.q.first + i, it.g * a.s.G + (rr - i * a.s.G), a.s.causal ? it.q.end_min + i : it.q.len};
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// A warp's share of an item in bf16: M row blocks of 16 against KEYS = 16 keys at a time.
+template <int D_, int M>
+struct TensorRows {
+  using T = __nv_bfloat16;
+  static constexpr int D = D_, kRows = 16 * M, kRowBytes = 2 * D, kKeys = 16;
+  static constexpr int kQBytes = M == 1 ? 0 : kRows * kRowBytes;   // M = 1 holds the queries in registers
+  static constexpr int kCtas = D == 64 && M == 1 ? 3 : 2;          // per SM: registers and shared memory
+  float o[M][D / 8][4];
+  float m[M][2], l[M][2];        // rows lane / 4 and lane / 4 + 8 of each block
+  int end[M][2];
+  uint32_t qf[M == 1 ? D / 16 : 1][4];
+  uint32_t q_smem;
+
+  __device__ void begin(const Params &a, const Item &it, uint8_t *q_buf) {
+    const int lane = threadIdx.x & 31;
+    q_smem = sm100::smem_u32(q_buf);
+#pragma unroll
+    for (int mi = 0; mi < M; ++mi) {
+#pragma unroll
+      for (int j = 0; j < D / 8; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[mi][j][e] = 0.f;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        m[mi][e] = -INFINITY, l[mi][e] = 0.f;
+        const int r = mi * 16 + e * 8 + (lane >> 2);
+        end[mi][e] = r < it.rows ? row_of(a, it, r).end : 0;
+      }
+    }
+    const T *q = reinterpret_cast<const T *>(a.p.q);
+    if constexpr (M == 1) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int r = e * 8 + (lane >> 2);
+        const bool there = r < it.rows;
+        const Row row = row_of(a, it, there ? r : 0);
+        const T *src = q + row.n * a.p.q_stride[0] + row.h * a.p.q_stride[1] + (lane & 3) * 2;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+          qf[k][e] = there ? *reinterpret_cast<const uint32_t *>(src + 16 * k) : 0u;
+          qf[k][2 + e] = there ? *reinterpret_cast<const uint32_t *>(src + 16 * k + 8) : 0u;
+        }
+      }
+    } else {
+      for (int c = threadIdx.x; c < kRows * (kRowBytes / 16); c += kThreads) {
+        const int r = c / (kRowBytes / 16), ch = c % (kRowBytes / 16);
+        uint4 w = make_uint4(0, 0, 0, 0);
+        if (r < it.rows) {
+          const Row row = row_of(a, it, r);
+          w = *reinterpret_cast<const uint4 *>(q + row.n * a.p.q_stride[0] + row.h * a.p.q_stride[1] + 8 * ch);
+        }
+        *reinterpret_cast<uint4 *>(q_buf + chunk_at<kRowBytes>(r, ch)) = w;
+      }
+      __syncthreads();
+    }
+  }
+
+  // 16 keys from x on; K and V as loaded, V is scratch afterwards.
+  __device__ __forceinline__ void step(const Params &a, const Item &it, uint8_t *kbuf, uint8_t *vbuf, int x, float scale2) {
+    const int lane = threadIdx.x & 31;
+    const uint32_t ks = sm100::smem_u32(kbuf), vs = sm100::smem_u32(vbuf);
+    float s[M][2][4];
+#pragma unroll
+    for (int mi = 0; mi < M; ++mi)
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[mi][t][e] = 0.f;
+    {
+      // matrices: keys 0-7 / 8-15 (lane bit 4), first / second 8 dimensions (lane bit 3)
+      const int key = (lane & 7) + ((lane >> 4) << 3), half = (lane >> 3) & 1;
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) {
+        uint32_t kf[4];
+        ldmatrix4(ks + chunk_at<kRowBytes>(key, 2 * k + half), kf);
+#pragma unroll
+        for (int mi = 0; mi < M; ++mi) {
+          uint32_t af[4];
+          if constexpr (M == 1) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) af[e] = qf[k][e];
+          } else {
+            ldmatrix4(q_smem + chunk_at<kRowBytes>(mi * 16 + (lane & 15), 2 * k + (lane >> 4)), af);
+          }
+          mma16816(s[mi][0], af, kf[0], kf[1]);
+          mma16816(s[mi][1], af, kf[2], kf[3]);
+        }
+      }
+    }
+    const bool partial = !paged_all_visible(a.s, it.q, x, kKeys);
+#pragma unroll
+    for (int mi = 0; mi < M; ++mi)
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[mi][t][e] *= scale2;
+    uint32_t seen[M][2] = {};    // only with partial: bit 2 t + c of a row: key 8 t + 2 (lane % 4) + c
+    if (partial) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const int pos = paged_key(it.q, x + 8 * t + 2 * (lane & 3) + c);
+#pragma unroll
+          for (int mi = 0; mi < M; ++mi)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const bool vis = paged_visible(a.s, pos, end[mi][e]);
+              if (vis) seen[mi][e] |= 1u << (2 * t + c);
+              else s[mi][t][2 * e + c] = -INFINITY;
+            }
+        }
+    }
+    uint32_t ph[M][4], pl[M][4];   // A fragments of the weights' halves
+#pragma unroll
+    for (int mi = 0; mi < M; ++mi) {
+      float nm[2];
+      bool moved = false;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float v = fmaxf(fmaxf(s[mi][0][2 * e], s[mi][0][2 * e + 1]), fmaxf(s[mi][1][2 * e], s[mi][1][2 * e + 1]));
+        v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 1));
+        v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 2));
+        // the reference moves only when a weight would pass 2^8: the result is the same, the sums are touched rarely
+        nm[e] = v > m[mi][e] + 8.f ? v : m[mi][e];
+        moved |= nm[e] != m[mi][e];
+      }
+      if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float keep = m[mi][e] == nm[e] ? 1.f : ex2_approx(m[mi][e] - nm[e]);
+          m[mi][e] = nm[e];
+          l[mi][e] *= keep;
+#pragma unroll
+          for (int j = 0; j < D / 8; ++j) o[mi][j][2 * e] *= keep, o[mi][j][2 * e + 1] *= keep;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float ref = m[mi][e] == -INFINITY ? 0.f : m[mi][e];   // nothing seen yet: weights exp(-inf) = 0
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const float p0 = ex2_approx(s[mi][t][2 * e] - ref), p1 = ex2_approx(s[mi][t][2 * e + 1] - ref);
+          l[mi][e] += p0 + p1;
+          const uint32_t hi = sm100::pack_bf16(p0, p1);
+          ph[mi][2 * t + e] = hi;
+          pl[mi][2 * t + e] = sm100::pack_bf16(p0 - bf16lo_to_f32(hi), p1 - bf16hi_to_f32(hi));
+        }
+      }
+    }
+    if (partial) keep_hidden_values_out(vbuf, ph, pl, seen);
+    {
+      // matrices: keys 0-7 / 8-15 (lane bit 3), dimensions +0 / +8 (lane bit 4)
+      const int key = lane & 15, half = lane >> 4;
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j) {
+        uint32_t vf[4];
+        ldmatrix4_trans(vs + chunk_at<kRowBytes>(key, 2 * j + half), vf);
+#pragma unroll
+        for (int mi = 0; mi < M; ++mi) {
+          mma16816(o[mi][2 * j], ph[mi], vf[0], vf[1]);
+          mma16816(o[mi][2 * j + 1], ph[mi], vf[2], vf[3]);
+          mma16816(o[mi][2 * j], pl[mi], vf[0], vf[1]);
+          mma16816(o[mi][2 * j + 1], pl[mi], vf[2], vf[3]);
+        }
+      }
+    }
+  }
+
+  // Keys that some rows see and others do not (or that are padding): a weight of zero times an infinite or NaN value
+  // would be NaN in the product.  If V holds such values (rare), their terms are added here for the rows that
+  // see them, one by one, and they are replaced by zero.
+  __device__ __forceinline__ void keep_hidden_values_out(uint8_t *vbuf, const uint32_t (&ph)[M][4], const uint32_t (&pl)[M][4],
+                                                      const uint32_t (&seen)[M][2]) {
+    const int lane = threadIdx.x & 31;
+    constexpr int kWords = kKeys * kRowBytes / 4;
+    uint32_t *words = reinterpret_cast<uint32_t *>(vbuf);
+    bool odd = false;
+    for (int w = lane; w < kWords; w += 32) {
+      const uint32_t v = words[w];
+      odd |= (v & 0x7f80u) == 0x7f80u || (v & 0x7f800000u) == 0x7f800000u;
+    }
+    if (!__any_sync(0xffffffffu, odd)) return;
+#pragma unroll 1
+    for (int key = 0; key < kKeys; ++key) {
+      const int src = (lane & ~3) | ((key & 7) >> 1), bit = 2 * (key >> 3) + (key & 1);
+#pragma unroll
+      for (int mi = 0; mi < M; ++mi)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t hi = __shfl_sync(0xffffffffu, key < 8 ? ph[mi][e] : ph[mi][2 + e], src);
+          const uint32_t lo = __shfl_sync(0xffffffffu, key < 8 ? pl[mi][e] : pl[mi][2 + e], src);
+          const bool vis = (__shfl_sync(0xffffffffu, seen[mi][e], src) >> bit) & 1;
+          const float w = key & 1 ? bf16hi_to_f32(hi) + bf16hi_to_f32(lo) : bf16lo_to_f32(hi) + bf16lo_to_f32(lo);
+          if (!vis) continue;
+#pragma unroll
+          for (int j = 0; j < D / 8; ++j) {
+            const uint32_t v = *reinterpret_cast<const uint32_t *>(vbuf + chunk_at<kRowBytes>(key, j) + (lane & 3) * 4);
+            const float v0 = bf16lo_to_f32(v), v1 = bf16hi_to_f32(v);
+            if (!isfinite(v0)) o[mi][j][2 * e] += w * v0;
+            if (!isfinite(v1)) o[mi][j][2 * e + 1] += w * v1;
+          }
+        }
+    }
+    __syncwarp();
+    for (int w = lane; w < kWords; w += 32) {
+      uint32_t v = words[w];
+      if ((v & 0x7f80u) == 0x7f80u) v &= 0xffff0000u;
+      if ((v & 0x7f800000u) == 0x7f800000u) v &= 0xffffu;
+      words[w] = v;
+    }
+    __syncwarp();
+  }
+
+  // The warp's sums to shared memory: out[kRows][D], ml[kRows].
+  __device__ void finish(const Item &it, float *out, float2 *ml) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int mi = 0; mi < M; ++mi)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int r = mi * 16 + e * 8 + (lane >> 2);
+        float sum = l[mi][e];
+        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+        if (r >= it.rows) continue;
+        if ((lane & 3) == 0) ml[r] = make_float2(m[mi][e], sum);
+#pragma unroll
+        for (int j = 0; j < D / 8; ++j)
+          *reinterpret_cast<float2 *>(out + r * D + 8 * j + 2 * (lane & 3)) = make_float2(o[mi][j][2 * e], o[mi][j][2 * e + 1]);
+      }
+  }
+};
+
+// ---------------------------------------------------------------------------------------------------------------
+// A warp's share of an item in fp32: R rows; 8 lanes per key, four keys side by side, each lane group with sums of
+// its own.  Lane u of a group holds 16-byte chunks u, u + 8, .. of a row.
+template <int D_, int R>
+struct ScalarRows {
+  using T = float;
+  static constexpr int D = D_, kRows = R, kRowBytes = 4 * D, kKeys = kRowBytes >= 512 ? 4096 / kRowBytes : 16;
+  static constexpr int kQBytes = 0, C = D / 32, kPer = kKeys / 4;
+  static constexpr int kCtas = D == 32 && R == 1 ? 4 : 2;
+  float4 q[R][C], o[R][C];
+  float m[R], l[R];
+  int end[R];
+
+  __device__ void begin(const Params &a, const Item &it, uint8_t *) {
+    const int u = threadIdx.x & 7;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const bool there = r < it.rows;
+      const Row row = row_of(a, it, there ? r : 0);
+      const float *src = reinterpret_cast<const float *>(a.p.q) + row.n * a.p.q_stride[0] + row.h * a.p.q_stride[1];
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        q[r][c] = there ? *reinterpret_cast<const float4 *>(src + 4 * (u + 8 * c)) : make_float4(0.f, 0.f, 0.f, 0.f);
+        o[r][c] = make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+      m[r] = -INFINITY, l[r] = 0.f;
+      end[r] = there ? row.end : 0;
+    }
+  }
+
+  __device__ __forceinline__ void step(const Params &a, const Item &it, uint8_t *kbuf, uint8_t *vbuf, int x, float scale2) {
+    const int lane = threadIdx.x & 31, u = lane & 7, group = lane >> 3;
+    const bool partial = !paged_all_visible(a.s, it.q, x, kKeys);
+    float z[kPer][R];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int key = 4 * i + group;
+#pragma unroll
+      for (int r = 0; r < R; ++r) z[i][r] = 0.f;
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const float4 k = *reinterpret_cast<const float4 *>(kbuf + chunk_at<kRowBytes>(key, u + 8 * c));
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+          z[i][r] = fmaf(q[r][c].w, k.w, fmaf(q[r][c].z, k.z, fmaf(q[r][c].y, k.y, fmaf(q[r][c].x, k.x, z[i][r]))));
+      }
+    }
+    uint32_t hidden = 0;      // bit i R + r
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int pos = partial ? paged_key(it.q, x + 4 * i + group) : 0;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        float v = z[i][r];
+        v += __shfl_xor_sync(0xffffffffu, v, 1);
+        v += __shfl_xor_sync(0xffffffffu, v, 2);
+        v += __shfl_xor_sync(0xffffffffu, v, 4);
+        z[i][r] = v * scale2;
+        if (partial && !paged_visible(a.s, pos, end[r])) {
+          z[i][r] = -INFINITY;
+          hidden |= 1u << (i * R + r);
+        }
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      float top = m[r];
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) top = fmaxf(top, z[i][r]);
+      if (top > m[r]) {
+        const float keep = ex2_approx(m[r] - top);
+        m[r] = top;
+        l[r] *= keep;
+#pragma unroll
+        for (int c = 0; c < C; ++c) o[r][c].x *= keep, o[r][c].y *= keep, o[r][c].z *= keep, o[r][c].w *= keep;
+      }
+      const float ref = m[r] == -INFINITY ? 0.f : m[r];
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        z[i][r] = ex2_approx(z[i][r] - ref);
+        l[r] += z[i][r];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int key = 4 * i + group;
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const float4 v = *reinterpret_cast<const float4 *>(vbuf + chunk_at<kRowBytes>(key, u + 8 * c));
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          // a value that the row does not see is not touched: zero times NaN would be NaN
+          if (partial && ((hidden >> (i * R + r)) & 1)) continue;
+          o[r][c].x = fmaf(z[i][r], v.x, o[r][c].x);
+          o[r][c].y = fmaf(z[i][r], v.y, o[r][c].y);
+          o[r][c].z = fmaf(z[i][r], v.z, o[r][c].z);
+          o[r][c].w = fmaf(z[i][r], v.w, o[r][c].w);
+        }
+      }
+    }
+  }
+
+  __device__ void finish(const Item &it, float *out, float2 *ml) {
+    const int lane = threadIdx.x & 31, u = lane & 7;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      float top = m[r];
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+      const float w = m[r] == -INFINITY ? 0.f : ex2_approx(m[r] - top);
+      float sum = l[r] * w;
+      sum += __shfl_xor_sync(0xffffffffu, sum, 8);
+      sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        float v[4] = {o[r][c].x * w, o[r][c].y * w, o[r][c].z * w, o[r][c].w * w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          v[e] += __shfl_xor_sync(0xffffffffu, v[e], 8);
+          v[e] += __shfl_xor_sync(0xffffffffu, v[e], 16);
+        }
+        if (lane < 8 && r < it.rows)
+          *reinterpret_cast<float4 *>(out + r * D + 4 * (u + 8 * c)) = make_float4(v[0], v[1], v[2], v[3]);
+      }
+      if (lane == 0 && r < it.rows) ml[r] = make_float2(top, sum);
+    }
+  }
+};
+
+// ---------------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ void store4(float *p, const float4 &v) { *reinterpret_cast<float4 *>(p) = v; }
+__device__ __forceinline__ void store4(__nv_bfloat16 *p, const float4 &v) {
+  *reinterpret_cast<uint2 *>(p) = make_uint2(sm100::pack_bf16(v.x, v.y), sm100::pack_bf16(v.z, v.w));
+}
+
+// Sums of a finished row -> output and log-sum-exp.  A row that saw nothing has sum 0; a NaN stays one.
+template <typename T>
+__device__ __forceinline__ void write_row4(const Params &a, const Row &row, int d, float4 v, float top, float sum) {
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  v.x *= inv, v.y *= inv, v.z *= inv, v.w *= inv;
+  store4(reinterpret_cast<T *>(a.p.out) + row.n * a.p.out_stride[0] + row.h * a.p.out_stride[1] + d, v);
+  if (a.p.lse && d == 0) a.p.lse[row.n * a.p.Hq + row.h] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+}
+
+template <class Rows>
+struct Layout {
+  static constexpr int kSub = Rows::kKeys * Rows::kRowBytes;        // K or V of one stage of a warp
+  static constexpr int kRing = kStages * 2 * kSub;                  // of one warp; holds its sums at the item's end
+  static constexpr int kOffQ = kWarps * kRing;
+  static constexpr int kOffMl = kOffQ + Rows::kQBytes;
+  static constexpr int kOffMisc = kOffMl + kWarps * Rows::kRows * 8;
+  static constexpr int kBytes = kOffMisc + 64;
+  static constexpr int kTile = kWarps * Rows::kKeys;
+  static_assert(Rows::kRows * Rows::D * 4 <= kRing, "the ring is reused for the warp's sums");
+  static_assert(Rows::kCtas * (kBytes + 1024) <= 228 * 1024, "shared memory of the resident CTAs");
+};
+
+template <class Rows>
+__global__ void __launch_bounds__(kThreads, Rows::kCtas) attn_paged_kernel(const __grid_constant__ Params a) {
+  using T = typename Rows::T;
+  using L = Layout<Rows>;
+  constexpr int D = Rows::D;
+  extern __shared__ __align__(128) uint8_t smem[];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const ds_paged_params &p = a.p;
+  uint32_t flags = 0;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+  // ---- this CTA's range of the units, and the sequence that it begins in
+  auto sequence = [&](int b) {
+    const int lo = p.row_start ? p.row_start[b] : b * p.max_q, hi = p.row_start ? p.row_start[b + 1] : lo + p.max_q;
+    return paged_seq(a.s, lo, hi, p.kv_len[b]);
+  };
+  long long *scan = reinterpret_cast<long long *>(smem + L::kOffMisc);   // warp sums; then: prefix, sequence
+  const int chunk = (p.B + kThreads - 1) / kThreads;
+  const int b0 = min(p.B, tid * chunk), b1 = min(p.B, b0 + chunk);
+  long long mine = 0;
+  for (int b = b0; b < b1; ++b) {
+    const PagedSeq q = sequence(b);
+    if (q.bad) flags |= DS_DEV_INDEX;
+    mine += paged_units(a.s, q);
+  }
+  long long inc = mine;
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) {
+    const long long y = __shfl_up_sync(0xffffffffu, inc, off);
+    if (lane >= off) inc += y;
+  }
+  if (lane == 31) scan[warp] = inc;
+  __syncthreads();
+  long long total = 0, before = inc - mine;
+  for (int w = 0; w < kWarps; ++w) {
+    if (w < warp) before += scan[w];
+    total += scan[w];
+  }
+  __syncthreads();
+  const long long per = paged_per_cta(total, gridDim.x, kMinTiles);
+  long long t = blockIdx.x * per;
+  const long long t_end = min(total, t + per);
+  if (t < total && before <= t && t < before + mine) {
+    for (int b = b0; b < b1; ++b) {
+      const long long w = paged_units(a.s, sequence(b));
+      if (t < before + w) {
+        scan[0] = before;
+        scan[1] = b;
+        break;
+      }
+      before += w;
+    }
+  }
+  __syncthreads();
+  if (flags && p.status) atomicOr(p.status, flags);
+  flags = 0;
+  PagedJoin join = {0, 0, 0, 0, 0, 0};
+  long long base = scan[0];
+  int b = (int)scan[1];
+  __syncthreads();
+
+  uint8_t *ring = smem + warp * L::kRing;
+  float2 *ml_all = reinterpret_cast<float2 *>(smem + L::kOffMl);
+  const float scale2 = p.scale * kLog2e;
+  bool first_segment = true;
+  Item it;
+  it.b = b;
+  if (t < t_end) it.q = sequence(b);
+  while (t < t_end) {
+    while (t >= base + paged_units(a.s, it.q)) {
+      base += paged_units(a.s, it.q);
+      it.q = sequence(++it.b);
+    }
+    const long long u = t - base, item = u / it.q.tiles;
+    const int tile0 = (int)(u - item * it.q.tiles);
+    it.g = (int)(item / it.q.row_tiles);
+    it.row0 = (int)(item % it.q.row_tiles) * Rows::kRows;
+    it.rows = min(Rows::kRows, it.q.count * a.s.G - it.row0);
+    int n_tiles = it.q.tiles - tile0;
+    if (a.split) n_tiles = (int)min((long long)n_tiles, t_end - t);
+    else if (tile0 != 0) {       // the item belongs to the range that it begins in
+      t += n_tiles;
+      continue;
+    }
+    if (a.split && tile0 != 0 && first_segment && paged_join_starts(t, per, t - tile0)) {
+      join.parts = paged_join_parts(t, per, t - tile0 + it.q.tiles);
+      join.first_slot = paged_slot(blockIdx.x - 1, t - per == t - tile0);
+      join.row = it.row0, join.rows = it.rows, join.first = it.q.first, join.kv_head = it.g;
+    }
+
+    // ---- stream the keys
+    Rows rows;
+    rows.begin(a, it, smem + L::kOffQ);
+    constexpr int kChunks = Rows::kRowBytes / 16, kOps = Rows::kKeys * kChunks / 32;
+    const int32_t *table = p.block_table + it.b * p.table_stride;
+    const uint8_t *kbase = reinterpret_cast<const uint8_t *>(reinterpret_cast<const T *>(p.k_cache) + it.g * p.cache_stride[1]);
+    const uint8_t *vbase = reinterpret_cast<const uint8_t *>(reinterpret_cast<const T *>(p.v_cache) + it.g * p.cache_stride[1]);
+    const int x_first = tile0 * L::kTile + warp * Rows::kKeys;
+    // a lane looks up the cache row of key lane % kKeys, one stage ahead of its use
+    int pos = paged_key(it.q, x_first + lane % Rows::kKeys);
+    int page = pos >= 0 ? table[fast_div(pos, a.page_div)] : 0;
+    auto issue = [&](int i) {
+      long long at = -1;
+      if (pos >= 0) {
+        const int ok = paged_clamp_page(page, p.n_pages);
+        if (ok != page) flags |= DS_DEV_INDEX;
+        const int slot = pos - fast_div(pos, a.page_div) * p.page_size;
+        at = (ok * p.cache_stride[0] + slot * p.cache_stride[2]) * (long long)sizeof(T);
+      }
+      const uint32_t dst = sm100::smem_u32(ring + (i % kStages) * 2 * L::kSub);
+#pragma unroll
+      for (int j = 0; j < kOps; ++j) {
+        const int c = j * 32 + lane, r = c / kChunks, ch = c % kChunks;
+        const long long off = __shfl_sync(0xffffffffu, at, r);
+        const bool there = off >= 0;
+        const uint32_t to = dst + chunk_at<Rows::kRowBytes>(r, ch);
+        const long long from = (there ? off : 0) + 16 * ch;
+        cp_async16(to, kbase + from, there);
+        cp_async16(to + L::kSub, vbase + from, there);
+      }
+      if (i + 1 < n_tiles) {
+        pos = paged_key(it.q, x_first + (i + 1) * L::kTile + lane % Rows::kKeys);
+        page = pos >= 0 ? table[fast_div(pos, a.page_div)] : 0;
+      }
+    };
+#pragma unroll
+    for (int i = 0; i < kStages - 1; ++i) {
+      if (i < n_tiles) issue(i);
+      cp_async_commit();
+    }
+    for (int i = 0; i < n_tiles; ++i) {
+      cp_async_wait<kStages - 2>();
+      __syncwarp();      // stage i is there for the whole warp, and the warp is done with stage i - 1
+      if (i + kStages - 1 < n_tiles) issue(i + kStages - 1);
+      cp_async_commit();
+      uint8_t *stage = ring + (i % kStages) * 2 * L::kSub;
+      rows.step(a, it, stage, stage + L::kSub, x_first + i * L::kTile, scale2);
+    }
+    cp_async_wait<0>();
+    __syncwarp();
+
+    // ---- join the warps; the rings hold their sums
+    rows.finish(it, reinterpret_cast<float *>(ring), ml_all + warp * Rows::kRows);
+    __syncthreads();
+    const bool whole = tile0 == 0 && n_tiles == it.q.tiles;
+    const int slot = paged_slot(blockIdx.x, first_segment);
+    for (int e = tid; e < it.rows * (D / 4); e += kThreads) {
+      const int r = e / (D / 4), d = e % (D / 4) * 4;
+      float top = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) top = fmaxf(top, ml_all[w * Rows::kRows + r].x);
+      float sum = 0.f;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float2 ml = ml_all[w * Rows::kRows + r];
+        const float4 x = *reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(smem + w * L::kRing) + r * D + d);
+        const float f = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - top);
+        sum = fmaf(ml.y, f, sum);
+        v.x = fmaf(x.x, f, v.x), v.y = fmaf(x.y, f, v.y), v.z = fmaf(x.z, f, v.z), v.w = fmaf(x.w, f, v.w);
+      }
+      if (whole) {
+        write_row4<T>(a, row_of(a, it, r), d, v, top, sum);
+      } else {
+        const long long at = (long long)slot * Rows::kRows + r;
+        *reinterpret_cast<float4 *>(a.part_o + at * D + d) = v;
+        if (d == 0) a.part_ml[at] = make_float2(top, sum);
+      }
+    }
+    __syncthreads();
+    first_segment = false;
+    t += n_tiles;
+  }
+  if (a.split && tid == 0) a.joins[blockIdx.x] = join;
+  if (flags && p.status) atomicOr(p.status, flags);
+}
+
+// Joins the parts of one item: CTA = (range that begins inside the item first, stacked row).  The four warps take the parts
+// in turn and are themselves joined in order, so the result does not depend on timing.
+template <typename T, int D, int kRows>
+__global__ void __launch_bounds__(kThreads) attn_paged_join_kernel(const __grid_constant__ Params a) {
+  __shared__ float2 ml_s[kWarps];
+  __shared__ float o_s[kWarps][D];
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const PagedJoin j = a.joins[blockIdx.x];
+  const int r = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (r >= j.rows || j.parts == 0) return;
+  constexpr int E = D / 32;
+  auto at = [&](int k) { return (long long)(k == 0 ? j.first_slot : 2 * ((int)blockIdx.x + k - 1)) * kRows + r; };
+  float top = -INFINITY;
+  for (int k = lane; k < j.parts; k += 32) top = fmaxf(top, a.part_ml[at(k)].x);
+#pragma unroll
+  for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+  float sum = 0.f, o[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) o[e] = 0.f;
+#pragma unroll 4
+  for (int k = warp; k < j.parts; k += kWarps) {
+    const long long s = at(k);
+    const float2 ml = a.part_ml[s];
+    const float f = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - top);
+    sum = fmaf(ml.y, f, sum);
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = fmaf(a.part_o[s * D + e * 32 + lane], f, o[e]);
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e) o_s[warp][e * 32 + lane] = o[e];
+  if (lane == 0) ml_s[warp] = make_float2(top, sum);
+  __syncthreads();
+  const int d = threadIdx.x * 4;
+  if (d >= D) return;
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+  sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    sum += ml_s[w].y;
+    v.x += o_s[w][d], v.y += o_s[w][d + 1], v.z += o_s[w][d + 2], v.w += o_s[w][d + 3];
+  }
+  const int rr = j.row + r, i = fast_div(rr, a.group_div);
+  write_row4<T>(a, {(long long)j.first + i, j.kv_head * a.s.G + (rr - i * a.s.G), 0}, d, v, top, sum);
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+struct Shape {
+  PagedShape s;
+  int grid, tiles;      // tiles: most key tiles of an item
+  size_t bytes_joins, bytes_ml, bytes_o;
+};
+size_t up256(size_t x) { return (x + 255) & ~size_t(255); }
+
+template <class Rows>
+Shape shape_of(const ds_paged_params &p) {
+  using L = Layout<Rows>;
+  Shape h;
+  const int cap = p.max_pages * p.page_size;
+  h.s = {p.B, p.Hq / p.Hkv, p.Hkv, p.N, p.max_q, p.max_len > 0 && p.max_len < cap ? p.max_len : cap,
+         p.causal != 0, p.window, p.sinks, L::kTile, Rows::kRows};
+  // the most that the lengths may turn out to be
+  const PagedSeq q = paged_seq(h.s, 0, p.max_q < p.N ? p.max_q : p.N, h.s.bound);
+  h.tiles = q.tiles;
+  long long ranges = (paged_units(h.s, q) * p.B + kMinTiles - 1) / kMinTiles;
+  const long long resident = (long long)Rows::kCtas * sm_count();
+  h.grid = (int)(ranges < resident ? (ranges > 0 ? ranges : 1) : resident);
+  h.bytes_joins = up256(sizeof(PagedJoin) * (size_t)h.grid);
+  h.bytes_ml = up256(sizeof(float2) * 2 * (size_t)h.grid * Rows::kRows);
+  h.bytes_o = sizeof(float) * 2 * (size_t)h.grid * Rows::kRows * Rows::D;
+  return h;
+}
+
+template <class Rows>
+size_t workspace_of(const ds_paged_params &p) {
+  const Shape h = shape_of<Rows>(p);
+  return h.tiles <= kWholeTiles || h.grid == 1 ? 0 : h.bytes_joins + h.bytes_ml + h.bytes_o;
+}
+
+template <class Rows>
 int launch_rows(const ds_paged_params &p, cudaStream_t stream) {
-  const long long blocks = ((long long)p.max_q * p.Hq + kWarps - 1) / kWarps;
-  if (blocks > 0x7fffffffLL) return DS_ERR_UNSUPPORTED;
-  attn_paged_row_kernel<T, D><<<dim3((unsigned)blocks, p.B), kWarps * 32, 0, stream>>>(p);
+  using L = Layout<Rows>;
+  const Shape h = shape_of<Rows>(p);
+  Params a;
+  a.p = p;
+  a.s = h.s;
+  a.page_div = make_fast_div(p.page_size);
+  a.group_div = make_fast_div(h.s.G);
+  const size_t need = workspace_of<Rows>(p);
+  a.split = need > 0 && p.workspace && (reinterpret_cast<uintptr_t>(p.workspace) & 255) == 0 && p.workspace_bytes >= need;
+  uint8_t *ws = reinterpret_cast<uint8_t *>(p.workspace);
+  a.joins = reinterpret_cast<PagedJoin *>(ws);
+  a.part_ml = reinterpret_cast<float2 *>(ws + h.bytes_joins);
+  a.part_o = reinterpret_cast<float *>(ws + h.bytes_joins + h.bytes_ml);
+  DS_CUDA_OK(cudaFuncSetAttribute(attn_paged_kernel<Rows>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes));
+  attn_paged_kernel<Rows><<<h.grid, kThreads, L::kBytes, stream>>>(a);
   DS_CUDA_OK(cudaGetLastError());
+  note_launch(1);
+  if (!a.split) return DS_OK;
+  const int rows = (int)((long long)p.max_q * h.s.G < Rows::kRows ? (long long)p.max_q * h.s.G : Rows::kRows);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(h.grid, rows);
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  DS_CUDA_OK(cudaLaunchKernelEx(&cfg, attn_paged_join_kernel<typename Rows::T, Rows::D, Rows::kRows>, a));
   note_launch(1);
   return DS_OK;
 }
 
+// Calls f with the row engine for the call's type, head dimension and rows per KV head.  One block of 16 rows keeps
+// the queries in registers; more rows than 32 are served 32 at a time.
+template <class F>
+auto with_rows(const ds_paged_params &p, F f) {
+  const long long rows = (long long)p.max_q * (p.Hq / p.Hkv);
+  if (p.dtype == DS_BF16) {
+    if (p.D == 64) return rows <= 16 ? f(TensorRows<64, 1>()) : f(TensorRows<64, 2>());
+    return rows <= 16 ? f(TensorRows<128, 1>()) : f(TensorRows<128, 2>());
+  }
+  switch (p.D) {
+    case 32: return rows == 1 ? f(ScalarRows<32, 1>()) : f(ScalarRows<32, 8>());
+    case 64: return rows == 1 ? f(ScalarRows<64, 1>()) : f(ScalarRows<64, 8>());
+    case 128: return rows == 1 ? f(ScalarRows<128, 1>()) : f(ScalarRows<128, 4>());
+    default: return rows == 1 ? f(ScalarRows<256, 1>()) : f(ScalarRows<256, 2>());
+  }
+}
+
 }  // namespace
 
-size_t attn_paged_workspace_bytes(const ds_paged_params &) { return 0; }
+size_t attn_paged_workspace_bytes(const ds_paged_params &p) {
+  if (p.B == 0 || p.N == 0) return 0;
+  return with_rows(p, [&](auto rows) { return workspace_of<decltype(rows)>(p); });
+}
 
 int launch_attn_paged(const ds_paged_params &p, cudaStream_t stream) {
-  if (p.dtype == DS_BF16)
-    return p.D == 64 ? launch_rows<__nv_bfloat16, 64>(p, stream) : launch_rows<__nv_bfloat16, 128>(p, stream);
-  switch (p.D) {
-    case 32: return launch_rows<float, 32>(p, stream);
-    case 64: return launch_rows<float, 64>(p, stream);
-    case 128: return launch_rows<float, 128>(p, stream);
-    default: return launch_rows<float, 256>(p, stream);
-  }
+  return with_rows(p, [&](auto rows) { return launch_rows<decltype(rows)>(p, stream); });
 }
 
 }  // namespace ds
