@@ -549,7 +549,7 @@ DS_API int ds_qk_norm_rope(const ds_qk_params *p, void *stream);
  * not an error; it runs unsplit.  Calls that may overlap must not share a workspace.
  * Errors: DS_ERR_INVALID_ARG (NULL or misaligned pointer, misaligned stride, Hq % Hkv != 0, window or sinks < 0, max_q < 1,
  * scale not finite, row_start == NULL with B * max_q > N, table_stride < max_pages); DS_ERR_UNSUPPORTED (D outside the
- * envelope, B > 8192, max_q * Hq / Hkv >= 2^30, max_pages * page_size or n_pages * page_size > 2^31 - 1). */
+ * envelope, B > 8192, max_q * Hq * max_len / 16 beyond 2^31, max_pages * page_size or n_pages * page_size > 2^31 - 1). */
 typedef struct {
   int32_t B, Hq, Hkv, D;
   int32_t dtype;

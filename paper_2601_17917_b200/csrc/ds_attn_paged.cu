@@ -492,75 +492,109 @@ __global__ void __launch_bounds__(kThreads, Rows::kCtas) attn_paged_kernel(const
     const int lo = p.row_start ? p.row_start[b] : b * p.max_q, hi = p.row_start ? p.row_start[b + 1] : lo + p.max_q;
     return paged_seq(a.s, lo, hi, p.kv_len[b]);
   };
-  long long *scan = reinterpret_cast<long long *>(smem + L::kOffMisc);   // warp sums; then: prefix, sequence
-  const int chunk = (p.B + kThreads - 1) / kThreads;
-  const int b0 = min(p.B, tid * chunk), b1 = min(p.B, b0 + chunk);
-  long long mine = 0;
-  for (int b = b0; b < b1; ++b) {
-    const PagedSeq q = sequence(b);
-    if (q.bad) flags |= DS_DEV_INDEX;
-    mine += paged_units(a.s, q);
-  }
-  long long inc = mine;
+  long long total, per, t, t_end, base;
+  Item it;
+  it.b = 0;
+  auto range = [&]() {
+    per = paged_per_cta(total, gridDim.x, kMinTiles);
+    t = blockIdx.x * per;
+    t_end = min(total, t + per);
+  };
+  auto warp_scan = [&](long long inc) {
 #pragma unroll
-  for (int off = 1; off < 32; off <<= 1) {
-    const long long y = __shfl_up_sync(0xffffffffu, inc, off);
-    if (lane >= off) inc += y;
-  }
-  if (lane == 31) scan[warp] = inc;
-  __syncthreads();
-  long long total = 0, before = inc - mine;
-  for (int w = 0; w < kWarps; ++w) {
-    if (w < warp) before += scan[w];
-    total += scan[w];
-  }
-  __syncthreads();
-  const long long per = paged_per_cta(total, gridDim.x, kMinTiles);
-  long long t = blockIdx.x * per;
-  const long long t_end = min(total, t + per);
-  if (t < total && before <= t && t < before + mine) {
-    for (int b = b0; b < b1; ++b) {
-      const long long w = paged_units(a.s, sequence(b));
-      if (t < before + w) {
-        scan[0] = before;
-        scan[1] = b;
-        break;
-      }
-      before += w;
+    for (int off = 1; off < 32; off <<= 1) {
+      const long long y = __shfl_up_sync(0xffffffffu, inc, off);
+      if (lane >= off) inc += y;
     }
+    return inc;
+  };
+  if (p.B <= 32) {      // every warp for itself
+    long long mine = 0;
+    if (lane < p.B) {
+      const PagedSeq q = sequence(lane);
+      if (q.bad) flags |= DS_DEV_INDEX;
+      mine = paged_units(a.s, q);
+    }
+    const long long inc = warp_scan(mine);
+    total = __shfl_sync(0xffffffffu, inc, 31);
+    range();
+    const uint32_t here = __ballot_sync(0xffffffffu, t < inc);      // inclusive sums: the first above t
+    const int src = here ? __ffs(here) - 1 : 0;
+    base = __shfl_sync(0xffffffffu, inc - mine, src);
+    it.b = src;
+  } else {
+    long long *scan = reinterpret_cast<long long *>(smem + L::kOffMisc);   // warp sums, then prefix and number
+    const int chunk = (p.B + kThreads - 1) / kThreads;
+    const int b0 = min(p.B, tid * chunk), b1 = min(p.B, b0 + chunk);
+    long long mine = 0;
+    for (int b = b0; b < b1; ++b) {
+      const PagedSeq q = sequence(b);
+      if (q.bad) flags |= DS_DEV_INDEX;
+      mine += paged_units(a.s, q);
+    }
+    const long long inc = warp_scan(mine);
+    if (lane == 31) scan[warp] = inc;
+    __syncthreads();
+    total = 0;
+    long long before = inc - mine;
+    for (int w = 0; w < kWarps; ++w) {
+      if (w < warp) before += scan[w];
+      total += scan[w];
+    }
+    range();
+    __syncthreads();
+    if (t < total && before <= t && t < before + mine) {
+      for (int b = b0; b < b1; ++b) {
+        const long long w = paged_units(a.s, sequence(b));
+        if (t < before + w) {
+          scan[0] = before;
+          scan[1] = b;
+          break;
+        }
+        before += w;
+      }
+    }
+    __syncthreads();
+    base = scan[0];
+    if (t < t_end) it.b = (int)scan[1];
   }
-  __syncthreads();
   if (flags && p.status) atomicOr(p.status, flags);
   flags = 0;
-  PagedJoin join = {0, 0, 0, 0, 0, 0};
-  long long base = scan[0];
-  int b = (int)scan[1];
-  __syncthreads();
+  PagedJoin join = {0, 0, 0, 0, 0, 0};      // thread 0's
 
   uint8_t *ring = smem + warp * L::kRing;
   float2 *ml_all = reinterpret_cast<float2 *>(smem + L::kOffMl);
   const float scale2 = p.scale * kLog2e;
   bool first_segment = true;
-  Item it;
-  it.b = b;
-  if (t < t_end) it.q = sequence(b);
+  int tile0 = 0, row_tile = 0;
+  if (t < t_end) {      // the one place that needs divisions: afterwards items follow one another
+    it.q = sequence(it.b);
+    const uint32_t u = (uint32_t)(t - base), item = u / (uint32_t)it.q.tiles;
+    tile0 = (int)(u - item * (uint32_t)it.q.tiles);
+    it.g = (int)(item / (uint32_t)it.q.row_tiles);
+    row_tile = (int)(item - it.g * (uint32_t)it.q.row_tiles);
+  }
+  auto next_item = [&]() {
+    tile0 = 0;
+    if (++row_tile < it.q.row_tiles) return;
+    row_tile = 0;
+    if (++it.g < p.Hkv) return;
+    it.g = 0;
+    if (t < t_end) do it.q = sequence(++it.b);
+      while (it.q.tiles == 0);
+  };
   while (t < t_end) {
-    while (t >= base + paged_units(a.s, it.q)) {
-      base += paged_units(a.s, it.q);
-      it.q = sequence(++it.b);
-    }
-    const long long u = t - base, item = u / it.q.tiles;
-    const int tile0 = (int)(u - item * it.q.tiles);
-    it.g = (int)(item / it.q.row_tiles);
-    it.row0 = (int)(item % it.q.row_tiles) * Rows::kRows;
+    it.row0 = row_tile << a.s.row_log2;
     it.rows = min(Rows::kRows, it.q.count * a.s.G - it.row0);
     int n_tiles = it.q.tiles - tile0;
-    if (a.split) n_tiles = (int)min((long long)n_tiles, t_end - t);
-    else if (tile0 != 0) {       // the item belongs to the range that it begins in
+    if (a.split) {
+      n_tiles = (int)min((long long)n_tiles, t_end - t);
+    } else if (tile0 != 0) {       // the item belongs to the range that it begins in
       t += n_tiles;
+      next_item();
       continue;
     }
-    if (a.split && tile0 != 0 && first_segment && paged_join_starts(t, per, t - tile0)) {
+    if (a.split && tid == 0 && tile0 != 0 && first_segment && paged_join_starts(t, per, t - tile0)) {
       join.parts = paged_join_parts(t, per, t - tile0 + it.q.tiles);
       join.first_slot = paged_slot(blockIdx.x - 1, t - per == t - tile0);
       join.row = it.row0, join.rows = it.rows, join.first = it.q.first, join.kv_head = it.g;
@@ -648,54 +682,58 @@ __global__ void __launch_bounds__(kThreads, Rows::kCtas) attn_paged_kernel(const
     __syncthreads();
     first_segment = false;
     t += n_tiles;
+    next_item();
   }
   if (a.split && tid == 0) a.joins[blockIdx.x] = join;
   if (flags && p.status) atomicOr(p.status, flags);
 }
 
-// Joins the parts of one item: CTA = (range that begins inside the item first, stacked row).  The four warps take the parts
-// in turn and are themselves joined in order, so the result does not depend on timing.
+// Joins the parts of one item: CTA = (range that begins inside the item first, stacked row).  D / 4 threads hold the
+// row, the CTA's groups of so many threads take the parts in turn, eight loads in flight each, and are themselves joined
+// in order: the result does not depend on timing.
+constexpr int kJoinThreads = 256;
 template <typename T, int D, int kRows>
-__global__ void __launch_bounds__(kThreads) attn_paged_join_kernel(const __grid_constant__ Params a) {
-  __shared__ float2 ml_s[kWarps];
-  __shared__ float o_s[kWarps][D];
+__global__ void __launch_bounds__(kJoinThreads) attn_paged_join_kernel(const __grid_constant__ Params a) {
+  constexpr int kLanes = D / 4, kGroups = kJoinThreads / kLanes;
+  __shared__ float4 o_s[kGroups][kLanes];
+  __shared__ float sum_s[kGroups], top_s[kJoinThreads / 32];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const PagedJoin j = a.joins[blockIdx.x];
-  const int r = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int r = blockIdx.y, tid = threadIdx.x, group = tid / kLanes, u = tid % kLanes;
   if (r >= j.rows || j.parts == 0) return;
-  constexpr int E = D / 32;
   auto at = [&](int k) { return (long long)(k == 0 ? j.first_slot : 2 * ((int)blockIdx.x + k - 1)) * kRows + r; };
   float top = -INFINITY;
-  for (int k = lane; k < j.parts; k += 32) top = fmaxf(top, a.part_ml[at(k)].x);
+  for (int k = tid; k < j.parts; k += kJoinThreads) top = fmaxf(top, a.part_ml[at(k)].x);
 #pragma unroll
   for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-  float sum = 0.f, o[E];
+  if ((tid & 31) == 0) top_s[tid >> 5] = top;
+  __syncthreads();
 #pragma unroll
-  for (int e = 0; e < E; ++e) o[e] = 0.f;
-#pragma unroll 4
-  for (int k = warp; k < j.parts; k += kWarps) {
+  for (int w = 0; w < kJoinThreads / 32; ++w) top = fmaxf(top, top_s[w]);
+  float sum = 0.f;
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+  for (int k = group; k < j.parts; k += kGroups) {
     const long long s = at(k);
     const float2 ml = a.part_ml[s];
+    const float4 x = *reinterpret_cast<const float4 *>(a.part_o + s * D + 4 * u);
     const float f = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - top);
     sum = fmaf(ml.y, f, sum);
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = fmaf(a.part_o[s * D + e * 32 + lane], f, o[e]);
+    v.x = fmaf(x.x, f, v.x), v.y = fmaf(x.y, f, v.y), v.z = fmaf(x.z, f, v.z), v.w = fmaf(x.w, f, v.w);
   }
-#pragma unroll
-  for (int e = 0; e < E; ++e) o_s[warp][e * 32 + lane] = o[e];
-  if (lane == 0) ml_s[warp] = make_float2(top, sum);
+  o_s[group][u] = v;
+  if (u == 0) sum_s[group] = sum;
   __syncthreads();
-  const int d = threadIdx.x * 4;
-  if (d >= D) return;
-  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-  sum = 0.f;
+  if (tid >= kLanes) return;
 #pragma unroll
-  for (int w = 0; w < kWarps; ++w) {
-    sum += ml_s[w].y;
-    v.x += o_s[w][d], v.y += o_s[w][d + 1], v.z += o_s[w][d + 2], v.w += o_s[w][d + 3];
+  for (int w = 1; w < kGroups; ++w) {
+    const float4 x = o_s[w][u];
+    v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
   }
+  sum = 0.f;
+  for (int w = 0; w < kGroups; ++w) sum += sum_s[w];
   const int rr = j.row + r, i = fast_div(rr, a.group_div);
-  write_row4<T>(a, {(long long)j.first + i, j.kv_head * a.s.G + (rr - i * a.s.G), 0}, d, v, top, sum);
+  write_row4<T>(a, {(long long)j.first + i, j.kv_head * a.s.G + (rr - i * a.s.G), 0}, 4 * u, v, top, sum);
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -704,6 +742,7 @@ struct Shape {
   int grid, tiles;      // tiles: most key tiles of an item
   size_t bytes_joins, bytes_ml, bytes_o;
 };
+constexpr int log2_of(int x) { return x <= 1 ? 0 : 1 + log2_of(x / 2); }
 size_t up256(size_t x) { return (x + 255) & ~size_t(255); }
 
 template <class Rows>
@@ -712,7 +751,7 @@ Shape shape_of(const ds_paged_params &p) {
   Shape h;
   const int cap = p.max_pages * p.page_size;
   h.s = {p.B, p.Hq / p.Hkv, p.Hkv, p.N, p.max_q, p.max_len > 0 && p.max_len < cap ? p.max_len : cap,
-         p.causal != 0, p.window, p.sinks, L::kTile, Rows::kRows};
+         p.causal != 0, p.window, p.sinks, log2_of(L::kTile), log2_of(Rows::kRows)};
   // the most that the lengths may turn out to be
   const PagedSeq q = paged_seq(h.s, 0, p.max_q < p.N ? p.max_q : p.N, h.s.bound);
   h.tiles = q.tiles;
@@ -754,7 +793,7 @@ int launch_rows(const ds_paged_params &p, cudaStream_t stream) {
   const int rows = (int)((long long)p.max_q * h.s.G < Rows::kRows ? (long long)p.max_q * h.s.G : Rows::kRows);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(h.grid, rows);
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(kJoinThreads);
   cfg.stream = stream;
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;

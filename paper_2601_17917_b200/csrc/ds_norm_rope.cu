@@ -1,21 +1,25 @@
 // ds_qk_norm_rope: RMS norm of every query and key head, rotary position, and the write of K and V into the pages,
 // in one pass over the projection's output.
 //
-// Bound by HBM: every element is read once and written once.  A warp owns one row and walks over its heads (a share of
-// them when there are few rows), W = 8, 16 or 32 lanes per head.  Lane u of a head holds eight elements in two
-// chunks of four, chosen so that both members of its rotary pairs 4u .. 4u + 3 are its own: d and d + R/2 in the half
-// layout, 8u .. 8u + 7 when interleaved.  The rotation then needs no exchange, the norm a few shuffles, and the four
-// sines and cosines of a lane serve all heads of the row.  The loads of four heads are in flight at once.
+// Bound by HBM, and close to being bound by instructions: every element is read once and written once, 4 bytes in bf16
+// for some 25 instructions per 8 elements.  A warp owns one row and walks over its heads (a share of them when there are
+// few rows), W = 8, 16 or 32 lanes per head.  Lane u of a head holds eight elements in two chunks of four, chosen so that
+// both members of its rotary pairs 4u .. 4u + 3 are its own: d and d + R/2 in the half layout, 8u .. 8u + 7 when
+// interleaved.  The rotation then needs no exchange and the norm a few shuffles.  Weight, sine and cosine are
+// multiplied once per row into two factors per element, out = r (x P + partner Q), which serve all its heads; the
+// products are two wide (fma.rn.f32x2).  The loads of four steps are in flight at once.
 // The phase of a pair is position * turn in integers modulo 2^64: exact for every position, and its top 32 bits are an
 // angle in [-1/2, 1/2) turns, which sincospif takes without a range reduction.
+#include <type_traits>
+
 #include "ds_common.cuh"
 #include "ds_paged_index.cuh"
 
 namespace ds {
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kBatch = 4;   // heads per lane group whose loads are in flight together
+constexpr int kThreads = 128, kWarps = kThreads / 32;
+constexpr int kBatch = 4;   // steps (a head per lane group) whose loads are in flight together
 
 // Four elements as they lie in memory.
 template <typename T>
@@ -28,20 +32,51 @@ template <>
 struct Raw4<__nv_bfloat16> {
   using type = uint2;
 };
-__device__ __forceinline__ void unpack4(const float4 &w, float *f) { f[0] = w.x, f[1] = w.y, f[2] = w.z, f[3] = w.w; }
-__device__ __forceinline__ void unpack4(const uint2 &w, float *f) {
-  f[0] = bf16lo_to_f32(w.x), f[1] = bf16hi_to_f32(w.x), f[2] = bf16lo_to_f32(w.y), f[3] = bf16hi_to_f32(w.y);
+// Two fp32 values side by side.
+using F2 = unsigned long long;
+__device__ __forceinline__ F2 f2(float lo, float hi) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
 }
-__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
-  const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+__device__ __forceinline__ float2 f2_get(F2 x) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
+  return r;
+}
+__device__ __forceinline__ F2 f2_swap(F2 x) {
+  const float2 v = f2_get(x);
+  return f2(v.y, v.x);
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ void unpack4(const float4 &w, F2 *f) { f[0] = f2(w.x, w.y), f[1] = f2(w.z, w.w); }
+__device__ __forceinline__ void unpack4(const uint2 &w, F2 *f) {
+  f[0] = f2(bf16lo_to_f32(w.x), bf16hi_to_f32(w.x)), f[1] = f2(bf16lo_to_f32(w.y), bf16hi_to_f32(w.y));
+}
+__device__ __forceinline__ uint32_t pack2(F2 x) {
+  const float2 f = f2_get(x);
+  const __nv_bfloat162 v = __floats2bfloat162_rn(f.x, f.y);
   return *reinterpret_cast<const uint32_t *>(&v);
 }
-__device__ __forceinline__ void pack4(const float *f, float4 &w) { w = make_float4(f[0], f[1], f[2], f[3]); }
-__device__ __forceinline__ void pack4(const float *f, uint2 &w) { w = make_uint2(pack2(f[0], f[1]), pack2(f[2], f[3])); }
+__device__ __forceinline__ void pack4(const F2 *f, float4 &w) {
+  const float2 a = f2_get(f[0]), b = f2_get(f[1]);
+  w = make_float4(a.x, a.y, b.x, b.y);
+}
+__device__ __forceinline__ void pack4(const F2 *f, uint2 &w) { w = make_uint2(pack2(f[0]), pack2(f[1])); }
 
 struct Launch {
   int chunks, heads_per_warp;   // units of a row, heads of a unit (a multiple of 32 / W)
   FastDiv chunk_div, page_div;
+  float inv_d;
 };
 
 template <typename T, int W, bool kInterleaved>
@@ -86,78 +121,105 @@ __global__ void __launch_bounds__(kThreads) norm_rope_kernel(const __grid_consta
     }
   }
 
-  for (int h0 = h_begin; h0 < h_end; h0 += kBatch * kGroups) {
-    Raw a[kBatch], b[kBatch];
+  // Heads lo .. hi - 1 of one of the three tensors.
+  enum { kQ, kK, kV };
+  auto walk = [&](auto kind, int lo, int hi, const T *src, long long src_step, const T *weight, T *dst, long long dst_step, T *dst2,
+                  long long dst2_step) {
+    constexpr int kKind = decltype(kind)::value;
+    if (lo >= hi) return;
+    F2 P[4], Q[4];
+    if (kKind != kV && live) {
+      float w[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+      if (weight) {
+        F2 x[4];
+        unpack4(*reinterpret_cast<const Raw *>(weight + da), x);
+        unpack4(*reinterpret_cast<const Raw *>(weight + db), x + 2);
 #pragma unroll
-    for (int i = 0; i < kBatch; ++i) {
-      const int hh = h0 + i * kGroups + group;
-      if (hh < h_end && live) {
-        const bool is_q = hh < p.Hq, is_v = hh >= p.Hq + p.Hkv;
-        const int h = is_q ? hh : hh - p.Hq - (is_v ? p.Hkv : 0);
-        const T *src = reinterpret_cast<const T *>(is_q ? p.q : is_v ? p.v : p.k) +
-                       (is_q ? n * p.q_stride[0] + h * p.q_stride[1] : n * p.kv_stride[0] + h * p.kv_stride[1]);
-        a[i] = *reinterpret_cast<const Raw *>(src + da);
-        b[i] = *reinterpret_cast<const Raw *>(src + db);
-      } else {
-        a[i] = Raw{}, b[i] = Raw{};
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < kBatch; ++i) {
-      const int hh = h0 + i * kGroups + group;
-      if (h0 + i * kGroups >= h_end) break;      // the whole warp
-      const bool is_q = hh < p.Hq, is_v = hh >= p.Hq + p.Hkv;
-      const int h = is_q ? hh : hh - p.Hq - (is_v ? p.Hkv : 0);
-      const T *weight = is_v ? nullptr : reinterpret_cast<const T *>(is_q ? p.q_weight : p.k_weight);
-      float x[8];
-      unpack4(a[i], x);
-      unpack4(b[i], x + 4);
-      float ss = 0.f;
-#pragma unroll
-      for (int k = 0; k < 8; ++k) ss = fmaf(x[k], x[k], ss);
-#pragma unroll
-      for (int o = W / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-      if (hh >= h_end || !live) continue;
-      if (!is_v) {
-        if (weight) {
-          const float r = rsqrtf(ss / (float)D + p.eps);
-          float w[8];
-          unpack4(*reinterpret_cast<const Raw *>(weight + da), w);
-          unpack4(*reinterpret_cast<const Raw *>(weight + db), w + 4);
-#pragma unroll
-          for (int k = 0; k < 8; ++k) x[k] = x[k] * r * w[k];
+        for (int j = 0; j < 4; ++j) {
+          const float2 v = f2_get(x[j]);
+          w[2 * j] = v.x, w[2 * j + 1] = v.y;
         }
-        if (rotated) {
+      }
+      float pf[8], qf[8];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            float &lo = kInterleaved ? x[2 * k] : x[k], &hi = kInterleaved ? x[2 * k + 1] : x[k + 4];
-            const float y = fmaf(hi, cs[k], lo * sn[k]);
-            lo = fmaf(lo, cs[k], -hi * sn[k]);
-            hi = y;
+      for (int i = 0; i < 4; ++i) {
+        const int l = kInterleaved ? 2 * i : i, h = kInterleaved ? 2 * i + 1 : i + 4;
+        pf[l] = w[l] * cs[i], qf[l] = -w[h] * sn[i];
+        pf[h] = w[h] * cs[i], qf[h] = w[l] * sn[i];
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) P[j] = f2(pf[2 * j], pf[2 * j + 1]), Q[j] = f2(qf[2 * j], qf[2 * j + 1]);
+    }
+    src += (long long)(lo + group) * src_step;
+    if (dst) dst += (long long)(lo + group) * dst_step;
+    if (dst2) dst2 += (long long)(lo + group) * dst2_step;
+    int left = hi - lo - group;      // of this lane group, in heads: > 0 while it has one
+    if (!live) left = 0;
+    for (int h0 = lo; h0 < hi; h0 += kBatch * kGroups) {
+      Raw a[kBatch], b[kBatch];
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        a[i] = Raw{}, b[i] = Raw{};
+        if (i * kGroups < left) {
+          a[i] = *reinterpret_cast<const Raw *>(src + i * kGroups * src_step + da);
+          b[i] = *reinterpret_cast<const Raw *>(src + i * kGroups * src_step + db);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        if (h0 + i * kGroups >= hi) break;      // the whole warp
+        Raw oa = a[i], ob = b[i];               // V: bits as they are
+        if constexpr (kKind != kV) {
+          F2 x[4];
+          unpack4(oa, x);
+          unpack4(ob, x + 2);
+          if (weight) {
+            const float2 t = f2_get(fma2(x[3], x[3], fma2(x[2], x[2], fma2(x[1], x[1], mul2(x[0], x[0])))));
+            float ss = t.x + t.y;
+#pragma unroll
+            for (int o = W / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+            const float r = rsqrtf(fmaf(ss, launch.inv_d, p.eps));
+            const F2 r2 = f2(r, r);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = mul2(x[j], r2);
+          }
+          F2 y[4];
+          if (rotated) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) y[j] = fma2(x[j], P[j], mul2(kInterleaved ? f2_swap(x[j]) : x[j ^ 2], Q[j]));
+          } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) y[j] = mul2(x[j], P[j]);
+          }
+          pack4(y, oa);
+          pack4(y + 2, ob);
+        }
+        if (i * kGroups < left) {
+          if (kKind == kQ || dst) {
+            *reinterpret_cast<Raw *>(dst + i * kGroups * dst_step + da) = oa;
+            *reinterpret_cast<Raw *>(dst + i * kGroups * dst_step + db) = ob;
+          }
+          if (kKind != kQ && dst2) {
+            *reinterpret_cast<Raw *>(dst2 + i * kGroups * dst2_step + da) = oa;
+            *reinterpret_cast<Raw *>(dst2 + i * kGroups * dst2_step + db) = ob;
           }
         }
       }
-      Raw oa, ob;
-      if (is_v) oa = a[i], ob = b[i];      // bits as they are
-      else pack4(x, oa), pack4(x + 4, ob);
-      if (is_q) {
-        T *dst = reinterpret_cast<T *>(p.q_out) + n * p.q_out_stride[0] + h * p.q_out_stride[1];
-        *reinterpret_cast<Raw *>(dst + da) = oa;
-        *reinterpret_cast<Raw *>(dst + db) = ob;
-        continue;
-      }
-      if (p.k_out) {
-        T *dst = reinterpret_cast<T *>(is_v ? p.v_out : p.k_out) + n * p.kv_out_stride[0] + h * p.kv_out_stride[1];
-        *reinterpret_cast<Raw *>(dst + da) = oa;
-        *reinterpret_cast<Raw *>(dst + db) = ob;
-      }
-      if (at >= 0) {
-        T *dst = reinterpret_cast<T *>(is_v ? p.v_cache : p.k_cache) + at + h * p.cache_stride[1];
-        *reinterpret_cast<Raw *>(dst + da) = oa;
-        *reinterpret_cast<Raw *>(dst + db) = ob;
-      }
+      constexpr int kStep = kBatch * kGroups;
+      src += kStep * src_step, left -= kStep;
+      if (kKind == kQ || dst) dst += kStep * dst_step;
+      if (kKind != kQ && dst2) dst2 += kStep * dst2_step;
     }
-  }
+  };
+  auto in = [&](const void *t, long long off) { return reinterpret_cast<const T *>(t) + off; };
+  auto out = [&](void *t, long long off) { return t && off >= 0 ? reinterpret_cast<T *>(t) + off : nullptr; };
+  walk(std::integral_constant<int, kQ>(), h_begin, min(h_end, p.Hq), in(p.q, n * p.q_stride[0]), p.q_stride[1],
+       reinterpret_cast<const T *>(p.q_weight), out(p.q_out, n * p.q_out_stride[0]), p.q_out_stride[1], nullptr, 0);
+  walk(std::integral_constant<int, kK>(), max(h_begin - p.Hq, 0), min(h_end - p.Hq, p.Hkv), in(p.k, n * p.kv_stride[0]),
+       p.kv_stride[1], reinterpret_cast<const T *>(p.k_weight), out(p.k_out, n * p.kv_out_stride[0]), p.kv_out_stride[1],
+       out(p.k_cache, at), p.cache_stride[1]);
+  walk(std::integral_constant<int, kV>(), max(h_begin - p.Hq - p.Hkv, 0), h_end - p.Hq - p.Hkv, in(p.v, n * p.kv_stride[0]),
+       p.kv_stride[1], nullptr, out(p.v_out, n * p.kv_out_stride[0]), p.kv_out_stride[1], out(p.v_cache, at), p.cache_stride[1]);
 }
 
 template <typename T, int W>
@@ -172,6 +234,7 @@ int launch_width(const ds_qk_params &p, cudaStream_t stream) {
   l.heads_per_warp = (int)((steps + chunks - 1) / chunks) * kGroups;
   l.chunks = (heads + l.heads_per_warp - 1) / l.heads_per_warp;
   l.chunk_div = make_fast_div(l.chunks);
+  l.inv_d = 1.f / (float)p.D;
   l.page_div = make_fast_div(p.page_size > 0 ? p.page_size : 1);
   if ((long long)p.N * l.chunks > 0x7fffffffLL) return DS_ERR_UNSUPPORTED;      // needs more than 400000 heads
   const long long blocks = ((long long)p.N * l.chunks + kWarps - 1) / kWarps;

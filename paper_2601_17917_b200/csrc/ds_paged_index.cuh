@@ -37,9 +37,11 @@ struct PagedShape {
   int B, G, Hkv, N, max_q;   // G = query heads per KV head
   int bound;                 // most cache rows of a sequence: min(max_len, max_pages * page_size)
   int causal, window, sinks;
-  int tile;                  // keys per unit of work (a CTA's warps take equal parts of it)
-  int row_tile;              // stacked rows (query, head of the group) per unit of work
+  int tile_log2;             // keys per unit of work (a CTA's warps take equal parts of it)
+  int row_log2;              // stacked rows (query, head of the group) per unit of work
 };
+DS_HD int paged_ceil_shift(int x, int log2) { return (int)(((unsigned)x + (1u << log2) - 1u) >> log2); }
+
 
 // One sequence.  Its queries see cache rows [0, sink_n) and [body, len) between them.  The keys are numbered x: the
 // first sink_n rows, padding to a whole tile, then the body.
@@ -65,12 +67,12 @@ DS_HD PagedSeq paged_seq(const PagedShape &s, int row_lo, int row_hi, int len) {
     q.sink_n = q.sink_pad = q.body = 0;
   } else {
     q.sink_n = s.sinks;
-    q.sink_pad = (s.sinks + s.tile - 1) / s.tile * s.tile;
+    q.sink_pad = paged_ceil_shift(s.sinks, s.tile_log2) << s.tile_log2;
     q.body = lo;
   }
-  q.row_tiles = (int)(((int64_t)q.count * s.G + s.row_tile - 1) / s.row_tile);
+  q.row_tiles = paged_ceil_shift(q.count * s.G, s.row_log2);      // max_q G < 2^30
   // a sequence with queries has at least one unit, even when they see nothing: their outputs are written
-  q.tiles = q.count == 0 ? 0 : paged_max(1, q.sink_pad / s.tile + (int)(((int64_t)q.len - q.body + s.tile - 1) / s.tile));
+  q.tiles = q.count == 0 ? 0 : paged_max(1, (q.sink_pad >> s.tile_log2) + paged_ceil_shift(q.len - q.body, s.tile_log2));
   return q;
 }
 DS_HD int64_t paged_units(const PagedShape &s, const PagedSeq &q) { return (int64_t)q.row_tiles * s.Hkv * q.tiles; }
@@ -78,8 +80,7 @@ DS_HD int64_t paged_units(const PagedShape &s, const PagedSeq &q) { return (int6
 // Cache row of key x, -1 for padding.
 DS_HD int paged_key(const PagedSeq &q, int x) {
   if (x < q.sink_pad) return x < q.sink_n ? x : -1;
-  const int t = q.body + (x - q.sink_pad);
-  return t < q.len ? t : -1;
+  return x - q.sink_pad < q.len - q.body ? q.body + (x - q.sink_pad) : -1;
 }
 DS_HD bool paged_visible(const PagedShape &s, int t, int end) {
   return t >= 0 && t < end && (s.window == 0 || t < s.sinks || t >= end - s.window);
@@ -87,15 +88,17 @@ DS_HD bool paged_visible(const PagedShape &s, int t, int end) {
 // Every one of the n keys from x on is there and seen by every query.
 DS_HD bool paged_all_visible(const PagedShape &s, const PagedSeq &q, int x, int n) {
   if (x < q.sink_pad) return x + n <= q.sink_n;
+  if (x - q.sink_pad > q.len - q.body - n) return false;
   const int t = q.body + (x - q.sink_pad);
-  return t + n <= q.end_min && (s.window == 0 || t >= q.end_max - s.window);
+  return t <= q.end_min - n && (s.window == 0 || t >= q.end_max - s.window);
 }
 
 // The work of a call, `total` units in the order sequence, KV head, row tile, key tile, cut into ranges of `per` units
 // for the CTAs.  An item (all key tiles of a sequence, KV head and row tile) may lie in several ranges; unsplit, the
 // range that an item begins in takes it whole.
 DS_HD int64_t paged_per_cta(int64_t total, int n_ctas, int min_tiles) {
-  const int64_t per = (total + n_ctas - 1) / n_ctas;
+  const int64_t up = total + n_ctas - 1;
+  const int64_t per = up >> 32 ? up / n_ctas : (int64_t)((uint32_t)up / (uint32_t)n_ctas);   // short division where it does
   return per > min_tiles ? per : min_tiles;
 }
 
@@ -109,7 +112,8 @@ struct PagedJoin {
 // `t0`: this CTA's first unit, inside an item that begins at `item` < t0 and ends before `item_end`.
 DS_HD bool paged_join_starts(int64_t t0, int64_t per, int64_t item) { return t0 - per <= item; }
 DS_HD int paged_join_parts(int64_t t0, int64_t per, int64_t item_end) {
-  return 2 + (int)((item_end - 1) / per - t0 / per);
+  const int64_t rest = item_end - 1 - t0;      // t0 is a multiple of per
+  return 2 + (rest < per ? 0 : rest >> 32 || per >> 32 ? (int)(rest / per) : (int)((uint32_t)rest / (uint32_t)per));
 }
 // A CTA writes the part of the item that its range begins with to slot 2c, that of the item it ends with to 2c + 1.
 DS_HD int paged_slot(int cta, bool first_segment) { return 2 * cta + (first_segment ? 0 : 1); }

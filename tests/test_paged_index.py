@@ -44,7 +44,8 @@ static void shapes() {
     s.B = in(1, 6), s.G = in(1, 8), s.Hkv = in(1, 3), s.max_q = in(1, 5) * (in(0, 3) ? 1 : 9);
     s.N = in(0, s.B * s.max_q), s.bound = in(1, 500), s.causal = in(0, 1);
     s.window = in(0, 2) ? 0 : in(1, 200), s.sinks = in(0, 2) ? in(0, 30) : in(0, 600);
-    s.tile = 16 << in(0, 2), s.row_tile = 1 << in(0, 5);
+    s.tile_log2 = in(4, 6), s.row_log2 = in(0, 5);
+    const int tile = 1 << s.tile_log2;
     const int page_size = in(1, 40), n_pages = in(1, 9);
     const FastDiv pd = make_fast_div(page_size);
     std::vector<PagedSeq> q;
@@ -59,10 +60,10 @@ static void shapes() {
       CHECK(x.first >= 0 && x.count >= 0 && x.first + x.count <= s.N && x.count <= s.max_q);
       CHECK(x.len >= 0 && x.len <= s.bound);
       CHECK(x.bad == !(lo >= 0 && lo <= s.N && hi >= lo && hi <= s.N && hi - lo <= s.max_q && len >= 0 && len <= s.bound));
-      CHECK((x.tiles == 0) == (x.count == 0) && x.row_tiles * s.row_tile >= x.count * s.G);
+      CHECK((x.tiles == 0) == (x.count == 0) && (x.row_tiles << s.row_log2) >= x.count * s.G && (x.row_tiles == 0 || ((x.row_tiles - 1) << s.row_log2) < x.count * s.G));
       // keys: each visible one once, in order, none that nobody sees beyond whole tiles
       std::map<int, int> at;
-      for (int k = 0; k < x.tiles * s.tile; ++k) {
+      for (int k = 0; k < x.tiles * tile; ++k) {
         const int t = paged_key(x, k);
         CHECK(t >= -1 && t < x.len);
         if (t >= 0) {
@@ -82,7 +83,7 @@ static void shapes() {
         CHECK(!paged_visible(s, -1, end));
       }
       for (int t : wanted) CHECK(at.count(t));
-      for (int k = 0; k + 16 <= x.tiles * s.tile && x.count; k += 16)
+      for (int k = 0; k + 16 <= x.tiles * tile && x.count; k += 16)
         if (paged_all_visible(s, x, k, 16))
           for (int i = 0; i < x.count; ++i)
             for (int j = 0; j < 16; ++j)
