@@ -499,7 +499,7 @@ DS_API int ds_rope_table_init(ds_rope_table *t, int32_t rotary_dim, int32_t inte
  *
  * Layout: element strides for row and head (cache: page, head, row), D contiguous; bases 16-byte aligned and strides
  * multiples of 16 bytes.  Types: DS_F32, DS_BF16.  Errors: DS_ERR_INVALID_ARG; DS_ERR_UNSUPPORTED (D > 256 or not a
- * multiple of 8, rotary_dim > D). */
+ * multiple of 16, rotary_dim > D). */
 typedef struct {
   int32_t N;                    /* rows of the packed arrays */
   int32_t Hq, Hkv, D;

@@ -113,7 +113,7 @@ int validate_qk(const ds_qk_params *p) {
     return DS_ERR_INVALID_ARG;
   if (p->k_out && !strides_ok(p->kv_out_stride, 2, unit)) return DS_ERR_INVALID_ARG;
   if (cache && !strides_ok(p->cache_stride, 3, unit)) return DS_ERR_INVALID_ARG;
-  if (p->D % 8 != 0 || p->D > 256 || p->rope->rotary_dim % 16 != 0 || p->rope->rotary_dim > p->D) return DS_ERR_UNSUPPORTED;
+  if (p->D % 16 != 0 || p->D > 256 || p->rope->rotary_dim % 16 != 0 || p->rope->rotary_dim > p->D) return DS_ERR_UNSUPPORTED;
   if (cache && (int64_t)p->n_pages * p->page_size > 0x7fffffffLL) return DS_ERR_UNSUPPORTED;
   return DS_OK;
 }

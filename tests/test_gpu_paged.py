@@ -322,7 +322,7 @@ def rope_close(got, x, w, eps, pos, table, dtype):
 
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("N,Hq,Hkv,D,R", [(1, 1, 1, 128, 128), (5, 4, 2, 64, 64), (33, 7, 1, 128, 64), (130, 3, 3, 256, 256),
-                                          (17, 4, 4, 96, 32), (9, 2, 1, 40, 16), (20, 28, 4, 128, 128), (3, 2, 2, 24, 16),
+                                          (17, 4, 4, 96, 32), (9, 2, 1, 48, 16), (20, 28, 4, 128, 128), (3, 2, 2, 32, 16),
                                           (6, 2, 2, 80, 80), (2, 1, 1, 16, 16)])
 @pytest.mark.parametrize("interleaved", [False, True])
 def test_norm_rotation_and_cache_write(dtype, N, Hq, Hkv, D, R, interleaved):

@@ -204,7 +204,7 @@ def test_qk_norm_rope_argument_validation(L):
                dict(kv_stride=(-8, 128)), dict(cache_stride=(4096, 2048, 4)), dict(n_rows=FAKE + 2)):
         assert L.ds_qk_norm_rope(ctypes.byref(_qk(t, **kw)), None) == ds.DS_ERR_INVALID_ARG, kw
     assert L.ds_qk_norm_rope(None, None) == ds.DS_ERR_INVALID_ARG
-    for kw in (dict(D=264), dict(D=100), dict(D=64), dict(n_pages=1 << 28)):
+    for kw in (dict(D=272), dict(D=136), dict(D=100), dict(D=64), dict(n_pages=1 << 28)):
         assert L.ds_qk_norm_rope(ctypes.byref(_qk(t, **kw)), None) == ds.DS_ERR_UNSUPPORTED, kw
     assert L.ds_qk_norm_rope(ctypes.byref(_qk(t, N=0)), None) == ds.DS_OK
 
