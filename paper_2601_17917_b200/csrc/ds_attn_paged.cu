@@ -56,10 +56,10 @@ __device__ __forceinline__ void ldmatrix4_trans(uint32_t addr, uint32_t (&r)[4])
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
 __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
-               "{%0, %1, %2, %3};"
-               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+      "{%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
 // Byte offset of 16-byte chunk `c` of row `r` in a tile of rows of ROW bytes: chunks are XOR-ed with the row number
@@ -146,20 +146,23 @@ struct TensorRows {
   __device__ __forceinline__ void step(const Params &a, const Item &it, uint8_t *kbuf, uint8_t *vbuf, int x, float scale2) {
     const int lane = threadIdx.x & 31;
     const uint32_t ks = sm100::smem_u32(kbuf), vs = sm100::smem_u32(vbuf);
-    float s[M][2][4];
+    // Two warps per scheduler hide little, so the products are laid out for independence: all fragments of K first,
+    // even and odd 16s of the dimensions in accumulators of their own.
+    float s[M][2][4], odd[M][2][4];
 #pragma unroll
     for (int mi = 0; mi < M; ++mi)
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[mi][t][e] = 0.f;
+        for (int e = 0; e < 4; ++e) s[mi][t][e] = odd[mi][t][e] = 0.f;
     {
       // matrices: keys 0-7 / 8-15 (lane bit 4), first / second 8 dimensions (lane bit 3)
       const int key = (lane & 7) + ((lane >> 4) << 3), half = (lane >> 3) & 1;
+      uint32_t kf[D / 16][4];
 #pragma unroll
-      for (int k = 0; k < D / 16; ++k) {
-        uint32_t kf[4];
-        ldmatrix4(ks + chunk_at<kRowBytes>(key, 2 * k + half), kf);
+      for (int k = 0; k < D / 16; ++k) ldmatrix4(ks + chunk_at<kRowBytes>(key, 2 * k + half), kf[k]);
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k)
 #pragma unroll
         for (int mi = 0; mi < M; ++mi) {
           uint32_t af[4];
@@ -169,10 +172,9 @@ struct TensorRows {
           } else {
             ldmatrix4(q_smem + chunk_at<kRowBytes>(mi * 16 + (lane & 15), 2 * k + (lane >> 4)), af);
           }
-          mma16816(s[mi][0], af, kf[0], kf[1]);
-          mma16816(s[mi][1], af, kf[2], kf[3]);
+          mma16816(k & 1 ? odd[mi][0] : s[mi][0], af, kf[k][0], kf[k][1]);
+          mma16816(k & 1 ? odd[mi][1] : s[mi][1], af, kf[k][2], kf[k][3]);
         }
-      }
     }
     const bool partial = !paged_all_visible(a.s, it.q, x, kKeys);
 #pragma unroll
@@ -180,7 +182,7 @@ struct TensorRows {
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[mi][t][e] *= scale2;
+        for (int e = 0; e < 4; ++e) s[mi][t][e] = (s[mi][t][e] + odd[mi][t][e]) * scale2;
     uint32_t seen[M][2] = {};    // only with partial: bit 2 t + c of a row: key 8 t + 2 (lane % 4) + c
     if (partial) {
 #pragma unroll
@@ -237,19 +239,24 @@ struct TensorRows {
     }
     if (partial) keep_hidden_values_out(vbuf, ph, pl, seen);
     {
-      // matrices: keys 0-7 / 8-15 (lane bit 3), dimensions +0 / +8 (lane bit 4)
+      // matrices: keys 0-7 / 8-15 (lane bit 3), dimensions +0 / +8 (lane bit 4); four fragments of V at a time, the
+      // low halves after the high ones of all four
       const int key = lane & 15, half = lane >> 4;
+      constexpr int kSet = 4;
 #pragma unroll
-      for (int j = 0; j < D / 16; ++j) {
-        uint32_t vf[4];
-        ldmatrix4_trans(vs + chunk_at<kRowBytes>(key, 2 * j + half), vf);
+      for (int j0 = 0; j0 < D / 16; j0 += kSet) {
+        uint32_t vf[kSet][4];
 #pragma unroll
-        for (int mi = 0; mi < M; ++mi) {
-          mma16816(o[mi][2 * j], ph[mi], vf[0], vf[1]);
-          mma16816(o[mi][2 * j + 1], ph[mi], vf[2], vf[3]);
-          mma16816(o[mi][2 * j], pl[mi], vf[0], vf[1]);
-          mma16816(o[mi][2 * j + 1], pl[mi], vf[2], vf[3]);
-        }
+        for (int j = 0; j < kSet; ++j) ldmatrix4_trans(vs + chunk_at<kRowBytes>(key, 2 * (j0 + j) + half), vf[j]);
+#pragma unroll
+        for (int part = 0; part < 2; ++part)
+#pragma unroll
+          for (int j = 0; j < kSet; ++j)
+#pragma unroll
+            for (int mi = 0; mi < M; ++mi) {
+              mma16816(o[mi][2 * (j0 + j)], part ? pl[mi] : ph[mi], vf[j][0], vf[j][1]);
+              mma16816(o[mi][2 * (j0 + j) + 1], part ? pl[mi] : ph[mi], vf[j][2], vf[j][3]);
+            }
       }
     }
   }

@@ -10,7 +10,8 @@
 // products are two wide (fma.rn.f32x2).
 // Loads are asynchronous copies to shared memory, some steps ahead through the heads of q, k and v alike; a lane
 // reads back what it copied, so nothing is synchronised.  (16384 rows of 36 x 128 bf16: with the loads of four steps
-// held in registers 74 us, waiting for them; with copies of 8 bytes, twice the steps, 58 us and 79 % of the issue slots.)
+// held in registers 74 us, waiting for them; with copies of 8 bytes, twice the steps, 58 us and 79 % of the issue slots;
+// as it is 56 us, 5.36 TB/s.  Eight steps ahead 64 us, two 60; CTAs of 128 threads 57, of 256 62.)
 // The phase of a pair is position * turn in integers modulo 2^64: exact for every position, and its top 32 bits are an
 // angle in [-1/2, 1/2) turns, which sincospif takes without a range reduction.
 #include <type_traits>
@@ -21,7 +22,7 @@
 namespace ds {
 namespace {
 
-constexpr int kThreads = 128, kWarps = kThreads / 32;
+constexpr int kThreads = 64, kWarps = kThreads / 32;
 constexpr int kAhead = 4;   // steps (a head per lane group) whose loads are in flight
 constexpr int kMaxPairs = 128;
 
@@ -133,8 +134,8 @@ __global__ void __launch_bounds__(kThreads) norm_rope_kernel(const __grid_consta
     }
     if (group < ahead_left && live) {
       const uint32_t to = ring_u + ahead_slot * 1024;
-      asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(to), "l"(ahead + da) : "memory");
-      asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(to + 512), "l"(ahead + db) : "memory");
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(ahead + da) : "memory");
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + 512), "l"(ahead + db) : "memory");
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
     ahead += ahead_step;
