@@ -6,6 +6,8 @@
 // device: uneven lengths cost nothing and one long sequence spreads over the whole GPU.  An item that crosses a range
 // boundary leaves partial results (unnormalised sums with their maximum) in the workspace; a second, small
 // kernel, launched early and waiting for the first, joins them in a fixed order.
+// Few items of moderate length (a small batch) are instead given a cluster of CTAs each, which join through
+// distributed shared memory: no second launch, no workspace, no search for the range's first item.
 //
 // Inside a CTA the four warps take equal parts of every key tile and share nothing until the item ends: each has its own
 // ring of cp.async stages in shared memory (16-byte chunks, XOR swizzle), its own running maximum, sum and output, so
@@ -15,6 +17,8 @@
 // nearly empty and the stream, not the products, bounds the kernel.  The weights enter the second product as two bf16
 // halves (hi + lo), which keeps 16 bits of them: the product is free here, and an output is then rounded once.
 // fp32: CUDA cores, 8 lanes per key.
+#include <cooperative_groups.h>
+
 #include <type_traits>
 
 #include "ds_common.cuh"
@@ -27,12 +31,15 @@ namespace {
 constexpr int kWarps = 4, kThreads = kWarps * 32, kStages = 3;
 constexpr int kMinTiles = 4;     // a range has at least so many key tiles
 constexpr int kWholeTiles = 8;   // items of at most so many key tiles are not split
+constexpr int kClusterTiles = 24;   // most key tiles of a CTA when an item has a cluster
 
 struct Params {
   ds_paged_params p;
   PagedShape s;
   FastDiv page_div, group_div;
   int split;
+  int cluster;        // CTAs of an item; 0: equal ranges
+  FastDiv item_div, row_div;      // by KV heads times row tiles, by row tiles (at most): with a cluster
   PagedJoin *joins;   // [gridDim.x]
   float2 *part_ml;    // [2 gridDim.x][row_tile]  maximum (base 2, scaled) and sum
   float *part_o;      // [2 gridDim.x][row_tile][D]
@@ -476,12 +483,143 @@ struct Layout {
   static constexpr int kRing = kStages * 2 * kSub;                  // of one warp; holds its sums at the item's end
   static constexpr int kOffQ = kWarps * kRing;
   static constexpr int kOffMl = kOffQ + Rows::kQBytes;
-  static constexpr int kOffMisc = kOffMl + kWarps * Rows::kRows * 8;
+  static constexpr int kOffTotal = kOffMl + kWarps * Rows::kRows * 8;      // the CTA's maximum and sum of each row
+  static constexpr int kOffMisc = kOffTotal + Rows::kRows * 8;
   static constexpr int kBytes = kOffMisc + 64;
   static constexpr int kTile = kWarps * Rows::kKeys;
   static_assert(Rows::kRows * Rows::D * 4 <= kRing, "the ring is reused for the warp's sums");
   static_assert(Rows::kCtas * (kBytes + 1024) <= 228 * 1024, "shared memory of the resident CTAs");
 };
+
+// Streams key tiles tile0 .. tile0 + n_tiles - 1 of an item; afterwards (and a barrier) the rings hold the warps' sums.
+template <class Rows>
+__device__ __forceinline__ void stream_keys(const Params &a, const Item &it, int tile0, int n_tiles, uint8_t *smem, uint32_t &flags) {
+  using T = typename Rows::T;
+  using L = Layout<Rows>;
+  const ds_paged_params &p = a.p;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  uint8_t *ring = smem + warp * L::kRing;
+  const float scale2 = p.scale * kLog2e;
+  Rows rows;
+  rows.begin(a, it, smem + L::kOffQ);
+  constexpr int kChunks = Rows::kRowBytes / 16, kOps = Rows::kKeys * kChunks / 32;
+  const int32_t *table = p.block_table + it.b * p.table_stride;
+  const uint8_t *kbase = reinterpret_cast<const uint8_t *>(reinterpret_cast<const T *>(p.k_cache) + it.g * p.cache_stride[1]);
+  const uint8_t *vbase = reinterpret_cast<const uint8_t *>(reinterpret_cast<const T *>(p.v_cache) + it.g * p.cache_stride[1]);
+  const int x_first = tile0 * L::kTile + warp * Rows::kKeys;
+  // a lane looks up the cache row of key lane % kKeys, one stage ahead of its use
+  int pos = paged_key(it.q, x_first + lane % Rows::kKeys);
+  int page = pos >= 0 ? table[fast_div(pos, a.page_div)] : 0;
+  auto issue = [&](int i) {
+    long long at = -1;
+    if (pos >= 0) {
+      const int ok = paged_clamp_page(page, p.n_pages);
+      if (ok != page) flags |= DS_DEV_INDEX;
+      const int slot = pos - fast_div(pos, a.page_div) * p.page_size;
+      at = (ok * p.cache_stride[0] + slot * p.cache_stride[2]) * (long long)sizeof(T);
+    }
+    const uint32_t dst = sm100::smem_u32(ring + (i % kStages) * 2 * L::kSub);
+#pragma unroll
+    for (int j = 0; j < kOps; ++j) {
+      const int c = j * 32 + lane, r = c / kChunks, ch = c % kChunks;
+      const long long off = __shfl_sync(0xffffffffu, at, r);
+      const bool there = off >= 0;
+      const uint32_t to = dst + chunk_at<Rows::kRowBytes>(r, ch);
+      const long long from = (there ? off : 0) + 16 * ch;
+      cp_async16(to, kbase + from, there);
+      cp_async16(to + L::kSub, vbase + from, there);
+    }
+    if (i + 1 < n_tiles) {
+      pos = paged_key(it.q, x_first + (i + 1) * L::kTile + lane % Rows::kKeys);
+      page = pos >= 0 ? table[fast_div(pos, a.page_div)] : 0;
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < kStages - 1; ++i) {
+    if (i < n_tiles) issue(i);
+    cp_async_commit();
+  }
+  for (int i = 0; i < n_tiles; ++i) {
+    cp_async_wait<kStages - 2>();
+    __syncwarp();      // stage i is there for the whole warp, and the warp is done with stage i - 1
+    if (i + kStages - 1 < n_tiles) issue(i + kStages - 1);
+    cp_async_commit();
+    uint8_t *stage = ring + (i % kStages) * 2 * L::kSub;
+    rows.step(a, it, stage, stage + L::kSub, x_first + i * L::kTile, scale2);
+  }
+  cp_async_wait<0>();
+  __syncwarp();
+
+  rows.finish(it, reinterpret_cast<float *>(ring), reinterpret_cast<float2 *>(smem + L::kOffMl) + warp * Rows::kRows);
+  __syncthreads();
+}
+
+// The four warps' sums of elements d .. d + 3 of row r.
+template <class Rows>
+__device__ __forceinline__ float4 join_warps(const uint8_t *smem, int r, int d, float &top, float &sum) {
+  using L = Layout<Rows>;
+  const float2 *ml_all = reinterpret_cast<const float2 *>(smem + L::kOffMl);
+  top = -INFINITY;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) top = fmaxf(top, ml_all[w * Rows::kRows + r].x);
+  sum = 0.f;
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    const float2 ml = ml_all[w * Rows::kRows + r];
+    const float4 x = *reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(smem + w * L::kRing) + r * Rows::D + d);
+    const float f = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - top);
+    sum = fmaf(ml.y, f, sum);
+    v.x = fmaf(x.x, f, v.x), v.y = fmaf(x.y, f, v.y), v.z = fmaf(x.z, f, v.z), v.w = fmaf(x.w, f, v.w);
+  }
+  return v;
+}
+
+// An item on a cluster: rank r takes the r-th part of its key tiles, then the ranks share out the output's elements.
+template <class Rows>
+__device__ __forceinline__ void cluster_item(const Params &a, const Item &it, uint8_t *smem, uint32_t &flags) {
+  namespace cg = cooperative_groups;
+  using T = typename Rows::T;
+  using L = Layout<Rows>;
+  constexpr int D = Rows::D;
+  auto cluster = cg::this_cluster();
+  const int rank = (int)cluster.block_rank(), n = a.cluster, tid = threadIdx.x;
+  const int per = (it.q.tiles + n - 1) / n;      // n is at most 8
+  const int tile0 = min(rank * per, it.q.tiles), n_tiles = min(per, it.q.tiles - tile0);
+  float2 *total = reinterpret_cast<float2 *>(smem + L::kOffTotal);
+  float *mine = reinterpret_cast<float *>(smem);      // over the first warp's sums, element by element
+  stream_keys<Rows>(a, it, tile0, n_tiles, smem, flags);
+  for (int e = tid; e < it.rows * (D / 4); e += kThreads) {
+    const int r = e / (D / 4), d = e % (D / 4) * 4;
+    float top, sum;
+    const float4 v = join_warps<Rows>(smem, r, d, top, sum);
+    *reinterpret_cast<float4 *>(mine + r * D + d) = v;
+    if (d == 0) total[r] = make_float2(top, sum);
+  }
+  cluster.sync();
+  for (int e = rank * kThreads + tid; e < it.rows * (D / 4); e += n * kThreads) {
+    const int r = e / (D / 4), d = e % (D / 4) * 4;
+    float2 ml[8];
+    float top = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (k < n) {
+        ml[k] = *cluster.map_shared_rank(total + r, k);
+        top = fmaxf(top, ml[k].x);
+      }
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (k < n) {
+        const float4 x = *cluster.map_shared_rank(reinterpret_cast<const float4 *>(mine + r * D + d), k);
+        const float f = ml[k].x == -INFINITY ? 0.f : ex2_approx(ml[k].x - top);
+        sum = fmaf(ml[k].y, f, sum);
+        v.x = fmaf(x.x, f, v.x), v.y = fmaf(x.y, f, v.y), v.z = fmaf(x.z, f, v.z), v.w = fmaf(x.w, f, v.w);
+      }
+    write_row4<T>(a, row_of(a, it, r), d, v, top, sum);
+  }
+  cluster.sync();      // nobody leaves while its shared memory is read
+}
 
 template <class Rows>
 __global__ void __launch_bounds__(kThreads, Rows::kCtas) attn_paged_kernel(const __grid_constant__ Params a) {
@@ -499,8 +637,21 @@ __global__ void __launch_bounds__(kThreads, Rows::kCtas) attn_paged_kernel(const
     const int lo = p.row_start ? p.row_start[b] : b * p.max_q, hi = p.row_start ? p.row_start[b + 1] : lo + p.max_q;
     return paged_seq(a.s, lo, hi, p.kv_len[b]);
   };
-  long long total, per, t, t_end, base;
   Item it;
+  if (a.cluster) {
+    const int item = (int)blockIdx.x / a.cluster;
+    it.b = fast_div(item, a.item_div);
+    const int rest = item - it.b * (int)a.item_div.d;
+    it.g = fast_div(rest, a.row_div);
+    it.row0 = (rest - it.g * (int)a.row_div.d) << a.s.row_log2;
+    it.q = sequence(it.b);
+    if (it.q.bad) flags |= DS_DEV_INDEX;
+    it.rows = min(Rows::kRows, it.q.count * a.s.G - it.row0);
+    if (it.rows > 0) cluster_item<Rows>(a, it, smem, flags);      // the whole cluster or none of it
+    if (flags && p.status) atomicOr(p.status, flags);
+    return;
+  }
+  long long total, per, t, t_end, base;
   it.b = 0;
   auto range = [&]() {
     per = paged_per_cta(total, gridDim.x, kMinTiles);
@@ -569,9 +720,6 @@ __global__ void __launch_bounds__(kThreads, Rows::kCtas) attn_paged_kernel(const
   flags = 0;
   PagedJoin join = {0, 0, 0, 0, 0, 0};      // thread 0's
 
-  uint8_t *ring = smem + warp * L::kRing;
-  float2 *ml_all = reinterpret_cast<float2 *>(smem + L::kOffMl);
-  const float scale2 = p.scale * kLog2e;
   bool first_segment = true;
   int tile0 = 0, row_tile = 0;
   if (t < t_end) {      // the one place that needs divisions: afterwards items follow one another
@@ -607,77 +755,13 @@ __global__ void __launch_bounds__(kThreads, Rows::kCtas) attn_paged_kernel(const
       join.row = it.row0, join.rows = it.rows, join.first = it.q.first, join.kv_head = it.g;
     }
 
-    // ---- stream the keys
-    Rows rows;
-    rows.begin(a, it, smem + L::kOffQ);
-    constexpr int kChunks = Rows::kRowBytes / 16, kOps = Rows::kKeys * kChunks / 32;
-    const int32_t *table = p.block_table + it.b * p.table_stride;
-    const uint8_t *kbase = reinterpret_cast<const uint8_t *>(reinterpret_cast<const T *>(p.k_cache) + it.g * p.cache_stride[1]);
-    const uint8_t *vbase = reinterpret_cast<const uint8_t *>(reinterpret_cast<const T *>(p.v_cache) + it.g * p.cache_stride[1]);
-    const int x_first = tile0 * L::kTile + warp * Rows::kKeys;
-    // a lane looks up the cache row of key lane % kKeys, one stage ahead of its use
-    int pos = paged_key(it.q, x_first + lane % Rows::kKeys);
-    int page = pos >= 0 ? table[fast_div(pos, a.page_div)] : 0;
-    auto issue = [&](int i) {
-      long long at = -1;
-      if (pos >= 0) {
-        const int ok = paged_clamp_page(page, p.n_pages);
-        if (ok != page) flags |= DS_DEV_INDEX;
-        const int slot = pos - fast_div(pos, a.page_div) * p.page_size;
-        at = (ok * p.cache_stride[0] + slot * p.cache_stride[2]) * (long long)sizeof(T);
-      }
-      const uint32_t dst = sm100::smem_u32(ring + (i % kStages) * 2 * L::kSub);
-#pragma unroll
-      for (int j = 0; j < kOps; ++j) {
-        const int c = j * 32 + lane, r = c / kChunks, ch = c % kChunks;
-        const long long off = __shfl_sync(0xffffffffu, at, r);
-        const bool there = off >= 0;
-        const uint32_t to = dst + chunk_at<Rows::kRowBytes>(r, ch);
-        const long long from = (there ? off : 0) + 16 * ch;
-        cp_async16(to, kbase + from, there);
-        cp_async16(to + L::kSub, vbase + from, there);
-      }
-      if (i + 1 < n_tiles) {
-        pos = paged_key(it.q, x_first + (i + 1) * L::kTile + lane % Rows::kKeys);
-        page = pos >= 0 ? table[fast_div(pos, a.page_div)] : 0;
-      }
-    };
-#pragma unroll
-    for (int i = 0; i < kStages - 1; ++i) {
-      if (i < n_tiles) issue(i);
-      cp_async_commit();
-    }
-    for (int i = 0; i < n_tiles; ++i) {
-      cp_async_wait<kStages - 2>();
-      __syncwarp();      // stage i is there for the whole warp, and the warp is done with stage i - 1
-      if (i + kStages - 1 < n_tiles) issue(i + kStages - 1);
-      cp_async_commit();
-      uint8_t *stage = ring + (i % kStages) * 2 * L::kSub;
-      rows.step(a, it, stage, stage + L::kSub, x_first + i * L::kTile, scale2);
-    }
-    cp_async_wait<0>();
-    __syncwarp();
-
-    // ---- join the warps; the rings hold their sums
-    rows.finish(it, reinterpret_cast<float *>(ring), ml_all + warp * Rows::kRows);
-    __syncthreads();
+    stream_keys<Rows>(a, it, tile0, n_tiles, smem, flags);
     const bool whole = tile0 == 0 && n_tiles == it.q.tiles;
     const int slot = paged_slot(blockIdx.x, first_segment);
     for (int e = tid; e < it.rows * (D / 4); e += kThreads) {
       const int r = e / (D / 4), d = e % (D / 4) * 4;
-      float top = -INFINITY;
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) top = fmaxf(top, ml_all[w * Rows::kRows + r].x);
-      float sum = 0.f;
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        const float2 ml = ml_all[w * Rows::kRows + r];
-        const float4 x = *reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(smem + w * L::kRing) + r * D + d);
-        const float f = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - top);
-        sum = fmaf(ml.y, f, sum);
-        v.x = fmaf(x.x, f, v.x), v.y = fmaf(x.y, f, v.y), v.z = fmaf(x.z, f, v.z), v.w = fmaf(x.w, f, v.w);
-      }
+      float top, sum;
+      const float4 v = join_warps<Rows>(smem, r, d, top, sum);
       if (whole) {
         write_row4<T>(a, row_of(a, it, r), d, v, top, sum);
       } else {
@@ -747,6 +831,7 @@ __global__ void __launch_bounds__(kJoinThreads) attn_paged_join_kernel(const __g
 struct Shape {
   PagedShape s;
   int grid, tiles;      // tiles: most key tiles of an item
+  int cluster, heads;   // CTAs of an item (0: equal ranges), items of a sequence
   size_t bytes_joins, bytes_ml, bytes_o;
 };
 constexpr int log2_of(int x) { return x <= 1 ? 0 : 1 + log2_of(x / 2); }
@@ -765,6 +850,19 @@ Shape shape_of(const ds_paged_params &p) {
   long long ranges = (paged_units(h.s, q) * p.B + kMinTiles - 1) / kMinTiles;
   const long long resident = (long long)Rows::kCtas * sm_count();
   h.grid = (int)(ranges < resident ? (ranges > 0 ? ranges : 1) : resident);
+  // A cluster per item where the items leave room for it and none is long: what the CTAs lose when the lengths
+  // are uneven, or their number does not fill the GPU, has to stay below what the second kernel costs.
+  const long long items = (long long)p.B * p.Hkv * q.row_tiles;
+  h.heads = p.Hkv * q.row_tiles;
+  h.cluster = 0;
+  if (q.row_tiles > 0 && items * 2 <= resident) {
+    int n = 8;
+    while (n > 1 && (items * n > resident || n > h.tiles)) n /= 2;
+    if (n > 1 && h.tiles <= n * kClusterTiles) {
+      h.cluster = n;
+      h.grid = (int)items * n;
+    }
+  }
   h.bytes_joins = up256(sizeof(PagedJoin) * (size_t)h.grid);
   h.bytes_ml = up256(sizeof(float2) * 2 * (size_t)h.grid * Rows::kRows);
   h.bytes_o = sizeof(float) * 2 * (size_t)h.grid * Rows::kRows * Rows::D;
@@ -774,7 +872,7 @@ Shape shape_of(const ds_paged_params &p) {
 template <class Rows>
 size_t workspace_of(const ds_paged_params &p) {
   const Shape h = shape_of<Rows>(p);
-  return h.tiles <= kWholeTiles || h.grid == 1 ? 0 : h.bytes_joins + h.bytes_ml + h.bytes_o;
+  return h.cluster || h.tiles <= kWholeTiles || h.grid == 1 ? 0 : h.bytes_joins + h.bytes_ml + h.bytes_o;
 }
 
 template <class Rows>
@@ -793,19 +891,29 @@ int launch_rows(const ds_paged_params &p, cudaStream_t stream) {
   a.part_ml = reinterpret_cast<float2 *>(ws + h.bytes_joins);
   a.part_o = reinterpret_cast<float *>(ws + h.bytes_joins + h.bytes_ml);
   DS_CUDA_OK(cudaFuncSetAttribute(attn_paged_kernel<Rows>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes));
-  attn_paged_kernel<Rows><<<h.grid, kThreads, L::kBytes, stream>>>(a);
-  DS_CUDA_OK(cudaGetLastError());
+  a.cluster = h.cluster;
+  a.item_div = make_fast_div(h.heads > 0 ? h.heads : 1);
+  a.row_div = make_fast_div(h.heads > 0 ? h.heads / p.Hkv : 1);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(h.grid);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = L::kBytes;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = h.cluster;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = h.cluster ? 1 : 0;
+  DS_CUDA_OK(cudaLaunchKernelEx(&cfg, attn_paged_kernel<Rows>, a));
   note_launch(1);
   if (!a.split) return DS_OK;
   const int rows = (int)((long long)p.max_q * h.s.G < Rows::kRows ? (long long)p.max_q * h.s.G : Rows::kRows);
-  cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(h.grid, rows);
   cfg.blockDim = dim3(kJoinThreads);
-  cfg.stream = stream;
-  cudaLaunchAttribute attr;
+  cfg.dynamicSmemBytes = 0;
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
   cfg.numAttrs = 1;
   DS_CUDA_OK(cudaLaunchKernelEx(&cfg, attn_paged_join_kernel<typename Rows::T, Rows::D, Rows::kRows>, a));
   note_launch(1);
