@@ -13,8 +13,8 @@
 // ring of cp.async stages in shared memory (16-byte chunks, XOR swizzle), its own running maximum, sum and output, so
 // the loop has no CTA-wide barrier.  At the end of an item the four results are joined through shared memory.
 //
-// bf16: mma.sync m16n8k16 (rows = the stacked queries, up to 16 M).  The few rows leave tcgen05's 128-row tile
-// nearly empty and the stream, not the products, bounds the kernel.  The weights enter the second product as two bf16
+// bf16: mma.sync m16n8k16.  The few rows leave tcgen05's 128-row tile nearly empty and the stream, not the products,
+// bounds the kernel.  The weights enter the second product as two bf16
 // halves (hi + lo), which keeps 16 bits of them: the product is free here, and an output is then rounded once.
 // fp32: CUDA cores, 8 lanes per key.
 #include <cooperative_groups.h>
@@ -69,6 +69,13 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// Transposes an 8 x 8 matrix of 16-bit values, lane 4i + q holding columns 2q and 2q + 1 of row i.
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+
 // Byte offset of 16-byte chunk `c` of row `r` in a tile of rows of ROW bytes: chunks are XOR-ed with the row number
 // within groups of eight, which makes ldmatrix and the float4 reads below free of bank conflicts.
 template <int ROW>
@@ -92,48 +99,39 @@ __device__ __forceinline__ Row row_of(const Params &a, const Item &it, int r) {
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// A warp's share of an item in bf16: M row blocks of 16 against KEYS = 16 keys at a time.
-template <int D_, int M>
+// A warp's share of an item in bf16: NB blocks of 8 rows against 16 keys at a time, with the keys as the products' 16-wide
+// side, S^T = K Q^T and O^T = V^T P^T, so that a block of 8 rows (a single token of most grouped-query models) costs
+// half of what 16 rows would.  Lane 4i + q holds, of S^T, keys i and i + 8 of rows 2q and 2q + 1 of every block; movmatrix
+// turns the weights into the second product's fragments.
+template <int D_, int NB>
 struct TensorRows {
   using T = __nv_bfloat16;
-  static constexpr int D = D_, kRows = 16 * M, kRowBytes = 2 * D, kKeys = 16;
-  static constexpr int kQBytes = M == 1 ? 0 : kRows * kRowBytes;   // M = 1 holds the queries in registers
-  static constexpr int kCtas = D == 64 && M == 1 ? 3 : 2;          // per SM: registers and shared memory
-  float o[M][D / 8][4];
-  float m[M][2], l[M][2];        // rows lane / 4 and lane / 4 + 8 of each block
-  int end[M][2];
-  uint32_t qf[M == 1 ? D / 16 : 1][4];
+  static constexpr int D = D_, kRows = 8 * NB, kRowBytes = 2 * D, kKeys = 16;
+  static constexpr bool kQRegs = NB <= 2;      // more rows read their queries' fragments from shared memory
+  static constexpr int kQBytes = kQRegs ? 0 : kRows * kRowBytes;
+  static constexpr int kCtas = D == 64 && NB == 1 ? 4 : D == 64 && NB == 2 ? 3 : 2;          // per SM: registers and shared memory
+  float o[NB][D / 16][4];        // dimensions 16 j + lane / 4 (+ 8), rows 2q, 2q + 1
+  float m[NB][2], l[NB][2];
+  int end[NB][2];
+  uint32_t qf[kQRegs ? NB : 1][kQRegs ? D / 16 : 1][2];
   uint32_t q_smem;
 
   __device__ void begin(const Params &a, const Item &it, uint8_t *q_buf) {
     const int lane = threadIdx.x & 31;
     q_smem = sm100::smem_u32(q_buf);
-#pragma unroll
-    for (int mi = 0; mi < M; ++mi) {
-#pragma unroll
-      for (int j = 0; j < D / 8; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[mi][j][e] = 0.f;
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        m[mi][e] = -INFINITY, l[mi][e] = 0.f;
-        const int r = mi * 16 + e * 8 + (lane >> 2);
-        end[mi][e] = r < it.rows ? row_of(a, it, r).end : 0;
-      }
-    }
     const T *q = reinterpret_cast<const T *>(a.p.q);
-    if constexpr (M == 1) {
+    if constexpr (kQRegs) {
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int r = e * 8 + (lane >> 2);
+      for (int nb = 0; nb < NB; ++nb) {
+        const int r = 8 * nb + (lane >> 2);
         const bool there = r < it.rows;
         const Row row = row_of(a, it, there ? r : 0);
         const T *src = q + row.n * a.p.q_stride[0] + row.h * a.p.q_stride[1] + (lane & 3) * 2;
 #pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-          qf[k][e] = there ? *reinterpret_cast<const uint32_t *>(src + 16 * k) : 0u;
-          qf[k][2 + e] = there ? *reinterpret_cast<const uint32_t *>(src + 16 * k + 8) : 0u;
-        }
+        for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            qf[nb][k][h] = there ? *reinterpret_cast<const uint32_t *>(src + 16 * k + 8 * h) : 0u;
       }
     } else {
       for (int c = threadIdx.x; c < kRows * (kRowBytes / 16); c += kThreads) {
@@ -147,161 +145,162 @@ struct TensorRows {
       }
       __syncthreads();
     }
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[nb][j][e] = 0.f;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        m[nb][e] = -INFINITY, l[nb][e] = 0.f;
+        const int r = 8 * nb + 2 * (lane & 3) + e;
+        end[nb][e] = r < it.rows ? row_of(a, it, r).end : 0;
+      }
+    }
   }
 
   // 16 keys from x on; K and V as loaded, V is scratch afterwards.
   __device__ __forceinline__ void step(const Params &a, const Item &it, uint8_t *kbuf, uint8_t *vbuf, int x, float scale2) {
     const int lane = threadIdx.x & 31;
     const uint32_t ks = sm100::smem_u32(kbuf), vs = sm100::smem_u32(vbuf);
-    // Two warps per scheduler hide little, so the products are laid out for independence: all fragments of K first,
-    // even and odd 16s of the dimensions in accumulators of their own.
-    float s[M][2][4], odd[M][2][4];
+    // even and odd 16s of the dimensions in accumulators of their own, all fragments of K first
+    float s[NB][4], odd[NB][4];
 #pragma unroll
-    for (int mi = 0; mi < M; ++mi)
+    for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[mi][t][e] = odd[mi][t][e] = 0.f;
+      for (int e = 0; e < 4; ++e) s[nb][e] = odd[nb][e] = 0.f;
     {
-      // matrices: keys 0-7 / 8-15 (lane bit 4), first / second 8 dimensions (lane bit 3)
-      const int key = (lane & 7) + ((lane >> 4) << 3), half = (lane >> 3) & 1;
       uint32_t kf[D / 16][4];
 #pragma unroll
-      for (int k = 0; k < D / 16; ++k) ldmatrix4(ks + chunk_at<kRowBytes>(key, 2 * k + half), kf[k]);
+      for (int k = 0; k < D / 16; ++k) ldmatrix4(ks + chunk_at<kRowBytes>(lane & 15, 2 * k + (lane >> 4)), kf[k]);
 #pragma unroll
-      for (int k = 0; k < D / 16; ++k)
+      for (int k = 0; k < D / 16; ++k) {
+        if constexpr (kQRegs) {
 #pragma unroll
-        for (int mi = 0; mi < M; ++mi) {
-          uint32_t af[4];
-          if constexpr (M == 1) {
+          for (int nb = 0; nb < NB; ++nb) mma16816(k & 1 ? odd[nb] : s[nb], kf[k], qf[nb][k][0], qf[nb][k][1]);
+        } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) af[e] = qf[k][e];
-          } else {
-            ldmatrix4(q_smem + chunk_at<kRowBytes>(mi * 16 + (lane & 15), 2 * k + (lane >> 4)), af);
+          for (int nb = 0; nb < NB; nb += 2) {
+            uint32_t bf[4];      // rows 8 nb .. + 7: two halves of the 16 dimensions, then the next block's
+            ldmatrix4(q_smem + chunk_at<kRowBytes>(8 * nb + (lane & 7) + ((lane >> 4) << 3), 2 * k + ((lane >> 3) & 1)), bf);
+            mma16816(k & 1 ? odd[nb] : s[nb], kf[k], bf[0], bf[1]);
+            mma16816(k & 1 ? odd[nb + 1] : s[nb + 1], kf[k], bf[2], bf[3]);
           }
-          mma16816(k & 1 ? odd[mi][0] : s[mi][0], af, kf[k][0], kf[k][1]);
-          mma16816(k & 1 ? odd[mi][1] : s[mi][1], af, kf[k][2], kf[k][3]);
         }
+      }
     }
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[nb][e] = (s[nb][e] + odd[nb][e]) * scale2;
     const bool partial = !paged_all_visible(a.s, it.q, x, kKeys);
-#pragma unroll
-    for (int mi = 0; mi < M; ++mi)
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[mi][t][e] = (s[mi][t][e] + odd[mi][t][e]) * scale2;
-    uint32_t seen[M][2] = {};    // only with partial: bit 2 t + c of a row: key 8 t + 2 (lane % 4) + c
+    uint32_t seen[NB] = {};      // only with partial: bit 2h + e: key lane / 4 + 8h, row 2q + e
     if (partial) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+      for (int h = 0; h < 2; ++h) {
+        const int pos = paged_key(it.q, x + 8 * h + (lane >> 2));
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const int pos = paged_key(it.q, x + 8 * t + 2 * (lane & 3) + c);
+        for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-          for (int mi = 0; mi < M; ++mi)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const bool vis = paged_visible(a.s, pos, end[mi][e]);
-              if (vis) seen[mi][e] |= 1u << (2 * t + c);
-              else s[mi][t][2 * e + c] = -INFINITY;
-            }
-        }
-    }
-    uint32_t ph[M][4], pl[M][4];   // A fragments of the weights' halves
-#pragma unroll
-    for (int mi = 0; mi < M; ++mi) {
-      float nm[2];
-      bool moved = false;
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        float v = fmaxf(fmaxf(s[mi][0][2 * e], s[mi][0][2 * e + 1]), fmaxf(s[mi][1][2 * e], s[mi][1][2 * e + 1]));
-        v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 1));
-        v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 2));
-        // the reference moves only when a weight would pass 2^8: the result is the same, the sums are touched rarely
-        nm[e] = v > m[mi][e] + 8.f ? v : m[mi][e];
-        moved |= nm[e] != m[mi][e];
+          for (int e = 0; e < 2; ++e) {
+            if (paged_visible(a.s, pos, end[nb][e])) seen[nb] |= 1u << (2 * h + e);
+            else s[nb][2 * h + e] = -INFINITY;
+          }
       }
-      if (__any_sync(0xffffffffu, moved)) {
+    }
+    // The reference of the exponents moves only when a weight would pass 2^8 (the result is the same): no maximum is
+    // exchanged until some lane finds such a score.
+    bool over = false;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) over |= fmaxf(s[nb][e], s[nb][2 + e]) > m[nb][e] + 8.f;
+    if (__any_sync(0xffffffffu, over)) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const float keep = m[mi][e] == nm[e] ? 1.f : ex2_approx(m[mi][e] - nm[e]);
-          m[mi][e] = nm[e];
-          l[mi][e] *= keep;
+          float top = fmaxf(m[nb][e], fmaxf(s[nb][e], s[nb][2 + e]));
 #pragma unroll
-          for (int j = 0; j < D / 8; ++j) o[mi][j][2 * e] *= keep, o[mi][j][2 * e + 1] *= keep;
+          for (int off = 4; off < 32; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+          const float keep = m[nb][e] == top ? 1.f : ex2_approx(m[nb][e] - top);
+          m[nb][e] = top;
+          l[nb][e] *= keep;
+#pragma unroll
+          for (int j = 0; j < D / 16; ++j) o[nb][j][e] *= keep, o[nb][j][2 + e] *= keep;
         }
-      }
+    }
+    uint32_t hi[NB][2], lo[NB][2];      // keys 0-7, 8-15: the weights' halves, rows 2q and 2q + 1
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const float ref = m[mi][e] == -INFINITY ? 0.f : m[mi][e];   // nothing seen yet: weights exp(-inf) = 0
+    for (int nb = 0; nb < NB; ++nb) {
+      // nothing seen yet: weights exp(-inf) = 0
+      const float ref0 = m[nb][0] == -INFINITY ? 0.f : m[nb][0], ref1 = m[nb][1] == -INFINITY ? 0.f : m[nb][1];
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const float p0 = ex2_approx(s[mi][t][2 * e] - ref), p1 = ex2_approx(s[mi][t][2 * e + 1] - ref);
-          l[mi][e] += p0 + p1;
-          const uint32_t hi = sm100::pack_bf16(p0, p1);
-          ph[mi][2 * t + e] = hi;
-          pl[mi][2 * t + e] = sm100::pack_bf16(p0 - bf16lo_to_f32(hi), p1 - bf16hi_to_f32(hi));
-        }
+      for (int h = 0; h < 2; ++h) {
+        const float p0 = ex2_approx(s[nb][2 * h] - ref0), p1 = ex2_approx(s[nb][2 * h + 1] - ref1);
+        l[nb][0] += p0;
+        l[nb][1] += p1;
+        hi[nb][h] = sm100::pack_bf16(p0, p1);
+        lo[nb][h] = sm100::pack_bf16(p0 - bf16lo_to_f32(hi[nb][h]), p1 - bf16hi_to_f32(hi[nb][h]));
       }
     }
-    if (partial) keep_hidden_values_out(vbuf, ph, pl, seen);
-    {
-      // matrices: keys 0-7 / 8-15 (lane bit 3), dimensions +0 / +8 (lane bit 4); four fragments of V at a time, the
-      // low halves after the high ones of all four
-      const int key = lane & 15, half = lane >> 4;
-      constexpr int kSet = 4;
+    if (partial) keep_hidden_values_out(vbuf, hi, lo, seen);
 #pragma unroll
-      for (int j0 = 0; j0 < D / 16; j0 += kSet) {
-        uint32_t vf[kSet][4];
+    for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-        for (int j = 0; j < kSet; ++j) ldmatrix4_trans(vs + chunk_at<kRowBytes>(key, 2 * (j0 + j) + half), vf[j]);
+      for (int h = 0; h < 2; ++h) hi[nb][h] = transpose8(hi[nb][h]), lo[nb][h] = transpose8(lo[nb][h]);
+    constexpr int kSet = 4;      // fragments of V at a time, the low halves after the high ones of all four
 #pragma unroll
-        for (int part = 0; part < 2; ++part)
+    for (int j0 = 0; j0 < D / 16; j0 += kSet) {
+      uint32_t vf[kSet][4];
 #pragma unroll
-          for (int j = 0; j < kSet; ++j)
+      for (int j = 0; j < kSet; ++j)
+        ldmatrix4_trans(vs + chunk_at<kRowBytes>((lane & 7) + ((lane >> 4) << 3), 2 * (j0 + j) + ((lane >> 3) & 1)), vf[j]);
 #pragma unroll
-            for (int mi = 0; mi < M; ++mi) {
-              mma16816(o[mi][2 * (j0 + j)], part ? pl[mi] : ph[mi], vf[j][0], vf[j][1]);
-              mma16816(o[mi][2 * (j0 + j) + 1], part ? pl[mi] : ph[mi], vf[j][2], vf[j][3]);
-            }
-      }
+      for (int part = 0; part < 2; ++part)
+#pragma unroll
+        for (int j = 0; j < kSet; ++j)
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+            mma16816(o[nb][j0 + j], vf[j], part ? lo[nb][0] : hi[nb][0], part ? lo[nb][1] : hi[nb][1]);
     }
   }
 
   // Keys that some rows see and others do not (or that are padding): a weight of zero times an infinite or NaN value
   // would be NaN in the product.  If V holds such values (rare), their terms are added here for the rows that
   // see them, one by one, and they are replaced by zero.
-  __device__ __forceinline__ void keep_hidden_values_out(uint8_t *vbuf, const uint32_t (&ph)[M][4], const uint32_t (&pl)[M][4],
-                                                      const uint32_t (&seen)[M][2]) {
+  __device__ __forceinline__ void keep_hidden_values_out(uint8_t *vbuf, const uint32_t (&hi)[NB][2], const uint32_t (&lo)[NB][2],
+                                                         const uint32_t (&seen)[NB]) {
     const int lane = threadIdx.x & 31;
     constexpr int kWords = kKeys * kRowBytes / 4;
     uint32_t *words = reinterpret_cast<uint32_t *>(vbuf);
-    bool odd = false;
+    bool bad = false;
     for (int w = lane; w < kWords; w += 32) {
       const uint32_t v = words[w];
-      odd |= (v & 0x7f80u) == 0x7f80u || (v & 0x7f800000u) == 0x7f800000u;
+      bad |= (v & 0x7f80u) == 0x7f80u || (v & 0x7f800000u) == 0x7f800000u;
     }
-    if (!__any_sync(0xffffffffu, odd)) return;
+    if (!__any_sync(0xffffffffu, bad)) return;
 #pragma unroll 1
     for (int key = 0; key < kKeys; ++key) {
-      const int src = (lane & ~3) | ((key & 7) >> 1), bit = 2 * (key >> 3) + (key & 1);
+      const int src = (key & 7) * 4 + (lane & 3), h = key >> 3;
 #pragma unroll
-      for (int mi = 0; mi < M; ++mi)
+      for (int nb = 0; nb < NB; ++nb) {
+        const uint32_t wh = __shfl_sync(0xffffffffu, h ? hi[nb][1] : hi[nb][0], src);
+        const uint32_t wl = __shfl_sync(0xffffffffu, h ? lo[nb][1] : lo[nb][0], src);
+        const uint32_t vis = __shfl_sync(0xffffffffu, seen[nb], src) >> (2 * h);
+        const float w0 = bf16lo_to_f32(wh) + bf16lo_to_f32(wl), w1 = bf16hi_to_f32(wh) + bf16hi_to_f32(wl);
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const uint32_t hi = __shfl_sync(0xffffffffu, key < 8 ? ph[mi][e] : ph[mi][2 + e], src);
-          const uint32_t lo = __shfl_sync(0xffffffffu, key < 8 ? pl[mi][e] : pl[mi][2 + e], src);
-          const bool vis = (__shfl_sync(0xffffffffu, seen[mi][e], src) >> bit) & 1;
-          const float w = key & 1 ? bf16hi_to_f32(hi) + bf16hi_to_f32(lo) : bf16lo_to_f32(hi) + bf16lo_to_f32(lo);
-          if (!vis) continue;
+        for (int j = 0; j < D / 16; ++j)
 #pragma unroll
-          for (int j = 0; j < D / 8; ++j) {
-            const uint32_t v = *reinterpret_cast<const uint32_t *>(vbuf + chunk_at<kRowBytes>(key, j) + (lane & 3) * 4);
-            const float v0 = bf16lo_to_f32(v), v1 = bf16hi_to_f32(v);
-            if (!isfinite(v0)) o[mi][j][2 * e] += w * v0;
-            if (!isfinite(v1)) o[mi][j][2 * e + 1] += w * v1;
+          for (int half = 0; half < 2; ++half) {
+            const float v = __bfloat162float(*reinterpret_cast<const __nv_bfloat16 *>(
+                vbuf + chunk_at<kRowBytes>(key, 2 * j + half) + (lane >> 2) * 2));
+            if (isfinite(v)) continue;
+            if (vis & 1) o[nb][j][2 * half] += w0 * v;
+            if (vis & 2) o[nb][j][2 * half + 1] += w1 * v;
           }
-        }
+      }
     }
     __syncwarp();
     for (int w = lane; w < kWords; w += 32) {
@@ -317,18 +316,20 @@ struct TensorRows {
   __device__ void finish(const Item &it, float *out, float2 *ml) {
     const int lane = threadIdx.x & 31;
 #pragma unroll
-    for (int mi = 0; mi < M; ++mi)
+    for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const int r = mi * 16 + e * 8 + (lane >> 2);
-        float sum = l[mi][e];
-        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-        if (r >= it.rows) continue;
-        if ((lane & 3) == 0) ml[r] = make_float2(m[mi][e], sum);
+        const int r = 8 * nb + 2 * (lane & 3) + e;
+        float sum = l[nb][e];
 #pragma unroll
-        for (int j = 0; j < D / 8; ++j)
-          *reinterpret_cast<float2 *>(out + r * D + 8 * j + 2 * (lane & 3)) = make_float2(o[mi][j][2 * e], o[mi][j][2 * e + 1]);
+        for (int off = 4; off < 32; off <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+        if (r >= it.rows) continue;
+        if (lane < 4) ml[r] = make_float2(m[nb][e], sum);
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) {
+          out[r * D + 16 * j + (lane >> 2)] = o[nb][j][e];
+          out[r * D + 16 * j + 8 + (lane >> 2)] = o[nb][j][2 + e];
+        }
       }
   }
 };
@@ -483,8 +484,12 @@ struct Layout {
   static constexpr int kRing = kStages * 2 * kSub;                  // of one warp; holds its sums at the item's end
   static constexpr int kOffQ = kWarps * kRing;
   static constexpr int kOffMl = kOffQ + Rows::kQBytes;
-  static constexpr int kOffTotal = kOffMl + kWarps * Rows::kRows * 8;      // the CTA's maximum and sum of each row
-  static constexpr int kOffMisc = kOffTotal + Rows::kRows * 8;
+  // what the ranks of a cluster write into each other's: sums, maxima and sums of weights.  Not in the rings, where the
+  // receiving rank may still be loading; 32 rows leave no room for it beside them.
+  static constexpr bool kClusters = Rows::kRows * Rows::D <= 2048;
+  static constexpr int kOffParts = kOffMl + kWarps * Rows::kRows * 8;
+  static constexpr int kOffTotals = kOffParts + (kClusters ? Rows::kRows * Rows::D * 4 : 0);
+  static constexpr int kOffMisc = kOffTotals + (kClusters ? 8 * Rows::kRows * 8 : 0);
   static constexpr int kBytes = kOffMisc + 64;
   static constexpr int kTile = kWarps * Rows::kKeys;
   static_assert(Rows::kRows * Rows::D * 4 <= kRing, "the ring is reused for the warp's sums");
@@ -506,6 +511,7 @@ __device__ __forceinline__ void stream_keys(const Params &a, const Item &it, int
   const int32_t *table = p.block_table + it.b * p.table_stride;
   const uint8_t *kbase = reinterpret_cast<const uint8_t *>(reinterpret_cast<const T *>(p.k_cache) + it.g * p.cache_stride[1]);
   const uint8_t *vbase = reinterpret_cast<const uint8_t *>(reinterpret_cast<const T *>(p.v_cache) + it.g * p.cache_stride[1]);
+  const long long row_bytes = p.cache_stride[2] * (long long)sizeof(T);
   const int x_first = tile0 * L::kTile + warp * Rows::kKeys;
   // a lane looks up the cache row of key lane % kKeys, one stage ahead of its use
   int pos = paged_key(it.q, x_first + lane % Rows::kKeys);
@@ -519,15 +525,30 @@ __device__ __forceinline__ void stream_keys(const Params &a, const Item &it, int
       at = (ok * p.cache_stride[0] + slot * p.cache_stride[2]) * (long long)sizeof(T);
     }
     const uint32_t dst = sm100::smem_u32(ring + (i % kStages) * 2 * L::kSub);
+    // keys that lie evenly (in one page) need one address; otherwise every row's is fetched from the lane that has it
+    const long long at0 = __shfl_sync(0xffffffffu, at, 0);
+    if (__all_sync(0xffffffffu, at == at0 + (lane % Rows::kKeys) * row_bytes && at0 >= 0)) {
+      long long from = at0 + (lane / kChunks) * row_bytes + 16 * (lane % kChunks);
 #pragma unroll
-    for (int j = 0; j < kOps; ++j) {
-      const int c = j * 32 + lane, r = c / kChunks, ch = c % kChunks;
-      const long long off = __shfl_sync(0xffffffffu, at, r);
-      const bool there = off >= 0;
-      const uint32_t to = dst + chunk_at<Rows::kRowBytes>(r, ch);
-      const long long from = (there ? off : 0) + 16 * ch;
-      cp_async16(to, kbase + from, there);
-      cp_async16(to + L::kSub, vbase + from, there);
+      for (int j = 0; j < kOps; ++j) {
+        const int c = j * 32 + lane;
+        const uint32_t to = dst + chunk_at<Rows::kRowBytes>(c / kChunks, c % kChunks);
+        cp_async16(to, kbase + from, true);
+        cp_async16(to + L::kSub, vbase + from, true);
+        from += kChunks >= 32 && j % (kChunks / 32 > 0 ? kChunks / 32 : 1) != kChunks / 32 - 1
+                    ? 512 : kChunks >= 32 ? row_bytes - (kChunks / 32 - 1) * 512 : (32 / kChunks) * row_bytes;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < kOps; ++j) {
+        const int c = j * 32 + lane, r = c / kChunks, ch = c % kChunks;
+        const long long off = __shfl_sync(0xffffffffu, at, r);
+        const bool there = off >= 0;
+        const uint32_t to = dst + chunk_at<Rows::kRowBytes>(r, ch);
+        const long long from = (there ? off : 0) + 16 * ch;
+        cp_async16(to, kbase + from, there);
+        cp_async16(to + L::kSub, vbase + from, there);
+      }
     }
     if (i + 1 < n_tiles) {
       pos = paged_key(it.q, x_first + (i + 1) * L::kTile + lane % Rows::kKeys);
@@ -575,7 +596,8 @@ __device__ __forceinline__ float4 join_warps(const uint8_t *smem, int r, int d, 
   return v;
 }
 
-// An item on a cluster: rank r takes the r-th part of its key tiles, then the ranks share out the output's elements.
+// An item on a cluster of n: rank k takes the k-th part of its key tiles and writes its sums into the other ranks' shared
+// memory, a n-th of the dimensions to each, which then adds up and writes that part of the output.
 template <class Rows>
 __device__ __forceinline__ void cluster_item(const Params &a, const Item &it, uint8_t *smem, uint32_t &flags) {
   namespace cg = cooperative_groups;
@@ -583,42 +605,37 @@ __device__ __forceinline__ void cluster_item(const Params &a, const Item &it, ui
   using L = Layout<Rows>;
   constexpr int D = Rows::D;
   auto cluster = cg::this_cluster();
+  cluster.barrier_arrive();      // waited for before the first write to another rank: it has started by then
   const int rank = (int)cluster.block_rank(), n = a.cluster, tid = threadIdx.x;
   const int per = (it.q.tiles + n - 1) / n;      // n is at most 8
   const int tile0 = min(rank * per, it.q.tiles), n_tiles = min(per, it.q.tiles - tile0);
-  float2 *total = reinterpret_cast<float2 *>(smem + L::kOffTotal);
-  float *mine = reinterpret_cast<float *>(smem);      // over the first warp's sums, element by element
+  const int quads = D / 4 / n;                   // float4 of a row that a rank adds up
+  float4 *parts = reinterpret_cast<float4 *>(smem + L::kOffParts);      // [n][rows][quads]
+  float2 *totals = reinterpret_cast<float2 *>(smem + L::kOffTotals);    // [n][rows]
   stream_keys<Rows>(a, it, tile0, n_tiles, smem, flags);
+  cluster.barrier_wait();
   for (int e = tid; e < it.rows * (D / 4); e += kThreads) {
-    const int r = e / (D / 4), d = e % (D / 4) * 4;
+    const int r = e / (D / 4), d = e % (D / 4), to = d / quads;
     float top, sum;
-    const float4 v = join_warps<Rows>(smem, r, d, top, sum);
-    *reinterpret_cast<float4 *>(mine + r * D + d) = v;
-    if (d == 0) total[r] = make_float2(top, sum);
+    const float4 v = join_warps<Rows>(smem, r, 4 * d, top, sum);
+    *cluster.map_shared_rank(parts + (rank * it.rows + r) * quads + (d - to * quads), to) = v;
+    if (d == to * quads) *cluster.map_shared_rank(totals + rank * it.rows + r, to) = make_float2(top, sum);
   }
   cluster.sync();
-  for (int e = rank * kThreads + tid; e < it.rows * (D / 4); e += n * kThreads) {
-    const int r = e / (D / 4), d = e % (D / 4) * 4;
-    float2 ml[8];
+  for (int e = tid; e < it.rows * quads; e += kThreads) {
+    const int r = e / quads, d = e - r * quads;
     float top = -INFINITY, sum = 0.f;
-#pragma unroll
-    for (int k = 0; k < 8; ++k)
-      if (k < n) {
-        ml[k] = *cluster.map_shared_rank(total + r, k);
-        top = fmaxf(top, ml[k].x);
-      }
+    for (int k = 0; k < n; ++k) top = fmaxf(top, totals[k * it.rows + r].x);
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int k = 0; k < 8; ++k)
-      if (k < n) {
-        const float4 x = *cluster.map_shared_rank(reinterpret_cast<const float4 *>(mine + r * D + d), k);
-        const float f = ml[k].x == -INFINITY ? 0.f : ex2_approx(ml[k].x - top);
-        sum = fmaf(ml[k].y, f, sum);
-        v.x = fmaf(x.x, f, v.x), v.y = fmaf(x.y, f, v.y), v.z = fmaf(x.z, f, v.z), v.w = fmaf(x.w, f, v.w);
-      }
-    write_row4<T>(a, row_of(a, it, r), d, v, top, sum);
+    for (int k = 0; k < n; ++k) {
+      const float2 ml = totals[k * it.rows + r];
+      const float4 x = parts[(k * it.rows + r) * quads + d];
+      const float f = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - top);
+      sum = fmaf(ml.y, f, sum);
+      v.x = fmaf(x.x, f, v.x), v.y = fmaf(x.y, f, v.y), v.z = fmaf(x.z, f, v.z), v.w = fmaf(x.w, f, v.w);
+    }
+    write_row4<T>(a, row_of(a, it, r), 4 * (rank * quads + d), v, top, sum);
   }
-  cluster.sync();      // nobody leaves while its shared memory is read
 }
 
 template <class Rows>
@@ -638,7 +655,7 @@ __global__ void __launch_bounds__(kThreads, Rows::kCtas) attn_paged_kernel(const
     return paged_seq(a.s, lo, hi, p.kv_len[b]);
   };
   Item it;
-  if (a.cluster) {
+  if (L::kClusters && a.cluster) {
     const int item = (int)blockIdx.x / a.cluster;
     it.b = fast_div(item, a.item_div);
     const int rest = item - it.b * (int)a.item_div.d;
@@ -647,7 +664,8 @@ __global__ void __launch_bounds__(kThreads, Rows::kCtas) attn_paged_kernel(const
     it.q = sequence(it.b);
     if (it.q.bad) flags |= DS_DEV_INDEX;
     it.rows = min(Rows::kRows, it.q.count * a.s.G - it.row0);
-    if (it.rows > 0) cluster_item<Rows>(a, it, smem, flags);      // the whole cluster or none of it
+    if constexpr (L::kClusters)
+      if (it.rows > 0) cluster_item<Rows>(a, it, smem, flags);      // the whole cluster or none of it
     if (flags && p.status) atomicOr(p.status, flags);
     return;
   }
@@ -855,7 +873,7 @@ Shape shape_of(const ds_paged_params &p) {
   const long long items = (long long)p.B * p.Hkv * q.row_tiles;
   h.heads = p.Hkv * q.row_tiles;
   h.cluster = 0;
-  if (q.row_tiles > 0 && items * 2 <= resident) {
+  if (L::kClusters && q.row_tiles > 0 && items * 2 <= resident) {
     int n = 8;
     while (n > 1 && (items * n > resident || n > h.tiles)) n /= 2;
     if (n > 1 && h.tiles <= n * kClusterTiles) {
@@ -920,14 +938,14 @@ int launch_rows(const ds_paged_params &p, cudaStream_t stream) {
   return DS_OK;
 }
 
-// Calls f with the row engine for the call's type, head dimension and rows per KV head.  One block of 16 rows keeps
-// the queries in registers; more rows than 32 are served 32 at a time.
+// Calls f with the row engine for the call's type, head dimension and rows per KV head.  More rows than 32 are
+// served 32 at a time.
 template <class F>
 auto with_rows(const ds_paged_params &p, F f) {
   const long long rows = (long long)p.max_q * (p.Hq / p.Hkv);
   if (p.dtype == DS_BF16) {
-    if (p.D == 64) return rows <= 16 ? f(TensorRows<64, 1>()) : f(TensorRows<64, 2>());
-    return rows <= 16 ? f(TensorRows<128, 1>()) : f(TensorRows<128, 2>());
+    if (p.D == 64) return rows <= 8 ? f(TensorRows<64, 1>()) : rows <= 16 ? f(TensorRows<64, 2>()) : f(TensorRows<64, 4>());
+    return rows <= 8 ? f(TensorRows<128, 1>()) : rows <= 16 ? f(TensorRows<128, 2>()) : f(TensorRows<128, 4>());
   }
   switch (p.D) {
     case 32: return rows == 1 ? f(ScalarRows<32, 1>()) : f(ScalarRows<32, 8>());
