@@ -28,7 +28,7 @@
 namespace ds {
 namespace {
 
-constexpr int kWarps = 4, kThreads = kWarps * 32, kStages = 3;
+constexpr int kWarps = 4, kThreads = kWarps * 32;
 constexpr int kMinTiles = 4;     // a range has at least so many key tiles
 constexpr int kWholeTiles = 8;   // items of at most so many key tiles are not split
 constexpr int kClusterTiles = 24;   // most key tiles of a CTA when an item has a cluster
@@ -109,7 +109,9 @@ struct TensorRows {
   static constexpr int D = D_, kRows = 8 * NB, kRowBytes = 2 * D, kKeys = 16;
   static constexpr bool kQRegs = NB <= 2;      // more rows read their queries' fragments from shared memory
   static constexpr int kQBytes = kQRegs ? 0 : kRows * kRowBytes;
-  static constexpr int kCtas = D == 64 && NB == 1 ? 4 : D == 64 && NB == 2 ? 3 : 2;          // per SM: registers and shared memory
+  // CTAs per SM and stages of a ring: what registers and shared memory hold.  For one block of rows three CTAs with two
+  // stages beat two with three (32 x 32 heads x 4128 rows, D = 128: 316 against 330 us).
+  static constexpr int kCtas = D == 64 && NB == 1 ? 4 : NB == 1 || (D == 64 && NB == 2) ? 3 : 2, kStages = D == 128 && NB == 1 ? 2 : 3;
   float o[NB][D / 16][4];        // dimensions 16 j + lane / 4 (+ 8), rows 2q, 2q + 1
   float m[NB][2], l[NB][2];
   int end[NB][2];
@@ -342,7 +344,7 @@ struct ScalarRows {
   using T = float;
   static constexpr int D = D_, kRows = R, kRowBytes = 4 * D, kKeys = kRowBytes >= 512 ? 4096 / kRowBytes : 16;
   static constexpr int kQBytes = 0, C = D / 32, kPer = kKeys / 4;
-  static constexpr int kCtas = D == 32 && R == 1 ? 4 : 2;
+  static constexpr int kCtas = D == 32 && R == 1 ? 4 : 2, kStages = 3;
   float4 q[R][C], o[R][C];
   float m[R], l[R];
   int end[R];
@@ -481,7 +483,7 @@ __device__ __forceinline__ void write_row4(const Params &a, const Row &row, int 
 template <class Rows>
 struct Layout {
   static constexpr int kSub = Rows::kKeys * Rows::kRowBytes;        // K or V of one stage of a warp
-  static constexpr int kRing = kStages * 2 * kSub;                  // of one warp; holds its sums at the item's end
+  static constexpr int kRing = Rows::kStages * 2 * kSub;                  // of one warp; holds its sums at the item's end
   static constexpr int kOffQ = kWarps * kRing;
   static constexpr int kOffMl = kOffQ + Rows::kQBytes;
   // what the ranks of a cluster write into each other's: sums, maxima and sums of weights.  Not in the rings, where the
@@ -507,7 +509,7 @@ __device__ __forceinline__ void stream_keys(const Params &a, const Item &it, int
   const float scale2 = p.scale * kLog2e;
   Rows rows;
   rows.begin(a, it, smem + L::kOffQ);
-  constexpr int kChunks = Rows::kRowBytes / 16, kOps = Rows::kKeys * kChunks / 32;
+  constexpr int kStages = Rows::kStages, kChunks = Rows::kRowBytes / 16, kOps = Rows::kKeys * kChunks / 32;
   const int32_t *table = p.block_table + it.b * p.table_stride;
   const uint8_t *kbase = reinterpret_cast<const uint8_t *>(reinterpret_cast<const T *>(p.k_cache) + it.g * p.cache_stride[1]);
   const uint8_t *vbase = reinterpret_cast<const uint8_t *>(reinterpret_cast<const T *>(p.v_cache) + it.g * p.cache_stride[1]);
@@ -647,7 +649,7 @@ __global__ void __launch_bounds__(kThreads, Rows::kCtas) attn_paged_kernel(const
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const ds_paged_params &p = a.p;
   uint32_t flags = 0;
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  dependent_sync();
 
   // ---- this CTA's range of the units, and the sequence that it begins in
   auto sequence = [&](int b) {
@@ -806,7 +808,7 @@ __global__ void __launch_bounds__(kJoinThreads) attn_paged_join_kernel(const __g
   constexpr int kLanes = D / 4, kGroups = kJoinThreads / kLanes;
   __shared__ float4 o_s[kGroups][kLanes];
   __shared__ float sum_s[kGroups], top_s[kJoinThreads / 32];
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  dependent_sync();
   const PagedJoin j = a.joins[blockIdx.x];
   const int r = blockIdx.y, tid = threadIdx.x, group = tid / kLanes, u = tid % kLanes;
   if (r >= j.rows || j.parts == 0) return;
@@ -908,32 +910,19 @@ int launch_rows(const ds_paged_params &p, cudaStream_t stream) {
   a.joins = reinterpret_cast<PagedJoin *>(ws);
   a.part_ml = reinterpret_cast<float2 *>(ws + h.bytes_joins);
   a.part_o = reinterpret_cast<float *>(ws + h.bytes_joins + h.bytes_ml);
-  DS_CUDA_OK(cudaFuncSetAttribute(attn_paged_kernel<Rows>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes));
+  static std::atomic<unsigned long long> allowed{0};
+  DS_CUDA_OK(allow_smem(attn_paged_kernel<Rows>, L::kBytes, allowed));
   a.cluster = h.cluster;
   a.item_div = make_fast_div(h.heads > 0 ? h.heads : 1);
   a.row_div = make_fast_div(h.heads > 0 ? h.heads / p.Hkv : 1);
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(h.grid);
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = L::kBytes;
-  cfg.stream = stream;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = h.cluster;
-  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = h.cluster ? 1 : 0;
-  DS_CUDA_OK(cudaLaunchKernelEx(&cfg, attn_paged_kernel<Rows>, a));
+  // not set up early: its CTAs would wait in the slots that the kernel before it, often this one, leaves (32 x 32 heads x
+  // 4128 rows back to back 403 instead of 316 us)
+  DS_CUDA_OK(launch_kernel(attn_paged_kernel<Rows>, dim3(h.grid), kThreads, L::kBytes, h.cluster, false, stream, a));
   note_launch(1);
   if (!a.split) return DS_OK;
   const int rows = (int)((long long)p.max_q * h.s.G < Rows::kRows ? (long long)p.max_q * h.s.G : Rows::kRows);
-  cfg.gridDim = dim3(h.grid, rows);
-  cfg.blockDim = dim3(kJoinThreads);
-  cfg.dynamicSmemBytes = 0;
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.numAttrs = 1;
-  DS_CUDA_OK(cudaLaunchKernelEx(&cfg, attn_paged_join_kernel<typename Rows::T, Rows::D, Rows::kRows>, a));
+  DS_CUDA_OK(launch_kernel(attn_paged_join_kernel<typename Rows::T, Rows::D, Rows::kRows>, dim3(h.grid, rows), kJoinThreads, 0,
+                           0, true, stream, a));
   note_launch(1);
   return DS_OK;
 }

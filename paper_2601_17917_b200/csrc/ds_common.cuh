@@ -4,6 +4,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "ds.h"
 
 namespace ds {
@@ -28,6 +30,51 @@ int sm_count();
       return DS_ERR_CUDA;                         \
     }                                             \
   } while (0)
+
+// Programmatic dependent launch, for the short kernels of the paged cache: one launched with `dependent` may be set up
+// while the previous kernel in the stream still runs.  dependent_sync() comes before its first access to memory: it returns
+// when everything before it in the stream is done; the next kernel may then be set up in turn.
+__device__ __forceinline__ void dependent_sync() {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+// Raises the limit of a kernel's dynamic shared memory, once per device and kernel (`done`: a static of the caller's).
+template <class K>
+cudaError_t allow_smem(K *kernel, int bytes, std::atomic<unsigned long long> &done) {
+  int dev = 0;
+  const cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const unsigned long long bit = 1ull << (dev & 63);
+  if (dev < 64 && (done.load(std::memory_order_acquire) & bit)) return cudaSuccess;
+  const cudaError_t rc = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (rc == cudaSuccess && dev < 64) done.fetch_or(bit, std::memory_order_release);
+  return rc;
+}
+// Launches a kernel, on clusters of so many CTAs (0: none).
+template <class... P, class... A>
+cudaError_t launch_kernel(void (*kernel)(P...), dim3 grid, int threads, size_t smem, int cluster, bool dependent,
+                          cudaStream_t stream, A... args) {
+  cudaLaunchAttribute attr[2];
+  int n = 0;
+  if (dependent) {
+    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[n++].val.programmaticStreamSerializationAllowed = 1;
+  }
+  if (cluster > 0) {
+    attr[n].id = cudaLaunchAttributeClusterDimension;
+    attr[n].val.clusterDim.x = cluster;
+    attr[n].val.clusterDim.y = 1;
+    attr[n++].val.clusterDim.z = 1;
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = n;
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
 
 __device__ __forceinline__ float ex2_approx(float x) {
   float y;

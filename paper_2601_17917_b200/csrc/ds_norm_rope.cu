@@ -98,6 +98,7 @@ __global__ void __launch_bounds__(kThreads) norm_rope_kernel(const __grid_consta
   constexpr int E = C::kElems, H = E / 2;      // elements and pairs of fp32 of a chunk
   __shared__ __align__(16) uint4 ring_s[kWarps][kAhead][2][32];
   __shared__ __align__(16) float2 turn_s[kWarps][kMaxPairs];
+  dependent_sync();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, u = lane % W, group = lane / W;
   const long long unit = (long long)blockIdx.x * kWarps + warp;
   const int n_rows = p.n_rows ? min(max(*p.n_rows, 0), p.N) : p.N;
@@ -280,9 +281,8 @@ int launch_width(const ds_qk_params &p, cudaStream_t stream) {
   l.page_div = make_fast_div(p.page_size > 0 ? p.page_size : 1);
   if ((long long)p.N * l.chunks > 0x7fffffffLL) return DS_ERR_UNSUPPORTED;      // needs more than 400000 heads
   const long long blocks = ((long long)p.N * l.chunks + kWarps - 1) / kWarps;
-  if (p.rope->interleaved) norm_rope_kernel<T, W, true><<<(unsigned)blocks, kThreads, 0, stream>>>(p, *p.rope, l);
-  else norm_rope_kernel<T, W, false><<<(unsigned)blocks, kThreads, 0, stream>>>(p, *p.rope, l);
-  DS_CUDA_OK(cudaGetLastError());
+  DS_CUDA_OK(launch_kernel(p.rope->interleaved ? norm_rope_kernel<T, W, true> : norm_rope_kernel<T, W, false>,
+                           dim3((unsigned)blocks), kThreads, 0, 0, true, stream, p, *p.rope, l));
   note_launch(1);
   return DS_OK;
 }

@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(kThreads) page_update_kernel(const __grid_cons
   namespace cg = cooperative_groups;
   extern __shared__ int smem[];
   __shared__ Sums warp_sums[2][kThreads / 32];
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  dependent_sync();
   const int n_ctas = gridDim.x;       // all in one cluster
   auto barrier = [&]() {
     if (n_ctas > 1) cg::this_cluster().sync();
@@ -248,7 +248,7 @@ __device__ __forceinline__ int warp_owner(const int *sum, int n, int x) {
 // positions and slot_map from row_start, kv_len_out and the finished tables.
 __global__ void __launch_bounds__(kFillThreads) page_rows_kernel(const __grid_constant__ ds_page_params p, const FastDiv ps_div,
                                                                  const bool vector) {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  dependent_sync();
   const int B = p.B, ps = p.page_size, warp_rows = 128;
   const long long w0 = ((long long)blockIdx.x * (kFillThreads / 32) + (threadIdx.x >> 5)) * warp_rows;
   if (w0 >= p.max_rows) return;
@@ -291,20 +291,10 @@ __global__ void __launch_bounds__(kFillThreads) page_rows_kernel(const __grid_co
 template <int kThreads>
 int launch_update(const ds_page_params &p, int ctas, bool vector, bool fill, cudaStream_t stream) {
   const size_t smem = sizeof(int) * (4 * (size_t)p.B + 4);
-  if (smem > 40 * 1024)
-    DS_CUDA_OK(cudaFuncSetAttribute(page_update_kernel<kThreads>, cudaFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024));
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(ctas);
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = stream;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = ctas;
-  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = ctas > 1 ? 1 : 0;
-  DS_CUDA_OK(cudaLaunchKernelEx(&cfg, page_update_kernel<kThreads>, p, make_fast_div(p.page_size), vector, fill));
+  static std::atomic<unsigned long long> allowed{0};
+  if (smem > 40 * 1024) DS_CUDA_OK(allow_smem(page_update_kernel<kThreads>, 160 * 1024, allowed));
+  DS_CUDA_OK(launch_kernel(page_update_kernel<kThreads>, dim3(ctas), kThreads, smem, ctas > 1 ? ctas : 0, true, stream, p,
+                           make_fast_div(p.page_size), vector, fill));
   note_launch(1);
   return DS_OK;
 }
@@ -318,16 +308,8 @@ int launch_page_update(const ds_page_params &p, cudaStream_t stream) {
     return p.B <= 256 ? launch_update<256>(p, 1, vector, rows, stream) : launch_update<1024>(p, 1, vector, rows, stream);
   const int rc = launch_update<1024>(p, kCluster, vector, false, stream);
   if (rc != DS_OK || !rows) return rc;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(((long long)p.max_rows + 4 * kFillThreads - 1) / (4 * kFillThreads)));
-  cfg.blockDim = dim3(kFillThreads);
-  cfg.stream = stream;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  DS_CUDA_OK(cudaLaunchKernelEx(&cfg, page_rows_kernel, p, make_fast_div(p.page_size), vector));
+  const dim3 grid((unsigned)(((long long)p.max_rows + 4 * kFillThreads - 1) / (4 * kFillThreads)));
+  DS_CUDA_OK(launch_kernel(page_rows_kernel, grid, kFillThreads, 0, 0, true, stream, p, make_fast_div(p.page_size), vector));
   note_launch(1);
   return DS_OK;
 }
