@@ -21,39 +21,18 @@
 
 #include <type_traits>
 
-#include "ds_common.cuh"
-#include "ds_paged_index.cuh"
-#include "ds_sm100.cuh"
+#include "ds_attn_paged.cuh"
 
 namespace ds {
 namespace {
+
+using namespace paged;
 
 constexpr int kWarps = 4, kThreads = kWarps * 32;
 constexpr int kMinTiles = 4;     // a range has at least so many key tiles
 constexpr int kWholeTiles = 8;   // items of at most so many key tiles are not split
 constexpr int kClusterTiles = 24;   // most key tiles of a CTA when an item has a cluster
 
-struct Params {
-  ds_paged_params p;
-  PagedShape s;
-  FastDiv page_div, group_div;
-  int split;
-  int cluster;        // CTAs of an item; 0: equal ranges
-  FastDiv item_div, row_div;      // by KV heads times row tiles, by row tiles (at most): with a cluster
-  PagedJoin *joins;   // [gridDim.x]
-  float2 *part_ml;    // [2 gridDim.x][row_tile]  maximum (base 2, scaled) and sum
-  float *part_o;      // [2 gridDim.x][row_tile][D]
-};
-
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, bool there) {
-  // a chunk that is not there is filled with zeros and not read
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_async_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
 __device__ __forceinline__ void ldmatrix4(uint32_t addr, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
@@ -80,23 +59,6 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
 // within groups of eight, which makes ldmatrix and the float4 reads below free of bank conflicts.
 template <int ROW>
 __device__ __forceinline__ uint32_t chunk_at(int r, int c) { return r * ROW + ((c ^ (r & 7)) << 4); }
-
-// The item a CTA works on.
-struct Item {
-  PagedSeq q;
-  int b, g;            // sequence, KV head
-  int row0, rows;      // stacked rows row0 .. row0 + rows - 1 of the sequence
-};
-
-// Stacked row -> query row of the packed arrays, head, and how much of the cache it sees.
-struct Row {
-  long long n;
-  int h, end;
-};
-__device__ __forceinline__ Row row_of(const Params &a, const Item &it, int r) {
-  const int rr = it.row0 + r, i = fast_div(rr, a.group_div);
-  return {(long long)it.q.first + i, it.g * a.s.G + (rr - i * a.s.G), a.s.causal ? it.q.end_min + i : it.q.len};
-}
 
 // ---------------------------------------------------------------------------------------------------------------
 // A warp's share of an item in bf16: NB blocks of 8 rows against 16 keys at a time, with the keys as the products' 16-wide
@@ -466,20 +428,6 @@ struct ScalarRows {
 };
 
 // ---------------------------------------------------------------------------------------------------------------
-__device__ __forceinline__ void store4(float *p, const float4 &v) { *reinterpret_cast<float4 *>(p) = v; }
-__device__ __forceinline__ void store4(__nv_bfloat16 *p, const float4 &v) {
-  *reinterpret_cast<uint2 *>(p) = make_uint2(sm100::pack_bf16(v.x, v.y), sm100::pack_bf16(v.z, v.w));
-}
-
-// Sums of a finished row -> output and log-sum-exp.  A row that saw nothing has sum 0; a NaN stays one.
-template <typename T>
-__device__ __forceinline__ void write_row4(const Params &a, const Row &row, int d, float4 v, float top, float sum) {
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  v.x *= inv, v.y *= inv, v.z *= inv, v.w *= inv;
-  store4(reinterpret_cast<T *>(a.p.out) + row.n * a.p.out_stride[0] + row.h * a.p.out_stride[1] + d, v);
-  if (a.p.lse && d == 0) a.p.lse[row.n * a.p.Hq + row.h] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
-}
-
 template <class Rows>
 struct Layout {
   static constexpr int kSub = Rows::kKeys * Rows::kRowBytes;        // K or V of one stage of a warp
@@ -646,138 +594,35 @@ __global__ void __launch_bounds__(kThreads, Rows::kCtas) attn_paged_kernel(const
   using L = Layout<Rows>;
   constexpr int D = Rows::D;
   extern __shared__ __align__(128) uint8_t smem[];
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x;
   const ds_paged_params &p = a.p;
   uint32_t flags = 0;
   dependent_sync();
 
-  // ---- this CTA's range of the units, and the sequence that it begins in
-  auto sequence = [&](int b) {
-    const int lo = p.row_start ? p.row_start[b] : b * p.max_q, hi = p.row_start ? p.row_start[b + 1] : lo + p.max_q;
-    return paged_seq(a.s, lo, hi, p.kv_len[b]);
-  };
-  Item it;
-  if (L::kClusters && a.cluster) {
-    const int item = (int)blockIdx.x / a.cluster;
-    it.b = fast_div(item, a.item_div);
-    const int rest = item - it.b * (int)a.item_div.d;
-    it.g = fast_div(rest, a.row_div);
-    it.row0 = (rest - it.g * (int)a.row_div.d) << a.s.row_log2;
-    it.q = sequence(it.b);
-    if (it.q.bad) flags |= DS_DEV_INDEX;
-    it.rows = min(Rows::kRows, it.q.count * a.s.G - it.row0);
-    if constexpr (L::kClusters)
+  Walk walk;
+  if constexpr (L::kClusters)
+    if (a.cluster) {
+      Item &it = walk.it;
+      const int item = (int)blockIdx.x / a.cluster;
+      it.b = fast_div(item, a.item_div);
+      const int rest = item - it.b * (int)a.item_div.d;
+      it.g = fast_div(rest, a.row_div);
+      it.row0 = (rest - it.g * (int)a.row_div.d) << a.s.row_log2;
+      it.q = sequence_of(a, it.b);
+      if (it.q.bad) flags |= DS_DEV_INDEX;
+      it.rows = min(Rows::kRows, it.q.count * a.s.G - it.row0);
       if (it.rows > 0) cluster_item<Rows>(a, it, smem, flags);      // the whole cluster or none of it
-    if (flags && p.status) atomicOr(p.status, flags);
-    return;
-  }
-  long long total, per, t, t_end, base;
-  it.b = 0;
-  auto range = [&]() {
-    per = paged_per_cta(total, gridDim.x, kMinTiles);
-    t = blockIdx.x * per;
-    t_end = min(total, t + per);
-  };
-  auto warp_scan = [&](long long inc) {
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-      const long long y = __shfl_up_sync(0xffffffffu, inc, off);
-      if (lane >= off) inc += y;
+      if (flags && p.status) atomicOr(p.status, flags);
+      return;
     }
-    return inc;
-  };
-  if (p.B <= 32) {      // every warp for itself
-    long long mine = 0;
-    if (lane < p.B) {
-      const PagedSeq q = sequence(lane);
-      if (q.bad) flags |= DS_DEV_INDEX;
-      mine = paged_units(a.s, q);
-    }
-    const long long inc = warp_scan(mine);
-    total = __shfl_sync(0xffffffffu, inc, 31);
-    range();
-    const uint32_t here = __ballot_sync(0xffffffffu, t < inc);      // inclusive sums: the first above t
-    const int src = here ? __ffs(here) - 1 : 0;
-    base = __shfl_sync(0xffffffffu, inc - mine, src);
-    it.b = src;
-  } else {
-    long long *scan = reinterpret_cast<long long *>(smem + L::kOffMisc);   // warp sums, then prefix and number
-    const int chunk = (p.B + kThreads - 1) / kThreads;
-    const int b0 = min(p.B, tid * chunk), b1 = min(p.B, b0 + chunk);
-    long long mine = 0;
-    for (int b = b0; b < b1; ++b) {
-      const PagedSeq q = sequence(b);
-      if (q.bad) flags |= DS_DEV_INDEX;
-      mine += paged_units(a.s, q);
-    }
-    const long long inc = warp_scan(mine);
-    if (lane == 31) scan[warp] = inc;
-    __syncthreads();
-    total = 0;
-    long long before = inc - mine;
-    for (int w = 0; w < kWarps; ++w) {
-      if (w < warp) before += scan[w];
-      total += scan[w];
-    }
-    range();
-    __syncthreads();
-    if (t < total && before <= t && t < before + mine) {
-      for (int b = b0; b < b1; ++b) {
-        const long long w = paged_units(a.s, sequence(b));
-        if (t < before + w) {
-          scan[0] = before;
-          scan[1] = b;
-          break;
-        }
-        before += w;
-      }
-    }
-    __syncthreads();
-    base = scan[0];
-    if (t < t_end) it.b = (int)scan[1];
-  }
-  if (flags && p.status) atomicOr(p.status, flags);
-  flags = 0;
+  walk.find<kThreads>(a, kMinTiles, reinterpret_cast<long long *>(smem + L::kOffMisc), flags);
   PagedJoin join = {0, 0, 0, 0, 0, 0};      // thread 0's
-
-  bool first_segment = true;
-  int tile0 = 0, row_tile = 0;
-  if (t < t_end) {      // the one place that needs divisions: afterwards items follow one another
-    it.q = sequence(it.b);
-    const uint32_t u = (uint32_t)(t - base), item = u / (uint32_t)it.q.tiles;
-    tile0 = (int)(u - item * (uint32_t)it.q.tiles);
-    it.g = (int)(item / (uint32_t)it.q.row_tiles);
-    row_tile = (int)(item - it.g * (uint32_t)it.q.row_tiles);
-  }
-  auto next_item = [&]() {
-    tile0 = 0;
-    if (++row_tile < it.q.row_tiles) return;
-    row_tile = 0;
-    if (++it.g < p.Hkv) return;
-    it.g = 0;
-    if (t < t_end) do it.q = sequence(++it.b);
-      while (it.q.tiles == 0);
-  };
-  while (t < t_end) {
-    it.row0 = row_tile << a.s.row_log2;
-    it.rows = min(Rows::kRows, it.q.count * a.s.G - it.row0);
-    int n_tiles = it.q.tiles - tile0;
-    if (a.split) {
-      n_tiles = (int)min((long long)n_tiles, t_end - t);
-    } else if (tile0 != 0) {       // the item belongs to the range that it begins in
-      t += n_tiles;
-      next_item();
-      continue;
-    }
-    if (a.split && tid == 0 && tile0 != 0 && first_segment && paged_join_starts(t, per, t - tile0)) {
-      join.parts = paged_join_parts(t, per, t - tile0 + it.q.tiles);
-      join.first_slot = paged_slot(blockIdx.x - 1, t - per == t - tile0);
-      join.row = it.row0, join.rows = it.rows, join.first = it.q.first, join.kv_head = it.g;
-    }
-
-    stream_keys<Rows>(a, it, tile0, n_tiles, smem, flags);
-    const bool whole = tile0 == 0 && n_tiles == it.q.tiles;
-    const int slot = paged_slot(blockIdx.x, first_segment);
+  for (; walk.piece(a); walk.next(a)) {
+    const Item &it = walk.it;
+    if (a.split && tid == 0) walk.note_join(join);
+    stream_keys<Rows>(a, it, walk.tile0, walk.n_tiles, smem, flags);
+    const bool whole = walk.whole();
+    const int slot = paged_slot(blockIdx.x, walk.first);
     for (int e = tid; e < it.rows * (D / 4); e += kThreads) {
       const int r = e / (D / 4), d = e % (D / 4) * 4;
       float top, sum;
@@ -785,146 +630,50 @@ __global__ void __launch_bounds__(kThreads, Rows::kCtas) attn_paged_kernel(const
       if (whole) {
         write_row4<T>(a, row_of(a, it, r), d, v, top, sum);
       } else {
-        const long long at = (long long)slot * Rows::kRows + r;
+        const long long at = (long long)slot * a.part_rows + r;
         *reinterpret_cast<float4 *>(a.part_o + at * D + d) = v;
         if (d == 0) a.part_ml[at] = make_float2(top, sum);
       }
     }
     __syncthreads();
-    first_segment = false;
-    t += n_tiles;
-    next_item();
   }
   if (a.split && tid == 0) a.joins[blockIdx.x] = join;
   if (flags && p.status) atomicOr(p.status, flags);
 }
 
-// Joins the parts of one item: CTA = (range that begins inside the item first, stacked row).  D / 4 threads hold the
-// row, the CTA's groups of so many threads take the parts in turn, eight loads in flight each, and are themselves joined
-// in order: the result does not depend on timing.
-constexpr int kJoinThreads = 256;
-template <typename T, int D, int kRows>
-__global__ void __launch_bounds__(kJoinThreads) attn_paged_join_kernel(const __grid_constant__ Params a) {
-  constexpr int kLanes = D / 4, kGroups = kJoinThreads / kLanes;
-  __shared__ float4 o_s[kGroups][kLanes];
-  __shared__ float sum_s[kGroups], top_s[kJoinThreads / 32];
-  dependent_sync();
-  const PagedJoin j = a.joins[blockIdx.x];
-  const int r = blockIdx.y, tid = threadIdx.x, group = tid / kLanes, u = tid % kLanes;
-  if (r >= j.rows || j.parts == 0) return;
-  auto at = [&](int k) { return (long long)(k == 0 ? j.first_slot : 2 * ((int)blockIdx.x + k - 1)) * kRows + r; };
-  float top = -INFINITY;
-  for (int k = tid; k < j.parts; k += kJoinThreads) top = fmaxf(top, a.part_ml[at(k)].x);
-#pragma unroll
-  for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-  if ((tid & 31) == 0) top_s[tid >> 5] = top;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kJoinThreads / 32; ++w) top = fmaxf(top, top_s[w]);
-  float sum = 0.f;
-  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-  for (int k = group; k < j.parts; k += kGroups) {
-    const long long s = at(k);
-    const float2 ml = a.part_ml[s];
-    const float4 x = *reinterpret_cast<const float4 *>(a.part_o + s * D + 4 * u);
-    const float f = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - top);
-    sum = fmaf(ml.y, f, sum);
-    v.x = fmaf(x.x, f, v.x), v.y = fmaf(x.y, f, v.y), v.z = fmaf(x.z, f, v.z), v.w = fmaf(x.w, f, v.w);
-  }
-  o_s[group][u] = v;
-  if (u == 0) sum_s[group] = sum;
-  __syncthreads();
-  if (tid >= kLanes) return;
-#pragma unroll
-  for (int w = 1; w < kGroups; ++w) {
-    const float4 x = o_s[w][u];
-    v.x += x.x, v.y += x.y, v.z += x.z, v.w += x.w;
-  }
-  sum = 0.f;
-  for (int w = 0; w < kGroups; ++w) sum += sum_s[w];
-  const int rr = j.row + r, i = fast_div(rr, a.group_div);
-  write_row4<T>(a, {(long long)j.first + i, j.kv_head * a.s.G + (rr - i * a.s.G), 0}, 4 * u, v, top, sum);
-}
-
 // ---------------------------------------------------------------------------------------------------------------
-struct Shape {
-  PagedShape s;
-  int grid, tiles;      // tiles: most key tiles of an item
-  int cluster, heads;   // CTAs of an item (0: equal ranges), items of a sequence
-  size_t bytes_joins, bytes_ml, bytes_o;
-};
-constexpr int log2_of(int x) { return x <= 1 ? 0 : 1 + log2_of(x / 2); }
-size_t up256(size_t x) { return (x + 255) & ~size_t(255); }
-
 template <class Rows>
-Shape shape_of(const ds_paged_params &p) {
+Shape shape_for(const ds_paged_params &p) {
   using L = Layout<Rows>;
-  Shape h;
-  const int cap = p.max_pages * p.page_size;
-  h.s = {p.B, p.Hq / p.Hkv, p.Hkv, p.N, p.max_q, p.max_len > 0 && p.max_len < cap ? p.max_len : cap,
-         p.causal != 0, p.window, p.sinks, log2_of(L::kTile), log2_of(Rows::kRows)};
-  // the most that the lengths may turn out to be
-  const PagedSeq q = paged_seq(h.s, 0, p.max_q < p.N ? p.max_q : p.N, h.s.bound);
-  h.tiles = q.tiles;
-  long long ranges = (paged_units(h.s, q) * p.B + kMinTiles - 1) / kMinTiles;
-  const long long resident = (long long)Rows::kCtas * sm_count();
-  h.grid = (int)(ranges < resident ? (ranges > 0 ? ranges : 1) : resident);
+  Shape h = shape_of(p, L::kTile, Rows::kRows, kMinTiles, Rows::kCtas);
   // A cluster per item where the items leave room for it and none is long: what the CTAs lose when the lengths
   // are uneven, or their number does not fill the GPU, has to stay below what the second kernel costs.
-  const long long items = (long long)p.B * p.Hkv * q.row_tiles;
-  h.heads = p.Hkv * q.row_tiles;
-  h.cluster = 0;
-  if (L::kClusters && q.row_tiles > 0 && items * 2 <= resident) {
+  const long long resident = (long long)Rows::kCtas * sm_count();
+  if (L::kClusters && h.items > 0 && h.items * 2 <= resident) {
     int n = 8;
-    while (n > 1 && (items * n > resident || n > h.tiles)) n /= 2;
+    while (n > 1 && (h.items * n > resident || n > h.tiles)) n /= 2;
     if (n > 1 && h.tiles <= n * kClusterTiles) {
       h.cluster = n;
-      h.grid = (int)items * n;
+      h.grid = (int)h.items * n;
     }
   }
-  h.bytes_joins = up256(sizeof(PagedJoin) * (size_t)h.grid);
-  h.bytes_ml = up256(sizeof(float2) * 2 * (size_t)h.grid * Rows::kRows);
-  h.bytes_o = sizeof(float) * 2 * (size_t)h.grid * Rows::kRows * Rows::D;
   return h;
 }
 
-template <class Rows>
-size_t workspace_of(const ds_paged_params &p) {
-  const Shape h = shape_of<Rows>(p);
-  return h.cluster || h.tiles <= kWholeTiles || h.grid == 1 ? 0 : h.bytes_joins + h.bytes_ml + h.bytes_o;
-}
+size_t workspace_of(const Shape &h) { return h.cluster || h.tiles <= kWholeTiles || h.grid == 1 ? 0 : h.workspace(); }
 
 template <class Rows>
 int launch_rows(const ds_paged_params &p, cudaStream_t stream) {
   using L = Layout<Rows>;
-  const Shape h = shape_of<Rows>(p);
-  Params a;
-  a.p = p;
-  a.s = h.s;
-  a.page_div = make_fast_div(p.page_size);
-  a.group_div = make_fast_div(h.s.G);
-  const size_t need = workspace_of<Rows>(p);
-  a.split = need > 0 && p.workspace && (reinterpret_cast<uintptr_t>(p.workspace) & 255) == 0 && p.workspace_bytes >= need;
-  uint8_t *ws = reinterpret_cast<uint8_t *>(p.workspace);
-  a.joins = reinterpret_cast<PagedJoin *>(ws);
-  a.part_ml = reinterpret_cast<float2 *>(ws + h.bytes_joins);
-  a.part_o = reinterpret_cast<float *>(ws + h.bytes_joins + h.bytes_ml);
+  const Shape h = shape_for<Rows>(p);
+  const Params a = params_of(p, h, workspace_of(h));
   static std::atomic<unsigned long long> allowed{0};
   DS_CUDA_OK(allow_smem(attn_paged_kernel<Rows>, L::kBytes, allowed));
-  a.cluster = h.cluster;
-  a.item_div = make_fast_div(h.heads > 0 ? h.heads : 1);
-  a.row_div = make_fast_div(h.heads > 0 ? h.heads / p.Hkv : 1);
   // not set up early: its CTAs would wait in the slots that the kernel before it, often this one, leaves (32 x 32 heads x
   // 4128 rows back to back 403 instead of 316 us)
   DS_CUDA_OK(launch_kernel(attn_paged_kernel<Rows>, dim3(h.grid), kThreads, L::kBytes, h.cluster, false, stream, a));
   note_launch(1);
-  if (!a.split) return DS_OK;
-  const int rows = (int)((long long)p.max_q * h.s.G < Rows::kRows ? (long long)p.max_q * h.s.G : Rows::kRows);
-  DS_CUDA_OK(launch_kernel(attn_paged_join_kernel<typename Rows::T, Rows::D, Rows::kRows>, dim3(h.grid, rows), kJoinThreads, 0,
-                           0, true, stream, a));
-  note_launch(1);
-  return DS_OK;
+  return a.split ? launch_join<typename Rows::T, Rows::D>(a, h, stream) : (int)DS_OK;
 }
 
 // Calls f with the row engine for the call's type, head dimension and rows per KV head.  More rows than 32 are
@@ -944,14 +693,22 @@ auto with_rows(const ds_paged_params &p, F f) {
   }
 }
 
+// Rows per KV head from which the kernel with tcgen05 tiles takes over.
+constexpr int kTensorTileRows = 17;
+bool wide(const ds_paged_params &p) {
+  return p.dtype == DS_BF16 && (long long)p.max_q * (p.Hq / p.Hkv) >= kTensorTileRows;
+}
+
 }  // namespace
 
 size_t attn_paged_workspace_bytes(const ds_paged_params &p) {
   if (p.B == 0 || p.N == 0) return 0;
-  return with_rows(p, [&](auto rows) { return workspace_of<decltype(rows)>(p); });
+  if (wide(p)) return attn_paged_tc_workspace_bytes(p);
+  return with_rows(p, [&](auto rows) { return workspace_of(shape_for<decltype(rows)>(p)); });
 }
 
 int launch_attn_paged(const ds_paged_params &p, cudaStream_t stream) {
+  if (wide(p)) return launch_attn_paged_tc(p, stream);
   return with_rows(p, [&](auto rows) { return launch_rows<decltype(rows)>(p, stream); });
 }
 

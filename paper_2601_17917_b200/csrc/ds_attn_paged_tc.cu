@@ -1,0 +1,503 @@
+// ds_attn_paged for many query rows per KV head (a decoding block, grouped queries of several tokens): bf16 on the 5th
+// generation tensor cores.
+//
+// An item is up to 128 stacked rows (query, head of the group) of a sequence and KV head, the rows of a tcgen05 tile:
+// S = Q K^T and O += P V in TMEM, 128 keys at a time, with the online softmax on the thread that owns the row.  The units
+// of work, their equal ranges over the SMs and the join of items that ranges share are those of the kernel for few
+// rows.  It is bound by HBM as long as the 1536 tensor cycles of a 64 KB key tile (512 for S, 1024 for P V, below) fit
+// into the 2800 that HBM needs for it.
+//
+// Warps:
+//   0-3  softmax and epilogue, thread = row = TMEM lane
+//   4    issues the products
+//   5    loads the queries of the next item
+//   6-9  load K and V, 32 keys each: 16-byte asynchronous copies from wherever the page table says, written in the
+//        128-byte swizzle that the products read.  (A page may be as small as one row, which leaves no box for TMA.)
+// K and V tiles pass through a ring of kStages.  The copies are issued two tiles ahead of their announcement: a warp
+// announces a tile when its copies are complete, after the next tile's have been issued.
+//
+// As with few rows the weights are kept as two bf16 halves, P V = P_hi V + P_lo V, so an output is rounded once; P_hi lies
+// over the first half of its own S, P_lo in columns of its own.  O is zeroed by the epilogue rather than by the first
+// product, so that a row may be corrected (below) before the first product as well as between others.
+//
+// Every wait is bounded; on expiry the kernel raises DS_DEV_TIMEOUT, drains and frees TMEM.
+#include "ds_attn_paged.cuh"
+
+namespace ds {
+namespace {
+
+using namespace paged;
+using namespace sm100;
+
+constexpr int kRows = 128, kKeys = 128;
+constexpr int kSoftmaxWarps = 4, kMmaWarp = 4, kQueryWarp = 5, kLoadWarp = 6, kLoadWarps = 4;
+constexpr int kThreads = 32 * (kLoadWarp + kLoadWarps);
+constexpr int kMinTiles = 2;       // a range has at least so many key tiles
+constexpr int kWholeTiles = 2;     // items of at most so many key tiles are not split
+constexpr uint32_t kTmemS = 0, kTmemO = 256, kTmemLo = 384, kTmemCols = 512;      // S (2), O, P_lo (2)
+constexpr int kHalfBytes = 128 * 128;      // 128 rows of 64 elements: a swizzled half of a tile of D = 128
+
+template <int D>
+struct Geo {
+  static constexpr int kTile = 128 * D * 2;
+  static constexpr int kStages = D == 128 ? 3 : 5;
+  static constexpr int kOffRing = kTile;      // behind the queries; K and V of stage s at + 2 s, 2 s + 1 tiles
+  static constexpr int kOffBar = kOffRing + 2 * kStages * kTile;
+  // full[kStages], empty[kStages], q_full, q_free, s_full[2], p_full[2], pv_done[2], o_free, vote
+  static constexpr int kNumBars = 2 * kStages + 10;
+  static constexpr int kOffMisc = kOffBar + 8 * kNumBars;      // TMEM base, abort flag, vote words (2 tiles)
+  static constexpr int kOffScan = (kOffMisc + 8 + 8 * kSoftmaxWarps + 7) / 8 * 8;
+  static constexpr int kBytes = kOffScan + 8 * (kThreads / 32 + 2) + 1024;      // slack: the base is aligned to 1024
+  static_assert(kBytes <= 227 * 1024, "shared memory");
+};
+
+// Byte offset of 16-byte chunk `c` of row `r` in a K, V or Q tile.
+__device__ __forceinline__ uint32_t tile_at(int r, int c) { return (c >> 3) * kHalfBytes + r * 128 + (((c & 7) ^ (r & 7)) << 4); }
+
+__device__ __forceinline__ uint32_t tmem_ld1(uint32_t taddr) {
+  uint32_t r;
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(r) : "r"(taddr) : "memory");
+  return r;
+}
+__device__ __forceinline__ void tmem_st1(uint32_t taddr, uint32_t r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(taddr), "r"(r) : "memory");
+}
+
+// The keys of a tile that a row sees: [0, hi) without [hole, back).
+struct Seen {
+  int hi, hole, back;
+  __device__ __forceinline__ bool operator()(int c) const { return c < hi && (c < hole || c >= back); }
+};
+__device__ __forceinline__ Seen seen_keys(const PagedShape &s, const PagedSeq &q, int x, int end) {
+  if (x < q.sink_pad) return {paged_min(q.sink_n, end) - x, kKeys, 0};
+  const int t = q.body + (x - q.sink_pad);
+  if (s.window == 0) return {end - t, kKeys, 0};
+  return {end - t, paged_max(s.sinks - t, 0), end - s.window - t};
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const __grid_constant__ Params a) {
+  using G = Geo<D>;
+  using T = __nv_bfloat16;
+  constexpr int S = G::kStages;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  const uint32_t sbase = smem_u32(smem);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const ds_paged_params &p = a.p;
+  const uint32_t bar_full = sbase + G::kOffBar, bar_empty = bar_full + 8 * S, bar_q_full = bar_empty + 8 * S,
+                 bar_q_free = bar_q_full + 8, bar_s_full = bar_q_free + 8, bar_p_full = bar_s_full + 16,
+                 bar_pv_done = bar_p_full + 16, bar_o_free = bar_pv_done + 16, bar_vote = bar_o_free + 8;
+  volatile uint32_t *tmem_s = reinterpret_cast<volatile uint32_t *>(smem + G::kOffMisc);
+  volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + G::kOffMisc + 4);
+  volatile uint32_t *vote_s = reinterpret_cast<volatile uint32_t *>(smem + G::kOffMisc + 8);
+
+  if (tid == 0) {
+    for (int s = 0; s < S; ++s) {
+      mbar_init(bar_full + 8 * s, kLoadWarps);
+      mbar_init(bar_empty + 8 * s, 1);
+    }
+    mbar_init(bar_q_full, 1);
+    mbar_init(bar_q_free, 1);
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(bar_s_full + 8 * s, 1);
+      mbar_init(bar_p_full + 8 * s, kSoftmaxWarps);
+      mbar_init(bar_pv_done + 8 * s, 1);
+    }
+    mbar_init(bar_o_free, kSoftmaxWarps);
+    mbar_init(bar_vote, kSoftmaxWarps);
+    *abort_flag = 0;
+    fence_barrier_init();
+  }
+  if (warp == kMmaWarp) tmem_alloc(sbase + G::kOffMisc, kTmemCols);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_s;
+  dependent_sync();
+  uint32_t flags = 0;
+  Walk walk;
+  walk.find<kThreads>(a, kMinTiles, reinterpret_cast<long long *>(smem + G::kOffScan), flags);
+  const Item &it = walk.it;
+  bool ok = true;
+
+  if (warp >= kLoadWarp) {
+    // ============================ K and V ============================
+    constexpr int kChunks = D / 8, kPer = 32 / kChunks > 0 ? 32 / kChunks : 1, kOps = 16 / kPer;      // rows of an instruction
+    const int first_key = 32 * (warp - kLoadWarp);
+    const long long row_bytes = p.cache_stride[2] * 2;
+    int f = 0;      // tiles issued
+    auto announce = [&](int tile) {
+      fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar_full + 8 * (tile % S));
+    };
+    for (; ok && walk.piece(a); walk.next(a)) {
+      const int32_t *table = p.block_table + it.b * p.table_stride;
+      const uint8_t *kbase = reinterpret_cast<const uint8_t *>(reinterpret_cast<const T *>(p.k_cache) + it.g * p.cache_stride[1]);
+      const uint8_t *vbase = reinterpret_cast<const uint8_t *>(reinterpret_cast<const T *>(p.v_cache) + it.g * p.cache_stride[1]);
+      const int x0 = walk.tile0 * kKeys + first_key + lane;
+      int pos = paged_key(it.q, x0), page = pos >= 0 ? table[fast_div(pos, a.page_div)] : 0;
+      for (int i = 0; i < walk.n_tiles; ++i, ++f) {
+        ok = __all_sync(0xffffffffu, mbar_wait(bar_empty + 8 * (f % S), ((f / S) & 1) ^ 1, abort_flag));
+        if (!ok) break;
+        long long at = -1;      // of key first_key + lane
+        if (pos >= 0) {
+          const int there = paged_clamp_page(page, p.n_pages);
+          if (there != page) flags |= DS_DEV_INDEX;
+          const int slot = pos - fast_div(pos, a.page_div) * p.page_size;
+          at = there * p.cache_stride[0] * 2 + slot * row_bytes;
+        }
+        const uint32_t dst = sbase + G::kOffRing + (f % S) * 2 * G::kTile;
+        const int ch = lane % kChunks;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {      // 16 keys that lie evenly (in one page) need one address
+          const long long at0 = __shfl_sync(0xffffffffu, at, 16 * half);
+          if (__all_sync(0xffffffffu, (lane >> 4) != half || (at0 >= 0 && at == at0 + (lane & 15) * row_bytes))) {
+            long long from = at0 + (lane / kChunks) * row_bytes + 16 * ch;
+#pragma unroll
+            for (int j = 0; j < kOps; ++j, from += kPer * row_bytes) {
+              const uint32_t to = dst + tile_at(first_key + 16 * half + j * kPer + lane / kChunks, ch);
+              cp_async16(to, kbase + from, true);
+              cp_async16(to + G::kTile, vbase + from, true);
+            }
+          } else {
+#pragma unroll
+            for (int j = 0; j < kOps; ++j) {
+              const int r = 16 * half + j * kPer + lane / kChunks;
+              const long long off = __shfl_sync(0xffffffffu, at, r);
+              const uint32_t to = dst + tile_at(first_key + r, ch);
+              cp_async16(to, kbase + (off >= 0 ? off : 0) + 16 * ch, off >= 0);
+              cp_async16(to + G::kTile, vbase + (off >= 0 ? off : 0) + 16 * ch, off >= 0);
+            }
+          }
+        }
+        cp_async_commit();
+        if (i + 1 < walk.n_tiles) {
+          pos = paged_key(it.q, x0 + (i + 1) * kKeys);
+          page = pos >= 0 ? table[fast_div(pos, a.page_div)] : 0;
+        }
+        if (f > 0) {
+          cp_async_wait<1>();
+          announce(f - 1);
+        }
+      }
+    }
+    cp_async_wait<0>();
+    if (ok && f > 0) announce(f - 1);
+  } else if (warp == kQueryWarp) {
+    // ============================ queries ============================
+    for (int k = 0; ok && walk.piece(a); walk.next(a), ++k) {
+      if (k > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar_q_free, (k - 1) & 1, abort_flag));
+      if (!ok) break;
+      for (int c = lane; c < it.rows * (D / 8); c += 32) {
+        const Row row = row_of(a, it, c / (D / 8));
+        cp_async16(sbase + tile_at(c / (D / 8), c % (D / 8)),
+                   reinterpret_cast<const T *>(p.q) + row.n * p.q_stride[0] + row.h * p.q_stride[1] + 8 * (c % (D / 8)), true);
+      }
+      cp_async_commit();
+      cp_async_wait<0>();
+      fence_proxy_async();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar_q_full);
+    }
+  } else if (warp == kMmaWarp) {
+    // ============================ products ============================
+    constexpr uint32_t idesc_qk = instr_desc(kRows, kKeys, false, false), idesc_pv = instr_desc(kRows, D, false, true);
+    const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+    const uint64_t dq = smem_desc(sbase, 16, 1024);
+    const uint64_t dk0 = smem_desc(sbase + G::kOffRing, 16, 1024), dv0 = smem_desc(sbase + G::kOffRing + G::kTile, kHalfBytes, 1024);
+    int g = 0, k = 0;
+    bool pv_first = false;      // tile g - 1 is the first of its piece, number k_pv
+    int k_pv = 0;
+    auto pv = [&]() {      // P V of tile g - 1
+      const int h = g - 1;
+      bool w = mbar_wait(bar_p_full + 8 * (h & 1), (h >> 1) & 1, abort_flag);
+      if (pv_first) w = w && mbar_wait(bar_o_free, k_pv & 1, abort_flag);
+      ok = __all_sync(0xffffffffu, w);
+      if (!ok) return;
+      tc_fence_after();
+      const uint64_t dv = dv0 + (uint64_t)(((h % S) * 2 * G::kTile) >> 4);
+      if (elect_one()) {
+#pragma unroll
+        for (int part = 0; part < 2; ++part)
+#pragma unroll
+          for (int ks = 0; ks < kKeys / 16; ++ks)
+            umma_ts(tm + kTmemO, tm + (part ? kTmemLo + (h & 1) * 64 : kTmemS + (h & 1) * 128) + ks * 8,
+                    dv + ((ks * 2048) >> 4), idesc_pv, 1u);
+        umma_commit(bar_empty + 8 * (h % S));
+        umma_commit(bar_pv_done + 8 * (h & 1));
+      }
+      __syncwarp();
+    };
+    for (; ok && walk.piece(a); walk.next(a), ++k) {
+      if (g > 0) pv();      // ends the piece before: the queries that the next product waits for may take a while
+      ok = ok && __all_sync(0xffffffffu, mbar_wait(bar_q_full, k & 1, abort_flag));
+      for (int i = 0; ok && i < walk.n_tiles; ++i, ++g) {
+        // the tile has landed, and S[g % 2] is free: P V of tile g - 2, the last to read it, has completed
+        ok = __all_sync(0xffffffffu, g < 2 ? mbar_wait(bar_full + 8 * (g % S), (g / S) & 1, abort_flag)
+                                           : mbar_wait2(bar_full + 8 * (g % S), (g / S) & 1, bar_pv_done + 8 * (g & 1),
+                                                        ((g - 2) >> 1) & 1, abort_flag));
+        if (!ok) break;
+        tc_fence_after();
+        const uint64_t dk = dk0 + (uint64_t)(((g % S) * 2 * G::kTile) >> 4);
+        if (elect_one()) {
+#pragma unroll
+          for (int ks = 0; ks < D / 16; ++ks) {
+            const uint32_t off = ((ks / 4) * kHalfBytes + (ks % 4) * 32) >> 4;
+            umma_ss(tm + kTmemS + (g & 1) * 128, dq + off, dk + off, idesc_qk, ks > 0);
+          }
+          umma_commit(bar_s_full + 8 * (g & 1));
+          if (i == walk.n_tiles - 1) umma_commit(bar_q_free);
+        }
+        __syncwarp();
+        if (i > 0) {
+          pv();
+          if (!ok) break;
+        }
+        pv_first = i == 0;
+        k_pv = k;
+      }
+    }
+    if (ok && g > 0) pv();
+  } else {
+    // ============================ softmax and epilogue ============================
+    const uint32_t tw = tmem + ((uint32_t)(32 * warp) << 16);
+    const int r = tid;
+    const float scale2 = p.scale * kLog2e;
+    PagedJoin join = {0, 0, 0, 0, 0, 0};      // thread 0's
+    auto zero_o = [&]() {
+      uint32_t z[32];
+#pragma unroll
+      for (int c = 0; c < 32; ++c) z[c] = 0;
+#pragma unroll
+      for (int c = 0; c < D; c += 32) tmem_st32(tw + kTmemO + c, z);
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar_o_free);
+    };
+    zero_o();
+    int g = 0, votes = 0;
+    for (; ok && walk.piece(a); walk.next(a)) {
+      if (a.split && tid == 0) walk.note_join(join);
+      const bool busy = 32 * warp < it.rows, mine = r < it.rows;
+      const Row row = row_of(a, it, mine ? r : 0);
+      const int end = mine ? row.end : 0;
+      float m = -INFINITY, l = 0.f;
+      for (int i = 0; i < walk.n_tiles; ++i, ++g) {
+        const int x = (walk.tile0 + i) * kKeys;
+        const bool all = paged_all_visible(a.s, it.q, x, kKeys);
+        const uint32_t ts = tw + kTmemS + (g & 1) * 128, tlo = tw + kTmemLo + (g & 1) * 64;
+        ok = __all_sync(0xffffffffu, mbar_wait(bar_s_full + 8 * (g & 1), (g >> 1) & 1, abort_flag));
+        if (!ok) break;
+        tc_fence_after();
+        const Seen seen = seen_keys(a.s, it.q, x, end);
+        if (busy) {
+          // ---- largest score
+          float top = -INFINITY;
+#pragma unroll 1
+          for (int c = 0; c < kKeys; c += 32) {
+            uint32_t s[32];
+            tmem_ld32(ts + c, s);
+            tmem_wait_ld();
+            if (all) {
+#pragma unroll
+              for (int e = 0; e < 32; e += 2)
+                top = fmax3(top, __uint_as_float(s[e]) * scale2, __uint_as_float(s[e + 1]) * scale2);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 32; ++e) top = fmaxf(top, seen(c + e) ? __uint_as_float(s[e]) * scale2 : -INFINITY);
+            }
+          }
+          // The reference moves only when a weight would pass 2^8: the result is the same, O is touched rarely.
+          const bool over = mine && top > m + 8.f;
+          if (__any_sync(0xffffffffu, over)) {
+            const float keep = !over ? 1.f : m == -INFINITY ? 0.f : ex2_approx(m - top);
+            if (over) m = top;
+            l *= keep;
+            if (i > 0) {
+              ok = __all_sync(0xffffffffu, mbar_wait(bar_pv_done + 8 * ((g - 1) & 1), ((g - 1) >> 1) & 1, abort_flag));
+              if (!ok) break;
+              tc_fence_after();
+#pragma unroll 1
+              for (int c = 0; c < D; c += 32) {
+                uint32_t o[32];
+                tmem_ld32(tw + kTmemO + c, o);
+                tmem_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * keep);
+                tmem_st32(tw + kTmemO + c, o);
+              }
+              tmem_wait_st();
+            }
+          }
+          // ---- weights
+          const float ref = m == -INFINITY ? 0.f : m;      // nothing seen yet: exp(-inf) = 0
+          float l0 = 0.f, l1 = 0.f;
+#pragma unroll 1
+          for (int c = 0; c < kKeys; c += 32) {
+            uint32_t s[32], hi[16], lo[16];
+            tmem_ld32(ts + c, s);
+            tmem_wait_ld();
+            if (!all) {
+#pragma unroll
+              for (int e = 0; e < 32; ++e)
+                if (!seen(c + e)) s[e] = scale2 < 0.f ? 0x7f800000u : 0xff800000u;
+            }
+#pragma unroll
+            for (int e = 0; e < 32; e += 2) {
+              float p0 = ex2_approx(fmaf(__uint_as_float(s[e]), scale2, -ref));
+              float p1 = ex2_approx(fmaf(__uint_as_float(s[e + 1]), scale2, -ref));
+              if (!all && scale2 == 0.f) {      // 0 times the infinity above
+                if (!seen(c + e)) p0 = 0.f;
+                if (!seen(c + e + 1)) p1 = 0.f;
+              }
+              l0 += p0;
+              l1 += p1;
+              const uint32_t h = pack_bf16(p0, p1);
+              hi[e / 2] = h;
+              lo[e / 2] = pack_bf16(p0 - bf16lo_to_f32(h), p1 - bf16hi_to_f32(h));
+            }
+            // over scores that have been read: columns c / 2 .. c / 2 + 15 <= c + 31
+            tmem_st8(ts + c / 2, hi);
+            tmem_st8(ts + c / 2 + 8, hi + 8);
+            tmem_st8(tlo + c / 2, lo);
+            tmem_st8(tlo + c / 2 + 8, lo + 8);
+          }
+          l += l0 + l1;
+          tmem_wait_st();
+        }
+        if (!all && a.s.causal && it.q.count > 1) {
+          // Keys that some rows see and others do not: a weight of zero times an infinite or NaN value would be NaN in
+          // the product.  If V holds such values (rare), their terms are added to O here for the rows that see them,
+          // one by one, and they are replaced by zero.
+          uint8_t *v = smem + G::kOffRing + (g % S) * 2 * G::kTile + G::kTile;
+          bool w = mbar_wait(bar_full + 8 * (g % S), (g / S) & 1, abort_flag);
+          bool bad = false;
+          for (int c = 0; c < D / 8; ++c) {
+            const uint4 q = *reinterpret_cast<const uint4 *>(v + tile_at(r, c));
+            const uint32_t x4[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) bad |= (x4[e] & 0x7f80u) == 0x7f80u || (x4[e] & 0x7f800000u) == 0x7f800000u;
+          }
+          const uint32_t word = __ballot_sync(0xffffffffu, bad);
+          volatile uint32_t *votes_s = vote_s + (g & 1) * kSoftmaxWarps;      // a warp may be one tile ahead of another
+          if (lane == 0) {
+            votes_s[warp] = word;
+            mbar_arrive(bar_vote);
+          }
+          w = w && mbar_wait(bar_vote, votes++ & 1, abort_flag);
+          ok = __all_sync(0xffffffffu, w);
+          if (!ok) break;
+          if (votes_s[0] | votes_s[1] | votes_s[2] | votes_s[3]) {
+            if (i > 0) w = mbar_wait(bar_pv_done + 8 * ((g - 1) & 1), ((g - 1) >> 1) & 1, abort_flag);
+            tc_fence_after();
+            for (int key = 0; busy && key < kKeys; ++key) {
+              if (!((votes_s[key >> 5] >> (key & 31)) & 1)) continue;
+              const uint32_t wh = tmem_ld1(ts + key / 2), wl = tmem_ld1(tlo + key / 2);
+              tmem_wait_ld();
+              const float weight = key & 1 ? bf16hi_to_f32(wh) + bf16hi_to_f32(wl) : bf16lo_to_f32(wh) + bf16lo_to_f32(wl);
+              for (int d = 0; d < D; ++d) {
+                const float value = __bfloat162float(*reinterpret_cast<const T *>(v + tile_at(key, d / 8) + (d & 7) * 2));
+                if (isfinite(value)) continue;
+                float o = __uint_as_float(tmem_ld1(tw + kTmemO + d));
+                tmem_wait_ld();
+                if (seen(key)) o += weight * value;
+                tmem_st1(tw + kTmemO + d, __float_as_uint(o));
+                tmem_wait_st();
+              }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_vote);      // all rows have read V
+            w = w && mbar_wait(bar_vote, votes++ & 1, abort_flag);
+            ok = __all_sync(0xffffffffu, w);
+            if (!ok) break;
+            for (int c = 0; bad && c < D / 8; ++c) {
+              uint4 *at = reinterpret_cast<uint4 *>(v + tile_at(r, c));
+              uint32_t x4[4] = {at->x, at->y, at->z, at->w};
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                if ((x4[e] & 0x7f80u) == 0x7f80u) x4[e] &= 0xffff0000u;
+                if ((x4[e] & 0x7f800000u) == 0x7f800000u) x4[e] &= 0xffffu;
+              }
+              *at = make_uint4(x4[0], x4[1], x4[2], x4[3]);
+            }
+            fence_proxy_async();
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_p_full + 8 * (g & 1));
+      }
+      if (!ok) break;
+      // ---- the piece is done
+      ok = __all_sync(0xffffffffu, mbar_wait(bar_pv_done + 8 * ((g - 1) & 1), ((g - 1) >> 1) & 1, abort_flag));
+      if (!ok) break;
+      tc_fence_after();
+      if (busy) {
+        const bool whole = walk.whole();
+        const long long at = (long long)paged_slot(blockIdx.x, walk.first) * a.part_rows + r;
+#pragma unroll 1
+        for (int c = 0; c < D; c += 32) {
+          uint32_t o[32];
+          tmem_ld32(tw + kTmemO + c, o);
+          tmem_wait_ld();
+          if (!mine) continue;
+          if (whole) {
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            uint4 *dst = reinterpret_cast<uint4 *>(reinterpret_cast<T *>(p.out) + row.n * p.out_stride[0] + row.h * p.out_stride[1] + c);
+#pragma unroll
+            for (int e = 0; e < 32; e += 8) {
+              uint32_t w[4];
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                w[k] = pack_bf16(__uint_as_float(o[e + 2 * k]) * inv, __uint_as_float(o[e + 2 * k + 1]) * inv);
+              dst[e / 8] = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+          } else {
+            uint4 *dst = reinterpret_cast<uint4 *>(a.part_o + at * D + c);
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) dst[e / 4] = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+          }
+        }
+        if (mine && whole && p.lse) p.lse[row.n * p.Hq + row.h] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+        if (mine && !whole) a.part_ml[at] = make_float2(m, l);
+      }
+      zero_o();
+    }
+    if (a.split && tid == 0) a.joins[blockIdx.x] = join;
+  }
+
+  if (!ok) flags |= DS_DEV_TIMEOUT;
+  if (flags && p.status) atomicOr(p.status, flags);
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kMmaWarp) {
+    tc_fence_after();
+    tmem_dealloc(tmem, kTmemCols);
+  }
+}
+
+size_t workspace_of(const Shape &h) { return h.tiles <= kWholeTiles || h.grid == 1 ? 0 : h.workspace(); }
+
+template <int D>
+int launch(const ds_paged_params &p, cudaStream_t stream) {
+  const Shape h = shape_of(p, kKeys, kRows, kMinTiles, 1);
+  const Params a = params_of(p, h, workspace_of(h));
+  static std::atomic<unsigned long long> allowed{0};
+  DS_CUDA_OK(allow_smem(attn_paged_tc_kernel<D>, Geo<D>::kBytes, allowed));
+  DS_CUDA_OK(launch_kernel(attn_paged_tc_kernel<D>, dim3(h.grid), kThreads, Geo<D>::kBytes, 0, false, stream, a));
+  note_launch(1);
+  return a.split ? launch_join<__nv_bfloat16, D>(a, h, stream) : (int)DS_OK;
+}
+
+}  // namespace
+
+size_t attn_paged_tc_workspace_bytes(const ds_paged_params &p) { return workspace_of(shape_of(p, kKeys, kRows, kMinTiles, 1)); }
+
+int launch_attn_paged_tc(const ds_paged_params &p, cudaStream_t stream) {
+  return p.D == 64 ? launch<64>(p, stream) : launch<128>(p, stream);
+}
+
+}  // namespace ds

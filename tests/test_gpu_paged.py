@@ -127,6 +127,16 @@ def test_several_new_rows(dtype, D, causal, counts):
     Case(lens, counts, 8, 4, D, 16, dtype, seed=sum(counts)).check(causal=causal)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Hq,Hkv,counts", [(8, 1, [3, 16, 0, 17]), (28, 4, [32, 1, 33, 5]), (2, 2, [64, 65, 128, 129]),
+                                           (16, 1, [8, 9, 1, 24])])
+@pytest.mark.parametrize("kw", [dict(), dict(causal=False), dict(window=100, sinks=9), dict(window=300, sinks=130, causal=False)])
+def test_many_rows_per_head(D, Hq, Hkv, counts, kw):
+    """From a fraction of a 128-row tile to several of them, peaked and flat scores, ends inside tiles."""
+    Case([129, 600, 1000, 257], counts, Hq, Hkv, D, 16, BF, seed=Hq, sharp=2.0).check(**kw)
+    Case([5000, 64, 0, 1], counts, Hq, Hkv, D, 24, BF, seed=Hq + 1, sharp=4.0).check(**kw)
+
+
 @pytest.mark.parametrize("dtype,D", [(BF, 128), (F32, 64)])
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("window,sinks", [(1, 0), (1, 4), (50, 4), (64, 64), (100, 17), (1000, 3), (7, 1000)])
@@ -185,12 +195,13 @@ def test_layouts_and_uniform_rows(dtype, D):
 
 
 @pytest.mark.parametrize("dtype,D", [(BF, 128), (BF, 64), (F32, 64)])
-def test_what_a_query_does_not_see_cannot_reach_it(dtype, D):
+@pytest.mark.parametrize("Hq", [2, 4, 12, 40])
+def test_what_a_query_does_not_see_cannot_reach_it(dtype, D, Hq):
     """NaN and infinities in K and V of the later new rows: a causal query before them must not notice; those that see
     them get NaN.  The same at the window's edge."""
-    c = Case([70, 40], [6, 1], 4, 2, D, 16, dtype, seed=3)
+    c = Case([70, 40], [6, 1], Hq, 2, D, 16, dtype, seed=3)
     clean, _, _ = c.run()
-    dirty = Case([70, 40], [6, 1], 4, 2, D, 16, dtype, seed=3)
+    dirty = Case([70, 40], [6, 1], Hq, 2, D, 16, dtype, seed=3)
     page, off = dirty.table[0, 67 // 16].long(), 67 % 16
     dirty.v[page, :, off] = float("nan")
     dirty.k[page, :, off] = float("inf")
@@ -200,20 +211,20 @@ def test_what_a_query_does_not_see_cannot_reach_it(dtype, D):
     assert torch.equal(out[:3], clean[:3]) and torch.equal(out[6:], clean[6:])     # rows 64, 65, 66 and the other sequence
     assert torch.isnan(out[3:6]).all()
     # V alone infinite, at the last row: only the last query, only there
-    dirty = Case([70, 40], [6, 1], 4, 2, D, 16, dtype, seed=3)
+    dirty = Case([70, 40], [6, 1], Hq, 2, D, 16, dtype, seed=3)
     dirty.v[page, :, off, 1::3] = float("inf")
     out, lse, _ = dirty.run()
     assert torch.equal(out[:5], clean[:5]) and torch.isinf(out[5, :, 1::3]).all()
     assert torch.equal(out[5, :, 0::3], clean[5, :, 0::3]) and torch.equal(out[5, :, 2::3], clean[5, :, 2::3])
     # window 5: query 0 (row 64) sees rows 60 .. 64, query 1 rows 61 .. 65: row 60 belongs to query 0 alone
     clean, _, _ = c.run(window=5)
-    dirty = Case([70, 40], [6, 1], 4, 2, D, 16, dtype, seed=3)
+    dirty = Case([70, 40], [6, 1], Hq, 2, D, 16, dtype, seed=3)
     page, off = dirty.table[0, 60 // 16].long(), 60 % 16
     dirty.v[page, :, off] = float("nan")
     out, _, _ = dirty.run(window=5)
     assert torch.isnan(out[0]).all() and torch.equal(out[1:], clean[1:])
     # a row that no query of a window sees
-    dirty = Case([70, 40], [6, 1], 4, 2, D, 16, dtype, seed=3)
+    dirty = Case([70, 40], [6, 1], Hq, 2, D, 16, dtype, seed=3)
     for r in (0, 33, 58, 59):
         dirty.v[dirty.table[0, r // 16].long(), :, r % 16] = float("nan")
         dirty.k[dirty.table[0, r // 16].long(), :, r % 16] = float("nan")
