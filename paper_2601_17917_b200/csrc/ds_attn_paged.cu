@@ -693,8 +693,10 @@ auto with_rows(const ds_paged_params &p, F f) {
   }
 }
 
-// Rows per KV head from which the kernel with tcgen05 tiles takes over.
-constexpr int kTensorTileRows = 17;
+// Rows per KV head from which the kernel with tcgen05 tiles takes over.  Up to 32 rows one pass of this kernel is no slower
+// (8 x 32 heads x 1550 rows, 32 queries: 62 against 72 us; 32 x 28/4 heads x 4000 rows, 4 queries: 67 against 69); from 33
+// on it would need a second.
+constexpr int kTensorTileRows = 33;
 bool wide(const ds_paged_params &p) {
   return p.dtype == DS_BF16 && (long long)p.max_q * (p.Hq / p.Hkv) >= kTensorTileRows;
 }

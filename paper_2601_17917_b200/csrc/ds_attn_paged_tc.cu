@@ -2,25 +2,32 @@
 // generation tensor cores.
 //
 // An item is up to 128 stacked rows (query, head of the group) of a sequence and KV head, the rows of a tcgen05 tile:
-// S = Q K^T and O += P V in TMEM, 128 keys at a time, with the online softmax on the thread that owns the row.  The units
-// of work, their equal ranges over the SMs and the join of items that ranges share are those of the kernel for few
-// rows.  It is bound by HBM as long as the 1536 tensor cycles of a 64 KB key tile (512 for S, 1024 for P V, below) fit
-// into the 2800 that HBM needs for it.
+// S = Q K^T and O += P V in TMEM, 128 keys at a time, with the online softmax on the thread that owns the tile's row.  The
+// units of work, their equal ranges over the SMs and the join of items that ranges share are those of the kernel for few
+// rows.  It is bound by HBM as long as the 1536 tensor cycles of a 64 KB key tile (512 for S, 1024 for P V, below) and
+// the softmax fit into the 2800 that HBM needs for it.  The softmax does not when 32 rows leave it to one warp (128 keys
+// a thread, 8 x 32 heads x 1550 rows with blocks of 32: 97 us), so up to 32 rows stand in the tile four times and up to 64
+// twice: each copy weighs its own part of the keys and holds zeros for the others, and the copies are joined when the
+// item ends.
 //
 // Warps:
-//   0-3  softmax and epilogue, thread = row = TMEM lane
+//   0-3  softmax and epilogue, thread = tile row = TMEM lane
 //   4    issues the products
 //   5    loads the queries of the next item
 //   6-9  load K and V, 32 keys each: 16-byte asynchronous copies from wherever the page table says, written in the
 //        128-byte swizzle that the products read.  (A page may be as small as one row, which leaves no box for TMA.)
-// K and V tiles pass through a ring of kStages.  The copies are issued two tiles ahead of their announcement: a warp
-// announces a tile when its copies are complete, after the next tile's have been issued.
+// K and V tiles pass through a ring of kSlots in the order in which the products need them, K0 K1 V0 K2 V1 .. V(n-1) for a
+// piece of n key tiles.  The copies themselves announce a tile (an asynchronous arrival of every loading thread), so a
+// loading warp waits for free slots only; the issuer of the products orders them behind the copies with a proxy fence.
+// (Loading warps that wait for their copies in order to announce them keep too little in flight: 81 to 98 us.)
 //
 // As with few rows the weights are kept as two bf16 halves, P V = P_hi V + P_lo V, so an output is rounded once; P_hi lies
 // over the first half of its own S, P_lo in columns of its own.  O is zeroed by the epilogue rather than by the first
 // product, so that a row may be corrected (below) before the first product as well as between others.
 //
 // Every wait is bounded; on expiry the kernel raises DS_DEV_TIMEOUT, drains and frees TMEM.
+#include <type_traits>
+
 #include "ds_attn_paged.cuh"
 
 namespace ds {
@@ -40,11 +47,13 @@ constexpr int kHalfBytes = 128 * 128;      // 128 rows of 64 elements: a swizzle
 template <int D>
 struct Geo {
   static constexpr int kTile = 128 * D * 2;
-  static constexpr int kStages = D == 128 ? 3 : 5;
-  static constexpr int kOffRing = kTile;      // behind the queries; K and V of stage s at + 2 s, 2 s + 1 tiles
-  static constexpr int kOffBar = kOffRing + 2 * kStages * kTile;
-  // full[kStages], empty[kStages], q_full, q_free, s_full[2], p_full[2], pv_done[2], o_free, vote
-  static constexpr int kNumBars = 2 * kStages + 10;
+  static constexpr int kSlots = D == 128 ? 5 : 10;
+  static constexpr int kOffRing = kTile;      // behind the queries
+  static constexpr int kOffJoin = kOffRing + kSlots * kTile;      // [128 tile rows][64] fp32: half the dimensions of O
+  static constexpr int kOffMl = kOffJoin + 128 * 256;             // [128] maximum and sum
+  static constexpr int kOffBar = kOffMl + 128 * 8;
+  // full[kSlots], empty[kSlots], q_full, q_free, s_full[2], p_full[2], pv_done[2], o_free, vote
+  static constexpr int kNumBars = 2 * kSlots + 10;
   static constexpr int kOffMisc = kOffBar + 8 * kNumBars;      // TMEM base, abort flag, vote words (2 tiles)
   static constexpr int kOffScan = (kOffMisc + 8 + 8 * kSoftmaxWarps + 7) / 8 * 8;
   static constexpr int kBytes = kOffScan + 8 * (kThreads / 32 + 2) + 1024;      // slack: the base is aligned to 1024
@@ -63,10 +72,25 @@ __device__ __forceinline__ void tmem_st1(uint32_t taddr, uint32_t r) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(taddr), "r"(r) : "memory");
 }
 
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t *r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+      ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
+      : "memory");
+}
+// Arrives at the barrier when this thread's copies so far are complete.
+__device__ __forceinline__ void arrive_when_copied(uint32_t bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+}
+
 // The keys of a tile that a row sees: [0, hi) without [hole, back).
 struct Seen {
   int hi, hole, back;
   __device__ __forceinline__ bool operator()(int c) const { return c < hi && (c < hole || c >= back); }
+  // Keys c .. c + 31 as bits.
+  __device__ __forceinline__ uint32_t bits(int c) const { return below(hi - c) & (below(hole - c) | ~below(back - c)); }
+  static __device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
 };
 __device__ __forceinline__ Seen seen_keys(const PagedShape &s, const PagedSeq &q, int x, int end) {
   if (x < q.sink_pad) return {paged_min(q.sink_n, end) - x, kKeys, 0};
@@ -75,11 +99,12 @@ __device__ __forceinline__ Seen seen_keys(const PagedShape &s, const PagedSeq &q
   return {end - t, paged_max(s.sinks - t, 0), end - s.window - t};
 }
 
-template <int D>
+// kCopies: how often a row stands in the tile.
+template <int D, int kCopies>
 __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const __grid_constant__ Params a) {
   using G = Geo<D>;
   using T = __nv_bfloat16;
-  constexpr int S = G::kStages;
+  constexpr int S = G::kSlots, kPad = kRows / kCopies, kMine = kKeys / kCopies;      // rows of a copy, keys that it weighs
   extern __shared__ uint8_t smem_raw[];
   uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   const uint32_t sbase = smem_u32(smem);
@@ -94,7 +119,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const __grid
 
   if (tid == 0) {
     for (int s = 0; s < S; ++s) {
-      mbar_init(bar_full + 8 * s, kLoadWarps);
+      mbar_init(bar_full + 8 * s, 32 * kLoadWarps);
       mbar_init(bar_empty + 8 * s, 1);
     }
     mbar_init(bar_q_full, 1);
@@ -127,64 +152,59 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const __grid
     const int first_key = 32 * (warp - kLoadWarp);
     const long long row_bytes = p.cache_stride[2] * 2;
     int f = 0;      // tiles issued
-    auto announce = [&](int tile) {
-      fence_proxy_async();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar_full + 8 * (tile % S));
-    };
     for (; ok && walk.piece(a); walk.next(a)) {
       const int32_t *table = p.block_table + it.b * p.table_stride;
       const uint8_t *kbase = reinterpret_cast<const uint8_t *>(reinterpret_cast<const T *>(p.k_cache) + it.g * p.cache_stride[1]);
       const uint8_t *vbase = reinterpret_cast<const uint8_t *>(reinterpret_cast<const T *>(p.v_cache) + it.g * p.cache_stride[1]);
       const int x0 = walk.tile0 * kKeys + first_key + lane;
-      int pos = paged_key(it.q, x0), page = pos >= 0 ? table[fast_div(pos, a.page_div)] : 0;
-      for (int i = 0; i < walk.n_tiles; ++i, ++f) {
+      const int ch = lane % kChunks;
+      auto issue = [&](const uint8_t *base, long long at) {      // at: of key first_key + lane
         ok = __all_sync(0xffffffffu, mbar_wait(bar_empty + 8 * (f % S), ((f / S) & 1) ^ 1, abort_flag));
-        if (!ok) break;
-        long long at = -1;      // of key first_key + lane
+        if (!ok) return;
+        const uint32_t dst = sbase + G::kOffRing + (f % S) * G::kTile;
+        // 16 keys that lie evenly (in one page) need one address
+        const long long at_lo = __shfl_sync(0xffffffffu, at, 0), at_hi = __shfl_sync(0xffffffffu, at, 16);
+        const uint32_t even = __ballot_sync(0xffffffffu, at >= 0 && at == (lane < 16 ? at_lo : at_hi) + (lane & 15) * row_bytes);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          if (((even >> (16 * half)) & 0xffffu) == 0xffffu) {
+            const uint8_t *from = base + (half ? at_hi : at_lo) + (lane / kChunks) * row_bytes + 16 * ch;
+#pragma unroll
+            for (int j = 0; j < kOps; ++j, from += kPer * row_bytes)
+              cp_async16(dst + tile_at(first_key + 16 * half + j * kPer + lane / kChunks, ch), from, true);
+          } else {
+#pragma unroll
+            for (int j = 0; j < kOps; ++j) {
+              const int r = 16 * half + j * kPer + lane / kChunks;
+              const long long off = __shfl_sync(0xffffffffu, at, r);
+              cp_async16(dst + tile_at(first_key + r, ch), base + (off >= 0 ? off : 0) + 16 * ch, off >= 0);
+            }
+          }
+        }
+        arrive_when_copied(bar_full + 8 * (f % S));
+        ++f;
+      };
+      int pos = paged_key(it.q, x0), page = pos >= 0 ? table[fast_div(pos, a.page_div)] : 0;
+      long long before = -1;      // of the previous key tile
+      for (int i = 0; ok && i < walk.n_tiles; ++i) {
+        long long at = -1;
         if (pos >= 0) {
           const int there = paged_clamp_page(page, p.n_pages);
           if (there != page) flags |= DS_DEV_INDEX;
           const int slot = pos - fast_div(pos, a.page_div) * p.page_size;
           at = there * p.cache_stride[0] * 2 + slot * row_bytes;
         }
-        const uint32_t dst = sbase + G::kOffRing + (f % S) * 2 * G::kTile;
-        const int ch = lane % kChunks;
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {      // 16 keys that lie evenly (in one page) need one address
-          const long long at0 = __shfl_sync(0xffffffffu, at, 16 * half);
-          if (__all_sync(0xffffffffu, (lane >> 4) != half || (at0 >= 0 && at == at0 + (lane & 15) * row_bytes))) {
-            long long from = at0 + (lane / kChunks) * row_bytes + 16 * ch;
-#pragma unroll
-            for (int j = 0; j < kOps; ++j, from += kPer * row_bytes) {
-              const uint32_t to = dst + tile_at(first_key + 16 * half + j * kPer + lane / kChunks, ch);
-              cp_async16(to, kbase + from, true);
-              cp_async16(to + G::kTile, vbase + from, true);
-            }
-          } else {
-#pragma unroll
-            for (int j = 0; j < kOps; ++j) {
-              const int r = 16 * half + j * kPer + lane / kChunks;
-              const long long off = __shfl_sync(0xffffffffu, at, r);
-              const uint32_t to = dst + tile_at(first_key + r, ch);
-              cp_async16(to, kbase + (off >= 0 ? off : 0) + 16 * ch, off >= 0);
-              cp_async16(to + G::kTile, vbase + (off >= 0 ? off : 0) + 16 * ch, off >= 0);
-            }
-          }
-        }
-        cp_async_commit();
         if (i + 1 < walk.n_tiles) {
           pos = paged_key(it.q, x0 + (i + 1) * kKeys);
           page = pos >= 0 ? table[fast_div(pos, a.page_div)] : 0;
         }
-        if (f > 0) {
-          cp_async_wait<1>();
-          announce(f - 1);
-        }
+        issue(kbase, at);
+        if (ok && i > 0) issue(vbase, before);
+        before = at;
       }
+      if (ok) issue(vbase, before);
     }
-    cp_async_wait<0>();
-    if (ok && f > 0) announce(f - 1);
+    asm volatile("cp.async.wait_all;" ::: "memory");
   } else if (warp == kQueryWarp) {
     // ============================ queries ============================
     for (int k = 0; ok && walk.piece(a); walk.next(a), ++k) {
@@ -192,8 +212,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const __grid
       if (!ok) break;
       for (int c = lane; c < it.rows * (D / 8); c += 32) {
         const Row row = row_of(a, it, c / (D / 8));
-        cp_async16(sbase + tile_at(c / (D / 8), c % (D / 8)),
-                   reinterpret_cast<const T *>(p.q) + row.n * p.q_stride[0] + row.h * p.q_stride[1] + 8 * (c % (D / 8)), true);
+        const T *from = reinterpret_cast<const T *>(p.q) + row.n * p.q_stride[0] + row.h * p.q_stride[1] + 8 * (c % (D / 8));
+#pragma unroll
+        for (int copy = 0; copy < kCopies; ++copy)
+          cp_async16(sbase + tile_at(copy * kPad + c / (D / 8), c % (D / 8)), from, true);
       }
       cp_async_commit();
       cp_async_wait<0>();
@@ -206,18 +228,19 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const __grid
     constexpr uint32_t idesc_qk = instr_desc(kRows, kKeys, false, false), idesc_pv = instr_desc(kRows, D, false, true);
     const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
     const uint64_t dq = smem_desc(sbase, 16, 1024);
-    const uint64_t dk0 = smem_desc(sbase + G::kOffRing, 16, 1024), dv0 = smem_desc(sbase + G::kOffRing + G::kTile, kHalfBytes, 1024);
-    int g = 0, k = 0;
+    const uint64_t dk0 = smem_desc(sbase + G::kOffRing, 16, 1024), dv0 = smem_desc(sbase + G::kOffRing, kHalfBytes, 1024);
+    int g = 0, k = 0, f = 0;      // key tiles, pieces, tiles of the ring
     bool pv_first = false;      // tile g - 1 is the first of its piece, number k_pv
     int k_pv = 0;
     auto pv = [&]() {      // P V of tile g - 1
       const int h = g - 1;
-      bool w = mbar_wait(bar_p_full + 8 * (h & 1), (h >> 1) & 1, abort_flag);
+      bool w = mbar_wait2(bar_p_full + 8 * (h & 1), (h >> 1) & 1, bar_full + 8 * (f % S), (f / S) & 1, abort_flag);
       if (pv_first) w = w && mbar_wait(bar_o_free, k_pv & 1, abort_flag);
       ok = __all_sync(0xffffffffu, w);
       if (!ok) return;
+      fence_proxy_async();
       tc_fence_after();
-      const uint64_t dv = dv0 + (uint64_t)(((h % S) * 2 * G::kTile) >> 4);
+      const uint64_t dv = dv0 + (uint64_t)(((f % S) * G::kTile) >> 4);
       if (elect_one()) {
 #pragma unroll
         for (int part = 0; part < 2; ++part)
@@ -225,22 +248,24 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const __grid
           for (int ks = 0; ks < kKeys / 16; ++ks)
             umma_ts(tm + kTmemO, tm + (part ? kTmemLo + (h & 1) * 64 : kTmemS + (h & 1) * 128) + ks * 8,
                     dv + ((ks * 2048) >> 4), idesc_pv, 1u);
-        umma_commit(bar_empty + 8 * (h % S));
+        umma_commit(bar_empty + 8 * (f % S));
         umma_commit(bar_pv_done + 8 * (h & 1));
       }
       __syncwarp();
+      ++f;
     };
     for (; ok && walk.piece(a); walk.next(a), ++k) {
       if (g > 0) pv();      // ends the piece before: the queries that the next product waits for may take a while
       ok = ok && __all_sync(0xffffffffu, mbar_wait(bar_q_full, k & 1, abort_flag));
       for (int i = 0; ok && i < walk.n_tiles; ++i, ++g) {
         // the tile has landed, and S[g % 2] is free: P V of tile g - 2, the last to read it, has completed
-        ok = __all_sync(0xffffffffu, g < 2 ? mbar_wait(bar_full + 8 * (g % S), (g / S) & 1, abort_flag)
-                                           : mbar_wait2(bar_full + 8 * (g % S), (g / S) & 1, bar_pv_done + 8 * (g & 1),
+        ok = __all_sync(0xffffffffu, g < 2 ? mbar_wait(bar_full + 8 * (f % S), (f / S) & 1, abort_flag)
+                                           : mbar_wait2(bar_full + 8 * (f % S), (f / S) & 1, bar_pv_done + 8 * (g & 1),
                                                         ((g - 2) >> 1) & 1, abort_flag));
         if (!ok) break;
+        fence_proxy_async();
         tc_fence_after();
-        const uint64_t dk = dk0 + (uint64_t)(((g % S) * 2 * G::kTile) >> 4);
+        const uint64_t dk = dk0 + (uint64_t)(((f % S) * G::kTile) >> 4);
         if (elect_one()) {
 #pragma unroll
           for (int ks = 0; ks < D / 16; ++ks) {
@@ -248,9 +273,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const __grid
             umma_ss(tm + kTmemS + (g & 1) * 128, dq + off, dk + off, idesc_qk, ks > 0);
           }
           umma_commit(bar_s_full + 8 * (g & 1));
+          umma_commit(bar_empty + 8 * (f % S));
           if (i == walk.n_tiles - 1) umma_commit(bar_q_free);
         }
         __syncwarp();
+        ++f;
         if (i > 0) {
           pv();
           if (!ok) break;
@@ -263,7 +290,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const __grid
   } else {
     // ============================ softmax and epilogue ============================
     const uint32_t tw = tmem + ((uint32_t)(32 * warp) << 16);
-    const int r = tid;
+    const int r = tid % kPad, copy = tid / kPad, key0 = copy * kMine;      // row of the item, keys of this copy
     const float scale2 = p.scale * kLog2e;
     PagedJoin join = {0, 0, 0, 0, 0, 0};      // thread 0's
     auto zero_o = [&]() {
@@ -277,11 +304,16 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const __grid
       __syncwarp();
       if (lane == 0) mbar_arrive(bar_o_free);
     };
+    {
+      uint32_t z[8] = {};      // P_lo of the keys of other copies stays zero
+#pragma unroll
+      for (int c = 0; c < 128; c += 8) tmem_st8(tw + kTmemLo + c, z);
+    }
     zero_o();
-    int g = 0, votes = 0;
-    for (; ok && walk.piece(a); walk.next(a)) {
+    int g = 0, votes = 0, ring0 = 0;      // votes: also those of the joins; ring0: where the piece begins in the ring
+    for (; ok && walk.piece(a); ring0 += 2 * walk.n_tiles, walk.next(a)) {
       if (a.split && tid == 0) walk.note_join(join);
-      const bool busy = 32 * warp < it.rows, mine = r < it.rows;
+      const bool busy = (32 * warp) % kPad < it.rows, mine = r < it.rows;
       const Row row = row_of(a, it, mine ? r : 0);
       const int end = mine ? row.end : 0;
       float m = -INFINITY, l = 0.f;
@@ -294,11 +326,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const __grid
         tc_fence_after();
         const Seen seen = seen_keys(a.s, it.q, x, end);
         if (busy) {
-          // ---- largest score
+          // ---- largest score of this copy's keys; 32 of them stay in registers
           float top = -INFINITY;
+          uint32_t s[32];
 #pragma unroll 1
-          for (int c = 0; c < kKeys; c += 32) {
-            uint32_t s[32];
+          for (int c = key0; c < key0 + kMine; c += 32) {
             tmem_ld32(ts + c, s);
             tmem_wait_ld();
             if (all) {
@@ -306,8 +338,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const __grid
               for (int e = 0; e < 32; e += 2)
                 top = fmax3(top, __uint_as_float(s[e]) * scale2, __uint_as_float(s[e + 1]) * scale2);
             } else {
+              const uint32_t bits = seen.bits(c);
 #pragma unroll
-              for (int e = 0; e < 32; ++e) top = fmaxf(top, seen(c + e) ? __uint_as_float(s[e]) * scale2 : -INFINITY);
+              for (int e = 0; e < 32; ++e) top = fmaxf(top, (bits >> e) & 1 ? __uint_as_float(s[e]) * scale2 : -INFINITY);
             }
           }
           // The reference moves only when a weight would pass 2^8: the result is the same, O is touched rarely.
@@ -335,48 +368,56 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const __grid
           // ---- weights
           const float ref = m == -INFINITY ? 0.f : m;      // nothing seen yet: exp(-inf) = 0
           float l0 = 0.f, l1 = 0.f;
+          auto weights = [&](auto every) {      // std::true_type: no key of the tile is hidden
+            constexpr bool kAll = decltype(every)::value;
 #pragma unroll 1
-          for (int c = 0; c < kKeys; c += 32) {
-            uint32_t s[32], hi[16], lo[16];
-            tmem_ld32(ts + c, s);
-            tmem_wait_ld();
-            if (!all) {
-#pragma unroll
-              for (int e = 0; e < 32; ++e)
-                if (!seen(c + e)) s[e] = scale2 < 0.f ? 0x7f800000u : 0xff800000u;
-            }
-#pragma unroll
-            for (int e = 0; e < 32; e += 2) {
-              float p0 = ex2_approx(fmaf(__uint_as_float(s[e]), scale2, -ref));
-              float p1 = ex2_approx(fmaf(__uint_as_float(s[e + 1]), scale2, -ref));
-              if (!all && scale2 == 0.f) {      // 0 times the infinity above
-                if (!seen(c + e)) p0 = 0.f;
-                if (!seen(c + e + 1)) p1 = 0.f;
+            for (int c = key0; c < key0 + kMine; c += 32) {
+              uint32_t hi[16], lo[16];
+              if (kMine > 32) {
+                tmem_ld32(ts + c, s);
+                tmem_wait_ld();
               }
-              l0 += p0;
-              l1 += p1;
-              const uint32_t h = pack_bf16(p0, p1);
-              hi[e / 2] = h;
-              lo[e / 2] = pack_bf16(p0 - bf16lo_to_f32(h), p1 - bf16hi_to_f32(h));
+              const uint32_t bits = kAll ? 0xffffffffu : seen.bits(c);
+#pragma unroll
+              for (int e = 0; e < 32; e += 2) {
+                float p0 = ex2_approx(fmaf(__uint_as_float(s[e]), scale2, -ref));
+                float p1 = ex2_approx(fmaf(__uint_as_float(s[e + 1]), scale2, -ref));
+                if (!kAll) {
+                  if (!((bits >> e) & 1)) p0 = 0.f;
+                  if (!((bits >> (e + 1)) & 1)) p1 = 0.f;
+                }
+                l0 += p0;
+                l1 += p1;
+                const uint32_t h = pack_bf16(p0, p1);
+                hi[e / 2] = h;
+                lo[e / 2] = pack_bf16(p0 - bf16lo_to_f32(h), p1 - bf16hi_to_f32(h));
+              }
+              // over scores that have been read, or are another copy's: columns c / 2 .. c / 2 + 15 <= c + 31
+              tmem_st16(ts + c / 2, hi);
+              tmem_st16(tlo + c / 2, lo);
             }
-            // over scores that have been read: columns c / 2 .. c / 2 + 15 <= c + 31
-            tmem_st8(ts + c / 2, hi);
-            tmem_st8(ts + c / 2 + 8, hi + 8);
-            tmem_st8(tlo + c / 2, lo);
-            tmem_st8(tlo + c / 2 + 8, lo + 8);
-          }
+          };
+          if (all) weights(std::true_type());
+          else weights(std::false_type());
           l += l0 + l1;
+          if constexpr (kCopies > 1) {      // no weight for the other copies' keys
+            uint32_t z[16] = {};
+#pragma unroll
+            for (int c = 0; c < kKeys / 2; c += 16)
+              if (c < key0 / 2 || c >= (key0 + kMine) / 2) tmem_st16(ts + c, z);
+          }
           tmem_wait_st();
         }
         if (!all && a.s.causal && it.q.count > 1) {
           // Keys that some rows see and others do not: a weight of zero times an infinite or NaN value would be NaN in
           // the product.  If V holds such values (rare), their terms are added to O here for the rows that see them,
           // one by one, and they are replaced by zero.
-          uint8_t *v = smem + G::kOffRing + (g % S) * 2 * G::kTile + G::kTile;
-          bool w = mbar_wait(bar_full + 8 * (g % S), (g / S) & 1, abort_flag);
+          const int f = ring0 + 2 * i + (i < walk.n_tiles - 1 ? 2 : 1);      // V of this tile in the ring
+          uint8_t *v = smem + G::kOffRing + (f % S) * G::kTile;
+          bool w = mbar_wait(bar_full + 8 * (f % S), (f / S) & 1, abort_flag);
           bool bad = false;
           for (int c = 0; c < D / 8; ++c) {
-            const uint4 q = *reinterpret_cast<const uint4 *>(v + tile_at(r, c));
+            const uint4 q = *reinterpret_cast<const uint4 *>(v + tile_at(tid, c));
             const uint32_t x4[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
             for (int e = 0; e < 4; ++e) bad |= (x4[e] & 0x7f80u) == 0x7f80u || (x4[e] & 0x7f800000u) == 0x7f800000u;
@@ -394,7 +435,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const __grid
             if (i > 0) w = mbar_wait(bar_pv_done + 8 * ((g - 1) & 1), ((g - 1) >> 1) & 1, abort_flag);
             tc_fence_after();
             for (int key = 0; busy && key < kKeys; ++key) {
-              if (!((votes_s[key >> 5] >> (key & 31)) & 1)) continue;
+              if (key < key0 || key >= key0 + kMine || !((votes_s[key >> 5] >> (key & 31)) & 1)) continue;      // the whole warp
               const uint32_t wh = tmem_ld1(ts + key / 2), wl = tmem_ld1(tlo + key / 2);
               tmem_wait_ld();
               const float weight = key & 1 ? bf16hi_to_f32(wh) + bf16hi_to_f32(wl) : bf16lo_to_f32(wh) + bf16lo_to_f32(wl);
@@ -414,7 +455,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const __grid
             ok = __all_sync(0xffffffffu, w);
             if (!ok) break;
             for (int c = 0; bad && c < D / 8; ++c) {
-              uint4 *at = reinterpret_cast<uint4 *>(v + tile_at(r, c));
+              uint4 *at = reinterpret_cast<uint4 *>(v + tile_at(tid, c));
               uint32_t x4[4] = {at->x, at->y, at->z, at->w};
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
@@ -435,34 +476,92 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const __grid
       ok = __all_sync(0xffffffffu, mbar_wait(bar_pv_done + 8 * ((g - 1) & 1), ((g - 1) >> 1) & 1, abort_flag));
       if (!ok) break;
       tc_fence_after();
-      if (busy) {
-        const bool whole = walk.whole();
-        const long long at = (long long)paged_slot(blockIdx.x, walk.first) * a.part_rows + r;
+      const bool whole = walk.whole();
+      const long long at = (long long)paged_slot(blockIdx.x, walk.first) * a.part_rows + r;
+      if constexpr (kCopies == 1) {
+        if (busy) {
 #pragma unroll 1
-        for (int c = 0; c < D; c += 32) {
-          uint32_t o[32];
-          tmem_ld32(tw + kTmemO + c, o);
-          tmem_wait_ld();
-          if (!mine) continue;
-          if (whole) {
-            const float inv = l == 0.f ? 0.f : 1.f / l;
-            uint4 *dst = reinterpret_cast<uint4 *>(reinterpret_cast<T *>(p.out) + row.n * p.out_stride[0] + row.h * p.out_stride[1] + c);
+          for (int c = 0; c < D; c += 32) {
+            uint32_t o[32];
+            tmem_ld32(tw + kTmemO + c, o);
+            tmem_wait_ld();
+            if (!mine) continue;
+            if (whole) {
+              const float inv = l == 0.f ? 0.f : 1.f / l;
+              uint4 *dst = reinterpret_cast<uint4 *>(reinterpret_cast<T *>(p.out) + row.n * p.out_stride[0] + row.h * p.out_stride[1] + c);
 #pragma unroll
-            for (int e = 0; e < 32; e += 8) {
-              uint32_t w[4];
+              for (int e = 0; e < 32; e += 8) {
+                uint32_t w[4];
 #pragma unroll
-              for (int k = 0; k < 4; ++k)
-                w[k] = pack_bf16(__uint_as_float(o[e + 2 * k]) * inv, __uint_as_float(o[e + 2 * k + 1]) * inv);
-              dst[e / 8] = make_uint4(w[0], w[1], w[2], w[3]);
+                for (int k = 0; k < 4; ++k)
+                  w[k] = pack_bf16(__uint_as_float(o[e + 2 * k]) * inv, __uint_as_float(o[e + 2 * k + 1]) * inv);
+                dst[e / 8] = make_uint4(w[0], w[1], w[2], w[3]);
+              }
+            } else {
+              uint4 *dst = reinterpret_cast<uint4 *>(a.part_o + at * D + c);
+#pragma unroll
+              for (int e = 0; e < 32; e += 4) dst[e / 4] = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
             }
-          } else {
-            uint4 *dst = reinterpret_cast<uint4 *>(a.part_o + at * D + c);
-#pragma unroll
-            for (int e = 0; e < 32; e += 4) dst[e / 4] = make_uint4(o[e], o[e + 1], o[e + 2], o[e + 3]);
           }
+          if (mine && whole && p.lse) p.lse[row.n * p.Hq + row.h] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+          if (mine && !whole) a.part_ml[at] = make_float2(m, l);
         }
-        if (mine && whole && p.lse) p.lse[row.n * p.Hq + row.h] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
-        if (mine && !whole) a.part_ml[at] = make_float2(m, l);
+      } else {
+        // ---- join the copies, 64 dimensions at a time; a thread adds up 64 / kCopies of them for its row
+        float2 *ml_s = reinterpret_cast<float2 *>(smem + G::kOffMl);
+        uint8_t *join_s = smem + G::kOffJoin;
+        auto quad = [&](int tile_row, int q) { return reinterpret_cast<float4 *>(join_s + tile_row * 256 + ((q ^ (tile_row & 15)) << 4)); };
+        auto meet = [&]() {
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar_vote);
+          ok = __all_sync(0xffffffffu, mbar_wait(bar_vote, votes++ & 1, abort_flag));
+        };
+        ml_s[tid] = make_float2(m, l);
+#pragma unroll 1
+        for (int half = 0; ok && half < D / 64; ++half) {      // code that runs once per item: kept short
+          if (busy) {
+#pragma unroll 1
+            for (int c = 0; c < 64; c += 32) {
+              uint32_t o[32];
+              tmem_ld32(tw + kTmemO + half * 64 + c, o);
+              tmem_wait_ld();
+#pragma unroll
+              for (int e = 0; e < 32; e += 4)
+                *quad(tid, c / 4 + e / 4) = make_float4(__uint_as_float(o[e]), __uint_as_float(o[e + 1]), __uint_as_float(o[e + 2]),
+                                                      __uint_as_float(o[e + 3]));
+            }
+          }
+          meet();
+          if (ok && mine) {
+            float top = -INFINITY, sum = 0.f, f[kCopies];
+#pragma unroll
+            for (int k = 0; k < kCopies; ++k) top = fmaxf(top, ml_s[k * kPad + r].x);
+#pragma unroll
+            for (int k = 0; k < kCopies; ++k) {
+              const float2 ml = ml_s[k * kPad + r];
+              f[k] = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - top);
+              sum = fmaf(ml.y, f[k], sum);
+            }
+#pragma unroll 1
+            for (int e = 0; e < 16 / kCopies; ++e) {
+              const int q = copy * (16 / kCopies) + e, d = half * 64 + 4 * q;
+              float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+              for (int k = 0; k < kCopies; ++k) {
+                const float4 o = *quad(k * kPad + r, q);
+                v.x = fmaf(o.x, f[k], v.x), v.y = fmaf(o.y, f[k], v.y), v.z = fmaf(o.z, f[k], v.z), v.w = fmaf(o.w, f[k], v.w);
+              }
+              if (whole) {
+                write_row4<T>(a, row, d, v, top, sum);
+              } else {
+                *reinterpret_cast<float4 *>(a.part_o + at * D + d) = v;
+                if (d == 0) a.part_ml[at] = make_float2(top, sum);
+              }
+            }
+          }
+          if (ok) meet();      // the buffer is read
+        }
+        if (!ok) break;
       }
       zero_o();
     }
@@ -481,23 +580,39 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const __grid
 
 size_t workspace_of(const Shape &h) { return h.tiles <= kWholeTiles || h.grid == 1 ? 0 : h.workspace(); }
 
-template <int D>
+// Copies of a row in the tile: as many as there is room for.
+int copies_for(const ds_paged_params &p) {
+  const long long rows = (long long)p.max_q * (p.Hq / p.Hkv);
+  return rows <= 32 ? 4 : rows <= 64 ? 2 : 1;
+}
+Shape shape_for(const ds_paged_params &p) { return shape_of(p, kKeys, kRows / copies_for(p), kMinTiles, 1); }
+
+template <int D, int kCopies>
 int launch(const ds_paged_params &p, cudaStream_t stream) {
-  const Shape h = shape_of(p, kKeys, kRows, kMinTiles, 1);
+  const Shape h = shape_for(p);
   const Params a = params_of(p, h, workspace_of(h));
   static std::atomic<unsigned long long> allowed{0};
-  DS_CUDA_OK(allow_smem(attn_paged_tc_kernel<D>, Geo<D>::kBytes, allowed));
-  DS_CUDA_OK(launch_kernel(attn_paged_tc_kernel<D>, dim3(h.grid), kThreads, Geo<D>::kBytes, 0, false, stream, a));
+  DS_CUDA_OK(allow_smem(attn_paged_tc_kernel<D, kCopies>, Geo<D>::kBytes, allowed));
+  DS_CUDA_OK(launch_kernel(attn_paged_tc_kernel<D, kCopies>, dim3(h.grid), kThreads, Geo<D>::kBytes, 0, false, stream, a));
   note_launch(1);
   return a.split ? launch_join<__nv_bfloat16, D>(a, h, stream) : (int)DS_OK;
 }
 
+template <int D>
+int launch_copies(const ds_paged_params &p, cudaStream_t stream) {
+  switch (copies_for(p)) {
+    case 4: return launch<D, 4>(p, stream);
+    case 2: return launch<D, 2>(p, stream);
+    default: return launch<D, 1>(p, stream);
+  }
+}
+
 }  // namespace
 
-size_t attn_paged_tc_workspace_bytes(const ds_paged_params &p) { return workspace_of(shape_of(p, kKeys, kRows, kMinTiles, 1)); }
+size_t attn_paged_tc_workspace_bytes(const ds_paged_params &p) { return workspace_of(shape_for(p)); }
 
 int launch_attn_paged_tc(const ds_paged_params &p, cudaStream_t stream) {
-  return p.D == 64 ? launch<64>(p, stream) : launch<128>(p, stream);
+  return p.D == 64 ? launch_copies<64>(p, stream) : launch_copies<128>(p, stream);
 }
 
 }  // namespace ds
