@@ -16,7 +16,7 @@
 // bf16: mma.sync m16n8k16.  The few rows leave tcgen05's 128-row tile nearly empty and the stream, not the products,
 // bounds the kernel.  The weights enter the second product as two bf16
 // halves (hi + lo), which keeps 16 bits of them: the product is free here, and an output is then rounded once.
-// fp32: CUDA cores, 8 lanes per key.
+// fp32: CUDA cores.
 #include <cooperative_groups.h>
 
 #include <type_traits>
@@ -299,135 +299,222 @@ struct TensorRows {
 };
 
 // ---------------------------------------------------------------------------------------------------------------
-// A warp's share of an item in fp32: R rows; 8 lanes per key, four keys side by side, each lane group with sums of
-// its own.  Lane u of a group holds 16-byte chunks u, u + 8, .. of a row.
+// A warp's share of an item in fp32: R rows against kKeys keys at a time, on the CUDA cores.  First product: lane = key and
+// a part of the dimensions, so that a score needs log2(kParts) shuffles and each lane weighs keys of its own; the queries
+// come from shared memory, the same word for a whole part.  Second product: lane = dimensions, the weights from
+// shared memory.  Products are two wide (fma.rn.f32x2), over dimensions and over pairs of rows.
+// (With 8 lanes per key, each computing every weight of it, 24 x 8 heads x 1007 rows of D = 64 with 8 rows took 62 us.)
 template <int D_, int R>
 struct ScalarRows {
   using T = float;
   static constexpr int D = D_, kRows = R, kRowBytes = 4 * D, kKeys = kRowBytes >= 512 ? 4096 / kRowBytes : 16;
-  static constexpr int kQBytes = 0, C = D / 32, kPer = kKeys / 4;
-  static constexpr int kCtas = D == 32 && R == 1 ? 4 : 2, kStages = 3;
-  float4 q[R][C], o[R][C];
-  float m[R], l[R];
+  static constexpr int kParts = 32 / kKeys, kDims = D / kParts, E = D / 32;      // dimensions of a lane in either product
+  static constexpr int kPartStride = R * kDims + 4;                              // floats; 4: parts in banks of their own
+  static constexpr int kOffP = kParts * kPartStride * 4;
+  static constexpr int kQBytes = (kOffP + kWarps * kKeys * R * 4 + 15) / 16 * 16;      // queries; weights of each warp
+  static constexpr int kCtas = D == 32 && R == 1 ? 4 : 2, kStages = D == 256 ? 2 : 3;
+  static constexpr int kMine = R >= kParts ? R / kParts : 1;      // rows whose weights a lane computes for its key
+  F2 o[(R + 1) / 2][E];                                            // pairs of rows (R = 1: the second is unused)
+  float m[R], l[kMine];
   int end[R];
+  float *q_s, *p_s;
 
-  __device__ void begin(const Params &a, const Item &it, uint8_t *) {
-    const int u = threadIdx.x & 7;
+  __device__ void begin(const Params &a, const Item &it, uint8_t *buf) {
+    q_s = reinterpret_cast<float *>(buf);
+    p_s = reinterpret_cast<float *>(buf + kOffP) + (threadIdx.x >> 5) * kKeys * R;
+    for (int c = threadIdx.x; c < R * (D / 4); c += kThreads) {
+      const int r = c / (D / 4), d = c % (D / 4) * 4;
+      float4 w = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (r < it.rows) {
+        const Row row = row_of(a, it, r);
+        w = *reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(a.p.q) + row.n * a.p.q_stride[0] + row.h * a.p.q_stride[1] + d);
+      }
+      *reinterpret_cast<float4 *>(q_s + d / kDims * kPartStride + r * kDims + d % kDims) = w;
+    }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      const bool there = r < it.rows;
-      const Row row = row_of(a, it, there ? r : 0);
-      const float *src = reinterpret_cast<const float *>(a.p.q) + row.n * a.p.q_stride[0] + row.h * a.p.q_stride[1];
-#pragma unroll
-      for (int c = 0; c < C; ++c) {
-        q[r][c] = there ? *reinterpret_cast<const float4 *>(src + 4 * (u + 8 * c)) : make_float4(0.f, 0.f, 0.f, 0.f);
-        o[r][c] = make_float4(0.f, 0.f, 0.f, 0.f);
-      }
-      m[r] = -INFINITY, l[r] = 0.f;
-      end[r] = there ? row.end : 0;
+      m[r] = -INFINITY;
+      end[r] = r < it.rows ? row_of(a, it, r).end : 0;
     }
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) l[i] = 0.f;
+#pragma unroll
+    for (int i = 0; i < (R + 1) / 2; ++i)
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[i][e] = 0;
+    __syncthreads();
   }
 
   __device__ __forceinline__ void step(const Params &a, const Item &it, uint8_t *kbuf, uint8_t *vbuf, int x, float scale2) {
-    const int lane = threadIdx.x & 31, u = lane & 7, group = lane >> 3;
+    const int lane = threadIdx.x & 31, key = lane % kKeys, part = lane / kKeys;
     const bool partial = !paged_all_visible(a.s, it.q, x, kKeys);
-    float z[kPer][R];
+    float z[R];
+    {
+      F2 z2[R];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int key = 4 * i + group;
+      for (int r = 0; r < R; ++r) z2[r] = 0;
+      const float *q = q_s + part * kPartStride;
 #pragma unroll
-      for (int r = 0; r < R; ++r) z[i][r] = 0.f;
-#pragma unroll
-      for (int c = 0; c < C; ++c) {
-        const float4 k = *reinterpret_cast<const float4 *>(kbuf + chunk_at<kRowBytes>(key, u + 8 * c));
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-          z[i][r] = fmaf(q[r][c].w, k.w, fmaf(q[r][c].z, k.z, fmaf(q[r][c].y, k.y, fmaf(q[r][c].x, k.x, z[i][r]))));
-      }
-    }
-    uint32_t hidden = 0;      // bit i R + r
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int pos = partial ? paged_key(it.q, x + 4 * i + group) : 0;
-#pragma unroll
-      for (int r = 0; r < R; ++r) {
-        float v = z[i][r];
-        v += __shfl_xor_sync(0xffffffffu, v, 1);
-        v += __shfl_xor_sync(0xffffffffu, v, 2);
-        v += __shfl_xor_sync(0xffffffffu, v, 4);
-        z[i][r] = v * scale2;
-        if (partial && !paged_visible(a.s, pos, end[r])) {
-          z[i][r] = -INFINITY;
-          hidden |= 1u << (i * R + r);
-        }
-      }
-    }
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      float top = m[r];
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) top = fmaxf(top, z[i][r]);
-      if (top > m[r]) {
-        const float keep = ex2_approx(m[r] - top);
-        m[r] = top;
-        l[r] *= keep;
-#pragma unroll
-        for (int c = 0; c < C; ++c) o[r][c].x *= keep, o[r][c].y *= keep, o[r][c].z *= keep, o[r][c].w *= keep;
-      }
-      const float ref = m[r] == -INFINITY ? 0.f : m[r];
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        z[i][r] = ex2_approx(z[i][r] - ref);
-        l[r] += z[i][r];
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int key = 4 * i + group;
-#pragma unroll
-      for (int c = 0; c < C; ++c) {
-        const float4 v = *reinterpret_cast<const float4 *>(vbuf + chunk_at<kRowBytes>(key, u + 8 * c));
+      for (int c = 0; c < kDims / 4; ++c) {
+        const ulonglong2 k = *reinterpret_cast<const ulonglong2 *>(kbuf + chunk_at<kRowBytes>(key, part * (kDims / 4) + c));
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-          // a value that the row does not see is not touched: zero times NaN would be NaN
-          if (partial && ((hidden >> (i * R + r)) & 1)) continue;
-          o[r][c].x = fmaf(z[i][r], v.x, o[r][c].x);
-          o[r][c].y = fmaf(z[i][r], v.y, o[r][c].y);
-          o[r][c].z = fmaf(z[i][r], v.z, o[r][c].z);
-          o[r][c].w = fmaf(z[i][r], v.w, o[r][c].w);
+          const ulonglong2 w = *reinterpret_cast<const ulonglong2 *>(q + r * kDims + 4 * c);
+          z2[r] = fma2(w.y, k.y, fma2(w.x, k.x, z2[r]));
         }
+      }
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const float2 t = f2_get(z2[r]);
+        z[r] = t.x + t.y;
+#pragma unroll
+        for (int off = kKeys; off < 32; off <<= 1) z[r] += __shfl_xor_sync(0xffffffffu, z[r], off);
+        z[r] *= scale2;
+      }
+    }
+    uint32_t hidden = 0;      // bit r: the row does not see this lane's key
+    if (partial) {
+      const int pos = paged_key(it.q, x + key);
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+        if (!paged_visible(a.s, pos, end[r])) {
+          z[r] = -INFINITY;
+          hidden |= 1u << r;
+        }
+    }
+    // The reference moves only when a weight would pass 2^8 (the result is the same).
+    bool over = false;
+#pragma unroll
+    for (int r = 0; r < R; ++r) over |= z[r] > m[r] + 8.f;
+    if (__any_sync(0xffffffffu, over)) {
+      float keep[R + 1];
+      keep[R] = 1.f;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        float top = fmaxf(m[r], z[r]);
+#pragma unroll
+        for (int off = 1; off < kKeys; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+        keep[r] = m[r] == top ? 1.f : ex2_approx(m[r] - top);
+        m[r] = top;
+      }
+#pragma unroll
+      for (int i = 0; i < (R + 1) / 2; ++i) {
+        const F2 k2 = f2(keep[2 * i], keep[2 * i + 1]);
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[i][e] = mul2(o[i][e], k2);
+      }
+#pragma unroll
+      for (int i = 0; i < kMine; ++i) l[i] *= mine(keep, i, part);
+    }
+    // ---- this lane's weights
+    float p[kMine];
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      const float ref = mine(m, i, part);
+      p[i] = ex2_approx(mine(z, i, part) - (ref == -INFINITY ? 0.f : ref));      // nothing seen yet: exp(-inf) = 0
+      l[i] += p[i];
+    }
+    float *to = p_s + key * R + part * kMine;
+    if constexpr (kMine == 4) *reinterpret_cast<float4 *>(to) = make_float4(p[0], p[1], p[2], p[3]);
+    else if constexpr (kMine == 2) *reinterpret_cast<float2 *>(to) = make_float2(p[0], p[1]);
+    else if (part < R) *to = p[0];
+    __syncwarp();
+    if (partial && odd_values(vbuf)) {
+      // keys that some rows see and others do not, and V holds infinities or NaN (rare): zero times those is not zero
+      for (int k = 0; k < kKeys; ++k) {
+        const uint32_t hide = __shfl_sync(0xffffffffu, hidden, k);
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const float v = value(vbuf, k, e);
+#pragma unroll
+          for (int r = 0; r < R; ++r)
+            if (!((hide >> r) & 1)) {
+              const float2 t = f2_get(o[r / 2][e]);
+              const float sum = fmaf(p_s[k * R + r], v, r & 1 ? t.y : t.x);
+              o[r / 2][e] = r & 1 ? f2(t.x, sum) : f2(sum, t.y);
+            }
+        }
+      }
+      return;
+    }
+#pragma unroll
+    for (int k = 0; k < kKeys; ++k) {
+      float v[E];
+      if constexpr (E == 1) {
+        v[0] = value(vbuf, k, 0);
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; e += E < 4 ? 2 : 4) {
+          const uint8_t *at = vbuf + chunk_at<kRowBytes>(k, (lane * E + e) / 4) + (lane * E + e) % 4 * 4;
+          if constexpr (E == 2) {
+            const float2 t = *reinterpret_cast<const float2 *>(at);
+            v[e] = t.x, v[e + 1] = t.y;
+          } else {
+            const float4 t = *reinterpret_cast<const float4 *>(at);
+            v[e] = t.x, v[e + 1] = t.y, v[e + 2] = t.z, v[e + 3] = t.w;
+          }
+        }
+      }
+      F2 w[(R + 1) / 2];
+      if constexpr (R == 1) {
+        w[0] = f2(p_s[k], 0.f);
+      } else {
+#pragma unroll
+        for (int i = 0; i < R / 2; i += 2) {
+          const ulonglong2 t = *reinterpret_cast<const ulonglong2 *>(p_s + k * R + 2 * i);
+          w[i] = t.x, w[i + 1] = t.y;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const F2 v2 = f2(v[e], v[e]);
+#pragma unroll
+        for (int i = 0; i < (R + 1) / 2; ++i) o[i][e] = fma2(w[i], v2, o[i][e]);
       }
     }
   }
 
+  // Element i of this lane's rows, without indexing registers by `part`.
+  template <int N>
+  static __device__ __forceinline__ float mine(const float (&x)[N], int i, int part) {
+    float y = x[i];
+#pragma unroll
+    for (int j = 1; j < kParts; ++j)
+      if (j * kMine + i < R && part == j) y = x[j * kMine + i];
+    return y;
+  }
+  static __device__ __forceinline__ float value(const uint8_t *vbuf, int k, int e) {
+    const int d = (threadIdx.x & 31) * E + e;
+    return *reinterpret_cast<const float *>(vbuf + chunk_at<kRowBytes>(k, d / 4) + d % 4 * 4);
+  }
+  static __device__ __forceinline__ bool odd_values(const uint8_t *vbuf) {
+    bool odd = false;
+    for (int w = threadIdx.x & 31; w < kKeys * D; w += 32)
+      odd |= (reinterpret_cast<const uint32_t *>(vbuf)[w] & 0x7f800000u) == 0x7f800000u;
+    return __any_sync(0xffffffffu, odd);
+  }
+
   __device__ void finish(const Item &it, float *out, float2 *ml) {
-    const int lane = threadIdx.x & 31, u = lane & 7;
+    const int lane = threadIdx.x & 31, part = lane / kKeys;
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+#pragma unroll
+      for (int off = 1; off < kKeys; off <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], off);
+      const int r = part * kMine + i;
+      if (lane % kKeys == 0 && r < it.rows) ml[r] = make_float2(mine(m, i, part), l[i]);
+    }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      float top = m[r];
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-      const float w = m[r] == -INFINITY ? 0.f : ex2_approx(m[r] - top);
-      float sum = l[r] * w;
-      sum += __shfl_xor_sync(0xffffffffu, sum, 8);
-      sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+      if (r >= it.rows) break;
 #pragma unroll
-      for (int c = 0; c < C; ++c) {
-        float v[4] = {o[r][c].x * w, o[r][c].y * w, o[r][c].z * w, o[r][c].w * w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          v[e] += __shfl_xor_sync(0xffffffffu, v[e], 8);
-          v[e] += __shfl_xor_sync(0xffffffffu, v[e], 16);
-        }
-        if (lane < 8 && r < it.rows)
-          *reinterpret_cast<float4 *>(out + r * D + 4 * (u + 8 * c)) = make_float4(v[0], v[1], v[2], v[3]);
+      for (int e = 0; e < E; ++e) {
+        const float2 t = f2_get(o[r / 2][e]);
+        out[r * D + lane * E + e] = r & 1 ? t.y : t.x;
       }
-      if (lane == 0 && r < it.rows) ml[r] = make_float2(top, sum);
     }
   }
 };
 
-// ---------------------------------------------------------------------------------------------------------------
 template <class Rows>
 struct Layout {
   static constexpr int kSub = Rows::kKeys * Rows::kRowBytes;        // K or V of one stage of a warp
@@ -688,8 +775,8 @@ auto with_rows(const ds_paged_params &p, F f) {
   switch (p.D) {
     case 32: return rows == 1 ? f(ScalarRows<32, 1>()) : f(ScalarRows<32, 8>());
     case 64: return rows == 1 ? f(ScalarRows<64, 1>()) : f(ScalarRows<64, 8>());
-    case 128: return rows == 1 ? f(ScalarRows<128, 1>()) : f(ScalarRows<128, 4>());
-    default: return rows == 1 ? f(ScalarRows<256, 1>()) : f(ScalarRows<256, 2>());
+    case 128: return rows == 1 ? f(ScalarRows<128, 1>()) : f(ScalarRows<128, 8>());
+    default: return rows == 1 ? f(ScalarRows<256, 1>()) : f(ScalarRows<256, 8>());
   }
 }
 

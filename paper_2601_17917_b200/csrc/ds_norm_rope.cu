@@ -26,32 +26,6 @@ constexpr int kThreads = 64, kWarps = kThreads / 32;
 constexpr int kAhead = 4;   // steps (a head per lane group) whose loads are in flight
 constexpr int kMaxPairs = 128;
 
-// Two fp32 values side by side.
-using F2 = unsigned long long;
-__device__ __forceinline__ F2 f2(float lo, float hi) {
-  F2 r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-  return r;
-}
-__device__ __forceinline__ float2 f2_get(F2 x) {
-  float2 r;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
-  return r;
-}
-__device__ __forceinline__ F2 f2_swap(F2 x) {
-  const float2 v = f2_get(x);
-  return f2(v.y, v.x);
-}
-__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
-  F2 r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
-  F2 r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
 // A chunk of 16 bytes as pairs of fp32 and back.
 template <typename T>
 struct Chunk;
