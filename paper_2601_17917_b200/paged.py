@@ -102,6 +102,15 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+# The stream's handle and the device without the objects around them: a launch costs the host about as much as these.
+def _raw_stream(index):
+    return torch._C._cuda_getCurrentRawStream(index)
+
+
+def _current_device():
+    return torch._C._cuda_getDevice()
+
+
 class _Plan:
     _name = ""
 
@@ -115,13 +124,12 @@ class _Plan:
 
     def _enqueue(self, stream):
         if stream is None:
-            s = torch.cuda.current_stream(self._index)
+            raw = _raw_stream(self._index)
         elif stream.device != self.device:
             raise ValueError(f"the stream is on {stream.device}, the tensors on {self.device}")
         else:
-            s = stream
-        raw = s.cuda_stream
-        if torch.cuda.current_device() == self._index:
+            raw = stream.cuda_stream
+        if _current_device() == self._index:
             rc = self._fn(self._ref, raw)
         else:
             with torch.cuda.device(self._index):
@@ -130,7 +138,7 @@ class _Plan:
             raise DsError(rc, self._name)
         if raw != self._own_stream:      # the allocator must not hand these out again before this stream is done
             for t in self._own:
-                t.record_stream(s)
+                t.record_stream(torch.cuda.current_stream(self._index) if stream is None else stream)
 
 
 class RopeTable:
