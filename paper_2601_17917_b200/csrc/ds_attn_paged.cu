@@ -6,7 +6,7 @@
 // device: uneven lengths cost nothing and one long sequence spreads over the whole GPU.  An item that crosses a range
 // boundary leaves partial results (unnormalised sums with their maximum) in the workspace; a second, small
 // kernel, launched early and waiting for the first, joins them in a fixed order.
-// Few items of moderate length (a small batch) are instead given a cluster of CTAs each, which join through
+// Few items of moderate length (a small batch) are instead given a CTA each, or a cluster of CTAs that join through
 // distributed shared memory: no second launch, no workspace, no search for the range's first item.
 //
 // Inside a CTA the four warps take equal parts of every key tile and share nothing until the item ends: each has its own
@@ -32,6 +32,7 @@ constexpr int kWarps = 4, kThreads = kWarps * 32;
 constexpr int kMinTiles = 4;     // a range has at least so many key tiles
 constexpr int kWholeTiles = 8;   // items of at most so many key tiles are not split
 constexpr int kClusterTiles = 24;   // most key tiles of a CTA when an item has a cluster
+constexpr int kAloneTiles = 20;     // and when it has a CTA, whatever the others' lengths
 
 __device__ __forceinline__ void ldmatrix4(uint32_t addr, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
@@ -530,7 +531,7 @@ struct Layout {
   static constexpr int kBytes = kOffMisc + 64;
   static constexpr int kTile = kWarps * Rows::kKeys;
   static_assert(Rows::kRows * Rows::D * 4 <= kRing, "the ring is reused for the warp's sums");
-  static_assert(Rows::kCtas * (kBytes + 1024) <= 228 * 1024, "shared memory of the resident CTAs");
+  static_assert(Rows::kCtas * (kBytes + sizeof(Walk) + 16 + 1024) <= 228 * 1024, "shared memory of the resident CTAs");
 };
 
 // Streams key tiles tile0 .. tile0 + n_tiles - 1 of an item; afterwards (and a barrier) the rings hold the warps' sums.
@@ -633,24 +634,20 @@ __device__ __forceinline__ float4 join_warps(const uint8_t *smem, int r, int d, 
   return v;
 }
 
-// An item on a cluster of n: rank k takes the k-th part of its key tiles and writes its sums into the other ranks' shared
-// memory, a n-th of the dimensions to each, which then adds up and writes that part of the output.
+// The parts of an item that the ranks of its cluster have streamed: a rank writes its sums into the other ranks' shared
+// memory, an n-th of the dimensions to each, which then adds up and writes that part of the output.
 template <class Rows>
-__device__ __forceinline__ void cluster_item(const Params &a, const Item &it, uint8_t *smem, uint32_t &flags) {
+__device__ __forceinline__ void cluster_join(const Params &a, const Item &it, int rank, uint8_t *smem) {
   namespace cg = cooperative_groups;
   using T = typename Rows::T;
   using L = Layout<Rows>;
   constexpr int D = Rows::D;
   auto cluster = cg::this_cluster();
-  cluster.barrier_arrive();      // waited for before the first write to another rank: it has started by then
-  const int rank = (int)cluster.block_rank(), n = a.cluster, tid = threadIdx.x;
-  const int per = (it.q.tiles + n - 1) / n;      // n is at most 8
-  const int tile0 = min(rank * per, it.q.tiles), n_tiles = min(per, it.q.tiles - tile0);
+  const int n = a.cluster, tid = threadIdx.x;
   const int quads = D / 4 / n;                   // float4 of a row that a rank adds up
   float4 *parts = reinterpret_cast<float4 *>(smem + L::kOffParts);      // [n][rows][quads]
   float2 *totals = reinterpret_cast<float2 *>(smem + L::kOffTotals);    // [n][rows]
-  stream_keys<Rows>(a, it, tile0, n_tiles, smem, flags);
-  cluster.barrier_wait();
+  cluster.barrier_wait();      // every rank has started
   for (int e = tid; e < it.rows * (D / 4); e += kThreads) {
     const int r = e / (D / 4), d = e % (D / 4), to = d / quads;
     float top, sum;
@@ -675,37 +672,72 @@ __device__ __forceinline__ void cluster_item(const Params &a, const Item &it, ui
   }
 }
 
+// An item per CTA or cluster of CTAs.
 template <class Rows>
-__global__ void __launch_bounds__(kThreads, Rows::kCtas) attn_paged_kernel(const __grid_constant__ Params a) {
+__global__ void __launch_bounds__(kThreads, Rows::kCtas) attn_paged_item_kernel(const __grid_constant__ Params a) {
   using T = typename Rows::T;
   using L = Layout<Rows>;
   constexpr int D = Rows::D;
   extern __shared__ __align__(128) uint8_t smem[];
   const int tid = threadIdx.x;
-  const ds_paged_params &p = a.p;
   uint32_t flags = 0;
   dependent_sync();
-
-  Walk walk;
-  if constexpr (L::kClusters)
-    if (a.cluster) {
-      Item &it = walk.it;
-      const int item = (int)blockIdx.x / a.cluster;
-      it.b = fast_div(item, a.item_div);
-      const int rest = item - it.b * (int)a.item_div.d;
-      it.g = fast_div(rest, a.row_div);
-      it.row0 = (rest - it.g * (int)a.row_div.d) << a.s.row_log2;
-      it.q = sequence_of(a, it.b);
-      if (it.q.bad) flags |= DS_DEV_INDEX;
-      it.rows = min(Rows::kRows, it.q.count * a.s.G - it.row0);
-      if (it.rows > 0) cluster_item<Rows>(a, it, smem, flags);      // the whole cluster or none of it
-      if (flags && p.status) atomicOr(p.status, flags);
-      return;
+  const int item = (int)blockIdx.x / a.cluster;
+  Item it;
+  it.b = fast_div(item, a.item_div);
+  const int rest = item - it.b * (int)a.item_div.d;
+  it.g = fast_div(rest, a.row_div);
+  it.row0 = (rest - it.g * (int)a.row_div.d) << a.s.row_log2;
+  it.q = sequence_of(a, it.b);
+  if (it.q.bad) flags |= DS_DEV_INDEX;
+  it.rows = min(Rows::kRows, it.q.count * a.s.G - it.row0);
+  const int n = a.cluster, rank = blockIdx.x - item * n;
+  if (it.rows > 0) {      // the whole cluster or none of it
+    if constexpr (L::kClusters)
+      if (n > 1) cooperative_groups::this_cluster().barrier_arrive();      // waited for in cluster_join
+    const int per = n > 1 ? (it.q.tiles + n - 1) / n : it.q.tiles;         // n is at most 8
+    const int tile0 = min(rank * per, it.q.tiles);
+    stream_keys<Rows>(a, it, tile0, min(per, it.q.tiles - tile0), smem, flags);
+    bool joined = false;
+    if constexpr (L::kClusters)
+      if (n > 1) {
+        cluster_join<Rows>(a, it, rank, smem);
+        joined = true;
+      }
+    for (int e = tid; !joined && e < it.rows * (D / 4); e += kThreads) {
+      const int r = e / (D / 4), d = e % (D / 4) * 4;
+      float top, sum;
+      const float4 v = join_warps<Rows>(smem, r, d, top, sum);
+      write_row4<T>(a, row_of(a, it, r), d, v, top, sum);
     }
-  walk.find<kThreads>(a, kMinTiles, reinterpret_cast<long long *>(smem + L::kOffMisc), flags);
+  }
+  if (flags && a.p.status) atomicOr(a.p.status, flags);
+}
+
+// Equal ranges.  The walk lives in shared memory, one thread moves it: the registers are for the rows.
+template <class Rows>
+__global__ void __launch_bounds__(kThreads, Rows::kCtas) attn_paged_range_kernel(const __grid_constant__ Params a) {
+  using T = typename Rows::T;
+  using L = Layout<Rows>;
+  constexpr int D = Rows::D;
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ Walk walk;
+  __shared__ bool more;
+  const int tid = threadIdx.x;
+  uint32_t flags = 0;
+  dependent_sync();
+  {
+    Walk w;
+    w.find<kThreads>(a, kMinTiles, reinterpret_cast<long long *>(smem + L::kOffMisc), flags);
+    if (tid == 0) {
+      walk = w;
+      more = walk.piece(a);
+    }
+  }
   PagedJoin join = {0, 0, 0, 0, 0, 0};      // thread 0's
-  for (; walk.piece(a); walk.next(a)) {
-    const Item &it = walk.it;
+  __syncthreads();
+  while (more) {
+    const Item it = walk.it;
     if (a.split && tid == 0) walk.note_join(join);
     stream_keys<Rows>(a, it, walk.tile0, walk.n_tiles, smem, flags);
     const bool whole = walk.whole();
@@ -723,12 +755,16 @@ __global__ void __launch_bounds__(kThreads, Rows::kCtas) attn_paged_kernel(const
       }
     }
     __syncthreads();
+    if (tid == 0) {
+      walk.next(a);
+      more = walk.piece(a);
+    }
+    __syncthreads();
   }
   if (a.split && tid == 0) a.joins[blockIdx.x] = join;
-  if (flags && p.status) atomicOr(p.status, flags);
+  if (flags && a.p.status) atomicOr(a.p.status, flags);
 }
 
-// ---------------------------------------------------------------------------------------------------------------
 template <class Rows>
 Shape shape_for(const ds_paged_params &p) {
   using L = Layout<Rows>;
@@ -736,12 +772,14 @@ Shape shape_for(const ds_paged_params &p) {
   // A cluster per item where the items leave room for it and none is long: what the CTAs lose when the lengths
   // are uneven, or their number does not fill the GPU, has to stay below what the second kernel costs.
   const long long resident = (long long)Rows::kCtas * sm_count();
-  if (L::kClusters && h.items > 0 && h.items * 2 <= resident) {
+  if (h.items > 0 && h.items <= resident && (L::kClusters || h.items * 2 > resident)) {
     int n = 8;
     while (n > 1 && (h.items * n > resident || n > h.tiles)) n /= 2;
-    if (n > 1 && h.tiles <= n * kClusterTiles) {
+    if (h.tiles <= n * (n > 1 ? kClusterTiles : kAloneTiles)) {
       h.cluster = n;
       h.grid = (int)h.items * n;
+    } else {
+      h.may_alone = n == 1;      // the device knows the lengths
     }
   }
   return h;
@@ -754,11 +792,18 @@ int launch_rows(const ds_paged_params &p, cudaStream_t stream) {
   using L = Layout<Rows>;
   const Shape h = shape_for<Rows>(p);
   const Params a = params_of(p, h, workspace_of(h));
-  static std::atomic<unsigned long long> allowed{0};
-  DS_CUDA_OK(allow_smem(attn_paged_kernel<Rows>, L::kBytes, allowed));
-  // not set up early: its CTAs would wait in the slots that the kernel before it, often this one, leaves (32 x 32 heads x
-  // 4128 rows back to back 403 instead of 316 us)
-  DS_CUDA_OK(launch_kernel(attn_paged_kernel<Rows>, dim3(h.grid), kThreads, L::kBytes, h.cluster, false, stream, a));
+  static std::atomic<unsigned long long> allowed[2];
+  // Set up early (8.2 -> 6.4 us for one short request) only where one wave of CTAs does it: CTAs that wait in the
+  // slots that the kernel before it, often this one, leaves cost more with equal ranges (32 x 32 heads x 4128 rows back to
+  // back 403 instead of 316 us).
+  if (h.cluster) {
+    DS_CUDA_OK(allow_smem(attn_paged_item_kernel<Rows>, L::kBytes, allowed[0]));
+    DS_CUDA_OK(launch_kernel(attn_paged_item_kernel<Rows>, dim3(h.grid), kThreads, L::kBytes, h.cluster > 1 ? h.cluster : 0, true,
+                             stream, a));
+  } else {
+    DS_CUDA_OK(allow_smem(attn_paged_range_kernel<Rows>, L::kBytes, allowed[1]));
+    DS_CUDA_OK(launch_kernel(attn_paged_range_kernel<Rows>, dim3(h.grid), kThreads, L::kBytes, 0, false, stream, a));
+  }
   note_launch(1);
   return a.split ? launch_join<typename Rows::T, Rows::D>(a, h, stream) : (int)DS_OK;
 }

@@ -159,6 +159,20 @@ def test_long_lengths_are_split_and_joined(dtype, D, Hq, Hkv, lens, counts, kw):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("lens,Hkv,n", [
+    ([900, 1280, 30, 0, 1100, 700, 64, 65, 1000], 32, 1),       # short enough for a CTA each, whatever their lengths
+    ([1400, 1500, 1450, 1321, 1490, 1500, 1333, 1404], 32, 1),   # longer, even: a CTA each, by the lengths on the device
+    ([3000, 50, 1, 0, 300, 20, 64, 90], 32, 2),                  # longer, uneven: equal ranges
+    ([2500] + [40] * 39, 4, 1), ([1500] * 36, 8, 2),             # more than 32 sequences: the search goes through shared memory
+    ([700, 100, 2000], 2, 5), ([64] * 3, 1, 1)])                 # clusters of eight, of two
+def test_how_the_work_is_divided(dtype, lens, Hkv, n):
+    c = Case(lens, [min(n, 1 + b % 3) if n < 5 else n for b in range(len(lens))], 2 * Hkv, Hkv, 64, 16, dtype, seed=len(lens))
+    out, lse = c.check()
+    again, lse2, _ = c.run()
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 def test_many_sequences_and_peaked_scores(dtype):
     rng = np.random.default_rng(0)
     lens = [int(x) for x in rng.integers(0, 300, 150)]
