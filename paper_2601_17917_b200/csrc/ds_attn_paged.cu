@@ -32,6 +32,7 @@ constexpr int kWarps = 4, kThreads = kWarps * 32;
 constexpr int kMinTiles = 4;     // a range has at least so many key tiles
 constexpr int kWholeTiles = 8;   // items of at most so many key tiles are not split
 constexpr int kClusterTiles = 24;   // most key tiles of a CTA when an item has a cluster
+constexpr int kManyTiles = 20;      // when there are more items than CTAs at a time
 constexpr int kAloneTiles = 20;     // and when it has a CTA, whatever the others' lengths
 
 __device__ __forceinline__ void ldmatrix4(uint32_t addr, uint32_t (&r)[4]) {
@@ -66,7 +67,7 @@ __device__ __forceinline__ uint32_t chunk_at(int r, int c) { return r * ROW + ((
 // side, S^T = K Q^T and O^T = V^T P^T, so that a block of 8 rows (a single token of most grouped-query models) costs
 // half of what 16 rows would.  Lane 4i + q holds, of S^T, keys i and i + 8 of rows 2q and 2q + 1 of every block; movmatrix
 // turns the weights into the second product's fragments.
-template <int D_, int NB>
+template <int D_, int NB, int kStages_ = D_ == 128 && NB == 1 ? 2 : 3>
 struct TensorRows {
   using T = __nv_bfloat16;
   static constexpr int D = D_, kRows = 8 * NB, kRowBytes = 2 * D, kKeys = 16;
@@ -74,7 +75,7 @@ struct TensorRows {
   static constexpr int kQBytes = kQRegs ? 0 : kRows * kRowBytes;
   // CTAs per SM and stages of a ring: what registers and shared memory hold.  For one block of rows three CTAs with two
   // stages beat two with three (32 x 32 heads x 4128 rows, D = 128: 316 against 330 us).
-  static constexpr int kCtas = D == 64 && NB == 1 ? 4 : NB == 1 || (D == 64 && NB == 2) ? 3 : 2, kStages = D == 128 && NB == 1 ? 2 : 3;
+  static constexpr int kCtas = D == 64 && NB == 1 ? 4 : NB == 1 || (D == 64 && NB == 2) ? 3 : 2, kStages = kStages_;
   float o[NB][D / 16][4];        // dimensions 16 j + lane / 4 (+ 8), rows 2q, 2q + 1
   float m[NB][2], l[NB][2];
   int end[NB][2];
@@ -524,7 +525,7 @@ struct Layout {
   static constexpr int kOffMl = kOffQ + Rows::kQBytes;
   // what the ranks of a cluster write into each other's: sums, maxima and sums of weights.  Not in the rings, where the
   // receiving rank may still be loading; 32 rows leave no room for it beside them.
-  static constexpr bool kClusters = Rows::kRows * Rows::D <= 2048;
+  static constexpr bool kClusters = Rows::kRows * Rows::D <= (Rows::kStages == 2 ? 4096 : 2048);
   static constexpr int kOffParts = kOffMl + kWarps * Rows::kRows * 8;
   static constexpr int kOffTotals = kOffParts + (kClusters ? Rows::kRows * Rows::D * 4 : 0);
   static constexpr int kOffMisc = kOffTotals + (kClusters ? 8 * Rows::kRows * 8 : 0);
@@ -769,17 +770,25 @@ template <class Rows>
 Shape shape_for(const ds_paged_params &p) {
   using L = Layout<Rows>;
   Shape h = shape_of(p, L::kTile, Rows::kRows, kMinTiles, Rows::kCtas);
-  // A cluster per item where the items leave room for it and none is long: what the CTAs lose when the lengths
-  // are uneven, or their number does not fill the GPU, has to stay below what the second kernel costs.
+  // Items by themselves: a cluster per item where the items leave room for it, else a CTA, scheduled by the hardware as
+  // others end.  What CTAs lose when lengths are uneven, or their number does not fill the GPU, has to stay below what
+  // several pieces in a range and the second kernel cost: not with long items.  (60 x 32 heads x 0 .. 813 rows: 122 -> 68 us; from
+  // 20 tiles on no gain, 32 x 32 heads x 4128 rows 320 -> 330.)
   const long long resident = (long long)Rows::kCtas * sm_count();
-  if (h.items > 0 && h.items <= resident && (L::kClusters || h.items * 2 > resident)) {
-    int n = 8;
+  if (h.items > resident) {
+    if (h.tiles <= kManyTiles && h.items <= 0x7fffffff) {
+      h.cluster = 1;
+      h.grid = (int)h.items;
+    }
+  } else if (h.items > 0) {
+    const bool fills = h.items * 2 > resident;
+    int n = L::kClusters ? 8 : 1;
     while (n > 1 && (h.items * n > resident || n > h.tiles)) n /= 2;
-    if (h.tiles <= n * (n > 1 ? kClusterTiles : kAloneTiles)) {
+    if (h.tiles <= (n > 1 ? n * kClusterTiles : fills ? kAloneTiles : kAloneTiles / 2)) {
       h.cluster = n;
       h.grid = (int)h.items * n;
     } else {
-      h.may_alone = n == 1;      // the device knows the lengths
+      h.may_alone = n == 1 && fills;      // the device knows the lengths
     }
   }
   return h;
@@ -815,7 +824,9 @@ auto with_rows(const ds_paged_params &p, F f) {
   const long long rows = (long long)p.max_q * (p.Hq / p.Hkv);
   if (p.dtype == DS_BF16) {
     if (p.D == 64) return rows <= 8 ? f(TensorRows<64, 1>()) : rows <= 16 ? f(TensorRows<64, 2>()) : f(TensorRows<64, 4>());
-    return rows <= 8 ? f(TensorRows<128, 1>()) : rows <= 16 ? f(TensorRows<128, 2>()) : f(TensorRows<128, 4>());
+    if (rows <= 16) return rows <= 8 ? f(TensorRows<128, 1>()) : f(TensorRows<128, 2>());
+    // two stages leave room for the cluster's buffers (2 x 8 heads x 375 .. 1127 rows: 25 -> 14 us), three are a little faster
+    return shape_for<TensorRows<128, 4, 2>>(p).cluster > 1 ? f(TensorRows<128, 4, 2>()) : f(TensorRows<128, 4, 3>());
   }
   switch (p.D) {
     case 32: return rows == 1 ? f(ScalarRows<32, 1>()) : f(ScalarRows<32, 8>());
