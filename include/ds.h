@@ -544,12 +544,15 @@ DS_API int ds_qk_norm_rope(const ds_qk_params *p, void *stream);
  * bases 16-byte aligned, strides multiples of 16 bytes.  Envelope: DS_BF16 with D in {64, 128}, DS_F32 with D in
  * {32, 64, 128, 256}; any Hq / Hkv, page_size, n_b.
  *
+ * out may be q itself (same strides); it may not overlap anything else that the call reads.
+ *
  * Workspace: ds_attn_paged_workspace(p) bytes, 256-byte aligned, contents need not be kept between calls.  It holds
  * the partial results of sequences whose length is split over CTAs.  A call without a (large enough) workspace is
  * not an error; it runs unsplit.  Calls that may overlap must not share a workspace.
  * Errors: DS_ERR_INVALID_ARG (NULL or misaligned pointer, misaligned stride, Hq % Hkv != 0, window or sinks < 0, max_q < 1,
  * scale not finite, row_start == NULL with B * max_q > N, table_stride < max_pages); DS_ERR_UNSUPPORTED (D outside the
- * envelope, B > 8192, max_q * Hq * max_len / 16 beyond 2^31, max_pages * page_size or n_pages * page_size > 2^31 - 1). */
+ * envelope, B > 8192, max_q * Hq * max_len / 16 beyond 2^31, max_pages * page_size or n_pages * page_size > 2^31 - 1,
+ * max_len > 2^31 - 1025). */
 typedef struct {
   int32_t B, Hq, Hkv, D;
   int32_t dtype;

@@ -5,6 +5,7 @@
 #include <new>
 
 #include "ds_common.cuh"
+#include "ds_paged_index.cuh"
 
 namespace ds {
 
@@ -141,7 +142,7 @@ int validate_paged(const ds_paged_params *p) {
   const int64_t rows = (int64_t)p->max_q * (p->Hq / p->Hkv), cap = (int64_t)p->max_pages * p->page_size;
   const int64_t len = p->max_len > 0 && p->max_len < cap ? p->max_len : cap;
   if (rows > 0x3fffffffLL || rows * p->Hkv > 0x7fffffffLL / (len / 16 + 2)) return DS_ERR_UNSUPPORTED;
-  if (!d_ok || p->B > 8192 || (int64_t)p->max_pages * p->page_size > 0x7fffffffLL ||
+  if (!d_ok || p->B > 8192 || cap > 0x7fffffffLL || len > kPagedMaxLen ||
       (int64_t)p->n_pages * p->page_size > 0x7fffffffLL)
     return DS_ERR_UNSUPPORTED;
   return DS_OK;

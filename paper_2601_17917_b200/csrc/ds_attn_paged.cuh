@@ -64,6 +64,7 @@ struct Walk {
   // An item to each CTA, when there are no more items than CTAs and the longest is not too far above the mean of the
   // ranges: several pieces in a range and their join cost as much as some ten tiles.  (8 x 32 heads x 1000 .. 2080 rows, 32
   // queries: 67 instead of 78 us, 24 x 8 heads x 50 .. 3000 rows in fp32: 70 instead of 49; the rule takes the better.)
+  // For more than 32 sequences the block-wide form of this cost the others 1 .. 5 % and gained as little.
   __device__ bool alone(const Params &a, long long total) {
     const int lane = threadIdx.x & 31;
     PagedSeq q;
@@ -329,9 +330,9 @@ struct Shape {
 // From the most that the lengths may turn out to be: resident CTAs, or fewer where the ranges would get short.
 inline Shape shape_of(const ds_paged_params &p, int tile, int rows, int min_tiles, int ctas_per_sm) {
   Shape h;
-  const int cap = p.max_pages * p.page_size;
-  h.s = {p.B, p.Hq / p.Hkv, p.Hkv, p.N, p.max_q, p.max_len > 0 && p.max_len < cap ? p.max_len : cap,
-         p.causal != 0, p.window, p.sinks, log2_of(tile), log2_of(rows)};
+  const int cap = p.max_pages * p.page_size, bound = p.max_len > 0 && p.max_len < cap ? p.max_len : cap;
+  h.s = {p.B, p.Hq / p.Hkv, p.Hkv, p.N, p.max_q, bound, p.causal != 0, paged_window(p.window, bound), p.sinks, log2_of(tile),
+         log2_of(rows)};
   const PagedSeq q = paged_seq(h.s, 0, p.max_q < p.N ? p.max_q : p.N, h.s.bound);
   h.tiles = q.tiles;
   h.min_tiles = min_tiles;

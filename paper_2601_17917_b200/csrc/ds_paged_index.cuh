@@ -36,12 +36,16 @@ DS_HD int fast_div(int x, const FastDiv &f) { return (int)(((uint64_t)(uint32_t)
 struct PagedShape {
   int B, G, Hkv, N, max_q;   // G = query heads per KV head
   int bound;                 // most cache rows of a sequence: min(max_len, max_pages * page_size)
-  int causal, window, sinks;
+  int causal, window, sinks; // window < bound
   int tile_log2;             // keys per unit of work (a CTA's warps take equal parts of it)
   int row_log2;              // stacked rows (query, head of the group) per unit of work
 };
 DS_HD int paged_ceil_shift(int x, int log2) { return (int)(((unsigned)x + (1u << log2) - 1u) >> log2); }
-
+// Sequences may be so long: key numbers run up to two tiles beyond the last row, and e_i - window down to -(max_q + bound),
+// in 32 bits.
+constexpr int kPagedMaxLen = 0x7fffffff - 1024;
+// A window that no length passes hides nothing.
+DS_HD int paged_window(int window, int bound) { return window >= bound ? 0 : window; }
 
 // One sequence.  Its queries see cache rows [0, sink_n) and [body, len) between them.  The keys are numbered x: the
 // first sink_n rows, padding to a whole tile, then the body.

@@ -173,6 +173,44 @@ def test_how_the_work_is_divided(dtype, lens, Hkv, n):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("lens,Hkv,n", [([1400] * 100, 4, 1), ([1400 - 7 * b for b in range(100)], 4, 2), ([0] * 20 + [3000] + [90] * 60, 5, 1),
+                                        ([2000] * 33, 8, 3), ([1500, 0] * 50 + [1600], 4, 1)])
+def test_how_the_work_of_many_sequences_is_divided(dtype, lens, Hkv, n):
+    """An item per CTA where the lengths are even enough, equal ranges else: with empty sequences, and sequences
+    without rows, among them."""
+    c = Case(lens, [0 if b % 11 == 5 else n for b in range(len(lens))], 2 * Hkv, Hkv, 64, 16, dtype, seed=len(lens))
+    out, lse = c.check()
+    again, lse2, _ = c.run()
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("dtype,D,G,n", [(BF, 128, 1, 1), (BF, 128, 4, 8), (BF, 128, 4, 9), (BF, 64, 2, 40), (F32, 64, 2, 3), (F32, 256, 1, 1)])
+@pytest.mark.parametrize("length", [40, 5000])
+def test_the_output_may_be_the_queries(dtype, D, G, n, length):
+    c = Case([length, 0, length // 3, n], [n, n, n - 1, n], 2 * G, 2, D, 16, dtype, seed=n)
+    want, _, scale = c.run()
+    q = c.q.to(DEV)
+    k, v, t = (x.to(DEV) for x in (c.k, c.v, c.table))
+    got = ds.ds_attn_paged(q, k, v, t, torch.tensor(c.lens, dtype=torch.int32, device=DEV), scale, torch.tensor(c.starts, device=DEV),
+                           max_q=n, out=q)
+    assert got is q and torch.equal(q[:c.N], want) and torch.equal(q[c.N:].cpu(), c.q[c.N:])
+
+
+@pytest.mark.parametrize("dtype,D,G", [(BF, 128, 1), (BF, 128, 8), (F32, 64, 2)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_windows_and_first_tokens_of_any_size(dtype, D, G, causal):
+    """2^31 - 1 as window or number of first tokens hides nothing, also from queries of sequences shorter than their
+    rows (whose first rows see nothing)."""
+    c = Case([700, 3, 0, 64], [5, 5, 5, 5], 2 * G, 2, D, 16, dtype, seed=G)
+    want, want_lse = c.check(causal=causal)
+    top = (1 << 31) - 1
+    c.check(causal=causal, window=1, sinks=top)
+    for kw in (dict(window=top), dict(window=top, sinks=top), dict(window=704), dict(window=top - 5)):
+        got, lse, _ = c.run(causal=causal, **kw)
+        assert torch.equal(got, want) and torch.equal(lse, want_lse), kw
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 def test_many_sequences_and_peaked_scores(dtype):
     rng = np.random.default_rng(0)
     lens = [int(x) for x in rng.integers(0, 300, 150)]
@@ -603,6 +641,39 @@ def test_serving_steps_end_to_end(dtype):
         n = starts[-1]
         ref = oracle.attn_paged(f64(write.q_out)[:n], dk, dv, np.arange(B)[:, None], [len(h) for h in held], starts, 0.125, True)
         compare(attend.out[:n], attend.lse[:n], ref, dtype, D, top)
+
+
+@pytest.mark.parametrize("dtype,D,G,n,lens", [(BF, 128, 4, 1, [2000, 300, 77]), (BF, 128, 1, 1, [3000] * 30), (BF, 128, 4, 16, [2000, 300, 77]),
+                                              (F32, 64, 2, 2, [900, 5000, 1])])
+def test_a_captured_call_reads_lengths_rows_and_tables_at_replay(dtype, D, G, n, lens):
+    """Captured once with the longest lengths, replayed with others, which put the work on the CTAs differently."""
+    B = len(lens)
+    c = Case(lens, [n] * B, 8 * G, 8, D, 16, dtype, seed=3)
+    q, k, v, t = (x.to(DEV) for x in (c.q, c.k, c.v, c.table))
+    length, rows = torch.tensor(lens, dtype=torch.int32, device=DEV), torch.tensor(c.starts, device=DEV)
+    plan = ds.PagedAttnPlan(q, k, v, t, length, 0.1, row_start=rows, max_q=n, max_len=max(lens))
+    plan.launch()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        plan.launch()
+        plan.launch()
+    for step in range(4):
+        new = [0 if step == 3 else max(0, x // (1 + (b + step) % 5) - step) for b, x in enumerate(lens)]
+        starts = [0]
+        for b in range(B):
+            starts.append(starts[-1] + (n if (b + step) % 3 else n - 1))
+        length.copy_(torch.tensor(new, dtype=torch.int32))
+        rows.copy_(torch.tensor(starts, dtype=torch.int32))
+        plan.out.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = plan.out.clone()
+        ref = oracle.attn_paged(f64(c.q)[:starts[-1]], f64(c.k), f64(c.v), c.table.numpy(), new, np.array(starts, np.int32), 0.1, True)
+        eager, lse = torch.full_like(got, 7.0), torch.zeros(got.shape[:2], device=DEV)
+        ds.ds_attn_paged(q, k, v, t, length, 0.1, rows, max_q=n, max_len=max(lens), out=eager, lse=lse)
+        compare(got[:starts[-1]], lse[:starts[-1]], ref, dtype, D, max(lens))
+        assert torch.equal(got, eager) and (got[starts[-1]:] == 7.0).all()
 
 
 def test_streams_devices_and_plans_that_share_nothing():

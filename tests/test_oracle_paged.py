@@ -229,7 +229,8 @@ def test_attn_paged_argument_validation(L):
         assert L.ds_attn_paged(ctypes.byref(_attn(**kw)), None) == ds.DS_ERR_INVALID_ARG, kw
         assert L.ds_attn_paged_workspace(ctypes.byref(_attn(**kw))) == 0
     assert L.ds_attn_paged(None, None) == ds.DS_ERR_INVALID_ARG
-    for kw in (dict(D=96), dict(D=32), dict(D=256), dict(dtype=0, D=96), dict(B=8193, N=8193), dict(page_size=1 << 29)):
+    for kw in (dict(D=96), dict(D=32), dict(D=256), dict(dtype=0, D=96), dict(B=8193, N=8193), dict(page_size=1 << 29),
+               dict(B=1, N=1, Hq=1, Hkv=1, max_pages=1, n_pages=1, page_size=(1 << 31) - 1)):
         assert L.ds_attn_paged(ctypes.byref(_attn(**kw)), None) == ds.DS_ERR_UNSUPPORTED, kw
     assert L.ds_attn_paged(ctypes.byref(_attn(B=0)), None) == ds.DS_OK
     assert L.ds_attn_paged(ctypes.byref(_attn(N=0, row_start=FAKE)), None) == ds.DS_OK

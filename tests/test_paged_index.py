@@ -149,9 +149,42 @@ static void shapes() {
   }
 }
 
+// Lengths, windows and first tokens up to the largest: nothing overflows, and the keys are the definition's.
+static void extremes() {
+  std::mt19937_64 g(3);
+  auto in = [&](long long lo, long long hi) { return lo + (long long)(g() % (unsigned long long)(hi - lo + 1)); };
+  for (int round = 0; round < 200000; ++round) {
+    PagedShape s;
+    s.B = 1, s.G = 1, s.Hkv = 1, s.causal = in(0, 1);
+    s.bound = in(0, 1) ? (int)in(kPagedMaxLen - 300, kPagedMaxLen) : (int)in(1, 1 << in(0, 30));
+    const long long rows = 0x7fffffffLL / (s.bound / 16 + 2);
+    s.max_q = (int)in(1, rows < 0x3fffffff ? rows : 0x3fffffff), s.N = s.max_q;
+    auto any = [&]() { return (int)(in(0, 2) == 0 ? in(0x7fffffff - 300, 0x7fffffff) : in(0, 1) ? in(0, 300) : in(0, s.bound)); };
+    const int window = any();
+    s.window = paged_window(window, s.bound), s.sinks = any();
+    s.tile_log2 = (int)in(4, 7), s.row_log2 = (int)in(0, 7);
+    const int len = in(0, 1) ? s.bound - (int)in(0, s.bound < 300 ? s.bound : 300) : (int)in(0, s.bound < 300 ? s.bound : 300);
+    const PagedSeq q = paged_seq(s, 0, (int)in(0, s.max_q), len);
+    CHECK(q.len == len && q.sink_n >= 0 && q.sink_n <= q.sink_pad && q.body >= 0 && q.body <= len && q.tiles >= 0);
+    CHECK(q.count == 0 || q.tiles <= (len >> s.tile_log2) + 2);
+    const int tile = 1 << s.tile_log2;
+    for (int k = 0; k < 20; ++k) {
+      const int x = (int)(k < 10 ? in(0, ((long long)q.tiles + 1) * tile - 1) : ((long long)q.tiles + 1) * tile - 1 - in(0, tile));
+      const int t = paged_key(q, x);
+      CHECK(t >= -1 && t < len);
+      const int i = q.count ? (int)in(0, q.count - 1) : 0, end = s.causal ? q.end_min + i : len;
+      if (t < 0 || q.count == 0) continue;
+      const bool see = t < end && (window == 0 || t < s.sinks || t >= (long long)end - window);
+      CHECK(see == paged_visible(s, t, end));
+      if (x + 16 <= q.tiles * (long long)tile && paged_all_visible(s, q, x, 16)) CHECK(see);
+    }
+  }
+}
+
 int main() {
   divisions();
   shapes();
+  extremes();
   puts("ok");
   return 0;
 }
