@@ -15,6 +15,11 @@
  *                     state update (Eq. 5), block-finished test and the
  *                     early-exit flag ("Early Exit For Block Diffusion")
  *
+ * Beside them stand the fused output projection and rotary gather of the same
+ * step, the block scheduler's bookkeeping, and, for requests of different
+ * lengths that share one pool of cache pages, ds_page_update, ds_qk_norm_rope
+ * and ds_attn_paged.
+ *
  * Conventions
  *   - Every function returns a ds_status.  Nothing throws, traps or aborts.
  *   - Unless a parameter is marked HOST, pointers are DEVICE pointers on the

@@ -838,10 +838,15 @@ auto with_rows(const ds_paged_params &p, F f) {
 
 // Rows per KV head from which the kernel with tcgen05 tiles takes over.  Up to 32 rows one pass of this kernel is no slower
 // (8 x 32 heads x 1550 rows, 32 queries: 62 against 72 us; 32 x 28/4 heads x 4000 rows, 4 queries: 67 against 69); from 33
-// on it would need a second.
-constexpr int kTensorTileRows = 33;
+// on it needs a second.  That pays while one wave of clusters does it with short pieces: a small call takes the other
+// kernel 14 .. 25 us whatever its size.  (2 x 8 heads, 33 queries: 800 rows 15 against 23 us, 2400 rows 20 against 26, 8000 rows,
+// 16 tiles a CTA, 38 against 32; 28/4 heads, 32 queries, 224 rows per KV head: 13 against 25, 18 against 28, 36 against 37.)
+constexpr int kTensorTileRows = 33, kFewTiles = 12;
 bool wide(const ds_paged_params &p) {
-  return p.dtype == DS_BF16 && (long long)p.max_q * (p.Hq / p.Hkv) >= kTensorTileRows;
+  if (p.dtype != DS_BF16 || (long long)p.max_q * (p.Hq / p.Hkv) < kTensorTileRows) return false;
+  using Rows = TensorRows<128, 4, 2>;      // resident CTAs and tiles are those of D = 64, too
+  const Shape h = shape_for<Rows>(p);
+  return h.cluster == 0 || h.items > (long long)Rows::kCtas * sm_count() || h.tiles > kFewTiles * h.cluster;
 }
 
 }  // namespace

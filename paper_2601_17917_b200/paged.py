@@ -3,7 +3,9 @@
 Each of them exists twice: as a plan, an object made once from the tensors of a loop's call (arguments checked,
 pointers and strides written down) whose ``launch`` only enqueues the kernels, and as a function that makes a plan
 and launches it.  A plan keeps references to its tensors; what they contain is read at every launch.  The launch goes
-to the tensors' device, on ``stream`` or that device's current stream, and may be captured into a CUDA graph.
+to the tensors' device, on ``stream`` or that device's current stream, and may be captured into a CUDA graph; the plan
+has to live as long as the graph.  Launches of one plan, and graphs that hold one, write the same results and share a
+workspace: they must not overlap.  Calls that may overlap need a plan each.
 """
 from __future__ import annotations
 

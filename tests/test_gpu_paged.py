@@ -39,7 +39,7 @@ def status_word():
 class Case:
     """A pool of pages with shuffled tables; unused rows, pages and table entries hold what must not be used."""
 
-    def __init__(self, lens, counts, Hq, Hkv, D, ps, dtype, seed=0, sharp=1.0, order="head", spare=2, cap=None):
+    def __init__(self, lens, counts, Hq, Hkv, D, ps, dtype, seed=0, sharp=1.0, order="head", spare=2, cap=None, room=0):
         g = torch.Generator().manual_seed(seed)
         B = len(lens)
         width = max(1, max(-(-n // ps) for n in lens)) if cap is None else cap
@@ -50,6 +50,8 @@ class Case:
         if order == "row":
             kc, vc = kc.transpose(1, 2), vc.transpose(1, 2)
         self.table = torch.randperm(n_pages, generator=g)[:B * width].view(B, width).to(torch.int32)
+        if room:      # columns of the table beyond every length: a call that may turn out long is divided otherwise
+            self.table = torch.cat([self.table, torch.full((B, room), -7, dtype=torch.int32)], 1)
         self.lens, self.counts, self.ps, self.dtype, self.D = lens, counts, ps, dtype, D
         starts = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
         self.starts, self.N = starts, int(starts[-1])
@@ -121,20 +123,29 @@ def test_page_sizes(ps, dtype, D):
 @pytest.mark.parametrize("dtype,D", [(BF, 128), (BF, 64), (F32, 64)])
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("counts", [[4, 0, 1, 9, 2], [33, 40, 1, 16, 17]])
-def test_several_new_rows(dtype, D, causal, counts):
+@pytest.mark.parametrize("room", [0, 500])
+def test_several_new_rows(dtype, D, causal, counts, room):
     """Uneven numbers of new rows, none at all, and more rows than the cache holds (the first ones see nothing)."""
     lens = [70, 5, 129, 200, 1] if counts[0] == 4 else [33, 300, 65, 10, 131]
-    Case(lens, counts, 8, 4, D, 16, dtype, seed=sum(counts)).check(causal=causal)
+    Case(lens, counts, 8, 4, D, 16, dtype, seed=sum(counts), room=room).check(causal=causal)
 
 
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("Hq,Hkv,counts", [(8, 1, [3, 16, 0, 17]), (28, 4, [32, 1, 33, 5]), (2, 2, [64, 65, 128, 129]),
                                            (16, 1, [8, 9, 1, 24])])
 @pytest.mark.parametrize("kw", [dict(), dict(causal=False), dict(window=100, sinks=9), dict(window=300, sinks=130, causal=False)])
-def test_many_rows_per_head(D, Hq, Hkv, counts, kw):
+@pytest.mark.parametrize("room", [0, 500])
+def test_many_rows_per_head(D, Hq, Hkv, counts, kw, room):
     """From a fraction of a 128-row tile to several of them, peaked and flat scores, ends inside tiles."""
-    Case([129, 600, 1000, 257], counts, Hq, Hkv, D, 16, BF, seed=Hq, sharp=2.0).check(**kw)
-    Case([5000, 64, 0, 1], counts, Hq, Hkv, D, 24, BF, seed=Hq + 1, sharp=4.0).check(**kw)
+    Case([129, 600, 1000, 257], counts, Hq, Hkv, D, 16, BF, seed=Hq, sharp=2.0, room=room).check(**kw)
+    Case([5000, 64, 0, 1], counts, Hq, Hkv, D, 24, BF, seed=Hq + 1, sharp=4.0, room=room).check(**kw)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("kw", [dict(), dict(window=100, sinks=9), dict(window=1), dict(window=300, sinks=130, causal=False)])
+def test_many_rows_of_many_sequences(D, kw):
+    lens = [(37 * b) % 450 for b in range(80)]
+    Case(lens, [20 - b % 9 if b % 13 else 0 for b in range(80)], 8, 4, D, 16, BF, seed=D).check(**kw)
 
 
 @pytest.mark.parametrize("dtype,D", [(BF, 128), (F32, 64)])
@@ -187,7 +198,7 @@ def test_how_the_work_of_many_sequences_is_divided(dtype, lens, Hkv, n):
 @pytest.mark.parametrize("dtype,D,G,n", [(BF, 128, 1, 1), (BF, 128, 4, 8), (BF, 128, 4, 9), (BF, 64, 2, 40), (F32, 64, 2, 3), (F32, 256, 1, 1)])
 @pytest.mark.parametrize("length", [40, 5000])
 def test_the_output_may_be_the_queries(dtype, D, G, n, length):
-    c = Case([length, 0, length // 3, n], [n, n, n - 1, n], 2 * G, 2, D, 16, dtype, seed=n)
+    c = Case([length, 0, length // 3, n], [n, n, n - 1, n], 2 * G, 2, D, 16, dtype, seed=n, room=500 if length > 40 else 0)
     want, _, scale = c.run()
     q = c.q.to(DEV)
     k, v, t = (x.to(DEV) for x in (c.k, c.v, c.table))
@@ -248,12 +259,13 @@ def test_layouts_and_uniform_rows(dtype, D):
 
 @pytest.mark.parametrize("dtype,D", [(BF, 128), (BF, 64), (F32, 64)])
 @pytest.mark.parametrize("Hq", [2, 4, 12, 40])
-def test_what_a_query_does_not_see_cannot_reach_it(dtype, D, Hq):
+@pytest.mark.parametrize("room", [0, 500])
+def test_what_a_query_does_not_see_cannot_reach_it(dtype, D, Hq, room):
     """NaN and infinities in K and V of the later new rows: a causal query before them must not notice; those that see
     them get NaN.  The same at the window's edge."""
-    c = Case([70, 40], [6, 1], Hq, 2, D, 16, dtype, seed=3)
+    c = Case([70, 40], [6, 1], Hq, 2, D, 16, dtype, seed=3, room=room)
     clean, _, _ = c.run()
-    dirty = Case([70, 40], [6, 1], Hq, 2, D, 16, dtype, seed=3)
+    dirty = Case([70, 40], [6, 1], Hq, 2, D, 16, dtype, seed=3, room=room)
     page, off = dirty.table[0, 67 // 16].long(), 67 % 16
     dirty.v[page, :, off] = float("nan")
     dirty.k[page, :, off] = float("inf")
@@ -263,20 +275,20 @@ def test_what_a_query_does_not_see_cannot_reach_it(dtype, D, Hq):
     assert torch.equal(out[:3], clean[:3]) and torch.equal(out[6:], clean[6:])     # rows 64, 65, 66 and the other sequence
     assert torch.isnan(out[3:6]).all()
     # V alone infinite, at the last row: only the last query, only there
-    dirty = Case([70, 40], [6, 1], Hq, 2, D, 16, dtype, seed=3)
+    dirty = Case([70, 40], [6, 1], Hq, 2, D, 16, dtype, seed=3, room=room)
     dirty.v[page, :, off, 1::3] = float("inf")
     out, lse, _ = dirty.run()
     assert torch.equal(out[:5], clean[:5]) and torch.isinf(out[5, :, 1::3]).all()
     assert torch.equal(out[5, :, 0::3], clean[5, :, 0::3]) and torch.equal(out[5, :, 2::3], clean[5, :, 2::3])
     # window 5: query 0 (row 64) sees rows 60 .. 64, query 1 rows 61 .. 65: row 60 belongs to query 0 alone
     clean, _, _ = c.run(window=5)
-    dirty = Case([70, 40], [6, 1], Hq, 2, D, 16, dtype, seed=3)
+    dirty = Case([70, 40], [6, 1], Hq, 2, D, 16, dtype, seed=3, room=room)
     page, off = dirty.table[0, 60 // 16].long(), 60 % 16
     dirty.v[page, :, off] = float("nan")
     out, _, _ = dirty.run(window=5)
     assert torch.isnan(out[0]).all() and torch.equal(out[1:], clean[1:])
     # a row that no query of a window sees
-    dirty = Case([70, 40], [6, 1], Hq, 2, D, 16, dtype, seed=3)
+    dirty = Case([70, 40], [6, 1], Hq, 2, D, 16, dtype, seed=3, room=room)
     for r in (0, 33, 58, 59):
         dirty.v[dirty.table[0, r // 16].long(), :, r % 16] = float("nan")
         dirty.k[dirty.table[0, r // 16].long(), :, r % 16] = float("nan")
@@ -644,7 +656,7 @@ def test_serving_steps_end_to_end(dtype):
 
 
 @pytest.mark.parametrize("dtype,D,G,n,lens", [(BF, 128, 4, 1, [2000, 300, 77]), (BF, 128, 1, 1, [3000] * 30), (BF, 128, 4, 16, [2000, 300, 77]),
-                                              (F32, 64, 2, 2, [900, 5000, 1])])
+                                              (BF, 64, 4, 16, [9000, 300, 77]), (F32, 64, 2, 2, [900, 5000, 1])])
 def test_a_captured_call_reads_lengths_rows_and_tables_at_replay(dtype, D, G, n, lens):
     """Captured once with the longest lengths, replayed with others, which put the work on the CTAs differently."""
     B = len(lens)
