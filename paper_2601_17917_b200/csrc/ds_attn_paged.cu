@@ -305,7 +305,7 @@ struct TensorRows {
 // a part of the dimensions, so that a score needs log2(kParts) shuffles and each lane weighs keys of its own; the queries
 // come from shared memory, the same word for a whole part.  Second product: lane = dimensions, the weights from
 // shared memory.  Products are two wide (fma.rn.f32x2), over dimensions and over pairs of rows.
-// (With 8 lanes per key, each computing every weight of it, 24 x 8 heads x 1007 rows of D = 64 with 8 rows took 62 us.)
+// (With 8 lanes per key, each computing every weight of it, 24 x 8 heads x 1007 rows of D = 64 with 8 rows took 62 us, now 27.)
 template <int D_, int R>
 struct ScalarRows {
   using T = float;
@@ -314,7 +314,10 @@ struct ScalarRows {
   static constexpr int kPartStride = R * kDims + 4;                              // floats; 4: parts in banks of their own
   static constexpr int kOffP = kParts * kPartStride * 4;
   static constexpr int kQBytes = (kOffP + kWarps * kKeys * R * 4 + 15) / 16 * 16;      // queries; weights of each warp
-  static constexpr int kCtas = D == 32 && R == 1 ? 4 : 2, kStages = D == 256 ? 2 : 3;
+  // Three CTAs with two stages beat two with three: 24 x 8 heads x 1007 rows of D = 64 with 8 rows 27 against 32 us, 64 x 8 heads
+  // x 1250 rows of D = 128 with one row 106 against 109; but one long sequence with 8 rows of D = 64 27 against 25 (more parts).
+  static constexpr int kCtas = R == 1 ? (D == 32 ? 4 : 3) : D <= 64 ? 3 : 2;
+  static constexpr int kStages = (R == 1 && D == 32) || (R == 8 && D == 128) ? 3 : 2;
   static constexpr int kMine = R >= kParts ? R / kParts : 1;      // rows whose weights a lane computes for its key
   F2 o[(R + 1) / 2][E];                                            // pairs of rows (R = 1: the second is unused)
   float m[R], l[kMine];

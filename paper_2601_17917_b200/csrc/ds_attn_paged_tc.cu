@@ -1,5 +1,5 @@
 // ds_attn_paged for many query rows per KV head (a decoding block, grouped queries of several tokens): bf16 on the 5th
-// generation tensor cores.
+// generation tensor cores.  Small calls go to the kernel for few rows all the same.
 //
 // An item is up to 128 stacked rows (query, head of the group) of a sequence and KV head, the rows of a tcgen05 tile:
 // S = Q K^T and O += P V in TMEM, 128 keys at a time, with the online softmax on the thread that owns the tile's row.  The
