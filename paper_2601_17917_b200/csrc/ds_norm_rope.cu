@@ -11,7 +11,8 @@
 // Loads are asynchronous copies to shared memory, some steps ahead through the heads of q, k and v alike; a lane
 // reads back what it copied, so nothing is synchronised.  (16384 rows of 36 x 128 bf16: with the loads of four steps
 // held in registers 74 us, waiting for them; with copies of 8 bytes, twice the steps, 58 us and 79 % of the issue slots;
-// as it is 56 us, 5.36 TB/s.  Eight steps ahead 64 us, two 60; CTAs of 128 threads 57, of 256 62.)
+// as it is 57 .. 59 us, 5.1 .. 5.3 TB/s.  Eight steps ahead 64 us, two 60; CTAs of 128 threads 57, of 256 62; resident warps
+// that load their next row's heads ahead of the row's end 62.)
 // The phase of a pair is position * turn in integers modulo 2^64: exact for every position, and its top 32 bits are an
 // angle in [-1/2, 1/2) turns, which sincospif takes without a range reduction.
 #include <type_traits>
