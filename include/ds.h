@@ -539,7 +539,9 @@ DS_API int ds_qk_norm_rope(const ds_qk_params *p, void *stream);
  * with KV head h / (Hq / Hkv), fp32 accumulation, out in the element type.  A query that sees nothing gets
  * out = 0, lse = -inf.  Rows of q/out that belong to no sequence are left as they are.  What the cache holds in rows
  * beyond L, in pages no table names, and in rows the window hides from every query is not used, whatever its bits; K
- * and V of a row that some query sees and another does not reach only the one that does (a NaN there stays there).
+ * and V of a row that some query sees and another does not reach only the one that does (a NaN there stays there).  An
+ * infinity in V of a row that a query sees is the query's output in that dimension (NaN where infinities of both signs, or a
+ * NaN, meet, or where the row's weight is too small for fp32, 2^-80 of the largest).
  *
  * max_q and max_len are HOST bounds of n_b and L that size the launch; a sequence beyond them raises DS_DEV_INDEX and
  * is clamped (max_len = 0: the capacity of the block table).  A page number outside [0, n_pages) raises DS_DEV_INDEX

@@ -207,8 +207,7 @@ struct TensorRows {
         const float p0 = ex2_approx(s[nb][2 * h] - ref0), p1 = ex2_approx(s[nb][2 * h + 1] - ref1);
         l[nb][0] += p0;
         l[nb][1] += p1;
-        hi[nb][h] = sm100::pack_bf16(p0, p1);
-        lo[nb][h] = sm100::pack_bf16(p0 - bf16lo_to_f32(hi[nb][h]), p1 - bf16hi_to_f32(hi[nb][h]));
+        split_weights(p0, p1, hi[nb][h], lo[nb][h]);
       }
     }
     if (partial) keep_hidden_values_out(vbuf, hi, lo, seen);

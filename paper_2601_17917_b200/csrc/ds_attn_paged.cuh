@@ -31,6 +31,15 @@ template <int N>
 __device__ __forceinline__ void cp_async_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
+// Two weights as two bf16 halves each.  hi is cut off and lo is what is left of the weight (times 1 + 2^-23, so that something
+// is): both are positive where the weight is, and an infinite value stays the infinity that it is by the formula.  (Rounded to
+// the nearest, lo would be 0 or negative for half of the weights: infinity times that is NaN.)  16 bits of a weight are kept.
+__device__ __forceinline__ void split_weights(float p0, float p1, uint32_t &hi, uint32_t &lo) {
+  const uint32_t b0 = __float_as_uint(p0), b1 = __float_as_uint(p1);
+  constexpr float kMore = 1.f + 0x1p-23f;
+  hi = __byte_perm(b0, b1, 0x7632);
+  lo = sm100::pack_bf16(fmaf(p0, kMore, -__uint_as_float(b0 & 0xffff0000u)), fmaf(p1, kMore, -__uint_as_float(b1 & 0xffff0000u)));
+}
 // The item a CTA works on.
 struct Item {
   PagedSeq q;

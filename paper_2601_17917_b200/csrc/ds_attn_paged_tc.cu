@@ -99,6 +99,36 @@ __device__ __forceinline__ Seen seen_keys(const PagedShape &s, const PagedSeq &q
   return {end - t, paged_max(s.sinks - t, 0), end - s.window - t};
 }
 
+// With copies of a row, a copy's zeros for the others' keys times an infinity in V are NaN in its sum.  So where the joined sum is
+// NaN and its sum of weights is not, the n keys from x on that it is over are gone through for infinities in elements d .. d + 3
+// of V: by definition one of them is the average; two of different signs, or a NaN, are NaN.
+__device__ __forceinline__ float4 average_of_infinities(const Params &a, const Item &it, int x, int n, int end, int d, float4 v) {
+  const ds_paged_params &p = a.p;
+  const int32_t *table = p.block_table + it.b * p.table_stride;
+  const __nv_bfloat16 *base = reinterpret_cast<const __nv_bfloat16 *>(p.v_cache) + it.g * p.cache_stride[1] + d;
+  uint32_t pos = 0, neg = 0, nan = 0;      // by element
+  const uint32_t open = (isnan(v.x) ? 1u : 0u) | (isnan(v.y) ? 2u : 0u) | (isnan(v.z) ? 4u : 0u) | (isnan(v.w) ? 8u : 0u);
+#pragma unroll 1
+  for (int i = 0; i < n && (open & ~(nan | (pos & neg))); ++i) {
+    const int t = paged_key(it.q, x + i);
+    if (!paged_visible(a.s, t, end)) continue;
+    const int j = fast_div(t, a.page_div), page = paged_clamp_page(table[j], p.n_pages);
+    const __nv_bfloat16 *row = base + page * p.cache_stride[0] + (t - j * p.page_size) * p.cache_stride[2];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float y = __bfloat162float(row[e]);
+      pos |= (y == INFINITY ? 1u : 0u) << e;
+      neg |= (y == -INFINITY ? 1u : 0u) << e;
+      nan |= (isnan(y) ? 1u : 0u) << e;
+    }
+  }
+  auto value = [&](float y, int e) {
+    const bool up = (pos >> e) & 1, down = (neg >> e) & 1;
+    return !((open >> e) & 1) || ((nan >> e) & 1) || up == down ? y : up ? INFINITY : -INFINITY;
+  };
+  return make_float4(value(v.x, 0), value(v.y, 1), value(v.z, 2), value(v.w, 3));
+}
+
 // kCopies: how often a row stands in the tile.
 template <int D, int kCopies>
 __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const __grid_constant__ Params a) {
@@ -388,9 +418,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const __grid
                 }
                 l0 += p0;
                 l1 += p1;
-                const uint32_t h = pack_bf16(p0, p1);
-                hi[e / 2] = h;
-                lo[e / 2] = pack_bf16(p0 - bf16lo_to_f32(h), p1 - bf16hi_to_f32(h));
+                split_weights(p0, p1, hi[e / 2], lo[e / 2]);
               }
               // over scores that have been read, or are another copy's: columns c / 2 .. c / 2 + 15 <= c + 31
               tmem_st16(ts + c / 2, hi);
@@ -551,6 +579,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const __grid
                 const float4 o = *quad(k * kPad + r, q);
                 v.x = fmaf(o.x, f[k], v.x), v.y = fmaf(o.y, f[k], v.y), v.z = fmaf(o.z, f[k], v.z), v.w = fmaf(o.w, f[k], v.w);
               }
+              if (__builtin_expect(isnan((v.x + v.y) + (v.z + v.w)) && !isnan(sum), 0))
+                v = average_of_infinities(a, it, walk.tile0 * kKeys, walk.n_tiles * kKeys, end, d, v);
               if (whole) {
                 write_row4<T>(a, row, d, v, top, sum);
               } else {

@@ -1,0 +1,65 @@
+"""``ds_attn_paged`` on infinite and very large values and scores, on every way that a call may be divided and for every
+kernel.  Tolerances: those of ``test_gpu_paged.py`` where nothing else is said."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged as oracle
+from test_gpu_paged import BF, F32, U, Case, compare, f64
+
+pytestmark = pytest.mark.gpu
+
+# dtype, D, Hq, Hkv, lengths, new rows, spare columns of the table (what a call may turn out to need decides its division)
+PATHS = {
+    "bf16 clusters": (BF, 128, 2, 2, [300, 70], [1, 1], 0),
+    "bf16 clusters, 16 rows": (BF, 64, 8, 1, [300, 70], [2, 1], 0),
+    "bf16 clusters, 32 rows": (BF, 128, 8, 1, [300, 70], [4, 3], 0),
+    "bf16 an item per CTA": (BF, 64, 32, 32, [300, 70] * 8, [1] * 16, 0),
+    "bf16 an item per CTA by the lengths": (BF, 128, 32, 32, [1450, 1400] * 4, [1] * 8, 0),
+    "bf16 ranges": (BF, 128, 4, 2, [3000, 70], [1, 1], 1000),
+    "bf16 ranges, 32 rows": (BF, 64, 16, 2, [3000, 70], [4, 1], 1000),
+    "bf16 ranges, many sequences": (BF, 64, 8, 8, [1500] * 36, [1] * 36, 0),
+    "bf16 33 rows, clusters": (BF, 128, 2, 2, [300, 70], [33, 1], 0),
+    "bf16 tcgen05, 40 rows": (BF, 128, 8, 2, [3000, 70], [10, 1], 1000),
+    "bf16 tcgen05, 64 rows": (BF, 64, 4, 2, [300, 70], [32, 1], 1000),
+    "bf16 tcgen05, 100 rows": (BF, 128, 8, 2, [3000, 70], [25, 1], 1000),
+    "bf16 tcgen05, 200 rows": (BF, 64, 8, 2, [500, 70], [50, 1], 1000),
+    "bf16 tcgen05, many sequences": (BF, 128, 8, 4, [600] * 36, [20] * 36, 1000),
+    "fp32 clusters": (F32, 128, 2, 2, [300, 70], [1, 1], 0),
+    "fp32 clusters, 8 rows": (F32, 64, 8, 2, [300, 70], [2, 1], 0),
+    "fp32 ranges, 20 rows": (F32, 32, 8, 2, [3000, 70], [5, 1], 1000),
+    "fp32 ranges": (F32, 256, 2, 2, [3000, 70], [1, 1], 1000),
+}
+every_path = pytest.mark.parametrize("path", list(PATHS))
+
+
+def case(path, seed=0, **kw):
+    dtype, D, Hq, Hkv, lens, counts, room = PATHS[path]
+    return Case(lens, counts, Hq, Hkv, D, 16, dtype, seed=seed, room=room, **kw)
+
+
+def reference(c, scale, causal):
+    with np.errstate(invalid="ignore"):
+        return oracle.attn_paged(f64(c.q)[:c.N], f64(c.k), f64(c.v), c.table.numpy(), c.lens, c.starts, scale, causal)
+
+
+@every_path
+@pytest.mark.parametrize("causal", [True, False])
+def test_an_infinite_value_that_every_query_sees_is_in_every_output(path, causal):
+    """Rows in tiles without any hidden key: the average is infinite where V is, NaN where infinities of both signs meet,
+    and what it was everywhere else."""
+    c = case(path)
+    clean, clean_lse, scale = c.run(causal=causal)
+    for row, dims, value in ((5, slice(0, None, 7), math.inf), (100, slice(1, None, 7), -math.inf), (101, slice(2, None, 7), math.inf),
+                             (130, slice(2, None, 7), math.inf), (199, slice(3, None, 7), math.inf), (200, slice(3, None, 7), -math.inf)):
+        c.v[c.table[0, row // 16].long(), :, row % 16, dims] = value
+    out, lse, _ = c.run(causal=causal)
+    want = reference(c, scale, causal)[0]
+    assert np.isposinf(want[:c.counts[0]]).any() and np.isneginf(want[:c.counts[0]]).any() and np.isnan(want[:c.counts[0]]).any()
+    got = f64(out)
+    for kind in (np.isposinf, np.isneginf, np.isnan):
+        assert np.array_equal(kind(got), kind(want)), kind
+    finite = torch.from_numpy(np.isfinite(want))
+    assert torch.equal(out.cpu()[finite], clean.cpu()[finite]) and torch.equal(lse, clean_lse)
