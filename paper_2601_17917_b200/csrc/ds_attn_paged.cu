@@ -207,7 +207,7 @@ struct TensorRows {
         const float p0 = ex2_approx(s[nb][2 * h] - ref0), p1 = ex2_approx(s[nb][2 * h + 1] - ref1);
         l[nb][0] += p0;
         l[nb][1] += p1;
-        split_weights(p0, p1, hi[nb][h], lo[nb][h]);
+        split_weights(mul2(f2(p0, p1), f2(a.shrink, a.shrink)), hi[nb][h], lo[nb][h]);
       }
     }
     if (partial) keep_hidden_values_out(vbuf, hi, lo, seen);
@@ -417,6 +417,7 @@ struct ScalarRows {
       const float ref = mine(m, i, part);
       p[i] = ex2_approx(mine(z, i, part) - (ref == -INFINITY ? 0.f : ref));      // nothing seen yet: exp(-inf) = 0
       l[i] += p[i];
+      p[i] *= a.shrink;
     }
     float *to = p_s + key * R + part * kMine;
     if constexpr (kMine == 4) *reinterpret_cast<float4 *>(to) = make_float4(p[0], p[1], p[2], p[3]);

@@ -16,6 +16,9 @@ struct Params {
   int cluster;        // CTAs of an item; 0: equal ranges
   int may_alone;      // with equal ranges: an item per CTA instead, if the lengths turn out to be even enough
   FastDiv item_div, row_div;      // by KV heads times row tiles, by row tiles (at most): with a cluster
+  // The sums of weighted values hold shrink = 2^-b times them, 2^b over 512 times the most keys: a weight may be up to 256 (the
+  // exponents' reference lags), and no sum then passes the largest value that it averages.  Exact down to values of 2^-126 / shrink.
+  float shrink, stretch;
   int part_rows;      // rows of a partial result's slot
   PagedJoin *joins;   // [gridDim.x]
   float2 *part_ml;    // [2 gridDim.x][part_rows]  maximum (base 2, scaled) and sum
@@ -34,11 +37,12 @@ __device__ __forceinline__ void cp_async_wait() {
 // Two weights as two bf16 halves each.  hi is cut off and lo is what is left of the weight (times 1 + 2^-23, so that something
 // is): both are positive where the weight is, and an infinite value stays the infinity that it is by the formula.  (Rounded to
 // the nearest, lo would be 0 or negative for half of the weights: infinity times that is NaN.)  16 bits of a weight are kept.
-__device__ __forceinline__ void split_weights(float p0, float p1, uint32_t &hi, uint32_t &lo) {
-  const uint32_t b0 = __float_as_uint(p0), b1 = __float_as_uint(p1);
+__device__ __forceinline__ void split_weights(F2 p, uint32_t &hi, uint32_t &lo) {
+  const float2 w = f2_get(p);
+  const uint32_t b0 = __float_as_uint(w.x), b1 = __float_as_uint(w.y);
   constexpr float kMore = 1.f + 0x1p-23f;
   hi = __byte_perm(b0, b1, 0x7632);
-  lo = sm100::pack_bf16(fmaf(p0, kMore, -__uint_as_float(b0 & 0xffff0000u)), fmaf(p1, kMore, -__uint_as_float(b1 & 0xffff0000u)));
+  lo = sm100::pack_bf16(fmaf(w.x, kMore, -__uint_as_float(b0 & 0xffff0000u)), fmaf(w.y, kMore, -__uint_as_float(b1 & 0xffff0000u)));
 }
 // The item a CTA works on.
 struct Item {
@@ -232,7 +236,7 @@ __device__ __forceinline__ void store4(__nv_bfloat16 *p, const float4 &v) {
 // Sums of a finished row -> output and log-sum-exp.  A row that saw nothing has sum 0; a NaN stays one.
 template <typename T>
 __device__ __forceinline__ void write_row4(const Params &a, const Row &row, int d, float4 v, float top, float sum) {
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  const float inv = sum == 0.f ? 0.f : a.stretch / sum;
   v.x *= inv, v.y *= inv, v.z *= inv, v.w *= inv;
   store4(reinterpret_cast<T *>(a.p.out) + row.n * a.p.out_stride[0] + row.h * a.p.out_stride[1] + d, v);
   if (a.p.lse && d == 0) a.p.lse[row.n * a.p.Hq + row.h] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
@@ -365,6 +369,9 @@ inline Params params_of(const ds_paged_params &p, const Shape &h, size_t need) {
   a.page_div = make_fast_div(p.page_size);
   a.group_div = make_fast_div(h.s.G);
   a.split = need > 0 && p.workspace && (reinterpret_cast<uintptr_t>(p.workspace) & 255) == 0 && p.workspace_bytes >= need;
+  int bits = 9;
+  while ((1ll << (bits - 9)) < h.s.bound) ++bits;
+  a.stretch = (float)(1ll << bits), a.shrink = 1.f / a.stretch;
   a.part_rows = h.part_rows;
   uint8_t *ws = reinterpret_cast<uint8_t *>(p.workspace);
   a.joins = reinterpret_cast<PagedJoin *>(ws);

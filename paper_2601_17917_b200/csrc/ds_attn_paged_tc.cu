@@ -418,7 +418,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const __grid
                 }
                 l0 += p0;
                 l1 += p1;
-                split_weights(p0, p1, hi[e / 2], lo[e / 2]);
+                split_weights(mul2(f2(p0, p1), f2(a.shrink, a.shrink)), hi[e / 2], lo[e / 2]);
               }
               // over scores that have been read, or are another copy's: columns c / 2 .. c / 2 + 15 <= c + 31
               tmem_st16(ts + c / 2, hi);
@@ -515,7 +515,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const __grid
             tmem_wait_ld();
             if (!mine) continue;
             if (whole) {
-              const float inv = l == 0.f ? 0.f : 1.f / l;
+              const float inv = l == 0.f ? 0.f : a.stretch / l;
               uint4 *dst = reinterpret_cast<uint4 *>(reinterpret_cast<T *>(p.out) + row.n * p.out_stride[0] + row.h * p.out_stride[1] + c);
 #pragma unroll
               for (int e = 0; e < 32; e += 8) {

@@ -63,3 +63,21 @@ def test_an_infinite_value_that_every_query_sees_is_in_every_output(path, causal
         assert np.array_equal(kind(got), kind(want)), kind
     finite = torch.from_numpy(np.isfinite(want))
     assert torch.equal(out.cpu()[finite], clean.cpu()[finite]) and torch.equal(lse, clean_lse)
+
+
+@every_path
+def test_averages_of_very_large_values_are_finite(path):
+    """|V| up to 0.95 2^127, of either sign and of one: no sum may pass the average it leads to.  Scores that rise along the
+    keys, and so fast that no maximum holds for long, are what a lagging reference is worst for."""
+    for rising in (False, True):
+        c = case(path, seed=1)
+        page, off = c.table.long(), c.ps
+        finite = torch.isfinite(c.v)
+        big = (c.v.float().clamp(-1.9, 1.9) * 2.0 ** 126).to(c.dtype)
+        c.v = torch.where(finite, big.abs() if rising else big, c.v)
+        if rising:
+            c.q = c.q.abs()
+            for b, n in enumerate(c.lens):
+                t = torch.arange(n)
+                c.k[page[b, t // off], :, t % off] = (0.02 * t)[:, None, None].expand(n, c.k.shape[1], c.D).to(c.dtype)
+        c.check()
