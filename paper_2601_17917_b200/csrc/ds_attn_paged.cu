@@ -159,7 +159,7 @@ struct TensorRows {
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[nb][e] = (s[nb][e] + odd[nb][e]) * scale2;
+      for (int e = 0; e < 4; ++e) s[nb][e] = __fmul_rn(s[nb][e] + odd[nb][e], scale2);      // not to be fused with the subtraction
     const bool partial = !paged_all_visible(a.s, it.q, x, kKeys);
     uint32_t seen[NB] = {};      // only with partial: bit 2h + e: key lane / 4 + 8h, row 2q + e
     if (partial) {
@@ -373,7 +373,7 @@ struct ScalarRows {
         z[r] = t.x + t.y;
 #pragma unroll
         for (int off = kKeys; off < 32; off <<= 1) z[r] += __shfl_xor_sync(0xffffffffu, z[r], off);
-        z[r] *= scale2;
+        z[r] = __fmul_rn(z[r], scale2);      // not to be fused with the subtraction of the maximum
       }
     }
     uint32_t hidden = 0;      // bit r: the row does not see this lane's key

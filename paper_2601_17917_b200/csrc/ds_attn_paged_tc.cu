@@ -321,7 +321,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const __grid
     // ============================ softmax and epilogue ============================
     const uint32_t tw = tmem + ((uint32_t)(32 * warp) << 16);
     const int r = tid % kPad, copy = tid / kPad, key0 = copy * kMine;      // row of the item, keys of this copy
-    const float scale2 = p.scale * kLog2e;
+    // The maximum is kept of the scores as they are (negated under a negative scale) and the difference to it scaled.  Scaled
+    // first, the two are fused into one operation, and what its exact product differs by from a maximum that was rounded is
+    // itself a large exponent where the scores are (keys of the type's lowest values).
+    const float scale2 = p.scale * kLog2e, steep = fabsf(scale2), sign = scale2 < 0.f ? -1.f : 1.f;
     PagedJoin join = {0, 0, 0, 0, 0, 0};      // thread 0's
     auto zero_o = [&]() {
       uint32_t z[32];
@@ -366,17 +369,17 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const __grid
             if (all) {
 #pragma unroll
               for (int e = 0; e < 32; e += 2)
-                top = fmax3(top, __uint_as_float(s[e]) * scale2, __uint_as_float(s[e + 1]) * scale2);
+                top = fmax3(top, __uint_as_float(s[e]) * sign, __uint_as_float(s[e + 1]) * sign);
             } else {
               const uint32_t bits = seen.bits(c);
 #pragma unroll
-              for (int e = 0; e < 32; ++e) top = fmaxf(top, (bits >> e) & 1 ? __uint_as_float(s[e]) * scale2 : -INFINITY);
+              for (int e = 0; e < 32; ++e) top = fmaxf(top, (bits >> e) & 1 ? __uint_as_float(s[e]) * sign : -INFINITY);
             }
           }
           // The reference moves only when a weight would pass 2^8: the result is the same, O is touched rarely.
-          const bool over = mine && top > m + 8.f;
+          const bool over = mine && (m == -INFINITY ? top > m : (top - m) * steep > 8.f);
           if (__any_sync(0xffffffffu, over)) {
-            const float keep = !over ? 1.f : m == -INFINITY ? 0.f : ex2_approx(m - top);
+            const float keep = !over ? 1.f : m == -INFINITY ? 0.f : ex2_approx((m - top) * steep);
             if (over) m = top;
             l *= keep;
             if (i > 0) {
@@ -396,8 +399,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const __grid
             }
           }
           // ---- weights
-          const float ref = m == -INFINITY ? 0.f : m;      // nothing seen yet: exp(-inf) = 0
-          float l0 = 0.f, l1 = 0.f;
+          const float ref = m == -INFINITY ? 0.f : m * sign;      // nothing seen yet: exp(-inf) = 0
+          const F2 scale_2 = f2(scale2, scale2), ref_2 = f2(-ref, -ref), shrink_2 = f2(a.shrink, a.shrink);
+          F2 l_2 = 0;
           auto weights = [&](auto every) {      // std::true_type: no key of the tile is hidden
             constexpr bool kAll = decltype(every)::value;
 #pragma unroll 1
@@ -410,15 +414,15 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const __grid
               const uint32_t bits = kAll ? 0xffffffffu : seen.bits(c);
 #pragma unroll
               for (int e = 0; e < 32; e += 2) {
-                float p0 = ex2_approx(fmaf(__uint_as_float(s[e]), scale2, -ref));
-                float p1 = ex2_approx(fmaf(__uint_as_float(s[e + 1]), scale2, -ref));
+                float2 w = f2_get(mul2(add2(f2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), ref_2), scale_2));
+                w.x = ex2_approx(w.x), w.y = ex2_approx(w.y);
                 if (!kAll) {
-                  if (!((bits >> e) & 1)) p0 = 0.f;
-                  if (!((bits >> (e + 1)) & 1)) p1 = 0.f;
+                  if (!((bits >> e) & 1)) w.x = 0.f;
+                  if (!((bits >> (e + 1)) & 1)) w.y = 0.f;
                 }
-                l0 += p0;
-                l1 += p1;
-                split_weights(mul2(f2(p0, p1), f2(a.shrink, a.shrink)), hi[e / 2], lo[e / 2]);
+                const F2 weight = f2(w.x, w.y);
+                l_2 = add2(l_2, weight);
+                split_weights(mul2(weight, shrink_2), hi[e / 2], lo[e / 2]);
               }
               // over scores that have been read, or are another copy's: columns c / 2 .. c / 2 + 15 <= c + 31
               tmem_st16(ts + c / 2, hi);
@@ -427,7 +431,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const __grid
           };
           if (all) weights(std::true_type());
           else weights(std::false_type());
-          l += l0 + l1;
+          l += f2_get(l_2).x + f2_get(l_2).y;
           if constexpr (kCopies > 1) {      // no weight for the other copies' keys
             uint32_t z[16] = {};
 #pragma unroll
@@ -501,6 +505,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const __grid
       }
       if (!ok) break;
       // ---- the piece is done
+      if (m != -INFINITY) m *= steep;
       ok = __all_sync(0xffffffffu, mbar_wait(bar_pv_done + 8 * ((g - 1) & 1), ((g - 1) >> 1) & 1, abort_flag));
       if (!ok) break;
       tc_fence_after();

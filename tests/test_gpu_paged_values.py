@@ -81,3 +81,28 @@ def test_averages_of_very_large_values_are_finite(path):
                 t = torch.arange(n)
                 c.k[page[b, t // off], :, t % off] = (0.02 * t)[:, None, None].expand(n, c.k.shape[1], c.D).to(c.dtype)
         c.check()
+
+
+@every_path
+def test_rows_whose_keys_are_all_of_the_lowest_values(path):
+    """Scores of -1e36 and the like (queries of sums 1/200), all the same (K is the type's lowest value everywhere): the plain average.  And with one
+    key at half of that: its value.  Equal keys have equal scores whatever their rounding, so the weights are 2^-20 or so
+    all alike, kept to 2^-22 in two bf16 halves; the sums add 4 (16 + sqrt(n)) u."""
+    c = case(path, seed=2)
+    c.q = (c.q.abs().float() / c.q.abs().float().sum(-1, keepdim=True) / 200).to(c.dtype)
+    low, b = torch.finfo(c.dtype).min, 0
+    t = torch.arange(c.lens[b])
+    place = (c.table[b].long()[t // c.ps], slice(None), t % c.ps)
+    c.k[place] = low
+    n, rows = c.lens[b], c.counts[b]
+    out, lse, scale = c.run(causal=False)
+    v = f64(c.v[place])                                                   # [n, Hkv, D]
+    G = c.q.shape[1] // c.k.shape[1]
+    want, spread = (x.mean(0).repeat(G, 0) for x in (v, np.abs(v)))
+    tol = (2.0 ** -8 if c.dtype == BF else U) * np.abs(want) + (2.0 ** -22 + 4 * (16 + math.sqrt(n)) * U) * spread
+    assert (np.abs(f64(out[:rows]) - want) <= tol).all()
+    assert torch.isfinite(lse[:rows]).all() and (lse[:rows] < -1e34).all()
+    one = n // 3
+    c.k[c.table[b, one // c.ps].long(), :, one % c.ps] = low / 2
+    out, _, _ = c.run(causal=False)
+    assert torch.equal(out[:rows].cpu(), c.v[c.table[b, one // c.ps].long(), :, one % c.ps].repeat_interleave(G, 0)[None].expand(rows, -1, -1))
