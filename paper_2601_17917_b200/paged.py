@@ -6,6 +6,12 @@ and launches it.  A plan keeps references to its tensors; what they contain is r
 to the tensors' device, on ``stream`` or that device's current stream, and may be captured into a CUDA graph; the plan
 has to live as long as the graph.  Launches of one plan, and graphs that hold one, write the same results and share a
 workspace: they must not overlap.  Calls that may overlap need a plan each.
+
+Results and workspaces that are not given are allocated on the stream that is current when the plan (or function) is
+called.  Their memory may have been freed there a moment ago with kernels still pending on it, so a launch on another stream
+first waits for what that stream had been given by then; the caller orders the inputs, and whoever reads the results.  A graph
+cannot hold that wait: one that is captured on another stream must first be replayed when that work is over (entering
+``torch.cuda.graph`` waits for it; ``CUDAGraph.capture_begin`` alone does not).
 """
 from __future__ import annotations
 
@@ -113,6 +119,11 @@ def _current_device():
     return torch._C._cuda_getDevice()
 
 
+def _capturing(stream):
+    with torch.cuda.stream(stream):
+        return torch.cuda.is_current_stream_capturing()
+
+
 class _Plan:
     _name = ""
 
@@ -122,7 +133,18 @@ class _Plan:
         self._ref, self._fn = ctypes.byref(params), getattr(lib(), self._name)
         self._index = device.index
         self._own = tuple(t for t in own if t is not None)
-        self._own_stream = torch.cuda.current_stream(device).cuda_stream
+        self._own_stream, self._own_event = torch.cuda.current_stream(device), None
+        self._own_raw = self._own_stream.cuda_stream
+        if self._own and not _capturing(self._own_stream):
+            self._own_event = self._own_stream.record_event()
+
+    def _wait_for_own(self, stream):
+        """Orders ``stream`` behind whatever used the memory of the plan's own tensors before it had them."""
+        if self._own_event is not None:
+            if not _capturing(stream):
+                stream.wait_event(self._own_event)
+        elif _capturing(stream) and _capturing(self._own_stream):      # made within the capture, launched on a fork of it
+            stream.wait_event(self._own_stream.record_event())
 
     def _enqueue(self, stream):
         if stream is None:
@@ -131,6 +153,11 @@ class _Plan:
             raise ValueError(f"the stream is on {stream.device}, the tensors on {self.device}")
         else:
             raw = stream.cuda_stream
+        foreign = raw != self._own_raw and self._own
+        if foreign:
+            if stream is None:
+                stream = torch.cuda.current_stream(self._index)
+            self._wait_for_own(stream)
         if _current_device() == self._index:
             rc = self._fn(self._ref, raw)
         else:
@@ -138,9 +165,9 @@ class _Plan:
                 rc = self._fn(self._ref, raw)
         if rc != DS_OK:
             raise DsError(rc, self._name)
-        if raw != self._own_stream:      # the allocator must not hand these out again before this stream is done
+        if foreign:      # the allocator must not hand these out again before this stream is done
             for t in self._own:
-                t.record_stream(torch.cuda.current_stream(self._index) if stream is None else stream)
+                t.record_stream(stream)
 
 
 class RopeTable:
