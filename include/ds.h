@@ -559,8 +559,9 @@ DS_API int ds_qk_norm_rope(const ds_qk_params *p, void *stream);
  * not an error; it runs unsplit.  Calls that may overlap must not share a workspace.
  * Errors: DS_ERR_INVALID_ARG (NULL or misaligned pointer, misaligned stride, Hq % Hkv != 0, window or sinks < 0, max_q < 1,
  * scale not finite, row_start == NULL with B * max_q > N, table_stride < max_pages); DS_ERR_UNSUPPORTED (D outside the
- * envelope, B > 8192, max_q * Hq * max_len / 16 beyond 2^31, max_pages * page_size or n_pages * page_size > 2^31 - 1,
- * max_len > 2^31 - 1025). */
+ * envelope, B > 8192, max_q * Hq / Hkv >= 2^30, 2^31 and more tiles of queries and keys in one sequence of max_q and max_len
+ * rows (bf16: 8 x 64 and larger, from 33 query rows per KV head on 64 x 128; fp32: 1 x 16 and larger), max_pages * page_size or
+ * n_pages * page_size > 2^31 - 1, max_len > 2^31 - 1025). */
 typedef struct {
   int32_t B, Hq, Hkv, D;
   int32_t dtype;

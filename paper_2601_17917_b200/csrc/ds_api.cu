@@ -138,13 +138,12 @@ int validate_paged(const ds_paged_params *p) {
   if (!strides_ok(p->q_stride, 2, unit) || !strides_ok(p->cache_stride, 3, unit) || !strides_ok(p->out_stride, 2, unit))
     return DS_ERR_INVALID_ARG;
   const bool d_ok = p->dtype == DS_BF16 ? (p->D == 64 || p->D == 128) : (p->D == 32 || p->D == 64 || p->D == 128 || p->D == 256);
-  // the kernels count a sequence's rows and its units of work in 32 bits
   const int64_t rows = (int64_t)p->max_q * (p->Hq / p->Hkv), cap = (int64_t)p->max_pages * p->page_size;
   const int64_t len = p->max_len > 0 && p->max_len < cap ? p->max_len : cap;
-  if (rows > 0x3fffffffLL || rows * p->Hkv > 0x7fffffffLL / (len / 16 + 2)) return DS_ERR_UNSUPPORTED;
-  if (!d_ok || p->B > 8192 || cap > 0x7fffffffLL || len > kPagedMaxLen ||
-      (int64_t)p->n_pages * p->page_size > 0x7fffffffLL)
+  if (!d_ok || p->B > 8192 || cap > 0x7fffffffLL || len > kPagedMaxLen || (int64_t)p->n_pages * p->page_size > 0x7fffffffLL)
     return DS_ERR_UNSUPPORTED;
+  // the kernels count a sequence's rows and its units of work in 32 bits
+  if (rows > 0x3fffffffLL || !attn_paged_counts_fit(*p)) return DS_ERR_UNSUPPORTED;
   return DS_OK;
 }
 

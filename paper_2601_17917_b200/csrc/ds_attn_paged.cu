@@ -854,6 +854,17 @@ bool wide(const ds_paged_params &p) {
 
 }  // namespace
 
+// The numbers of units of the kernel that the call goes to.  (Of 33 rows and more this file's kernels take small calls only.)
+bool attn_paged_counts_fit(const ds_paged_params &p) {
+  const long long rows = (long long)p.max_q * (p.Hq / p.Hkv);
+  if (p.dtype == DS_BF16 && rows >= kTensorTileRows) return attn_paged_tc_counts_fit(p);
+  return with_rows(p, [&](auto engine) {
+    using Rows = decltype(engine);
+    const PagedShape s = units_of(p, Layout<Rows>::kTile, Rows::kRows);
+    return paged_units_fit(s, longest_of(s));
+  });
+}
+
 size_t attn_paged_workspace_bytes(const ds_paged_params &p) {
   if (p.B == 0 || p.N == 0) return 0;
   if (wide(p)) return attn_paged_tc_workspace_bytes(p);

@@ -58,7 +58,7 @@ struct Row {
 };
 __device__ __forceinline__ Row row_of(const Params &a, const Item &it, int r) {
   const int rr = it.row0 + r, i = fast_div(rr, a.group_div);
-  return {(long long)it.q.first + i, it.g * a.s.G + (rr - i * a.s.G), a.s.causal ? it.q.end_min + i : it.q.len};
+  return {(long long)it.q.first + i, it.g * a.s.G + (rr - i * a.s.G), a.s.causal ? max(it.q.end_min + i, 0) : it.q.len};
 }
 
 __device__ __forceinline__ PagedSeq sequence_of(const Params &a, int b) {
@@ -340,13 +340,19 @@ struct Shape {
   size_t workspace() const { return bytes_joins() + bytes_ml() + sizeof(float) * 2 * (size_t)grid * part_rows * D; }
 };
 
+// The most rows that a sequence may hold, and the numbers of a call's units with tiles of so many keys and rows.
+inline PagedShape units_of(const ds_paged_params &p, int tile, int rows) {
+  const int cap = p.max_pages * p.page_size, bound = p.max_len > 0 && p.max_len < cap ? p.max_len : cap;
+  return {p.B, p.Hq / p.Hkv, p.Hkv, p.N, p.max_q, bound, p.causal != 0, paged_window(p.window, bound), p.sinks, log2_of(tile),
+          log2_of(rows)};
+}
+inline PagedSeq longest_of(const PagedShape &s) { return paged_seq(s, 0, s.max_q < s.N ? s.max_q : s.N, s.bound); }
+
 // From the most that the lengths may turn out to be: resident CTAs, or fewer where the ranges would get short.
 inline Shape shape_of(const ds_paged_params &p, int tile, int rows, int min_tiles, int ctas_per_sm) {
   Shape h;
-  const int cap = p.max_pages * p.page_size, bound = p.max_len > 0 && p.max_len < cap ? p.max_len : cap;
-  h.s = {p.B, p.Hq / p.Hkv, p.Hkv, p.N, p.max_q, bound, p.causal != 0, paged_window(p.window, bound), p.sinks, log2_of(tile),
-         log2_of(rows)};
-  const PagedSeq q = paged_seq(h.s, 0, p.max_q < p.N ? p.max_q : p.N, h.s.bound);
+  h.s = units_of(p, tile, rows);
+  const PagedSeq q = longest_of(h.s);
   h.tiles = q.tiles;
   h.min_tiles = min_tiles;
   h.D = p.D;

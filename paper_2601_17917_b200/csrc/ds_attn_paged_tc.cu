@@ -96,7 +96,7 @@ __device__ __forceinline__ Seen seen_keys(const PagedShape &s, const PagedSeq &q
   if (x < q.sink_pad) return {paged_min(q.sink_n, end) - x, kKeys, 0};
   const int t = q.body + (x - q.sink_pad);
   if (s.window == 0) return {end - t, kKeys, 0};
-  return {end - t, paged_max(s.sinks - t, 0), end - s.window - t};
+  return {end - t, paged_max(s.sinks - t, 0), paged_max(end - s.window, 0) - t};
 }
 
 // With copies of a row, a copy's zeros for the others' keys times an infinity in V are NaN in its sum.  So where the joined sum is
@@ -643,6 +643,11 @@ int launch_copies(const ds_paged_params &p, cudaStream_t stream) {
 }
 
 }  // namespace
+
+bool attn_paged_tc_counts_fit(const ds_paged_params &p) {
+  const PagedShape s = units_of(p, kKeys, kRows / copies_for(p));
+  return paged_units_fit(s, longest_of(s));
+}
 
 size_t attn_paged_tc_workspace_bytes(const ds_paged_params &p) { return workspace_of(shape_for(p)); }
 

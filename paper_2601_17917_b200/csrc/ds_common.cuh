@@ -135,6 +135,8 @@ int launch_page_update(const ds_page_params &p, cudaStream_t stream);
 int launch_qk_norm_rope(const ds_qk_params &p, cudaStream_t stream);
 int launch_attn_paged(const ds_paged_params &p, cudaStream_t stream);
 size_t attn_paged_workspace_bytes(const ds_paged_params &p);
+bool attn_paged_counts_fit(const ds_paged_params &p);
+bool attn_paged_tc_counts_fit(const ds_paged_params &p);
 int launch_attn_paged_tc(const ds_paged_params &p, cudaStream_t stream);
 size_t attn_paged_tc_workspace_bytes(const ds_paged_params &p);
 int launch_bounded_wait_selftest(uint32_t poll_limit, uint32_t *status, int32_t *report, cudaStream_t stream);

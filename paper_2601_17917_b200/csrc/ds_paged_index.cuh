@@ -41,8 +41,7 @@ struct PagedShape {
   int row_log2;              // stacked rows (query, head of the group) per unit of work
 };
 DS_HD int paged_ceil_shift(int x, int log2) { return (int)(((unsigned)x + (1u << log2) - 1u) >> log2); }
-// Sequences may be so long: key numbers run up to two tiles beyond the last row, and e_i - window down to -(max_q + bound),
-// in 32 bits.
+// Sequences may be so long: key numbers run up to two tiles beyond the last row, in 32 bits.
 constexpr int kPagedMaxLen = 0x7fffffff - 1024;
 // A window that no length passes hides nothing.
 DS_HD int paged_window(int window, int bound) { return window >= bound ? 0 : window; }
@@ -66,7 +65,7 @@ DS_HD PagedSeq paged_seq(const PagedShape &s, int row_lo, int row_hi, int len) {
   q.bad = q.first != row_lo || n != q.count || q.len != len;
   q.end_max = q.len;
   q.end_min = s.causal ? q.len - q.count + 1 : q.len;
-  const int lo = s.window > 0 ? paged_max(0, q.end_min - s.window) : 0;
+  const int lo = s.window > 0 && q.end_min > s.window ? q.end_min - s.window : 0;
   if (lo <= s.sinks) {
     q.sink_n = q.sink_pad = q.body = 0;
   } else {
@@ -80,6 +79,12 @@ DS_HD PagedSeq paged_seq(const PagedShape &s, int row_lo, int row_hi, int len) {
   return q;
 }
 DS_HD int64_t paged_units(const PagedShape &s, const PagedSeq &q) { return (int64_t)q.row_tiles * s.Hkv * q.tiles; }
+// The units of a sequence within the bounds, and the products on the way there, stay below 2^31 (the kernels number them in 32
+// bits).  `most`: with the most queries and the largest length; padding behind the first rows may give another one tile more.
+DS_HD bool paged_units_fit(const PagedShape &s, const PagedSeq &most) {
+  const int64_t items = (int64_t)most.row_tiles * s.Hkv;
+  return items <= 0x7fffffffLL && items * paged_min(most.tiles + 1, (s.bound >> s.tile_log2) + 2) <= 0x7fffffffLL;
+}
 
 // Cache row of key x, -1 for padding.
 DS_HD int paged_key(const PagedSeq &q, int x) {
@@ -122,7 +127,7 @@ DS_HD int paged_join_parts(int64_t t0, int64_t per, int64_t item_end) {
 // A CTA writes the part of the item that its range begins with to slot 2c, that of the item it ends with to 2c + 1.
 DS_HD int paged_slot(int cta, bool first_segment) { return 2 * cta + (first_segment ? 0 : 1); }
 
-// Offset (elements) of cache row t of a head; `page` as the table has it.
+// A page as the table has it -> one of the pool.
 DS_HD int paged_clamp_page(int page, int n_pages) { return page < 0 ? 0 : page >= n_pages ? n_pages - 1 : page; }
 
 }  // namespace ds
