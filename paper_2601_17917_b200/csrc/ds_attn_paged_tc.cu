@@ -5,10 +5,10 @@
 // S = Q K^T and O += P V in TMEM, 128 keys at a time, with the online softmax on the thread that owns the tile's row.  The
 // units of work, their equal ranges over the SMs and the join of items that ranges share are those of the kernel for few
 // rows.  It is bound by HBM as long as the 1536 tensor cycles of a 64 KB key tile (512 for S, 1024 for P V, below) and
-// the softmax fit into the 2800 that HBM needs for it.  The softmax does not when 32 rows leave it to one warp (128 keys
-// a thread, 8 x 32 heads x 1550 rows with blocks of 32: 97 us), so up to 32 rows stand in the tile four times and up to 64
-// twice: each copy weighs its own part of the keys and holds zeros for the others, and the copies are joined when the
-// item ends.
+// the softmax fit into the 2800 that HBM needs for it.  The softmax does not when up to 64 rows leave it to two warps (128
+// keys a thread: 8 x 32 heads x 1550 rows of D = 64 with blocks of 48 take 70 us, 16 x 32/8 heads x 4000 rows of D = 128 with 10
+// queries 81), so up to 64 rows stand in the tile twice (60 and 74): each copy weighs half of the keys and holds zeros for the
+// others, and the copies are joined when the item ends.
 //
 // Warps:
 //   0-3  softmax and epilogue, thread = tile row = TMEM lane
@@ -359,7 +359,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const __grid
         tc_fence_after();
         const Seen seen = seen_keys(a.s, it.q, x, end);
         if (busy) {
-          // ---- largest score of this copy's keys; 32 of them stay in registers
+          // ---- largest score of this copy's keys
           float top = -INFINITY;
           uint32_t s[32];
 #pragma unroll 1
@@ -407,10 +407,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const __grid
 #pragma unroll 1
             for (int c = key0; c < key0 + kMine; c += 32) {
               uint32_t hi[16], lo[16];
-              if (kMine > 32) {
-                tmem_ld32(ts + c, s);
-                tmem_wait_ld();
-              }
+              tmem_ld32(ts + c, s);
+              tmem_wait_ld();
               const uint32_t bits = kAll ? 0xffffffffu : seen.bits(c);
 #pragma unroll
               for (int e = 0; e < 32; e += 2) {
@@ -615,11 +613,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const __grid
 
 size_t workspace_of(const Shape &h) { return h.tiles <= kWholeTiles || h.grid == 1 ? 0 : h.workspace(); }
 
-// Copies of a row in the tile: as many as there is room for.
-int copies_for(const ds_paged_params &p) {
-  const long long rows = (long long)p.max_q * (p.Hq / p.Hkv);
-  return rows <= 32 ? 4 : rows <= 64 ? 2 : 1;
-}
+// Copies of a row in the tile: two where there is room for them.  (Calls of up to 32 rows do not come here.)
+int copies_for(const ds_paged_params &p) { return (long long)p.max_q * (p.Hq / p.Hkv) <= kRows / 2 ? 2 : 1; }
 Shape shape_for(const ds_paged_params &p) { return shape_of(p, kKeys, kRows / copies_for(p), kMinTiles, 1); }
 
 template <int D, int kCopies>
@@ -635,11 +630,7 @@ int launch(const ds_paged_params &p, cudaStream_t stream) {
 
 template <int D>
 int launch_copies(const ds_paged_params &p, cudaStream_t stream) {
-  switch (copies_for(p)) {
-    case 4: return launch<D, 4>(p, stream);
-    case 2: return launch<D, 2>(p, stream);
-    default: return launch<D, 1>(p, stream);
-  }
+  return copies_for(p) == 2 ? launch<D, 2>(p, stream) : launch<D, 1>(p, stream);
 }
 
 }  // namespace
