@@ -106,3 +106,9 @@ def test_rows_whose_keys_are_all_of_the_lowest_values(path):
     c.k[c.table[b, one // c.ps].long(), :, one % c.ps] = low / 2
     out, _, _ = c.run(causal=False)
     assert torch.equal(out[:rows].cpu(), c.v[c.table[b, one // c.ps].long(), :, one % c.ps].repeat_interleave(G, 0)[None].expand(rows, -1, -1))
+
+
+@every_path
+@pytest.mark.parametrize("scale", [0.0, -0.2, 3.0, 1e-30])
+def test_any_scale(path, scale):
+    case(path, seed=5).check(scale=scale)
