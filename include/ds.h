@@ -432,6 +432,8 @@ DS_API int ds_block_begin(const ds_block_params *p, void *stream);
  *   4. kv_len_out[b] = old_b + rows granted, *free_cnt_out = F' - pages handed out, row_start[0 .. B] = exclusive
  *      sum of the rows granted; for the i-th new row of sequence b, r = row_start[b] + i:
  *      positions[r] = old_b + i, slot_map[r] = its slot.  Rows r >= row_start[B]: positions 0, slot_map -1.
+ * Between calls lengths only change here: a kv_len[b] that the caller lowers past a page boundary leaves the pages above it
+ * in the table, where the next call writes over them (they are lost to the pool).
  * kv_len_out may be kv_len and free_cnt_out may be free_cnt; no other two arguments may overlap.  Entries of
  * block_table and free_list that the rules do not name are left as they are.
  * A length or count that is negative, and a length or request beyond max_pages pages, raise DS_DEV_INDEX: the length

@@ -314,7 +314,8 @@ struct ScalarRows {
   static constexpr int kOffP = kParts * kPartStride * 4;
   static constexpr int kQBytes = (kOffP + kWarps * kKeys * R * 4 + 15) / 16 * 16;      // queries; weights of each warp
   // Three CTAs with two stages beat two with three: 24 x 8 heads x 1007 rows of D = 64 with 8 rows 27 against 32 us, 64 x 8 heads
-  // x 1250 rows of D = 128 with one row 106 against 109; but one long sequence with 8 rows of D = 64 27 against 25 (more parts).
+  // x 1250 rows of D = 128 with one row 106 against 109; but one long sequence with 8 rows of D = 64 27 against 25 (more parts),
+  // which a second instance of the kernel for such calls would not be worth.
   static constexpr int kCtas = R == 1 ? (D == 32 ? 4 : 3) : D <= 64 ? 3 : 2;
   static constexpr int kStages = (R == 1 && D == 32) || (R == 8 && D == 128) ? 3 : 2;
   static constexpr int kMine = R >= kParts ? R / kParts : 1;      // rows whose weights a lane computes for its key
@@ -805,9 +806,9 @@ int launch_rows(const ds_paged_params &p, cudaStream_t stream) {
   const Shape h = shape_for<Rows>(p);
   const Params a = params_of(p, h, workspace_of(h));
   static std::atomic<unsigned long long> allowed[2];
-  // Set up early (8.2 -> 6.4 us for one short request) only where one wave of CTAs does it: CTAs that wait in the
-  // slots that the kernel before it, often this one, leaves cost more with equal ranges (32 x 32 heads x 4128 rows back to
-  // back 403 instead of 316 us).
+  // Set up early (8.2 -> 6.4 us for one short request) where items have CTAs of their own.  Not with equal ranges: CTAs that
+  // wait in the slots that the kernel before it, often this one, leaves hold up its long CTAs (32 x 32 heads x 4128 rows back
+  // to back 403 instead of 316 us).
   if (h.cluster) {
     DS_CUDA_OK(allow_smem(attn_paged_item_kernel<Rows>, L::kBytes, allowed[0]));
     DS_CUDA_OK(launch_kernel(attn_paged_item_kernel<Rows>, dim3(h.grid), kThreads, L::kBytes, h.cluster > 1 ? h.cluster : 0, true,
@@ -820,8 +821,8 @@ int launch_rows(const ds_paged_params &p, cudaStream_t stream) {
   return a.split ? launch_join<typename Rows::T, Rows::D>(a, h, stream) : (int)DS_OK;
 }
 
-// Calls f with the row engine for the call's type, head dimension and rows per KV head.  More rows than 32 are
-// served 32 at a time.
+// Calls f with the row engine for the call's type, head dimension and rows per KV head.  More rows than an engine holds (32
+// in bf16, 8 in fp32) are several items, each of which streams K and V again.
 template <class F>
 auto with_rows(const ds_paged_params &p, F f) {
   const long long rows = (long long)p.max_q * (p.Hq / p.Hkv);
@@ -840,8 +841,8 @@ auto with_rows(const ds_paged_params &p, F f) {
 }
 
 // Rows per KV head from which the kernel with tcgen05 tiles takes over.  Up to 32 rows one pass of this kernel is no slower
-// (8 x 32 heads x 1550 rows, 32 queries: 62 against 72 us; 32 x 28/4 heads x 4000 rows, 4 queries: 67 against 69); from 33
-// on it needs a second.  That pays while one wave of clusters does it with short pieces: a small call takes the other
+// (8 x 32 heads x 1550 rows each, 32 queries: 59 us, and 72 with a form of the other that held every row four times; 32 x 28/4
+// heads x 4000 rows, 4 queries: 67 against 69); from 33 on it needs a second.  That pays while one wave of clusters does it with short pieces: a small call takes the other
 // kernel 14 .. 25 us whatever its size.  (2 x 8 heads, 33 queries: 800 rows 15 against 23 us, 2400 rows 20 against 26, 8000 rows,
 // 16 tiles a CTA, 38 against 32; 28/4 heads, 32 queries, 224 rows per KV head: 13 against 25, 18 against 28, 36 against 37.)
 constexpr int kTensorTileRows = 33, kFewTiles = 12;
