@@ -543,7 +543,7 @@ DS_API int ds_qk_norm_rope(const ds_qk_params *p, void *stream);
  * beyond L, in pages no table names, and in rows the window hides from every query is not used, whatever its bits; K
  * and V of a row that some query sees and another does not reach only the one that does (a NaN there stays there).  An
  * infinity in V of a row that a query sees is the query's output in that dimension (NaN where infinities of both signs, or a
- * NaN, meet, or where the row's weight is too small for fp32, 2^-80 of the largest).  Finite values have finite averages up to
+ * NaN, meet, or where the row's weight is too small for fp32, 2^-60 of the largest).  Finite values have finite averages up to
  * the type's largest; in exchange values below 2^-117 times the bound of the lengths lose bits.
  *
  * max_q and max_len are HOST bounds of n_b and L that size the launch; a sequence beyond them raises DS_DEV_INDEX and

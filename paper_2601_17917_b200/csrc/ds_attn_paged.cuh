@@ -18,7 +18,7 @@ struct Params {
   FastDiv item_div, row_div;      // by KV heads times row tiles, by row tiles (at most): with a cluster
   // The sums of weighted values hold shrink = 2^-b times them, 2^b over 512 times the most keys: a weight may be up to 256 (the
   // exponents' reference lags), and no sum then passes the largest value that it averages.  Exact down to values of 2^-126 / shrink.
-  float shrink, stretch;
+  float shrink, stretch, shrink_log2;
   int part_rows;      // rows of a partial result's slot
   PagedJoin *joins;   // [gridDim.x]
   float2 *part_ml;    // [2 gridDim.x][part_rows]  maximum (base 2, scaled) and sum
@@ -377,7 +377,7 @@ inline Params params_of(const ds_paged_params &p, const Shape &h, size_t need) {
   a.split = need > 0 && p.workspace && (reinterpret_cast<uintptr_t>(p.workspace) & 255) == 0 && p.workspace_bytes >= need;
   int bits = 9;
   while ((1ll << (bits - 9)) < h.s.bound) ++bits;
-  a.stretch = (float)(1ll << bits), a.shrink = 1.f / a.stretch;
+  a.stretch = (float)(1ll << bits), a.shrink = 1.f / a.stretch, a.shrink_log2 = -(float)bits;
   a.part_rows = h.part_rows;
   uint8_t *ws = reinterpret_cast<uint8_t *>(p.workspace);
   a.joins = reinterpret_cast<PagedJoin *>(ws);

@@ -400,7 +400,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const __grid
           }
           // ---- weights
           const float ref = m == -INFINITY ? 0.f : m * sign;      // nothing seen yet: exp(-inf) = 0
-          const F2 scale_2 = f2(scale2, scale2), ref_2 = f2(-ref, -ref), shrink_2 = f2(a.shrink, a.shrink);
+          // weights are scaled down in the exponent (16 x 32/8 heads x 4000 rows with 10 queries: 73.4 us, multiplied afterwards 74.3);
+          // that rounds them at 2^-19, their halves do at 2^-16
+          const F2 scale_2 = f2(scale2, scale2), ref_2 = f2(-ref, -ref), shrink_2 = f2(a.shrink_log2, a.shrink_log2);
           F2 l_2 = 0;
           auto weights = [&](auto every) {      // std::true_type: no key of the tile is hidden
             constexpr bool kAll = decltype(every)::value;
@@ -412,7 +414,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const __grid
               const uint32_t bits = kAll ? 0xffffffffu : seen.bits(c);
 #pragma unroll
               for (int e = 0; e < 32; e += 2) {
-                float2 w = f2_get(mul2(add2(f2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), ref_2), scale_2));
+                float2 w = f2_get(fma2(add2(f2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), ref_2), scale_2, shrink_2));
                 w.x = ex2_approx(w.x), w.y = ex2_approx(w.y);
                 if (!kAll) {
                   if (!((bits >> e) & 1)) w.x = 0.f;
@@ -420,7 +422,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const __grid
                 }
                 const F2 weight = f2(w.x, w.y);
                 l_2 = add2(l_2, weight);
-                split_weights(mul2(weight, shrink_2), hi[e / 2], lo[e / 2]);
+                split_weights(weight, hi[e / 2], lo[e / 2]);
               }
               // over scores that have been read, or are another copy's: columns c / 2 .. c / 2 + 15 <= c + 31
               tmem_st16(ts + c / 2, hi);
@@ -504,6 +506,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged_tc_kernel(const __grid
       if (!ok) break;
       // ---- the piece is done
       if (m != -INFINITY) m *= steep;
+      l *= a.stretch;
       ok = __all_sync(0xffffffffu, mbar_wait(bar_pv_done + 8 * ((g - 1) & 1), ((g - 1) >> 1) & 1, abort_flag));
       if (!ok) break;
       tc_fence_after();

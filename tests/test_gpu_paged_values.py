@@ -112,3 +112,18 @@ def test_rows_whose_keys_are_all_of_the_lowest_values(path):
 @pytest.mark.parametrize("scale", [0.0, -0.2, 3.0, 1e-30])
 def test_any_scale(path, scale):
     case(path, seed=5).check(scale=scale)
+
+
+@every_path
+def test_an_infinite_value_of_small_weight(path):
+    """A key some 10 to 40 nats below the others (2^-60 at the least): its infinity is in the output all the same."""
+    c = case(path, seed=6)
+    c.q = c.q.abs()
+    page, off = c.table[0, 6].long(), 5
+    c.k[page, :, off] = -3.0
+    c.v[page, :, off, 1::5] = -math.inf
+    out, lse, scale = c.run(causal=False)
+    want, want_lse = reference(c, scale, False)[:2]
+    got = f64(out)
+    assert np.isneginf(want[:c.counts[0], :, 1::5]).all()
+    assert np.array_equal(np.isneginf(got), np.isneginf(want)) and not np.isnan(got).any()
