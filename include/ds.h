@@ -18,7 +18,8 @@
  * Beside them stand the fused output projection and rotary gather of the same
  * step, the block scheduler's bookkeeping, and, for requests of different
  * lengths that share one pool of cache pages, ds_page_update, ds_qk_norm_rope
- * and ds_attn_paged.
+ * and ds_attn_paged, with the 8-bit form of that cache: ds_kv8_write,
+ * ds_kv8_read and ds_attn_paged8.
  *
  * Conventions
  *   - Every function returns a ds_status.  Nothing throws, traps or aborts.
@@ -593,6 +594,124 @@ typedef struct {
 DS_API size_t ds_attn_paged_workspace(const ds_paged_params *p);
 /* `p` is a HOST pointer; the pointers inside it are device pointers. */
 DS_API int ds_attn_paged(const ds_paged_params *p, void *stream);
+
+/* ------------------------------------------------------------------------
+ * The paged cache in 8 bits: half of the bytes of a bf16 cache.
+ *   ds_kv8_write     K and V of the new rows quantised into their pages
+ *   ds_kv8_read      rows of the cache back in bf16 or fp32
+ *   ds_attn_paged8   ds_attn_paged over such a cache
+ *
+ * k_cache and v_cache hold e4m3 values (1 sign, 4 exponent, 3 fraction bits, largest 448, 0x7f and 0xff NaN, no
+ * infinity), k_scale and v_scale an fp32 scale for every block of scale_block rows (T below; it divides page_size) and KV
+ * head: block o / T of row o of a page, a row's value is the e4m3 value times its block's scale.  T = 1 is a scale per
+ * token, T = page_size one per page.  Strides of the caches are for page, head and row, D contiguous, multiples
+ * of 16 bytes on a 16-byte aligned base; those of the scales are for page, head and block, of any size.  Block tables,
+ * lengths and packed rows are those of ds_page_update.  The readers take any scale, ds_kv8_write writes powers of two.
+ * ------------------------------------------------------------------------ */
+
+/* ds_kv8_write: the n_b = row_start[b + 1] - row_start[b] packed rows of sequence b (max_q each without row_start) are
+ * its rows kv_len[b] - n_b .. kv_len[b] - 1, the last ones, new or rewritten.  For every block of T rows that some of
+ * them fall into, for every head, for K and V each:
+ *     a  = largest |x| of the call's finite values in the block
+ *     2^e with e the smallest integer >= -126 for which a <= 448 * 2^e, and
+ *          2^e >= |s| where the block holds rows from before the call (before kv_len[b] - n_b) and its scale has |s| <= 2^127
+ *     the new rows become  RN(x / 2^e), the rows from before  RN(value * s / 2^e)  unless s = 2^e;  the scale becomes 2^e
+ * with RN to the nearest e4m3 value, ties to even.  The division by a power of two is exact, so that there is one
+ * rounding, and rows from before change only where they fall below 2^-6 of the new scale.  Infinities and NaN are held as
+ * NaN, as are rows from before under an infinite or NaN scale; |x| > 1.875 * 2^127 is held as that (what it would be rounded to
+ * has no fp32 value).  Rows of the block at and beyond kv_len[b], other blocks and other pages are left as they are.
+ * The result is the same whatever rows a block's rows arrive with, but for the rounding of a scale that grows later.
+ * A scale follows what was written: rewriting rows of a block that has rows from before keeps its scale or raises it, rewriting
+ * all rows of a block starts it anew.
+ *
+ * Two sequences whose tables name the same page must not write into the same block of it in one call.  A page number outside
+ * [0, n_pages) raises DS_DEV_INDEX and nothing is written for it.  So does a sequence whose length is outside 0 .. min(max_len,
+ * capacity of the table) (max_len = 0: the capacity), whose row range is outside 0 .. N or runs backwards, or has more rows than max_q or
+ * than its length: none of its rows is written.  Rows of k and v that belong to no sequence are not read.  row_start may not decrease;
+ * if it does, which of the rows are written is not defined (DS_DEV_INDEX is raised).
+ *
+ * Layout of k and v: element strides for row and head, D contiguous, bases 16-byte aligned, strides multiples of 16 bytes.
+ * Types: DS_F32, DS_BF16; D a multiple of 16 up to 256.  Errors: DS_ERR_INVALID_ARG (NULL or misaligned pointer or stride, counts
+ * below 1, page_size not a multiple of scale_block, row_start == NULL with B * max_q > N, table_stride < max_pages);
+ * DS_ERR_UNSUPPORTED (D outside the envelope, B > 8192, Hkv > 32767, scale_block > 65536, max_pages * page_size or n_pages * page_size
+ * > 2^31 - 1). */
+typedef struct {
+  int32_t B, Hkv, D;
+  int32_t dtype;                /* of k and v */
+  int32_t N;                    /* rows of k and v */
+  int32_t max_q;                /* most new rows of a sequence */
+  int32_t max_len;              /* most rows of a sequence, 0 = max_pages * page_size */
+  int32_t page_size, max_pages, n_pages;
+  int32_t scale_block;          /* rows that share a scale */
+  const int32_t *row_start;     /* optional [B + 1] */
+  const int32_t *kv_len;        /* [B], the new rows included */
+  const int32_t *block_table;   /* [B][max_pages] */
+  int64_t table_stride;
+  const void *k, *v;            /* [N][Hkv][D] */
+  int64_t kv_stride[2];         /* row, head */
+  void *k_cache, *v_cache;      /* [n_pages][Hkv][page_size][D] e4m3 */
+  int64_t cache_stride[3];      /* page, head, row */
+  float *k_scale, *v_scale;     /* [n_pages][Hkv][page_size / scale_block] */
+  int64_t scale_stride[3];      /* page, head, block */
+  uint32_t *status;             /* optional device word */
+} ds_kv8_write_params;
+
+/* `p` is a HOST pointer; the pointers inside it are device pointers. */
+DS_API int ds_kv8_write(const ds_kv8_write_params *p, void *stream);
+
+/* ds_kv8_read: rows first[b] .. of sequence b (first == NULL: from row 0 on) times their scales, rounded once to the element type.
+ * Packed (out_start given): out_start[b + 1] - out_start[b] rows of b go to rows out_start[b] .. of k_out and v_out
+ * ([N][Hkv][D]); a row at or beyond kv_len[b] is not written and raises DS_DEV_INDEX, as does a row range that is outside 0 .. N or
+ * runs backwards.  Dense (out_start == NULL): row first[b] + i goes to row i of sequence b of [B][N][Hkv][D], as far as there are
+ * rows and room; the other rows of the output are left as they are.  With head and row strides exchanged that is the prefix
+ * cache [B][Hkv][N][D] of ds_attn_pruned.  A length outside 0 .. max_pages * page_size, a first[b] < 0 and a page number outside
+ * [0, n_pages) raise DS_DEV_INDEX and the rows are not written.  Values beyond the element type's range are infinite.
+ * Layout, types and errors as in ds_kv8_write, and DS_ERR_UNSUPPORTED for B * N > 2^31 - 1 (dense); out_stride: sequence (dense only),
+ * row, head.  The output may not overlap anything that the call reads. */
+typedef struct {
+  int32_t B, Hkv, D;
+  int32_t dtype;                /* of k_out and v_out */
+  int32_t N;                    /* rows of the output (dense: of each sequence) */
+  int32_t page_size, max_pages, n_pages;
+  int32_t scale_block;
+  const int32_t *out_start;     /* optional [B + 1] */
+  const int32_t *first;         /* optional [B] */
+  const int32_t *kv_len;        /* [B] */
+  const int32_t *block_table;   /* [B][max_pages] */
+  int64_t table_stride;
+  const void *k_cache, *v_cache;
+  int64_t cache_stride[3];
+  const float *k_scale, *v_scale;
+  int64_t scale_stride[3];
+  void *k_out, *v_out;
+  int64_t out_stride[3];
+  uint32_t *status;             /* optional device word */
+} ds_kv8_read_params;
+
+/* `p` is a HOST pointer; the pointers inside it are device pointers. */
+DS_API int ds_kv8_read(const ds_kv8_read_params *p, void *stream);
+
+/* ds_attn_paged8: ds_attn_paged with k_t and v_t from an 8-bit cache,
+ *     out[r][h] = sum_t softmax_t(scale * ks_t <q[r][h], k_t>) vs_t v_t     (ks_t, vs_t: scales of row t's block)
+ * and lse likewise, with fp32 accumulation.  Everything that ds_attn_paged says of rows, lengths, visibility, bounds, flags,
+ * workspace and errors holds; `a` is its parameter struct, where dtype and strides of q and out are those of the
+ * queries (DS_BF16 or DS_F32), k_cache, v_cache and cache_stride those of the 8-bit cache.  K, V and the scales of a row reach only
+ * the queries that see it: NaN in it stays there (a scale that is infinite or NaN counts as such).  Envelope: D in {64, 128}.
+ * Queries smaller than 2^-85 lose bits, and so do outputs below 2^-117 times the bound of the lengths and values whose scale
+ * is below 2^-24 of the largest one met, or below 2^-124.
+ * In addition DS_ERR_INVALID_ARG: page_size not a multiple of scale_block, scale_block < 1, a NULL or misaligned scale pointer, a
+ * negative scale stride; DS_ERR_UNSUPPORTED: scale_block > 65536. */
+typedef struct {
+  ds_paged_params a;
+  int32_t scale_block;
+  const float *k_scale, *v_scale;
+  int64_t scale_stride[3];      /* page, head, block */
+} ds_paged8_params;
+
+/* HOST, pure: bytes of workspace ds_attn_paged8 needs for *p (0 when none). */
+DS_API size_t ds_attn_paged8_workspace(const ds_paged8_params *p);
+/* `p` is a HOST pointer; the pointers inside it are device pointers. */
+DS_API int ds_attn_paged8(const ds_paged8_params *p, void *stream);
 
 /* ------------------------------------------------------------------------
  * Utilities

@@ -25,6 +25,7 @@ __all__ = [
     "DS_ATTN_KERNEL_AUTO", "DS_ATTN_KERNEL_ONE_TILE", "DS_ATTN_KERNEL_TWO_TILE",
     "DS_DEV_PAGES", "RopeTable", "ds_page_update", "ds_qk_norm_rope", "ds_attn_paged", "ds_attn_paged_workspace",
     "PageUpdatePlan", "QkNormRopePlan", "PagedAttnPlan",
+    "ds_kv8_write", "ds_kv8_read", "ds_attn_paged8", "ds_attn_paged8_workspace", "Kv8WritePlan", "Kv8ReadPlan", "PagedAttn8Plan",
 ]
 
 DS_F32, DS_BF16 = 0, 1
@@ -142,11 +143,13 @@ def lib() -> ctypes.CDLL:
         L.ds_block_begin.argtypes = [ctypes.POINTER(_BlockParams), ctypes.c_void_p]
         L.ds_unmask_select.restype = ctypes.c_int
         L.ds_unmask_select.argtypes = [ctypes.POINTER(_SelectParams), ctypes.c_void_p]
-        for name, struct in paged.ENTRY_POINTS:
+        for name, struct in paged.ENTRY_POINTS + paged8.ENTRY_POINTS:
             getattr(L, name).restype = ctypes.c_int
             getattr(L, name).argtypes = [ctypes.POINTER(struct), ctypes.c_void_p]
         L.ds_attn_paged_workspace.restype = ctypes.c_size_t
         L.ds_attn_paged_workspace.argtypes = [ctypes.POINTER(paged.PagedParams)]
+        L.ds_attn_paged8_workspace.restype = ctypes.c_size_t
+        L.ds_attn_paged8_workspace.argtypes = [ctypes.POINTER(paged8.Paged8Params)]
         L.ds_rope_table_init.restype = ctypes.c_int
         L.ds_rope_table_init.argtypes = [ctypes.POINTER(paged.RopeTableStruct), ctypes.c_int32, ctypes.c_int32,
                                          ctypes.c_double, ctypes.c_int32] + [ctypes.c_double] * 4
@@ -571,6 +574,8 @@ def ds_read_status(status: torch.Tensor, stream=None) -> int:
     return int(host.value)
 
 
-from . import paged  # noqa: E402  (needs the helpers above)
+from . import paged, paged8  # noqa: E402  (they need the helpers above)
 from .paged import (PagedAttnPlan, PageUpdatePlan, QkNormRopePlan, RopeTable, ds_attn_paged,  # noqa: E402
                     ds_attn_paged_workspace, ds_page_update, ds_qk_norm_rope)
+from .paged8 import (Kv8ReadPlan, Kv8WritePlan, PagedAttn8Plan, ds_attn_paged8, ds_attn_paged8_workspace,  # noqa: E402
+                     ds_kv8_read, ds_kv8_write)

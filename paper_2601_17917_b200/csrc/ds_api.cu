@@ -69,6 +69,8 @@ int validate_attn(const ds_attn_params *p) {
   return DS_OK;
 }
 
+constexpr int kMaxScaleBlock = 65536;
+
 // Strides of the paged-cache entry points: non-negative multiples of 16 bytes.
 bool strides_ok(const int64_t *s, int n, int64_t unit) {
   for (int d = 0; d < n; ++d)
@@ -119,7 +121,8 @@ int validate_qk(const ds_qk_params *p) {
   return DS_OK;
 }
 
-int validate_paged(const ds_paged_params *p) {
+// `unit`: elements of the cache in 16 bytes.
+int validate_paged_but_envelope(const ds_paged_params *p, int64_t unit_cache) {
   if (!p) return DS_ERR_INVALID_ARG;
   if (p->dtype != DS_F32 && p->dtype != DS_BF16) return DS_ERR_INVALID_ARG;
   if (p->B < 0 || p->Hq <= 0 || p->Hkv <= 0 || p->D <= 0 || p->N < 0 || p->max_q < 1 || p->max_len < 0) return DS_ERR_INVALID_ARG;
@@ -135,16 +138,80 @@ int validate_paged(const ds_paged_params *p) {
   for (const void *w : words)
     if (!aligned(w, 4)) return DS_ERR_INVALID_ARG;
   const int64_t unit = p->dtype == DS_BF16 ? 8 : 4;
-  if (!strides_ok(p->q_stride, 2, unit) || !strides_ok(p->cache_stride, 3, unit) || !strides_ok(p->out_stride, 2, unit))
+  if (!strides_ok(p->q_stride, 2, unit) || !strides_ok(p->cache_stride, 3, unit_cache) || !strides_ok(p->out_stride, 2, unit))
     return DS_ERR_INVALID_ARG;
-  const bool d_ok = p->dtype == DS_BF16 ? (p->D == 64 || p->D == 128) : (p->D == 32 || p->D == 64 || p->D == 128 || p->D == 256);
+  return DS_OK;
+}
+
+// Sizes that the kernels count in 32 bits.
+bool paged_sizes_ok(const ds_paged_params *p) {
   const int64_t rows = (int64_t)p->max_q * (p->Hq / p->Hkv), cap = (int64_t)p->max_pages * p->page_size;
   const int64_t len = p->max_len > 0 && p->max_len < cap ? p->max_len : cap;
-  if (!d_ok || p->B > 8192 || cap > 0x7fffffffLL || len > kPagedMaxLen || (int64_t)p->n_pages * p->page_size > 0x7fffffffLL)
-    return DS_ERR_UNSUPPORTED;
+  return p->B <= 8192 && cap <= 0x7fffffffLL && len <= kPagedMaxLen && (int64_t)p->n_pages * p->page_size <= 0x7fffffffLL && rows <= 0x3fffffffLL;
+}
+
+int validate_paged(const ds_paged_params *p) {
+  const int rc = validate_paged_but_envelope(p, p && p->dtype == DS_BF16 ? 8 : 4);
+  if (rc != DS_OK) return rc;
+  const bool d_ok = p->dtype == DS_BF16 ? (p->D == 64 || p->D == 128) : (p->D == 32 || p->D == 64 || p->D == 128 || p->D == 256);
   // the kernels count a sequence's rows and its units of work in 32 bits
-  if (rows > 0x3fffffffLL || !attn_paged_counts_fit(*p)) return DS_ERR_UNSUPPORTED;
+  if (!d_ok || !paged_sizes_ok(p) || !attn_paged_counts_fit(*p)) return DS_ERR_UNSUPPORTED;
   return DS_OK;
+}
+
+// The scales of an 8-bit cache.
+int validate_scales(int32_t scale_block, int32_t page_size, const float *k_scale, const float *v_scale, const int64_t *stride) {
+  if (scale_block < 1 || page_size % scale_block != 0) return DS_ERR_INVALID_ARG;
+  if (!aligned(k_scale, 4) || !aligned(v_scale, 4) || !strides_ok(stride, 3, 1)) return DS_ERR_INVALID_ARG;
+  return DS_OK;
+}
+
+int validate_paged8(const ds_paged8_params *p) {
+  const int rc = validate_paged_but_envelope(p ? &p->a : nullptr, 16);
+  if (rc != DS_OK) return rc;
+  if (p->a.B > 0 && p->a.N > 0 && (!p->k_scale || !p->v_scale)) return DS_ERR_INVALID_ARG;
+  const int rs = validate_scales(p->scale_block, p->a.page_size, p->k_scale, p->v_scale, p->scale_stride);
+  if (rs != DS_OK) return rs;
+  if ((p->a.D != 64 && p->a.D != 128) || p->scale_block > kMaxScaleBlock || !paged_sizes_ok(&p->a) || !attn_paged8_counts_fit(*p))
+    return DS_ERR_UNSUPPORTED;
+  return DS_OK;
+}
+
+// What ds_kv8_write and ds_kv8_read have in common; `rows`, `rows_stride`: the packed K and V.
+template <class P>
+int validate_kv8(const P *p, const void *k, const void *v, const int64_t *rows_stride, int n_strides, const int32_t *starts) {
+  if (p->dtype != DS_F32 && p->dtype != DS_BF16) return DS_ERR_INVALID_ARG;
+  if (p->B < 0 || p->Hkv < 1 || p->D < 1 || p->N < 0 || p->page_size < 1 || p->max_pages < 1 || p->n_pages < 1) return DS_ERR_INVALID_ARG;
+  if (p->table_stride < p->max_pages) return DS_ERR_INVALID_ARG;
+  const int rs = validate_scales(p->scale_block, p->page_size, p->k_scale, p->v_scale, p->scale_stride);
+  if (rs != DS_OK) return rs;
+  if (p->B > 0 && p->N > 0 && (!p->kv_len || !p->block_table || !k || !v || !p->k_cache || !p->v_cache || !p->k_scale || !p->v_scale))
+    return DS_ERR_INVALID_ARG;
+  const void *ptrs[] = {k, v, p->k_cache, p->v_cache};
+  for (const void *q : ptrs)
+    if (!aligned(q, 16)) return DS_ERR_INVALID_ARG;
+  const void *words[] = {starts, p->kv_len, p->block_table, p->status};
+  for (const void *w : words)
+    if (!aligned(w, 4)) return DS_ERR_INVALID_ARG;
+  if (!strides_ok(rows_stride, n_strides, p->dtype == DS_BF16 ? 8 : 4) || !strides_ok(p->cache_stride, 3, 16)) return DS_ERR_INVALID_ARG;
+  if (p->D % 16 != 0 || p->D > 256 || p->B > 8192 || p->Hkv > 32767 || p->scale_block > kMaxScaleBlock ||
+      (int64_t)p->max_pages * p->page_size > 0x7fffffffLL || (int64_t)p->n_pages * p->page_size > 0x7fffffffLL)
+    return DS_ERR_UNSUPPORTED;
+  return DS_OK;
+}
+
+int validate_kv8_write(const ds_kv8_write_params *p) {
+  if (!p || p->max_q < 1 || p->max_len < 0) return DS_ERR_INVALID_ARG;
+  if (!p->row_start && (int64_t)p->B * p->max_q > p->N) return DS_ERR_INVALID_ARG;
+  return validate_kv8(p, p->k, p->v, p->kv_stride, 2, p->row_start);
+}
+
+int validate_kv8_read(const ds_kv8_read_params *p) {
+  if (!p || !aligned(p->first, 4)) return DS_ERR_INVALID_ARG;
+  const int64_t *strides = p->out_start ? p->out_stride + 1 : p->out_stride;
+  const int rc = validate_kv8(p, p->k_out, p->v_out, strides, p->out_start ? 2 : 3, p->out_start);
+  if (rc != DS_OK) return rc;
+  return p->out_start || (int64_t)p->B * p->N <= 0x7fffffffLL ? DS_OK : DS_ERR_UNSUPPORTED;
 }
 
 }  // namespace
@@ -420,6 +487,31 @@ int ds_attn_paged(const ds_paged_params *p, void *stream) {
   if (rc != DS_OK) return rc;
   if (p->B == 0 || p->N == 0) return DS_OK;
   return ds::launch_attn_paged(*p, reinterpret_cast<cudaStream_t>(stream));
+}
+
+int ds_kv8_write(const ds_kv8_write_params *p, void *stream) {
+  const int rc = ds::validate_kv8_write(p);
+  if (rc != DS_OK) return rc;
+  if (p->B == 0 || p->N == 0) return DS_OK;
+  return ds::launch_kv8_write(*p, reinterpret_cast<cudaStream_t>(stream));
+}
+
+int ds_kv8_read(const ds_kv8_read_params *p, void *stream) {
+  const int rc = ds::validate_kv8_read(p);
+  if (rc != DS_OK) return rc;
+  if (p->B == 0 || p->N == 0) return DS_OK;
+  return ds::launch_kv8_read(*p, reinterpret_cast<cudaStream_t>(stream));
+}
+
+size_t ds_attn_paged8_workspace(const ds_paged8_params *p) {
+  return ds::validate_paged8(p) == DS_OK ? ds::attn_paged8_workspace_bytes(*p) : 0;
+}
+
+int ds_attn_paged8(const ds_paged8_params *p, void *stream) {
+  const int rc = ds::validate_paged8(p);
+  if (rc != DS_OK) return rc;
+  if (p->a.B == 0 || p->a.N == 0) return DS_OK;
+  return ds::launch_attn_paged8(*p, reinterpret_cast<cudaStream_t>(stream));
 }
 
 int ds_selftest_bounded_wait(uint32_t poll_limit, uint32_t *status, int32_t *report, void *stream) {

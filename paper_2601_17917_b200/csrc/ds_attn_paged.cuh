@@ -1,4 +1,4 @@
-// What the kernels of ds_attn_paged share: a call's parameters, the walk of a CTA over its range of the units of work, the
+// What the kernels of ds_attn_paged and ds_attn_paged8 share: a call's parameters, the walk of a CTA over its range of the units of work, the
 // output of a row, and the join of items that several ranges share.
 #pragma once
 #include "ds_common.cuh"
@@ -28,6 +28,9 @@ struct Params {
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void *src, bool there) {
   // a chunk that is not there is filled with zeros and not read
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void *src, bool there) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4 : 0) : "memory");
 }
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>

@@ -1,0 +1,416 @@
+// ds_attn_paged8: ds_attn_paged over a cache of e4m3 values with a scale for every block of rows and KV head.
+//
+// The stream is half as long as bf16's, so a key has half the time.  As with bf16 the keys are the 16-wide side of the products
+// (mma.sync m16n8k16), S^T = K Q^T and O^T = V^T P^T, blocks of 8 rows the other; K and V become fp16 in registers, two values an
+// instruction, which holds every e4m3 value.
+//
+// K: a lane's four bytes of an ldmatrix are four neighbouring dimensions of a key, two and two of which stand where the
+// product has dimensions 2q, 2q + 1 and 2q + 8, 2q + 9: the queries are laid out in the same order.  V: transposed, a lane's four
+// bytes are two neighbouring dimensions of two neighbouring keys; a byte permutation makes them two fragments, of even and of odd
+// dimensions, and the output is put back in order where it is written.
+//
+// Queries enter as fp16 too: a row is scaled by a power of two that puts its largest element into [2^14, 2^15), and 11 bits hold bf16's 8
+// down to 2^-31 of that.  fp32 queries are two such parts (22 bits).  The scale of K and the row's factor multiply the score, the scale of V
+// the weight, relative to the largest that the warp has met (vref, a power of two).  The weights are fp16, up to 2^14 where the
+// largest is 2^10 .. 2^14 (the exponents' reference lags), which keeps 11 bits down to 2^-24 of the largest and 2^-35 of it at all: a weight's
+// rounding, 2^-11, is an eighth of the output's in bf16.  For fp32 outputs the weights are two such parts.
+#include <type_traits>
+
+#include "ds_attn_paged_rows.cuh"
+#include "ds_e4m3.cuh"
+
+namespace ds {
+namespace {
+
+using namespace paged;
+
+struct Args8 : Params {
+  const float *k_scale, *v_scale;
+  long long scale_stride[3];
+  FastDiv scale_div;      // by rows of a block
+};
+
+__device__ __forceinline__ void mma_half(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+constexpr float kWeight = 1024.f;      // of the reference in fp16
+constexpr float kLag = 4.f;            // weights may pass that by 2^4
+
+template <typename T_, int D_, int NB>
+struct ByteRows {
+  using T = T_;
+  using Cache = uint8_t;
+  using Args = Args8;
+  static constexpr bool kScaled = true;
+  static constexpr int D = D_, kRows = 8 * NB, kRowBytes = D, kKeys = 32;
+  static constexpr int kParts = std::is_same<T, float>::value ? 2 : 1;      // of a query, of a weight
+  static constexpr int kBlocks = kParts * NB;                                // of 8 rows of queries
+  static constexpr bool kQRegs = kBlocks <= 2;
+  static constexpr int kQRowBytes = 2 * D;
+  static constexpr int kOffFactor = kBlocks * 8 * kQRowBytes;
+  static constexpr int kQBytes = kOffFactor + kRows * 4;
+  static constexpr int kGroups = NB * kParts <= 2 ? 2 : 1;      // 16s of keys at a time
+  static constexpr int kCtas = NB == 1 ? (D == 64 ? 4 : 3) : 2, kStages = 2;
+  float o[NB][D / 16][4];      // dimensions 16 j + 2 (lane / 4) (+ 1), rows 2q, 2q + 1
+  float m[NB][2], l[NB][2], factor[NB][2];
+  int end[NB][2];
+  uint32_t qf[kQRegs ? kBlocks : 1][kQRegs ? D / 16 : 1][2];
+  uint32_t q_smem;
+  float vref, vinv;
+
+  __device__ void begin(const Args8 &a, const Item &it, uint8_t *q_buf) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    q_smem = sm100::smem_u32(q_buf);
+    float *factor_s = reinterpret_cast<float *>(q_buf + kOffFactor);
+    constexpr int kLanes = D / 4, kPer = 32 / kLanes;      // lanes of a row, four elements each; rows of a warp at a time
+    const int u = lane % kLanes;
+#pragma unroll 1
+    for (int r0 = warp * kPer; r0 < kRows; r0 += kWarps * kPer) {
+      const int r = r0 + lane / kLanes;
+      float x[4] = {0.f, 0.f, 0.f, 0.f};
+      if (r < it.rows) {
+        const Row row = row_of(a, it, r);
+        const T *src = reinterpret_cast<const T *>(a.p.q) + row.n * a.p.q_stride[0] + row.h * a.p.q_stride[1] + 4 * u;
+        if constexpr (kParts == 2) {
+          const float4 w = *reinterpret_cast<const float4 *>(src);
+          x[0] = w.x, x[1] = w.y, x[2] = w.z, x[3] = w.w;
+        } else {
+          const uint2 w = *reinterpret_cast<const uint2 *>(src);
+          x[0] = bf16lo_to_f32(w.x), x[1] = bf16hi_to_f32(w.x), x[2] = bf16lo_to_f32(w.y), x[3] = bf16hi_to_f32(w.y);
+        }
+      }
+      uint32_t top = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t b = __float_as_uint(x[e]) & 0x7fffffffu;
+        top = max(top, b < 0x7f800000u ? b : 0u);
+      }
+#pragma unroll
+      for (int off = 1; off < kLanes; off <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, off));
+      const int shift = min(100, 14 + 127 - (int)(top >> 23));
+      const float up = __uint_as_float((uint32_t)(127 + shift) << 23);
+      if (u == 0) factor_s[r] = __uint_as_float((uint32_t)(127 - shift) << 23) * (a.p.scale * kLog2e);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] *= up;
+#pragma unroll
+      for (int part = 0; part < kParts; ++part) {
+        // dimensions 4q, 4q + 1 of 16 stand at 2q, 2q + 1, dimensions 4q + 2, 4q + 3 at 2q + 8, 2q + 9
+        const uint32_t first = pack_half(x[0], x[1]), second = pack_half(x[2], x[3]);
+        uint8_t *to = q_buf + (u & 3) * 4;
+        *reinterpret_cast<uint32_t *>(to + chunk_at<kQRowBytes>(part * kRows + r, 2 * (u >> 2))) = first;
+        *reinterpret_cast<uint32_t *>(to + chunk_at<kQRowBytes>(part * kRows + r, 2 * (u >> 2) + 1)) = second;
+        if constexpr (kParts == 2) {      // what is left; of an infinity, nothing
+          const float2 f = halves_f32(first), s = halves_f32(second);
+          const float y[4] = {f.x, f.y, s.x, s.y};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = isfinite(y[e]) ? x[e] - y[e] : 0.f;
+        }
+      }
+    }
+    __syncthreads();
+    if constexpr (kQRegs) {
+#pragma unroll
+      for (int t = 0; t < kBlocks; ++t)
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            qf[t][k][h] = *reinterpret_cast<const uint32_t *>(q_buf + chunk_at<kQRowBytes>(8 * t + (lane >> 2), 2 * k + h) + (lane & 3) * 4);
+    }
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[nb][j][e] = 0.f;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int r = 8 * nb + 2 * (lane & 3) + e;
+        m[nb][e] = -INFINITY, l[nb][e] = 0.f, factor[nb][e] = factor_s[r];
+        end[nb][e] = r < it.rows ? row_of(a, it, r).end : 0;
+      }
+    }
+    set_vref(27);      // 2^-100
+  }
+
+  // vref = 2^(e - 127), vinv = 2^10 / vref
+  __device__ __forceinline__ void set_vref(uint32_t e) {
+    vref = __uint_as_float(e << 23);
+    vinv = __uint_as_float((264u - e) << 23);
+  }
+
+  // Makes vref the power of two at or above the largest finite scale of V of the stage.
+  __device__ __forceinline__ void raise(float mine) {
+    const uint32_t b = __float_as_uint(mine) & 0x7fffffffu;
+    const bool more = b < 0x7f800000u && b > __float_as_uint(vref);
+    if (!__any_sync(0xffffffffu, more)) return;
+    const uint32_t top = __reduce_max_sync(0xffffffffu, more ? b : 0u);
+    const uint32_t e = min((top + 0x7fffffu) >> 23, 254u);
+    const int fall = 127 + (int)(__float_as_uint(vref) >> 23) - (int)e;
+    const float keep = __uint_as_float(fall > 0 ? (uint32_t)fall << 23 : 0u);
+    set_vref(e);
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[nb][j][k] *= keep;
+  }
+
+  // 32 keys from x on; K, V and their scales (behind V: 32 of K, 32 of V) as loaded, V is scratch afterwards.
+  __device__ __forceinline__ void step(const Args8 &a, const Item &it, uint8_t *kbuf, uint8_t *vbuf, int x, float) {
+    const float *scales = reinterpret_cast<const float *>(vbuf + kKeys * kRowBytes);
+    raise(scales[32 + (threadIdx.x & 31)]);
+#pragma unroll
+    for (int g = 0; g < 2; g += kGroups) keys16(a, it, kbuf, vbuf, scales, x, g);
+  }
+
+  // Groups g .. g + kGroups - 1 of 16 keys.
+  __device__ __forceinline__ void keys16(const Args8 &a, const Item &it, const uint8_t *kbuf, uint8_t *vbuf, const float *scales, int x, int g0) {
+    const int lane = threadIdx.x & 31;
+    const uint32_t ks = sm100::smem_u32(kbuf), vs = sm100::smem_u32(vbuf);
+    float s[NB][kGroups][4];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[nb][g][e] = 0.f;
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) {
+      uint32_t qs[kQRegs ? 1 : 2][kQRegs ? 1 : kBlocks][2];
+      if constexpr (!kQRegs) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int t = 0; t < kBlocks; t += 2) {
+            uint32_t w[4];
+            ldmatrix4(q_smem + chunk_at<kQRowBytes>(8 * t + (lane & 7) + ((lane >> 4) << 3), 2 * (2 * c + k) + ((lane >> 3) & 1)), w);
+            qs[k][t][0] = w[0], qs[k][t][1] = w[1], qs[k][t + 1][0] = w[2], qs[k][t + 1][1] = w[3];
+          }
+      }
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) {
+        uint32_t w[4];      // keys 0-7 and 8-15 of dimensions 32 c .. + 15, the same of + 16 .. + 31
+        ldmatrix4(ks + chunk_at<kRowBytes>(16 * (g0 + g) + (lane & 15), 2 * c + (lane >> 4)), w);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const uint32_t a0 = halves_lo(w[2 * k]), a1 = halves_lo(w[2 * k + 1]), a2 = halves_hi(w[2 * k]), a3 = halves_hi(w[2 * k + 1]);
+#pragma unroll
+          for (int t = 0; t < kBlocks; ++t) {
+            const uint32_t b0 = kQRegs ? qf[kQRegs ? t : 0][kQRegs ? 2 * c + k : 0][0] : qs[kQRegs ? 0 : k][kQRegs ? 0 : t][0];
+            const uint32_t b1 = kQRegs ? qf[kQRegs ? t : 0][kQRegs ? 2 * c + k : 0][1] : qs[kQRegs ? 0 : k][kQRegs ? 0 : t][1];
+            mma_half(s[t % NB][g], a0, a1, a2, a3, b0, b1);
+          }
+        }
+      }
+    }
+    float vscale[kGroups][2];
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int key = 16 * (g0 + g) + 8 * h + (lane >> 2);
+        const float kscale = scales[key];
+        vscale[g][h] = scales[32 + key] * vinv;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) s[nb][g][2 * h + e] = __fmul_rn(s[nb][g][2 * h + e], factor[nb][e] * kscale);
+      }
+    const bool partial = !paged_all_visible(a.s, it.q, x + 16 * g0, 16 * kGroups);
+    uint32_t seen[NB] = {};      // only with partial: bit 4g + 2h + e: key 16g + 8h + lane / 4, row 2q + e
+    if (partial) {
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int pos = paged_key(it.q, x + 16 * (g0 + g) + 8 * h + (lane >> 2));
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              if (paged_visible(a.s, pos, end[nb][e])) seen[nb] |= 1u << (4 * g + 2 * h + e);
+              else s[nb][g][2 * h + e] = -INFINITY;
+            }
+        }
+    }
+    // The reference of the exponents moves only when a weight would pass 2^14 (the result is the same): no maximum is
+    // exchanged until some lane finds such a score.
+    bool over = false;
+    float top[NB][2];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        top[nb][e] = fmaxf(s[nb][0][e], s[nb][0][2 + e]);
+#pragma unroll
+        for (int g = 1; g < kGroups; ++g) top[nb][e] = fmaxf(top[nb][e], fmaxf(s[nb][g][e], s[nb][g][2 + e]));
+        over |= top[nb][e] > m[nb][e] + kLag;
+      }
+    if (__any_sync(0xffffffffu, over)) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float t = fmaxf(m[nb][e], top[nb][e]);
+#pragma unroll
+          for (int off = 4; off < 32; off <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, off));
+          const float keep = m[nb][e] == t ? 1.f : ex2_approx(m[nb][e] - t);
+          m[nb][e] = t;
+          l[nb][e] *= keep;
+#pragma unroll
+          for (int j = 0; j < D / 16; ++j) o[nb][j][e] *= keep, o[nb][j][2 + e] *= keep;
+        }
+    }
+    uint32_t w[NB][kGroups][kParts][2];      // keys 0-7, 8-15: the weights (their parts), rows 2q and 2q + 1
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      // nothing seen yet: weights exp(-inf) = 0
+      const float ref0 = m[nb][0] == -INFINITY ? 0.f : m[nb][0], ref1 = m[nb][1] == -INFINITY ? 0.f : m[nb][1];
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float p0 = ex2_approx(s[nb][g][2 * h] - ref0), p1 = ex2_approx(s[nb][g][2 * h + 1] - ref1);
+          l[nb][0] += p0;
+          l[nb][1] += p1;
+          float w0 = p0 * vscale[g][h], w1 = p1 * vscale[g][h];
+          if (partial) {      // zero times a scale that is not finite
+            if (!((seen[nb] >> (4 * g + 2 * h)) & 1)) w0 = 0.f;
+            if (!((seen[nb] >> (4 * g + 2 * h + 1)) & 1)) w1 = 0.f;
+          }
+          w[nb][g][0][h] = pack_half(w0, w1);
+          if constexpr (kParts == 2) {
+            const float2 f = halves_f32(w[nb][g][0][h]);
+            w[nb][g][1][h] = pack_half(isfinite(f.x) ? w0 - f.x : 0.f, isfinite(f.y) ? w1 - f.y : 0.f);
+          }
+        }
+    }
+    if (partial) keep_hidden_values_out(vbuf, g0, seen);
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+        for (int part = 0; part < kParts; ++part)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) w[nb][g][part][h] = transpose8(w[nb][g][part][h]);
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) {
+        uint32_t v[4];      // dimensions 32 c .. + 15 of keys 0-7 and 8-15, the same of + 16 .. + 31
+        ldmatrix4_trans(vs + chunk_at<kRowBytes>(16 * (g0 + g) + (lane & 15), 2 * c + (lane >> 4)), v);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = __byte_perm(v[k], 0, 0x3120);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const uint32_t a0 = halves_lo(v[2 * k]), a1 = halves_hi(v[2 * k]), a2 = halves_lo(v[2 * k + 1]), a3 = halves_hi(v[2 * k + 1]);
+#pragma unroll
+          for (int part = 0; part < kParts; ++part)
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) mma_half(o[nb][2 * c + k], a0, a1, a2, a3, w[nb][g][part][0], w[nb][g][part][1]);
+        }
+      }
+  }
+
+  // Keys that some rows see and others do not (or that are padding): a weight of zero times NaN would be NaN in the product.  If V
+  // holds NaN there (rare), the rows that see it get it here, and it is replaced by zero.
+  __device__ __forceinline__ void keep_hidden_values_out(uint8_t *vbuf, int g0, const uint32_t (&seen)[NB]) {
+    const int lane = threadIdx.x & 31;
+    constexpr int kWords = 16 * kGroups * kRowBytes / 4;
+    uint32_t *words = reinterpret_cast<uint32_t *>(vbuf + 16 * g0 * kRowBytes);
+    bool bad = false;
+    for (int i = lane; i < kWords; i += 32) bad |= any_nan_e4m3(words[i]);
+    if (!__any_sync(0xffffffffu, bad)) return;
+#pragma unroll 1
+    for (int key = 0; key < 16 * kGroups; ++key) {
+      const int src = (key & 7) * 4 + (lane & 3), at = 4 * (key >> 4) + 2 * ((key >> 3) & 1);
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        const uint32_t vis = __shfl_sync(0xffffffffu, seen[nb], src) >> at;
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+          for (int odd = 0; odd < 2; ++odd) {
+            const uint8_t b = vbuf[chunk_at<kRowBytes>(16 * g0 + key, j) + 2 * (lane >> 2) + odd];
+            if ((b & 0x7f) != 0x7f) continue;
+            if (vis & 1) o[nb][j][2 * odd] = __uint_as_float(0x7fffffffu);
+            if (vis & 2) o[nb][j][2 * odd + 1] = __uint_as_float(0x7fffffffu);
+          }
+      }
+    }
+    __syncwarp();
+    for (int i = lane; i < kWords; i += 32) words[i] &= ~__vcmpeq4(words[i] & 0x7f7f7f7fu, 0x7f7f7f7fu);
+    __syncwarp();
+  }
+
+  // The warp's sums to shared memory: out[kRows][D], ml[kRows].
+  __device__ void finish(const Args8 &a, const Item &it, float *out, float2 *ml) {
+    const int lane = threadIdx.x & 31;
+    const float down = a.shrink / kWeight;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int r = 8 * nb + 2 * (lane & 3) + e;
+        float sum = l[nb][e];
+#pragma unroll
+        for (int off = 4; off < 32; off <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+        if (r >= it.rows) continue;
+        if (lane < 4) ml[r] = make_float2(m[nb][e], sum);
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j)
+          *reinterpret_cast<float2 *>(out + r * D + 16 * j + 2 * (lane >> 2)) = make_float2(o[nb][j][e] * down * vref, o[nb][j][2 + e] * down * vref);
+      }
+  }
+};
+
+// Calls f with the row engine for the call's type, head dimension and rows per KV head; more rows are several items.
+template <class F>
+auto with_rows(const ds_paged_params &p, F f) {
+  const long long rows = (long long)p.max_q * (p.Hq / p.Hkv);
+  if (p.dtype == DS_BF16) {
+    using T = __nv_bfloat16;
+    if (p.D == 64) return rows <= 8 ? f(ByteRows<T, 64, 1>()) : rows <= 16 ? f(ByteRows<T, 64, 2>()) : f(ByteRows<T, 64, 4>());
+    return rows <= 8 ? f(ByteRows<T, 128, 1>()) : rows <= 16 ? f(ByteRows<T, 128, 2>()) : f(ByteRows<T, 128, 4>());
+  }
+  if (p.D == 64) return rows <= 8 ? f(ByteRows<float, 64, 1>()) : f(ByteRows<float, 64, 2>());
+  return rows <= 8 ? f(ByteRows<float, 128, 1>()) : f(ByteRows<float, 128, 2>());
+}
+
+}  // namespace
+
+bool attn_paged8_counts_fit(const ds_paged8_params &p) {
+  return with_rows(p.a, [&](auto engine) {
+    using Rows = decltype(engine);
+    const PagedShape s = units_of(p.a, Layout<Rows>::kTile, Rows::kRows);
+    return paged_units_fit(s, longest_of(s));
+  });
+}
+
+size_t attn_paged8_workspace_bytes(const ds_paged8_params &p) {
+  if (p.a.B == 0 || p.a.N == 0) return 0;
+  return with_rows(p.a, [&](auto rows) { return rows_workspace_of(shape_for<decltype(rows)>(p.a)); });
+}
+
+int launch_attn_paged8(const ds_paged8_params &p, cudaStream_t stream) {
+  return with_rows(p.a, [&](auto rows) {
+    return launch_rows<decltype(rows)>(p.a, stream, [&](Args8 &a) {
+      a.k_scale = p.k_scale, a.v_scale = p.v_scale;
+      for (int d = 0; d < 3; ++d) a.scale_stride[d] = p.scale_stride[d];
+      a.scale_div = make_fast_div(p.scale_block);
+    });
+  });
+}
+
+}  // namespace ds

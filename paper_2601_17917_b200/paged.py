@@ -328,7 +328,7 @@ def ds_qk_norm_rope(q, k, v, positions, rope, q_weight=None, k_weight=None, eps=
 
 
 def _paged_params(q, k_cache, v_cache, block_table, kv_len, scale, row_start, max_q, max_len, causal, window, sinks,
-                  out, lse, status):
+                  out, lse, status, cache_dtype=None):
     if q.dim() != 3:
         raise ValueError("q must be [N, Hq, D]")
     N, Hq, D = q.shape
@@ -345,7 +345,7 @@ def _paged_params(q, k_cache, v_cache, block_table, kv_len, scale, row_start, ma
     if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or tuple(lse.shape) != (N, Hq)):
         raise ValueError("lse must be contiguous f32 [N, Hq]")
     p = PagedParams()
-    p.n_pages, p.page_size = _cache(k_cache, v_cache, Hkv, D, q.dtype)
+    p.n_pages, p.page_size = _cache(k_cache, v_cache, Hkv, D, q.dtype if cache_dtype is None else cache_dtype)
     p.B, p.Hq, p.Hkv, p.D, p.dtype, p.N = B, Hq, Hkv, D, _dtype_code(q), N
     p.max_q, p.max_len, p.max_pages = int(max_q), int(max_len), block_table.shape[1]
     p.causal, p.window, p.sinks, p.scale = int(bool(causal)), int(window), int(sinks), float(scale)
