@@ -20,21 +20,34 @@ namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 
-// How many of the n values do not exceed r, by the whole warp: 32 probes at a time.  The values ascend; if they do not, some
+// How many of the n values do not exceed r, by the whole warp: 128 probes at a time.  The values ascend; if they do not, some
 // number between 0 and n.
 __device__ __forceinline__ int count_up_to(const int32_t *values, int n, int r) {
   const int lane = threadIdx.x & 31;
   int lo = 0, hi = n;
   while (lo < hi) {
-    const int step = (hi - lo + 31) / 32, at = lo + (lane + 1) * step - 1;
-    const uint32_t past = ~__ballot_sync(0xffffffffu, at < hi && values[at < hi ? at : hi - 1] <= r);
-    const int c = past ? __ffs(past) - 1 : 32;
+    const int step = (hi - lo + 127) / 128;
+    int c = 0;      // probes that do not exceed r, up to the first that does
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int at = lo + (32 * k + lane + 1) * step - 1;
+      const uint32_t past = ~__ballot_sync(0xffffffffu, at < hi && values[at < hi ? at : hi - 1] <= r);
+      if (c == 32 * k) c += past ? __ffs(past) - 1 : 32;
+    }
     const int stop = lo + (c + 1) * step - 1;
     lo = min(hi, lo + c * step);
-    if (c < 32 && stop < hi) hi = stop;
+    if (c < 128 && stop < hi) hi = stop;
   }
   return lo;
 }
+
+// Copies of 16 bytes to shared memory in the background; a thread reads back what it copied.
+__device__ __forceinline__ void copy16(uint4 *to, const void *from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 template <typename T>
 struct Chunk;      // 16 bytes of K or V
@@ -81,128 +94,280 @@ __device__ __forceinline__ NewRows new_rows(const ds_kv8_write_params &p, int bo
   return {lo, (int)n, len, lo >= 0 && n >= 0 && hi <= p.N && n <= p.max_q && len <= bound && n <= len};
 }
 
-// One run in one head of K or V by L lanes (u: the lane's number): `count` rows from `src` on, into rows from `code` on; `held` rows
-// before them in the block, at `before`.  Every lane of the warp comes here; those without an item have count 0.
-template <typename T, int L>
-__device__ __forceinline__ void write_run(const T *src, long long src_row, int count, uint8_t *code, long long code_row, uint8_t *before,
-                                          int held, float *scale, int D, const FastDiv &chunk_div, int u) {
-  using C = Chunk<T>;
-  constexpr int E = C::kElems, kKeep = 8;      // chunks of a lane that stay in registers
-  const int chunks = (int)chunk_div.d, total = count * chunks;
-  uint4 keep[kKeep];
-  uint32_t top = 0;
-  auto load = [&](int c) {
-    const int row = fast_div(c, chunk_div);
-    return *reinterpret_cast<const uint4 *>(src + row * src_row + (c - row * chunks) * E);
-  };
-  auto peak = [&](const uint4 &w) {
-    float f[E];
-    C::wide(w, f);
+// The scale of a run whose largest magnitude has the bits `top`, with `held` rows under the scale s0 before it in the block.
+struct Scale {
+  uint32_t bits;
+  float by;      // 1 / scale, exactly
+};
+__device__ __forceinline__ Scale scale_of(uint32_t top, int held, float s0) {
+  int e = (int)((min(top, kMostBits) + 0x1fffffu) >> 23) - 8;      // biased exponents
+  const uint32_t b0 = __float_as_uint(s0) & 0x7fffffffu;
+  if (held > 0 && b0 <= 0x7f000000u) e = max(e, (int)((b0 + 0x7fffffu) >> 23));
+  e = max(e, 1);
+  return {(uint32_t)e << 23, __uint_as_float(e == 254 ? 0x00400000u : (uint32_t)(254 - e) << 23)};
+}
+// The largest magnitude, of finite values if `finite`, else of all but NaN.
+template <typename T>
+__device__ __forceinline__ uint32_t peak_of(const uint4 &w, uint32_t top, bool finite) {
+  if (finite) {
+    float f[Chunk<T>::kElems];
+    Chunk<T>::wide(w, f);
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
+    for (int e = 0; e < Chunk<T>::kElems; ++e) {
       const uint32_t b = __float_as_uint(f[e]) & 0x7fffffffu;
       top = max(top, b < kInfBits ? b : 0u);
     }
-  };
-  const float s0 = held > 0 ? *scale : 0.f;
+    return top;
+  }
+  const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+  if constexpr (std::is_same<T, float>::value) {
+    float t = __uint_as_float(top);
 #pragma unroll
-  for (int i = 0; i < kKeep; ++i)
-    if (u + i * L < total) keep[i] = load(u + i * L);
+    for (int k = 0; k < 4; ++k) t = fmaxf(t, fabsf(__uint_as_float(x[k])));      // NaN is not the larger
+    return __float_as_uint(t);
+  } else {
+    // pairs: the larger of two bf16, NaN is not
+    auto larger = [](uint32_t a, uint32_t b) {
+      uint32_t r;
+      asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+      return r;
+    };
+    constexpr uint32_t kAbs = 0x7fff7fffu;
+    const uint32_t t = larger(larger(x[0] & kAbs, x[1] & kAbs), larger(x[2] & kAbs, x[3] & kAbs));
+    return __float_as_uint(fmaxf(__uint_as_float(top), fmaxf(bf16lo_to_f32(t), bf16hi_to_f32(t))));
+  }
+}
+// `plain`: nothing is infinite or beyond the largest value held.  NaN comes out as NaN of itself.
+template <typename T>
+__device__ __forceinline__ void store_codes(uint8_t *to, const uint4 &w, float by, bool plain) {
+  constexpr int E = Chunk<T>::kElems;
+  float f[E];
+  Chunk<T>::wide(w, f);
+  if (plain) {
 #pragma unroll
-  for (int i = 0; i < kKeep; ++i)
-    if (u + i * L < total) peak(keep[i]);
-#pragma unroll 4
-  for (int c = u + kKeep * L; c < total; c += L) peak(load(c));
-#pragma unroll
-  for (int off = 1; off < L; off <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, off));
-  // biased exponents
-  int e = (int)((min(top, kMostBits) + 0x1fffffu) >> 23) - 8;
-  const uint32_t b0 = __float_as_uint(s0) & 0x7fffffffu;
-  if (b0 <= 0x7f000000u) e = max(e, (int)((b0 + 0x7fffffu) >> 23));
-  e = max(e, 1);
-  const uint32_t to_bits = (uint32_t)e << 23;
-  const float by = __uint_as_float(e == 254 ? 0x00400000u : (uint32_t)(254 - e) << 23);      // 2^-e, exactly
-  auto store = [&](int c, const uint4 &w) {
-    float f[E];
-    C::wide(w, f);
+    for (int k = 0; k < E; ++k) f[k] *= by;
+  } else {
 #pragma unroll
     for (int k = 0; k < E; ++k) f[k] = scaled(f[k], by);
-    const int row = fast_div(c, chunk_div);
-    uint8_t *to = code + row * code_row + (c - row * chunks) * E;
-    if constexpr (E == 8) *reinterpret_cast<uint2 *>(to) = make_uint2(pack_e4m3x4(f[0], f[1], f[2], f[3]), pack_e4m3x4(f[4], f[5], f[6], f[7]));
-    else *reinterpret_cast<uint32_t *>(to) = pack_e4m3x4(f[0], f[1], f[2], f[3]);
-  };
-#pragma unroll
-  for (int i = 0; i < kKeep; ++i)
-    if (u + i * L < total) store(u + i * L, keep[i]);
-#pragma unroll 4
-  for (int c = u + kKeep * L; c < total; c += L) store(c, load(c));
-  if (count == 0) return;
-  if (held > 0 && __float_as_uint(s0) != to_bits) {
-    const float f = s0 * by;
-    for (int c = u; c < held * (D / 16); c += L) {
-      uint4 *at = reinterpret_cast<uint4 *>(before + c / (D / 16) * code_row + c % (D / 16) * 16);
-      const uint4 w = *at;
-      uint32_t x[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float2 lo = halves_f32(halves_lo(x[k])), hi = halves_f32(halves_hi(x[k]));
-        x[k] = pack_e4m3x4(scaled(lo.x * f, 1.f), scaled(lo.y * f, 1.f), scaled(hi.x * f, 1.f), scaled(hi.y * f, 1.f));
-      }
-      *at = make_uint4(x[0], x[1], x[2], x[3]);
-    }
   }
-  if (u == 0 && !(held > 0 && __float_as_uint(s0) == to_bits)) *scale = __uint_as_float(to_bits);
+  if constexpr (E == 8) *reinterpret_cast<uint2 *>(to) = make_uint2(pack_e4m3x4(f[0], f[1], f[2], f[3]), pack_e4m3x4(f[4], f[5], f[6], f[7]));
+  else *reinterpret_cast<uint32_t *>(to) = pack_e4m3x4(f[0], f[1], f[2], f[3]);
+}
+// Rows under the scale s0 that come under another: lane u of n.
+__device__ __forceinline__ void rescale(uint8_t *rows, long long row_bytes, int held, int D, float f, int u, int n) {
+  for (int c = u; c < held * (D / 16); c += n) {
+    uint4 *at = reinterpret_cast<uint4 *>(rows + c / (D / 16) * row_bytes + c % (D / 16) * 16);
+    const uint4 w = *at;
+    uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float2 lo = halves_f32(halves_lo(x[k])), hi = halves_f32(halves_hi(x[k]));
+      x[k] = pack_e4m3x4(scaled(lo.x * f, 1.f), scaled(lo.y * f, 1.f), scaled(hi.x * f, 1.f), scaled(hi.y * f, 1.f));
+    }
+    *at = make_uint4(x[0], x[1], x[2], x[3]);
+  }
 }
 
+constexpr int kKeep = 8;      // chunks of a lane, at most
+
+// One run in one head of K or V by L lanes (u: the lane's number), at most kKeep L chunks: `count` rows from `src` on, into rows from
+// `code` on; `held` rows before them in the block, at `before`.  Every lane of the warp comes here; those without an item have count 0.
 template <typename T, int L>
-__global__ void __launch_bounds__(kThreads) kv8_write_kernel(const __grid_constant__ ds_kv8_write_params p,
-                                                             const __grid_constant__ WriteLaunch launch) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, u = lane % L;
-  constexpr int kGroups = 32 / L;
-  uint32_t flags = 0;
-  dependent_sync();
-  if (blockIdx.x == 0 && blockIdx.y == 0)
-    for (int b = threadIdx.x; b < p.B; b += kThreads)
-      if (!new_rows(p, launch.bound, b).ok) flags |= DS_DEV_INDEX;
-  int r = blockIdx.x * launch.rows;
-  const int r_end = r + min(launch.rows, p.N - r);
-  const int item_end = min(launch.items, (int)(blockIdx.y + 1) * launch.per_cta);
-  while (r < r_end) {
-    const int b = p.row_start ? count_up_to(p.row_start + 1, p.B, r) : r / p.max_q;
-    if (b >= p.B) break;
-    const NewRows q = new_rows(p, launch.bound, b);
-    if (r < q.lo) {
-      r = q.lo;
-      continue;
-    }
-    const int hi = (int)min((long long)p.N, (long long)q.lo + max(q.n, 0));
-    if (!q.ok || r >= hi) {
-      r = max(r + 1, hi);
-      continue;
-    }
-    const int pos = q.len - q.n + (r - q.lo), block = fast_div(pos, launch.block_div), in_block = pos - block * p.scale_block;
-    const int next = (int)min((long long)hi, (long long)r + p.scale_block - in_block);
-    if (r == q.lo || in_block == 0) {
+__device__ __forceinline__ void write_run(uint4 *buf, const T *src, long long src_row, int count, uint8_t *code, long long code_row,
+                                          uint8_t *before, int held, float *scale, int D, const FastDiv &chunk_div, int u) {
+  constexpr int E = Chunk<T>::kElems;
+  const int chunks = (int)chunk_div.d, total = count * chunks, lane = threadIdx.x & 31;
+  for (int i = 0, c = u; c < total; ++i, c += L) {
+    const int row = fast_div(c, chunk_div);
+    copy16(buf + 32 * i + lane, src + row * src_row + (c - row * chunks) * E);
+  }
+  copies_end();
+  const float s0 = held > 0 ? *scale : 0.f;
+  copies_wait<0>();
+  auto peak = [&](bool finite) {
+    uint32_t top = 0;
+    for (int i = 0, c = u; c < total; ++i, c += L) top = peak_of<T>(buf[32 * i + lane], top, finite);
+    __syncwarp();
+#pragma unroll
+    for (int off = 1; off < L; off <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, off));
+    return top;
+  };
+  uint32_t top = peak(false);
+  const bool plain = top <= kMostBits;
+  if (!__all_sync(0xffffffffu, plain)) top = peak(true);
+  const Scale now = scale_of(top, held, s0);
+  for (int i = 0, c = u; c < total; ++i, c += L) {
+    const int row = fast_div(c, chunk_div);
+    store_codes<T>(code + row * code_row + (c - row * chunks) * E, buf[32 * i + lane], now.by, plain);
+  }
+  if (count > 0) {
+    const bool same = held > 0 && __float_as_uint(s0) == now.bits;
+    if (held > 0 && !same) rescale(before, code_row, held, D, s0 * now.by, u, L);
+    if (u == 0 && !same) *scale = __uint_as_float(now.bits);
+  }
+  __syncwarp();
+}
+
+// The runs that begin in a CTA's share of the packed rows, one after the other, found by every warp for itself.
+struct Run {
+  int row, count, held;              // packed rows; rows before them in the block, from before the call
+  long long code, scale;             // offsets of its first row and of its block in head 0
+};
+struct RunWalk {
+  int r, r_end;
+  __device__ __forceinline__ RunWalk(const ds_kv8_write_params &p, const WriteLaunch &launch) {
+    r = blockIdx.x * launch.rows;
+    r_end = r + min(launch.rows, p.N - r);
+  }
+  __device__ __forceinline__ bool next(const ds_kv8_write_params &p, const WriteLaunch &launch, Run &run, uint32_t &flags) {
+    while (r < r_end) {
+      const int b = p.row_start ? count_up_to(p.row_start + 1, p.B, r) : r / p.max_q;
+      if (b >= p.B) break;
+      const NewRows q = new_rows(p, launch.bound, b);
+      if (r < q.lo) {
+        r = q.lo;
+        continue;
+      }
+      const int hi = (int)min((long long)p.N, (long long)q.lo + max(q.n, 0));
+      if (!q.ok || r >= hi) {
+        r = max(r + 1, hi);
+        continue;
+      }
+      const int pos = q.len - q.n + (r - q.lo), in_block = pos - fast_div(pos, launch.block_div) * p.scale_block, first = r;
+      r = (int)min((long long)hi, (long long)r + p.scale_block - in_block);
+      if (first != q.lo && in_block != 0) continue;
       const int j = fast_div(pos, launch.page_div), slot = pos - j * p.page_size;
       const int page = p.block_table[b * p.table_stride + j];
       if (page < 0 || page >= p.n_pages) {
         flags |= DS_DEV_INDEX;
-      } else {
-        const long long cache = page * p.cache_stride[0], at_scale = page * p.scale_stride[0] + fast_div(slot, launch.block_div) * p.scale_stride[2];
-        for (int first = blockIdx.y * launch.per_cta + warp * kGroups; first < item_end; first += kWarps * kGroups) {
-          const int item = first + lane / L, h = item >> 1;
-          const bool mine = item < item_end, value = item & 1;
-          const T *src = reinterpret_cast<const T *>(value ? p.v : p.k) + r * p.kv_stride[0] + h * p.kv_stride[1];
-          uint8_t *code = reinterpret_cast<uint8_t *>(value ? p.v_cache : p.k_cache) + cache + h * p.cache_stride[1] + slot * p.cache_stride[2];
-          float *scale = (value ? p.v_scale : p.k_scale) + at_scale + h * p.scale_stride[1];
-          const int held = mine && r == q.lo ? in_block : 0;
-          write_run<T, L>(src, p.kv_stride[0], mine ? next - r : 0, code, p.cache_stride[2], code - held * p.cache_stride[2], held, scale, p.D,
-                          launch.chunk_div, u);
-        }
+        continue;
       }
+      run.row = first, run.count = r - first, run.held = first == q.lo ? in_block : 0;
+      run.code = page * p.cache_stride[0] + slot * p.cache_stride[2];
+      run.scale = page * p.scale_stride[0] + fast_div(slot, launch.block_div) * p.scale_stride[2];
+      return true;
     }
-    r = next;
+    return false;
+  }
+};
+__device__ __forceinline__ uint32_t check_sequences(const ds_kv8_write_params &p, int bound) {
+  uint32_t flags = 0;
+  if (blockIdx.x == 0 && blockIdx.y == 0)
+    for (int b = threadIdx.x; b < p.B; b += kThreads)
+      if (!new_rows(p, bound, b).ok) flags |= DS_DEV_INDEX;
+  return flags;
+}
+
+template <typename T, int L>
+__global__ void __launch_bounds__(kThreads, 5) kv8_write_kernel(const __grid_constant__ ds_kv8_write_params p,
+                                                                const __grid_constant__ WriteLaunch launch) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, u = lane % L;
+  constexpr int kGroups = 32 / L;
+  __shared__ __align__(16) uint4 buf_s[kWarps][kKeep * 32];
+  dependent_sync();
+  uint32_t flags = check_sequences(p, launch.bound);
+  const int item_end = min(launch.items, (int)(blockIdx.y + 1) * launch.per_cta);
+  RunWalk walk(p, launch);
+  Run run;
+  while (walk.next(p, launch, run, flags)) {
+    for (int first = blockIdx.y * launch.per_cta + warp * kGroups; first < item_end; first += kWarps * kGroups) {
+      const int item = first + lane / L, h = item >> 1;
+      const bool mine = item < item_end, value = item & 1;
+      const T *src = reinterpret_cast<const T *>(value ? p.v : p.k) + run.row * p.kv_stride[0] + h * p.kv_stride[1];
+      uint8_t *code = reinterpret_cast<uint8_t *>(value ? p.v_cache : p.k_cache) + run.code + h * p.cache_stride[1];
+      float *scale = (value ? p.v_scale : p.k_scale) + run.scale + h * p.scale_stride[1];
+      const int held = mine ? run.held : 0;
+      write_run<T, L>(buf_s[warp], src, p.kv_stride[0], mine ? run.count : 0, code, p.cache_stride[2], code - held * p.cache_stride[2], held, scale, p.D,
+                      launch.chunk_div, u);
+    }
+  }
+  if (flags && p.status) atomicOr(p.status, flags);
+}
+
+// Longer runs: the whole CTA takes an item; the next ones' first chunks are on their way while the exponent of this one is settled.
+constexpr int kWideKeep = 4, kAhead = 2;      // chunks of a thread that are held; items ahead
+template <typename T>
+__global__ void __launch_bounds__(kThreads, 4) kv8_write_wide_kernel(const __grid_constant__ ds_kv8_write_params p,
+                                                                     const __grid_constant__ WriteLaunch launch) {
+  constexpr int E = Chunk<T>::kElems;
+  extern __shared__ __align__(16) uint4 ring[];      // [kAhead + 1][kWideKeep][kThreads]
+  __shared__ uint32_t top_s[2][kWarps];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  dependent_sync();
+  uint32_t flags = check_sequences(p, launch.bound);
+  const int item0 = blockIdx.y * launch.per_cta, item_end = min(launch.items, item0 + launch.per_cta);
+  const int chunks = (int)launch.chunk_div.d;
+  RunWalk walk(p, launch);
+  Run run;
+  int turn = 0;
+  while (walk.next(p, launch, run, flags)) {
+    const int total = run.count * chunks, n_keep = min(kWideKeep, (total - tid + kThreads - 1) / kThreads);
+    long long src_at[kWideKeep], code_at[kWideKeep];      // of this thread's chunks, from the run's first row
+#pragma unroll
+    for (int i = 0; i < kWideKeep; ++i) {
+      const int c = tid + i * kThreads, row = fast_div(c, launch.chunk_div), ch = (c - row * chunks) * E;
+      src_at[i] = row * p.kv_stride[0] + ch;
+      code_at[i] = row * p.cache_stride[2] + ch;
+    }
+    auto src_of = [&](int item) {
+      return reinterpret_cast<const T *>(item & 1 ? p.v : p.k) + run.row * p.kv_stride[0] + (item >> 1) * p.kv_stride[1];
+    };
+    auto stage_of = [&](int item) { return ring + (item % (kAhead + 1)) * (kWideKeep * kThreads) + tid; };
+    auto load = [&](int item) {
+      if (item < item_end) {
+        const T *src = src_of(item);
+        uint4 *to = stage_of(item);
+#pragma unroll
+        for (int i = 0; i < kWideKeep; ++i)
+          if (i < n_keep) copy16(to + i * kThreads, src + src_at[i]);
+      }
+      copies_end();
+    };
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) load(item0 + k);
+#pragma unroll 1
+    for (int item = item0; item < item_end; ++item) {
+      const T *src = src_of(item);
+      const int h = item >> 1;
+      uint8_t *code = reinterpret_cast<uint8_t *>(item & 1 ? p.v_cache : p.k_cache) + run.code + h * p.cache_stride[1];
+      float *scale = (item & 1 ? p.v_scale : p.k_scale) + run.scale + h * p.scale_stride[1];
+      const float s0 = run.held > 0 ? *scale : 0.f;
+      load(item + kAhead);
+      copies_wait<kAhead>();
+      const uint4 *mine = stage_of(item);
+      auto at = [&](int c) {
+        const int row = fast_div(c, launch.chunk_div);
+        return src + row * p.kv_stride[0] + (c - row * chunks) * E;
+      };
+      auto peak = [&](bool finite) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < kWideKeep; ++i)
+          if (i < n_keep) top = peak_of<T>(mine[i * kThreads], top, finite);
+        for (int c = tid + kWideKeep * kThreads; c < total; c += kThreads) top = peak_of<T>(*reinterpret_cast<const uint4 *>(at(c)), top, finite);
+        top = __reduce_max_sync(0xffffffffu, top);
+        if (lane == 0) top_s[turn][warp] = top;
+        turn ^= 1;
+        __syncthreads();      // also: every thread has read the old scale; the buffer of two turns ago is read
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) top = max(top, top_s[turn ^ 1][w]);
+        return top;
+      };
+      uint32_t top = peak(false);
+      const bool plain = top <= kMostBits;
+      if (!plain) top = peak(true);
+      const Scale now = scale_of(top, run.held, s0);
+#pragma unroll
+      for (int i = 0; i < kWideKeep; ++i)
+        if (i < n_keep) store_codes<T>(code + code_at[i], mine[i * kThreads], now.by, plain);
+      for (int c = tid + kWideKeep * kThreads; c < total; c += kThreads) {
+        const int row = fast_div(c, launch.chunk_div);
+        store_codes<T>(code + row * p.cache_stride[2] + (c - row * chunks) * E, *reinterpret_cast<const uint4 *>(at(c)), now.by, plain);
+      }
+      const bool same = run.held > 0 && __float_as_uint(s0) == now.bits;
+      if (run.held > 0 && !same) rescale(code - run.held * p.cache_stride[2], p.cache_stride[2], run.held, p.D, s0 * now.by, tid, kThreads);
+      if (tid == 0 && !same) *scale = __uint_as_float(now.bits);
+    }
   }
   if (flags && p.status) atomicOr(p.status, flags);
 }
@@ -212,9 +377,23 @@ struct ReadLaunch {
   int rows;      // of the output, per CTA; of one sequence when dense
   int per_seq;   // dense: CTAs of a sequence
   int items, per_cta;
-  FastDiv page_div, block_div, chunk_div, seq_div;
+  int groups;    // of threads, with heads of their own
+  FastDiv page_div, block_div, chunk_div, seq_div, row_div;
 };
 constexpr int kReadRows = 32;
+
+template <typename T>
+__device__ __forceinline__ void store_values(T *to, const uint2 &w, float s) {
+  const float2 a0 = halves_f32(halves_lo(w.x)), a1 = halves_f32(halves_hi(w.x)), a2 = halves_f32(halves_lo(w.y)), a3 = halves_f32(halves_hi(w.y));
+  if constexpr (std::is_same<T, float>::value) {
+    reinterpret_cast<float4 *>(to)[0] = make_float4(a0.x * s, a0.y * s, a1.x * s, a1.y * s);
+    reinterpret_cast<float4 *>(to)[1] = make_float4(a2.x * s, a2.y * s, a3.x * s, a3.y * s);
+  } else {
+    const __nv_bfloat162 v[4] = {__floats2bfloat162_rn(a0.x * s, a0.y * s), __floats2bfloat162_rn(a1.x * s, a1.y * s),
+                                 __floats2bfloat162_rn(a2.x * s, a2.y * s), __floats2bfloat162_rn(a3.x * s, a3.y * s)};
+    *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(v);
+  }
+}
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads) kv8_read_kernel(const __grid_constant__ ds_kv8_read_params p,
@@ -263,25 +442,36 @@ __global__ void __launch_bounds__(kThreads) kv8_read_kernel(const __grid_constan
     code_s[i] = code, scale_s[i] = scale, out_s[i] = out;
   }
   __syncthreads();
-  const int chunks = p.D / 8, item0 = blockIdx.y * launch.per_cta, items = min(launch.per_cta, launch.items - item0);
-  const int total = n * items * chunks;
-#pragma unroll 4
-  for (int c = tid; c < total; c += kThreads) {
-    const int q = fast_div(c, launch.chunk_div), ch = c - q * chunks, i = q / items, item = item0 + q - i * items, h = item >> 1;
-    const long long code = code_s[i];
-    if (code < 0) continue;
-    const bool value = item & 1;
-    const uint2 w = *reinterpret_cast<const uint2 *>(reinterpret_cast<const uint8_t *>(value ? p.v_cache : p.k_cache) + code + h * p.cache_stride[1] + 8 * ch);
-    const float s = (value ? p.v_scale : p.k_scale)[scale_s[i] + h * p.scale_stride[1]];
-    const float2 a0 = halves_f32(halves_lo(w.x)), a1 = halves_f32(halves_hi(w.x)), a2 = halves_f32(halves_lo(w.y)), a3 = halves_f32(halves_hi(w.y));
-    T *to = reinterpret_cast<T *>(value ? p.v_out : p.k_out) + out_s[i] + h * p.out_stride[2] + 8 * ch;
-    if constexpr (std::is_same<T, float>::value) {
-      reinterpret_cast<float4 *>(to)[0] = make_float4(a0.x * s, a0.y * s, a1.x * s, a1.y * s);
-      reinterpret_cast<float4 *>(to)[1] = make_float4(a2.x * s, a2.y * s, a3.x * s, a3.y * s);
-    } else {
-      const __nv_bfloat162 v[4] = {__floats2bfloat162_rn(a0.x * s, a0.y * s), __floats2bfloat162_rn(a1.x * s, a1.y * s),
-                                   __floats2bfloat162_rn(a2.x * s, a2.y * s), __floats2bfloat162_rn(a3.x * s, a3.y * s)};
-      *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(v);
+  // A thread stays with a row and eight of its dimensions and goes through the heads, or some of them.
+  const int chunks = (int)launch.chunk_div.d, side = fast_div(tid, launch.chunk_div), ch = tid - side * chunks;
+  const int group = fast_div(side, launch.row_div), i = side - group * launch.rows;
+  const int item0 = blockIdx.y * launch.per_cta, item_end = min(launch.items, item0 + launch.per_cta);
+  if (group < launch.groups && i < n) {
+    const long long code = code_s[i], scale = scale_s[i], out = out_s[i];
+    if (code >= 0) {
+      const uint8_t *from[2] = {reinterpret_cast<const uint8_t *>(p.k_cache) + code + 8 * ch, reinterpret_cast<const uint8_t *>(p.v_cache) + code + 8 * ch};
+      const float *by[2] = {p.k_scale + scale, p.v_scale + scale};
+      T *to[2] = {reinterpret_cast<T *>(p.k_out) + out + 8 * ch, reinterpret_cast<T *>(p.v_out) + out + 8 * ch};
+      const int step = 2 * launch.groups;
+      constexpr int kBatch = 4;      // heads whose loads are in flight
+      for (int item = item0 + 2 * group; item < item_end; item += kBatch * step) {      // K and V of a head
+        uint2 w[kBatch][2];
+        float s[kBatch][2];
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k)
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+            if (item + k * step < item_end) {
+              const int h = (item + k * step) >> 1;
+              w[k][x] = *reinterpret_cast<const uint2 *>(from[x] + h * p.cache_stride[1]);
+              s[k][x] = by[x][h * p.scale_stride[1]];
+            }
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k)
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+            if (item + k * step < item_end) store_values(to[x] + ((item + k * step) >> 1) * p.out_stride[2], w[k][x], s[k][x]);
+      }
     }
   }
   if (flags && p.status) atomicOr(p.status, flags);
@@ -294,10 +484,10 @@ int launch_write(const ds_kv8_write_params &p, cudaStream_t stream) {
   w.bound = p.max_len > 0 && p.max_len < cap ? p.max_len : cap;
   w.items = 2 * p.Hkv;
   const int at_a_time = kWarps * (32 / L);      // items of a CTA
-  // One row to a CTA while the calls are few, more where the CTAs would otherwise be many waves.
+  // As many rows to a CTA as a run has, so that few CTAs find none, more where the CTAs would otherwise be many waves.
   w.per_cta = w.items < at_a_time ? w.items : at_a_time;
   const long long groups = (w.items + w.per_cta - 1) / w.per_cta, enough = 8LL * sm_count();
-  w.rows = 1;
+  w.rows = p.max_q < p.scale_block ? p.max_q : p.scale_block;
   while (w.rows < 64 && (p.N + 2LL * w.rows - 1) / (2LL * w.rows) * groups >= enough) w.rows *= 2;
   w.page_div = make_fast_div(p.page_size);
   w.block_div = make_fast_div(p.scale_block);
@@ -309,9 +499,32 @@ int launch_write(const ds_kv8_write_params &p, cudaStream_t stream) {
 }
 
 template <typename T>
+int launch_write_wide(const ds_kv8_write_params &p, cudaStream_t stream) {
+  WriteLaunch w;
+  const int cap = p.max_pages * p.page_size;
+  w.bound = p.max_len > 0 && p.max_len < cap ? p.max_len : cap;
+  w.items = 2 * p.Hkv;
+  w.rows = p.scale_block < 64 ? p.scale_block : 64;
+  const long long shares = ((long long)p.N + w.rows - 1) / w.rows;
+  w.per_cta = w.items;      // the more the better: they overlap; but a CTA for every slot
+  while (w.per_cta > 1 && shares * ((w.items + w.per_cta - 1) / w.per_cta) < 8LL * sm_count()) w.per_cta = (w.per_cta + 1) / 2;
+  w.page_div = make_fast_div(p.page_size);
+  w.block_div = make_fast_div(p.scale_block);
+  w.chunk_div = make_fast_div(p.D / Chunk<T>::kElems);
+  const dim3 grid((unsigned)shares, (unsigned)((w.items + w.per_cta - 1) / w.per_cta));
+  constexpr int kBytes = (kAhead + 1) * kWideKeep * kThreads * 16;
+  static std::atomic<unsigned long long> allowed{0};
+  DS_CUDA_OK(allow_smem(kv8_write_wide_kernel<T>, kBytes, allowed));
+  DS_CUDA_OK(launch_kernel(kv8_write_wide_kernel<T>, grid, kThreads, kBytes, 0, true, stream, p, w));
+  note_launch(1);
+  return DS_OK;
+}
+
+template <typename T>
 int launch_write_lanes(const ds_kv8_write_params &p, cudaStream_t stream) {
   // lanes of an item: a run of one row should not leave most of them idle
   const long long chunks = (long long)(p.max_q < p.scale_block ? p.max_q : p.scale_block) * (p.D / Chunk<T>::kElems);
+  if (chunks > 32 * kKeep) return launch_write_wide<T>(p, stream);
   return chunks <= 8 ? launch_write<T, 8>(p, stream) : chunks <= 16 ? launch_write<T, 16>(p, stream) : launch_write<T, 32>(p, stream);
 }
 
@@ -319,11 +532,15 @@ template <typename T>
 int launch_read(const ds_kv8_read_params &p, cudaStream_t stream) {
   ReadLaunch w;
   w.items = 2 * p.Hkv;
-  const long long units = (long long)p.D / 8 * w.items, rows = p.out_start ? p.N : (long long)p.B * p.N;
-  w.rows = kReadRows;
-  while (w.rows > 1 && (rows / w.rows) * ((units + 511) / 512) < 4LL * sm_count()) w.rows /= 2;
+  // Rows of a CTA: what its threads hold at a time, fewer where there are few; then the heads are divided, too.
+  const long long rows = p.out_start ? p.N : (long long)p.B * p.N, enough = 4LL * sm_count();
+  const int at_a_time = kThreads / (p.D / 8);
+  w.rows = at_a_time < kReadRows ? at_a_time : kReadRows;      // kThreads / (D / 8) is at least 8
+  while (w.rows > 1 && rows / w.rows < enough) w.rows = (w.rows + 1) / 2;
   w.per_cta = w.items;
-  while (w.per_cta > 1 && (long long)w.rows * w.per_cta * (p.D / 8) > 4 * kThreads) w.per_cta = (w.per_cta + 1) / 2;
+  while (w.per_cta > 2 && rows / w.rows * (w.items / w.per_cta) < enough) w.per_cta = (w.per_cta / 2 + 1) / 2 * 2;
+  w.groups = at_a_time / w.rows;
+  w.row_div = make_fast_div(w.rows);
   w.per_seq = (int)(((long long)p.N + w.rows - 1) / w.rows);
   w.page_div = make_fast_div(p.page_size);
   w.block_div = make_fast_div(p.scale_block);
