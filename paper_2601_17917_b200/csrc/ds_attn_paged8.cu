@@ -18,38 +18,25 @@
 
 #include "ds_attn_paged_rows.cuh"
 #include "ds_e4m3.cuh"
+#include "ds_paged8.cuh"
 
 namespace ds {
 namespace {
 
 using namespace paged;
 
-struct Args8 : Params {
-  const float *k_scale, *v_scale;
-  long long scale_stride[3];
-  FastDiv scale_div;      // by rows of a block
-};
-
 __device__ __forceinline__ void mma_half(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-
-constexpr float kWeight = 1024.f;      // of the reference in fp16
-constexpr float kLag = 4.f;            // weights may pass that by 2^4
-
 template <typename T_, int D_, int NB>
 struct ByteRows {
   using T = T_;
   using Cache = uint8_t;
   using Args = Args8;
   static constexpr bool kScaled = true;
+  using W = Weights8<!std::is_same<T, float>::value>;
   static constexpr int D = D_, kRows = 8 * NB, kRowBytes = D, kKeys = 32;
   static constexpr int kParts = std::is_same<T, float>::value ? 2 : 1;      // of a query, of a weight
   static constexpr int kBlocks = kParts * NB;                                // of 8 rows of queries
@@ -99,7 +86,7 @@ struct ByteRows {
       const float up = __uint_as_float((uint32_t)(127 + shift) << 23);
       if (u == 0) factor_s[r] = __uint_as_float((uint32_t)(127 - shift) << 23) * (a.p.scale * kLog2e);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] *= up;
+      for (int e = 0; e < 4; ++e) x[e] = isfinite(x[e]) ? x[e] * up : __uint_as_float(0x7fffffffu);
 #pragma unroll
       for (int part = 0; part < kParts; ++part) {
         // dimensions 4q, 4q + 1 of 16 stand at 2q, 2q + 1, dimensions 4q + 2, 4q + 3 at 2q + 8, 2q + 9
@@ -107,11 +94,9 @@ struct ByteRows {
         uint8_t *to = q_buf + (u & 3) * 4;
         *reinterpret_cast<uint32_t *>(to + chunk_at<kQRowBytes>(part * kRows + r, 2 * (u >> 2))) = first;
         *reinterpret_cast<uint32_t *>(to + chunk_at<kQRowBytes>(part * kRows + r, 2 * (u >> 2) + 1)) = second;
-        if constexpr (kParts == 2) {      // what is left; of an infinity, nothing
+        if constexpr (kParts == 2) {      // what is left
           const float2 f = halves_f32(first), s = halves_f32(second);
-          const float y[4] = {f.x, f.y, s.x, s.y};
-#pragma unroll
-          for (int e = 0; e < 4; ++e) x[e] = isfinite(y[e]) ? x[e] - y[e] : 0.f;
+          x[0] -= f.x, x[1] -= f.y, x[2] -= s.x, x[3] -= s.y;
         }
       }
     }
@@ -141,10 +126,10 @@ struct ByteRows {
     set_vref(27);      // 2^-100
   }
 
-  // vref = 2^(e - 127), vinv = 2^10 / vref
+  // vref = 2^(e - 127), vinv = the reference's weight / vref
   __device__ __forceinline__ void set_vref(uint32_t e) {
     vref = __uint_as_float(e << 23);
-    vinv = __uint_as_float((264u - e) << 23);
+    vinv = __uint_as_float((254u + W::kLog2 - e) << 23);
   }
 
   // Makes vref the power of two at or above the largest finite scale of V of the stage.
@@ -254,7 +239,7 @@ struct ByteRows {
         top[nb][e] = fmaxf(s[nb][0][e], s[nb][0][2 + e]);
 #pragma unroll
         for (int g = 1; g < kGroups; ++g) top[nb][e] = fmaxf(top[nb][e], fmaxf(s[nb][g][e], s[nb][g][2 + e]));
-        over |= top[nb][e] > m[nb][e] + kLag;
+        over |= top[nb][e] > m[nb][e] + W::kLag;
       }
     if (__any_sync(0xffffffffu, over)) {
 #pragma unroll
@@ -357,7 +342,7 @@ struct ByteRows {
   // The warp's sums to shared memory: out[kRows][D], ml[kRows].
   __device__ void finish(const Args8 &a, const Item &it, float *out, float2 *ml) {
     const int lane = threadIdx.x & 31;
-    const float down = a.shrink / kWeight;
+    const float down = a.shrink / W::kOne;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -388,9 +373,14 @@ auto with_rows(const ds_paged_params &p, F f) {
   return rows <= 8 ? f(ByteRows<float, 128, 1>()) : f(ByteRows<float, 128, 2>());
 }
 
+// Rows per KV head from which the kernel with tcgen05 tiles takes over.
+constexpr int kTensorTileRows = 33;
+bool wide(const ds_paged_params &p) { return p.dtype == DS_BF16 && (long long)p.max_q * (p.Hq / p.Hkv) >= kTensorTileRows; }
+
 }  // namespace
 
 bool attn_paged8_counts_fit(const ds_paged8_params &p) {
+  if (wide(p.a)) return attn_paged8_tc_counts_fit(p.a);
   return with_rows(p.a, [&](auto engine) {
     using Rows = decltype(engine);
     const PagedShape s = units_of(p.a, Layout<Rows>::kTile, Rows::kRows);
@@ -400,16 +390,14 @@ bool attn_paged8_counts_fit(const ds_paged8_params &p) {
 
 size_t attn_paged8_workspace_bytes(const ds_paged8_params &p) {
   if (p.a.B == 0 || p.a.N == 0) return 0;
+  if (wide(p.a)) return attn_paged8_tc_workspace_bytes(p.a);
   return with_rows(p.a, [&](auto rows) { return rows_workspace_of(shape_for<decltype(rows)>(p.a)); });
 }
 
 int launch_attn_paged8(const ds_paged8_params &p, cudaStream_t stream) {
+  if (wide(p.a)) return launch_attn_paged8_tc(p, stream);
   return with_rows(p.a, [&](auto rows) {
-    return launch_rows<decltype(rows)>(p.a, stream, [&](Args8 &a) {
-      a.k_scale = p.k_scale, a.v_scale = p.v_scale;
-      for (int d = 0; d < 3; ++d) a.scale_stride[d] = p.scale_stride[d];
-      a.scale_div = make_fast_div(p.scale_block);
-    });
+    return launch_rows<decltype(rows)>(p.a, stream, [&](Args8 &a) { set_scales(p, a); });
   });
 }
 

@@ -1,0 +1,814 @@
+// ds_attn_paged8 for more query rows per KV head (a decoding block, grouped queries of several tokens): bf16 queries on the 5th
+// generation tensor cores.
+//
+// S = Q K^T takes K as it is, e4m3.  A bf16 query, scaled by a power of two so that its row's largest element lies in [2^7, 2^8), is the
+// sum of an e4m3 value (rounded to the nearest 4 bits) and an e5m2 one: what is left of 8 bits is at most 8 of their units, which 3 bits
+// hold.  So two products of 8-bit operands, in one accumulator, are exact in the queries down to 2^-14 of the row's largest element and
+// within 2^-21 of it below.  O += P V takes fp16: four warps turn the e4m3 values of a tile into fp16, which holds them all, in the layout
+// of the product; weights are fp16 with V's scale in them, as in the kernel for few rows.  (P in 8-bit halves would drop what lies below
+// 2^-22 of the largest weight, a per cent of the sum in a long cache.)
+//
+// Two streams of 128 tile rows each, with a warpgroup, S and O of their own, keep the tensor pipe and the exponentials busy at once:
+//   kPair      rows 0 .. 127 and 128 .. 255 of an item, over the same key tiles
+//   otherwise  the same rows, the even and the odd key tiles, joined when the item ends.  Up to 64 rows stand in the tile kCopies
+//              times: each copy weighs 1 / kCopies of the keys and has zeros for the others.
+// Step u of a piece is stream u % 2, key tile u (kPair: u / 2).  The products go out in the order QK0 QK1 PV0 QK2 PV1 ..; they execute
+// in order, so a stream's S may be written once the product that reads its P has been issued.
+//
+// Warps:
+//   0-7    softmax and epilogue, thread = tile row = TMEM lane, four warps a stream
+//   8      issues the products
+//   9-11   load, each the tiles of one slot of the rings: 16-byte asynchronous copies of K (in the swizzle of the products) and V from
+//          wherever the page table says, and the scales
+//   12-15  at the start of a piece the queries, four threads a row; then V to fp16, 32 keys each
+// (One set of four warps that loaded and converted took 5500 cycles a tile, most of them in its own instructions: 120 us where this takes
+// KK.)
+//
+// Bound by HBM while a key tile's 32 KB (1430 cycles of an SM's share) hide its products (256 + 256 cycles) and exponentials, which 128
+// rows do: 1024 cycles; beyond, by the exponentials.
+//
+// Every wait is bounded; on expiry the kernel raises DS_DEV_TIMEOUT, drains and frees TMEM.
+#include <type_traits>
+
+#include "ds_attn_paged.cuh"
+#include "ds_e4m3.cuh"
+#include "ds_paged8.cuh"
+
+namespace ds {
+namespace {
+
+using namespace paged;
+using namespace sm100;
+
+constexpr int kKeys = 128;
+constexpr int kSoftmaxWarps = 8, kMmaWarp = 8, kLoadWarp = 9, kConvertWarp = 12, kConvertWarps = 4;
+constexpr int kThreads = 32 * (kConvertWarp + kConvertWarps);
+constexpr int kMinTiles = 2;       // a range has at least so many key tiles
+constexpr int kWholeTiles = 2;     // items of at most so many key tiles are not split
+constexpr uint32_t kTmemS = 0, kTmemO = 256, kTmemCols = 512;      // S (2 x 128), O (2 x 128); P over S
+constexpr int kHalfBytes = 128 * 128;      // 128 keys of 64 dimensions in fp16: a swizzled half of a tile of D = 128
+constexpr int kScaleRing = 4;              // key tiles whose scales are held
+
+template <int D, bool kPair>
+struct Geo {
+  static constexpr int kTile = 128 * D;      // bytes of 128 e4m3 rows
+  static constexpr int kRows = kPair ? 256 : 128;
+  static constexpr int kSlots = kPair ? 2 : 3;      // of the rings of K and of V; a loading warp each
+  static constexpr int kQPart = kRows * D;          // one part of the queries
+  static constexpr int kOffK = 2 * kQPart;
+  static constexpr int kOffV = kOffK + kSlots * kTile;
+  static constexpr int kOffV16 = kOffV + kSlots * kTile;                  // [2] tiles in fp16; at the end of an item sums to be joined
+  static constexpr int kOffScale = kOffV16 + 2 * 2 * kTile;               // [kScaleRing][2][128]
+  static constexpr int kOffFactor = kOffScale + kScaleRing * 1024;        // [kRows]
+  static constexpr int kOffMl = kOffFactor + kRows * 4;                   // [256]
+  static constexpr int kOffBar = kOffMl + (kPair ? 0 : 256 * 8);
+  // k_full, k_empty, v_full, v_empty [kSlots], v16_full, v16_free [2], scale_ready, scale_free [kScaleRing], s_full, p_full, pv_done, o_free
+  // [2], q_full, q_free, meet, joined
+  static constexpr int kNumBars = 4 * kSlots + 4 + 2 * kScaleRing + 8 + 4;
+  static constexpr int kOffMisc = kOffBar + 8 * kNumBars;      // TMEM base, abort flag, NaN in V, references of the scales [kScaleRing]
+  static constexpr int kOffScan = (kOffMisc + 12 + 4 * kScaleRing + 7) / 8 * 8;
+  static constexpr int kBytes = kOffScan + 8 * (kThreads / 32 + 2) + 1024;      // slack: the base is aligned to 1024
+  static constexpr int kJoinDims = D == 128 ? 64 : 32;                          // 256 rows of so many fp32 fit into the tiles of V
+  static_assert(kBytes <= 227 * 1024, "shared memory");
+  static_assert(256 * kJoinDims * 4 <= 4 * kTile, "sums to be joined");
+};
+
+// Byte offset of 16-byte chunk `c` of row `r` of e4m3 values: the 128-byte swizzle for rows of 128 bytes, the 64-byte one for 64.
+template <int D>
+__device__ __forceinline__ uint32_t row_at(int r, int c) { return r * D + ((c ^ (D == 64 ? (r >> 1) & 3 : r & 7)) << 4); }
+// The same of a tile of fp16 values, halves of 64 dimensions.
+__device__ __forceinline__ uint32_t half_at(int r, int c) { return (c >> 3) * kHalfBytes + r * 128 + (((c & 7) ^ (r & 7)) << 4); }
+
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t *r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+      ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t *r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr)
+      : "memory");
+}
+// D[tmem] (+)= A[smem] * B[smem], 8-bit operands.
+__device__ __forceinline__ void umma_ss8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// Descriptor of rows of `row` bytes (128 or 64) in the swizzle of that width, groups of eight rows one after the other.
+__device__ __forceinline__ uint64_t rows_desc(uint32_t addr, int row) {
+  return (uint64_t)((addr & 0x3FFFFu) >> 4) | (1ull << 16) | ((uint64_t)((8 * row) >> 4) << 32) | (1ull << 46) | ((row == 64 ? 4ull : 2ull) << 61);
+}
+// Instruction descriptors: fp32 accumulation; A of e5m2 or e4m3 and B of e4m3, K-major; A and B of fp16, B with its N side contiguous.
+__host__ __device__ constexpr uint32_t idesc8(int n, bool a_e5m2) { return (1u << 4) | ((a_e5m2 ? 1u : 0u) << 7) | ((uint32_t)(n >> 3) << 17) | (8u << 24); }
+__host__ __device__ constexpr uint32_t idesc16(int n) { return (1u << 4) | (1u << 16) | ((uint32_t)(n >> 3) << 17) | (8u << 24); }
+
+// Bounded wait that sleeps between its polls: many warps of this kernel wait at a time, and polls take issue slots from the others.
+__device__ __forceinline__ bool mbar_wait_nap(uint32_t bar, uint32_t parity, volatile int *abort_flag) {
+  for (uint32_t it = 0; it < kSpinLimit; ++it) {
+    if (mbar_try_wait(bar, parity)) return true;
+    if (it > 128) __nanosleep(64);
+    if (it > 64 && *abort_flag) return false;
+  }
+  *abort_flag = 1;
+  return false;
+}
+// Registers of a thread: the block's 512 x 128 at launch, for the eight softmax warps 168 and for the eight others 80.
+__device__ __forceinline__ void registers_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 168;"); }
+__device__ __forceinline__ void registers_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 80;"); }
+
+// Arrives at the barrier when this thread's copies so far are complete.
+__device__ __forceinline__ void arrive_when_copied(uint32_t bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ uint32_t mul_halves(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
+// The keys of a tile that a row sees: [0, hi) without [hole, back).
+struct Seen {
+  int hi, hole, back;
+  // Keys c .. c + 31 as bits.
+  __device__ __forceinline__ uint32_t bits(int c) const { return below(hi - c) & (below(hole - c) | ~below(back - c)); }
+  static __device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
+};
+__device__ __forceinline__ Seen seen_keys(const PagedShape &s, const PagedSeq &q, int x, int end) {
+  if (x < q.sink_pad) return {paged_min(q.sink_n, end) - x, kKeys, 0};
+  const int t = q.body + (x - q.sink_pad);
+  if (s.window == 0) return {end - t, kKeys, 0};
+  return {end - t, paged_max(s.sinks - t, 0), paged_max(end - s.window, 0) - t};
+}
+
+// V's NaN are zeros in the product.  Where there were any, the n keys from x on are gone through for those that the row sees: bit e
+// of the result: element d + e, of four, is NaN.
+__device__ __noinline__ uint32_t nan_elements(const Args8 &a, const Item it, int x, int n, int end, int d) {
+  const ds_paged_params &p = a.p;
+  const int32_t *table = p.block_table + it.b * p.table_stride;
+  const uint8_t *base = reinterpret_cast<const uint8_t *>(p.v_cache) + it.g * p.cache_stride[1] + d;
+  uint32_t found = 0;
+#pragma unroll 1
+  for (int i = 0; i < n; ++i) {
+    const int t = paged_key(it.q, x + i);
+    if (!paged_visible(a.s, t, end)) continue;
+    const int j = fast_div(t, a.page_div), page = paged_clamp_page(table[j], p.n_pages);
+    found |= __vcmpeq4(*reinterpret_cast<const uint32_t *>(base + page * p.cache_stride[0] + (t - j * p.page_size) * p.cache_stride[2]) & 0x7f7f7f7fu,
+                       0x7f7f7f7fu);
+  }
+  return found;
+}
+__device__ __forceinline__ float4 with_nan(float4 v, uint32_t bytes) {
+  const float nan = __uint_as_float(0x7fffffffu);
+  if (bytes & 0xffu) v.x = nan;
+  if (bytes & 0xff00u) v.y = nan;
+  if (bytes & 0xff0000u) v.z = nan;
+  if (bytes & 0xff000000u) v.w = nan;
+  return v;
+}
+
+template <int D, bool kPair, int kCopies>
+__global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __grid_constant__ Args8 a) {
+  using G = Geo<D, kPair>;
+  using T = __nv_bfloat16;
+  using W = Weights8<true>;
+  static_assert(!kPair || kCopies == 1, "");
+  constexpr int kPad = 128 / kCopies, kMine = kKeys / kCopies;      // rows of a copy, keys that it weighs
+  extern __shared__ uint8_t smem_raw[];
+  // (as an offset from the array: the accesses are then known to be to shared memory, and generic ones took twice as long here)
+  uint8_t *smem = smem_raw + ((0u - smem_u32(smem_raw)) & 1023u);
+  const uint32_t sbase = smem_u32(smem);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const ds_paged_params &p = a.p;
+  constexpr int S = G::kSlots;
+  const uint32_t bar_k_full = sbase + G::kOffBar, bar_k_empty = bar_k_full + 8 * S, bar_v_full = bar_k_empty + 8 * S, bar_v_empty = bar_v_full + 8 * S,
+                 bar_v16_full = bar_v_empty + 8 * S, bar_v16_free = bar_v16_full + 16, bar_sc_ready = bar_v16_free + 16,
+                 bar_sc_free = bar_sc_ready + 8 * kScaleRing, bar_s_full = bar_sc_free + 8 * kScaleRing, bar_p_full = bar_s_full + 16,
+                 bar_pv_done = bar_p_full + 16, bar_o_free = bar_pv_done + 16, bar_q_full = bar_o_free + 16, bar_q_free = bar_q_full + 8,
+                 bar_meet = bar_q_free + 8, bar_joined = bar_meet + 8;
+  volatile uint32_t *tmem_s = reinterpret_cast<volatile uint32_t *>(smem + G::kOffMisc);
+  volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + G::kOffMisc + 4);
+  volatile int *v_nan = reinterpret_cast<volatile int *>(smem + G::kOffMisc + 8);      // some tile of V held NaN so far
+  volatile uint32_t *vref_s = reinterpret_cast<volatile uint32_t *>(smem + G::kOffMisc + 12);      // biased exponents
+  float *scale_s = reinterpret_cast<float *>(smem + G::kOffScale);
+  float *factor_s = reinterpret_cast<float *>(smem + G::kOffFactor);
+
+  if (tid == 0) {
+    for (int s = 0; s < S; ++s) {
+      mbar_init(bar_k_full + 8 * s, 32);
+      mbar_init(bar_k_empty + 8 * s, 1);
+      mbar_init(bar_v_full + 8 * s, 32);
+      mbar_init(bar_v_empty + 8 * s, kConvertWarps);
+    }
+    for (int s = 0; s < kScaleRing; ++s) {
+      mbar_init(bar_sc_ready + 8 * s, 1);
+      mbar_init(bar_sc_free + 8 * s, kPair ? kSoftmaxWarps : kSoftmaxWarps / 2);
+    }
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(bar_v16_full + 8 * s, kConvertWarps);
+      mbar_init(bar_v16_free + 8 * s, 1);
+      mbar_init(bar_s_full + 8 * s, 1);
+      mbar_init(bar_p_full + 8 * s, kSoftmaxWarps / 2);
+      mbar_init(bar_pv_done + 8 * s, 1);
+      mbar_init(bar_o_free + 8 * s, kSoftmaxWarps / 2);
+    }
+    mbar_init(bar_q_full, kConvertWarps);
+    mbar_init(bar_q_free, 1 + kSoftmaxWarps);
+    mbar_init(bar_meet, kSoftmaxWarps);
+    mbar_init(bar_joined, kSoftmaxWarps);
+    *abort_flag = 0;
+    *v_nan = 0;
+    fence_barrier_init();
+  }
+  if (warp == kMmaWarp) tmem_alloc(sbase + G::kOffMisc, kTmemCols);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_s;
+  dependent_sync();
+  uint32_t flags = 0;
+  Walk walk;
+  walk.find<kThreads>(a, kMinTiles, reinterpret_cast<long long *>(smem + G::kOffScan), flags);
+  const Item &it = walk.it;
+  bool ok = true;
+  // Every wait is the whole warp's.
+  auto wait = [&](uint32_t bar, int phase) { return __all_sync(0xffffffffu, mbar_wait_nap(bar, phase & 1, abort_flag)) != 0; };
+
+  if (warp >= kConvertWarp) {
+    registers_down();
+    // ============================ queries, V to fp16 ============================
+    const int cw = warp - kConvertWarp, cid = tid - 32 * kConvertWarp;
+    int g = 0;      // key tiles of the pieces before
+    for (int k = 0; ok && walk.piece(a); g += walk.n_tiles, walk.next(a), ++k) {
+      // ---- the queries, once the products and the factors of the piece before are done with; four threads a row
+      if (k > 0) ok = wait(bar_q_free, k - 1);
+      if (!ok) break;
+      {
+        constexpr int E = D / 4, kLoads = E / 8;      // elements of a thread, 16 bytes at a time
+        const int u = cid & 3;
+#pragma unroll 1
+        for (int r = cid >> 2; r < (it.rows + 7) / 8 * 8; r += 8 * kConvertWarps) {      // whole warps
+          uint4 w[kLoads];
+          const bool there = r < it.rows;
+          {
+            const Row row = row_of(a, it, there ? r : 0);
+            const T *src = reinterpret_cast<const T *>(p.q) + row.n * p.q_stride[0] + row.h * p.q_stride[1] + E * u;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) w[i] = *reinterpret_cast<const uint4 *>(src + 8 * i);
+          }
+          const QueryScale q = query_scale<kLoads>(w, p.scale);
+          if (there && u == 0) factor_s[r] = q.factor;
+#pragma unroll
+          for (int i = 0; i < kLoads; i += 2) {
+            uint32_t hi[4], lo[4];
+            query_parts(w + i, q.up, hi, lo);
+            if (there) {
+#pragma unroll
+              for (int c = 0; c < kCopies; ++c) {
+                uint8_t *to = smem + row_at<D>(c * kPad + r, u * (E / 16) + i / 2);
+                *reinterpret_cast<uint4 *>(to) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                *reinterpret_cast<uint4 *>(to + G::kQPart) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+              }
+            }
+          }
+        }
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_q_full);
+      }
+      if (!kPair && k > 0) ok = wait(bar_joined, k - 1);      // the sums of the piece before, which lie in the tiles' place
+      // ---- V, tile by tile
+      uint32_t vref = 27;      // biased exponent of the reference of V's scales: 2^-100
+      for (int i = 0; ok && i < walk.n_tiles; ++i) {
+        const int t = g + i;
+        ok = wait(bar_v_full + 8 * (t % S), t / S);
+        if (!ok) break;
+        if (cw == 0) {
+          // the scales of V relative to the power of two at or above the largest finite one so far, times the reference's weight
+          float *vs = scale_s + (t % kScaleRing) * 256 + 128 + lane;
+          float v[4];
+          uint32_t big = 0;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            v[c] = vs[32 * c];
+            const uint32_t b = __float_as_uint(v[c]) & 0x7fffffffu;
+            big = max(big, b < 0x7f800000u ? b : 0u);
+          }
+          vref = max(vref, min((__reduce_max_sync(0xffffffffu, big) + 0x7fffffu) >> 23, 254u));
+          const float vinv = __uint_as_float((254u + W::kLog2 - vref) << 23);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) vs[32 * c] = v[c] * vinv, vs[32 * c - 128] *= 0x1p-24f;      // a product of queries and K is below 2^24
+          if (lane == 0) vref_s[t % kScaleRing] = vref;
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar_sc_ready + 8 * (t % kScaleRing));
+        }
+        ok = wait(bar_v16_free + 8 * (t & 1), t / 2 + 1);
+        if (!ok) break;
+        const uint8_t *from = smem + G::kOffV + (t % S) * G::kTile;
+        uint8_t *to = smem + G::kOffV16 + (t & 1) * (2 * G::kTile);
+        // eight rows side by side, four chunks of each; rows r and r ^ 5 next to each other meet no bank twice, in either layout
+        constexpr int kOps = D / 16;
+        const int r8 = 32 * cw + ((lane >> 3) ^ (lane & 4 ? 5 : 0)), c4 = lane & 3;
+#pragma unroll 4
+        for (int o = 0; o < kOps; ++o) {
+          const int r = r8 + 8 * (o & 3), c = c4 + 4 * (o >> 2);
+          const uint4 w = *reinterpret_cast<const uint4 *>(from + row_at<D>(r, c));
+          *reinterpret_cast<uint4 *>(to + half_at(r, 2 * c)) = make_uint4(halves_lo(w.x), halves_hi(w.x), halves_lo(w.y), halves_hi(w.y));
+          *reinterpret_cast<uint4 *>(to + half_at(r, 2 * c + 1)) = make_uint4(halves_lo(w.z), halves_hi(w.z), halves_lo(w.w), halves_hi(w.w));
+        }
+        if (!paged_all_visible(a.s, it.q, (walk.tile0 + i) * kKeys, kKeys)) {
+          // Keys that some rows see and others do not: a weight of zero times NaN would be NaN.  NaN becomes zero here, and the epilogue
+          // is told to look for it.  (Where every row sees every key, the product does what it should.)
+          bool nan = false;
+#pragma unroll 1
+          for (int o = 0; o < kOps; ++o) {
+            const int r = r8 + 8 * (o & 3), c = c4 + 4 * (o >> 2);
+            const uint4 w = *reinterpret_cast<const uint4 *>(from + row_at<D>(r, c));
+            const uint32_t x = (((w.x & 0x7f7f7f7fu) + 0x01010101u) | ((w.y & 0x7f7f7f7fu) + 0x01010101u) | ((w.z & 0x7f7f7f7fu) + 0x01010101u) |
+                                ((w.w & 0x7f7f7f7fu) + 0x01010101u)) & 0x80808080u;
+            if (x == 0) continue;
+            nan = true;
+#pragma unroll 1
+            for (int e = 0; e < 8; ++e) {
+              uint32_t *h = reinterpret_cast<uint32_t *>(to + half_at(r, 2 * c + e / 4)) + (e & 3);
+              const uint32_t v = *h;
+              *h = v & ~(((v & 0x7c00u) == 0x7c00u ? 0xffffu : 0u) | ((v & 0x7c000000u) == 0x7c000000u ? 0xffff0000u : 0u));
+            }
+          }
+          if (nan) *v_nan = 1;
+        }
+        fence_proxy_async();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(bar_v16_full + 8 * (t & 1));
+          mbar_arrive(bar_v_empty + 8 * (t % S));
+        }
+      }
+    }
+  } else if (warp >= kMmaWarp) {
+   registers_down();
+   if (warp >= kLoadWarp) {
+    // ============================ K, V, scales ============================
+    constexpr int kChunks = D / 16, kPer = 32 / kChunks, kOps = 16 / kPer;      // chunks of a row, rows of an instruction
+    const int lw = warp - kLoadWarp, ch = lane % kChunks;
+    const long long row_bytes = p.cache_stride[2];
+    int g = 0;      // key tiles of the pieces before
+    for (; ok && lw < S && walk.piece(a); g += walk.n_tiles, walk.next(a)) {
+      const int32_t *table = p.block_table + it.b * p.table_stride;
+      const uint8_t *kbase = reinterpret_cast<const uint8_t *>(p.k_cache) + it.g * p.cache_stride[1];
+      const uint8_t *vbase = reinterpret_cast<const uint8_t *>(p.v_cache) + it.g * p.cache_stride[1];
+      const float *kscale = a.k_scale + it.g * a.scale_stride[1], *vscale = a.v_scale + it.g * a.scale_stride[1];
+      int i = (lw + S - g % S) % S;      // this warp's first tile of the piece
+      int pos[4], page[4];               // of keys lane + 32 j
+      auto look_up = [&]() {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          pos[j] = i < walk.n_tiles ? paged_key(it.q, (walk.tile0 + i) * kKeys + 32 * j + lane) : -1;
+          page[j] = pos[j] >= 0 ? table[fast_div(pos[j], a.page_div)] : 0;
+        }
+      };
+      look_up();
+      for (; i < walk.n_tiles; i += S) {
+        const int t = g + i;
+        // Code that runs for every tile is kept short: five roles share the instruction caches, and with all loops of these copies
+        // unrolled (24 KB) every role waited for its instructions (123 us instead of KK).
+        long long at[4], scale_at[4];
+        uint32_t even = 0;      // bit 2 j + half: 16 keys that lie evenly (in one page) need one address
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          at[j] = -1, scale_at[j] = -1;
+          if (pos[j] >= 0) {
+            const int there = paged_clamp_page(page[j], p.n_pages);
+            if (there != page[j]) flags |= DS_DEV_INDEX;
+            const int slot = pos[j] - fast_div(pos[j], a.page_div) * p.page_size;
+            at[j] = there * p.cache_stride[0] + slot * row_bytes;
+            scale_at[j] = there * a.scale_stride[0] + fast_div(slot, a.scale_div) * a.scale_stride[2];
+          }
+          const long long first = __shfl_sync(0xffffffffu, at[j], lane & 16);
+          const uint32_t b = __ballot_sync(0xffffffffu, at[j] >= 0 && at[j] == first + (lane & 15) * row_bytes);
+          even |= ((b & 0xffffu) == 0xffffu ? 1u : 0u) << (2 * j) | (b >> 16 == 0xffffu ? 2u : 0u) << (2 * j);
+        }
+#pragma unroll 1
+        for (int v = 0; ok && v < 2; ++v) {
+          ok = wait((v ? bar_v_empty : bar_k_empty) + 8 * lw, t / S + 1);
+          if (!ok) break;
+          const uint8_t *base = (v ? vbase : kbase) + 16 * ch;
+          const uint32_t dst = sbase + (v ? G::kOffV : G::kOffK) + lw * G::kTile;
+#pragma unroll 1
+          for (int jh = 0; jh < 8; ++jh) {
+            const long long mine = jh < 4 ? (jh < 2 ? at[0] : at[1]) : jh < 6 ? at[2] : at[3];
+            const int r0 = 16 * jh + lane / kChunks, src = 16 * (jh & 1);
+            if ((even >> jh) & 1) {
+              const uint8_t *from = base + __shfl_sync(0xffffffffu, mine, src) + (lane / kChunks) * row_bytes;
+#pragma unroll
+              for (int o = 0; o < kOps; ++o, from += kPer * row_bytes) cp_async16(dst + row_at<D>(r0 + o * kPer, ch), from, true);
+            } else {
+#pragma unroll
+              for (int o = 0; o < kOps; ++o) {
+                const long long off = __shfl_sync(0xffffffffu, mine, src + o * kPer + lane / kChunks);
+                cp_async16(dst + row_at<D>(r0 + o * kPer, ch), base + (off >= 0 ? off : 0), off >= 0);
+              }
+            }
+          }
+          arrive_when_copied((v ? bar_v_full : bar_k_full) + 8 * lw);
+          if (v == 0) {
+            ok = wait(bar_sc_free + 8 * (t % kScaleRing), t / kScaleRing + 1);
+            if (!ok) break;
+            const uint32_t sc = sbase + G::kOffScale + (t % kScaleRing) * 1024 + 4 * lane;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              cp_async4(sc + 128 * j, kscale + (scale_at[j] >= 0 ? scale_at[j] : 0), scale_at[j] >= 0);
+              cp_async4(sc + 512 + 128 * j, vscale + (scale_at[j] >= 0 ? scale_at[j] : 0), scale_at[j] >= 0);
+            }
+          }
+        }
+        i += S;
+        look_up();      // of this warp's next tile
+        i -= S;
+      }
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+   } else {
+    // ============================ products ============================
+    const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+    const uint64_t dq0 = rows_desc(sbase, D), dk0 = rows_desc(sbase + G::kOffK, D), dv0 = smem_desc(sbase + G::kOffV16, kHalfBytes, 1024);
+    int g = 0, n_pv[2] = {0, 0};      // key tiles of the pieces before; products P V of a stream
+    for (int k = 0; ok && walk.piece(a); g += walk.n_tiles, walk.next(a), ++k) {
+      const int steps = kPair ? 2 * walk.n_tiles : walk.n_tiles;
+      auto qk = [&](int u) {
+        const int s = u & 1, t = g + (kPair ? u >> 1 : u);
+        ok = wait(bar_k_full + 8 * (t % S), t / S);
+        if (!ok) return;
+        fence_proxy_async();
+        tc_fence_after();
+        const uint64_t dq = dq0 + (uint64_t)((kPair ? s * 128 * D : 0) >> 4), dk = dk0 + (uint64_t)(((t % S) * G::kTile) >> 4);
+        if (elect_one()) {
+#pragma unroll 1
+          for (int part = 0; part < 2; ++part)
+#pragma unroll 1
+            for (int ks = 0; ks < D / 32; ++ks)
+              umma_ss8(tm + kTmemS + s * 128, dq + ((part * G::kQPart + ks * 32) >> 4), dk + ((ks * 32) >> 4), idesc8(kKeys, part == 1),
+                       part > 0 || ks > 0);
+          umma_commit(bar_s_full + 8 * s);
+          if (!kPair || s == 1) umma_commit(bar_k_empty + 8 * (t % S));
+          if (u == steps - 1) umma_commit(bar_q_free);
+        }
+        __syncwarp();
+      };
+      ok = wait(bar_q_full, k);
+#pragma unroll 1
+      for (int u = -2; ok && u < steps; ++u) {
+        if (u >= 0) {
+          const int s = u & 1, t = g + (kPair ? u >> 1 : u), first = u < 2;
+          bool w = wait(bar_p_full + 8 * s, n_pv[s]) && wait(bar_v16_full + 8 * (t & 1), t / 2);
+          if (first && k > 0) w = w && wait(bar_o_free + 8 * s, k - 1);
+          ok = w;
+          if (!ok) break;
+          n_pv[0] += 1 - s, n_pv[1] += s;
+          tc_fence_after();
+          const uint64_t dv = dv0 + (uint64_t)(((t & 1) * 2 * G::kTile) >> 4);
+          if (elect_one()) {
+#pragma unroll 1
+            for (int ks = 0; ks < kKeys / 16; ++ks)
+              umma_ts(tm + kTmemO + s * 128, tm + kTmemS + s * 128 + ks * 8, dv + ((ks * 2048) >> 4), idesc16(D), !first || ks > 0);
+            if (!kPair || s == 1) umma_commit(bar_v16_free + 8 * (t & 1));
+            umma_commit(bar_pv_done + 8 * s);
+          }
+          __syncwarp();
+        }
+        if (u + 2 < steps) qk(u + 2);
+      }
+    }
+   }
+  } else {
+    registers_up();
+    // ============================ softmax and epilogue ============================
+    const int s = warp >> 2, tr = tid & 127;      // stream, tile row
+    const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
+    const uint32_t ts = tmem + lanes + kTmemS + s * 128, to = tmem + lanes + kTmemO + s * 128;
+    const int copy = tr / kPad, key0 = copy * kMine, r = kPair ? tid : tr % kPad;      // row of the item
+    PagedJoin join = {0, 0, 0, 0, 0, 0};      // thread 0's
+    int g = 0, n = 0, meets = 0;      // key tiles of the pieces before, steps of this stream
+    for (int k = 0; ok && walk.piece(a); g += walk.n_tiles, walk.next(a), ++k) {
+      if (a.split && tid == 0) walk.note_join(join);
+      const bool mine = r < it.rows, busy = (kPair ? 32 * warp : (32 * (warp & 3)) % kPad) < it.rows;
+      const Row row = row_of(a, it, mine ? r : 0);
+      const int end = mine ? row.end : 0;
+      ok = wait(bar_q_full, k);
+      if (!ok) break;
+      const float steep = mine ? fminf(factor_s[r] * 0x1p24f, 0x1p126f) : 1.f;      // K's scales are 2^-24 of themselves
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar_q_free);
+      float m = -INFINITY, l = 0.f;      // m: the largest score before its factor
+      uint32_t vref = 27;                // biased exponent of the reference of V's scales
+      const int steps = kPair ? 2 * walk.n_tiles : walk.n_tiles;
+      int done = 0;
+      for (int u = s; u < steps; u += 2, ++n, ++done) {
+        const int i = kPair ? u >> 1 : u, t = g + i, x = (walk.tile0 + i) * kKeys;
+        const bool all = paged_all_visible(a.s, it.q, x, kKeys);
+        ok = wait(bar_sc_ready + 8 * (t % kScaleRing), t / kScaleRing) && wait(bar_s_full + 8 * s, n);
+        if (!ok) break;
+        tc_fence_after();
+        if (busy) {
+          const float *ks = scale_s + (t % kScaleRing) * 256, *vs = ks + 128;
+          const Seen seen = seen_keys(a.s, it.q, x, end);
+          // V's scales are relative to a reference that may have risen
+          const uint32_t vnow = vref_s[t % kScaleRing];
+          const int drop = 127 + (int)vref - (int)vnow;
+          float keep = vnow == vref ? 1.f : __uint_as_float(drop > 0 ? (uint32_t)drop << 23 : 0u);      // of O
+          vref = vnow;
+          // kHeld keys at a time, whose scores stay in registers: their largest, then their weights.  The reference m of the scores moves only
+          // when a weight would pass it by 2^4, and O with it, and the weights of the tile's keys before: rarely.
+          constexpr int kHeld = kMine < 64 ? kMine : 64;
+          auto weigh = [&](auto every, int c0) {      // std::true_type: no key of the tile is hidden
+            constexpr bool kAll = decltype(every)::value;
+            uint32_t z[kHeld];
+#pragma unroll
+            for (int c = 0; c < kHeld; c += 32) tmem_ld32(ts + key0 + c0 + c, z + c);
+            const float *kc = ks + key0 + c0, *vc = vs + key0 + c0;
+            uint32_t bits[kHeld / 32];
+#pragma unroll
+            for (int c = 0; c < kHeld / 32; ++c) bits[c] = kAll ? 0xffffffffu : seen.bits(key0 + c0 + 32 * c);
+            tmem_wait_ld();
+            float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+            for (int e = 0; e < kHeld; e += 4) {
+              const float4 f = *reinterpret_cast<const float4 *>(kc + e);
+              // rounded before the reference is taken off: equal keys stay equal
+              float y[4] = {__fmul_rn(__uint_as_float(z[e]), f.x), __fmul_rn(__uint_as_float(z[e + 1]), f.y),
+                            __fmul_rn(__uint_as_float(z[e + 2]), f.z), __fmul_rn(__uint_as_float(z[e + 3]), f.w)};
+#pragma unroll
+              for (int h = 0; h < 4; ++h) {
+                if (!kAll && !((bits[e / 32] >> ((e + h) & 31)) & 1)) y[h] = -INFINITY;
+                z[e + h] = __float_as_uint(y[h]);
+              }
+              tops[e / 4 & 1] = fmax3(tops[e / 4 & 1], y[0], y[1]), tops[2 + (e / 4 & 1)] = fmax3(tops[2 + (e / 4 & 1)], y[2], y[3]);
+            }
+            const float top = fmaxf(fmax3(tops[0], tops[1], tops[2]), tops[3]);
+            const bool over = mine && (m == -INFINITY ? top > m : (top - m) * steep > W::kLag);
+            if (__any_sync(0xffffffffu, over || keep != 1.f)) {
+              const float fall = !over ? 1.f : m == -INFINITY ? 0.f : ex2_approx((m - top) * steep);
+              if (over) m = top;
+              l *= fall;
+              keep *= fall;
+              if (done > 0) {
+                ok = wait(bar_pv_done + 8 * s, n - 1);
+                if (!ok) return;
+                tc_fence_after();
+#pragma unroll 1
+                for (int c = 0; c < D; c += 16) {
+                  uint32_t o[16];
+                  tmem_ld16(to + c, o);
+                  tmem_wait_ld();
+#pragma unroll
+                  for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * keep);
+                  tmem_st16(to + c, o);
+                }
+              }
+              if (c0 > 0) {
+                tmem_wait_st();
+                const uint32_t f2x = pack_half(fall, fall);
+#pragma unroll 1
+                for (int c = 0; c < c0 / 2; c += 8) {
+                  uint32_t o[8];
+                  tmem_ld8(ts + (key0 / 2) + c, o);
+                  tmem_wait_ld();
+#pragma unroll
+                  for (int e = 0; e < 8; ++e) o[e] = mul_halves(o[e], f2x);
+                  tmem_st8(ts + (key0 / 2) + c, o);
+                }
+              }
+              keep = 1.f;
+            }
+            const float ref = m == -INFINITY ? 0.f : m;      // nothing seen yet: exp(-inf) = 0
+            const F2 ref2 = f2(-ref, -ref), steep2 = f2(steep, steep);
+            F2 l2[2] = {0, 0};
+#pragma unroll
+            for (int e = 0; e < kHeld; e += 4) {
+              const ulonglong2 v = *reinterpret_cast<const ulonglong2 *>(vc + e);
+#pragma unroll
+              for (int h = 0; h < 4; h += 2) {
+                float2 q = f2_get(mul2(add2(f2(__uint_as_float(z[e + h]), __uint_as_float(z[e + h + 1])), ref2), steep2));
+                q.x = ex2_approx(q.x), q.y = ex2_approx(q.y);
+                const F2 weight = f2(q.x, q.y);
+                l2[h / 2] = add2(l2[h / 2], weight);
+                float2 b = f2_get(mul2(weight, h ? v.y : v.x));
+                if (!kAll) {      // zero times a scale that is not finite
+                  if (!((bits[e / 32] >> ((e + h) & 31)) & 1)) b.x = 0.f;
+                  if (!((bits[e / 32] >> ((e + h + 1) & 31)) & 1)) b.y = 0.f;
+                }
+                z[(e + h) / 2] = pack_half(b.x, b.y);
+              }
+            }
+            const float2 sum = f2_get(add2(l2[0], l2[1]));
+            l += sum.x + sum.y;
+            // over scores that have been read, or are another copy's
+#pragma unroll
+            for (int c = 0; c < kHeld / 2; c += 16) tmem_st16(ts + (key0 + c0) / 2 + c, z + c);
+          };
+#pragma unroll 1
+          for (int c0 = 0; ok && c0 < kMine; c0 += kHeld) {
+            if (all) weigh(std::true_type(), c0);
+            else weigh(std::false_type(), c0);
+          }
+          if (!ok) break;
+          if constexpr (kCopies > 1) {      // no weight for the other copies' keys
+            uint32_t z[16] = {};
+#pragma unroll
+            for (int c = 0; c < kKeys / 2; c += 16)
+              if (c < key0 / 2 || c >= (key0 + kMine) / 2) tmem_st16(ts + c, z);
+          }
+          tmem_wait_st();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(bar_p_full + 8 * s);
+          mbar_arrive(bar_sc_free + 8 * (t % kScaleRing));
+        }
+      }
+      if (!ok) break;
+      // ---- the piece is done
+      if (m != -INFINITY) m *= steep;
+      if (done > 0) {
+        ok = wait(bar_pv_done + 8 * s, n - 1);
+        if (!ok) break;
+        tc_fence_after();
+      }
+      const bool whole = walk.whole();
+      const int x0 = walk.tile0 * kKeys, n_keys = walk.n_tiles * kKeys;
+      const long long slot = (long long)paged_slot(blockIdx.x, walk.first) * a.part_rows;
+      const float vfull = __uint_as_float(vref << 23);
+      // O times this is a share of the output, or of the part's sums: O vref by the reference's weight, over the sum of weights or shrunk
+      auto share = [&](float sum) { return whole ? (sum == 0.f ? 0.f : 1.f / (W::kOne * sum)) : a.shrink / W::kOne; };
+      // to be called when all products of the piece, of both streams, are done: the tiles that they read have then been looked through
+      bool nan = false;
+      auto checked = [&](float4 v, int end, int d) {
+        return __builtin_expect(nan, 0) ? with_nan(v, nan_elements(a, walk.it, x0, n_keys, end, d)) : v;
+      };
+      auto finish_row = [&](const Row &row, int r, float top, float sum) {
+        if (!whole) a.part_ml[slot + r] = make_float2(top, sum);
+        else if (p.lse) p.lse[row.n * p.Hq + row.h] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
+      };
+      if constexpr (kPair) {
+        nan = *v_nan != 0;
+        if (busy) {
+          const float by = share(l);
+#pragma unroll 1
+          for (int c = 0; c < D; c += 32) {
+            uint32_t o[32];
+            tmem_ld32(to + c, o);
+            tmem_wait_ld();
+            if (!mine) continue;
+#pragma unroll
+            for (int e = 0; e < 32; e += 8) {
+              float4 v[2];
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                const uint32_t *q = o + e + 4 * h;
+                v[h] = checked(make_float4(__uint_as_float(q[0]) * by * vfull, __uint_as_float(q[1]) * by * vfull,
+                                           __uint_as_float(q[2]) * by * vfull, __uint_as_float(q[3]) * by * vfull), end, c + e + 4 * h);
+              }
+              if (whole) {
+                *reinterpret_cast<uint4 *>(reinterpret_cast<T *>(p.out) + row.n * p.out_stride[0] + row.h * p.out_stride[1] + c + e) =
+                    make_uint4(pack_bf16(v[0].x, v[0].y), pack_bf16(v[0].z, v[0].w), pack_bf16(v[1].x, v[1].y), pack_bf16(v[1].z, v[1].w));
+              } else {
+                float4 *dst = reinterpret_cast<float4 *>(a.part_o + (slot + r) * D + c + e);
+                dst[0] = v[0], dst[1] = v[1];
+              }
+            }
+          }
+          if (mine) finish_row(row, r, m, l);
+        }
+      } else {
+        // ---- join the streams and copies of a row: each brings its O to the row's reference and writes it down, and they are added up
+        constexpr int J = G::kJoinDims, kQuads = J / 4;
+        float2 *ml_s = reinterpret_cast<float2 *>(smem + G::kOffMl);
+        auto quad = [&](int i, int q) { return reinterpret_cast<float4 *>(smem + G::kOffV16 + i * (4 * J)) + (q ^ (i & 7)); };
+        auto meet = [&]() {
+          __syncwarp();
+          if (lane == 0) mbar_arrive(bar_meet);
+          ok = wait(bar_meet, meets++);
+        };
+        ml_s[tid] = make_float2(m, l);
+        meet();      // all products have been waited for, too: V's tiles are free
+        if (!ok) break;
+        nan = *v_nan != 0;
+        const int rr = tr % kPad;
+        float top = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < 2 * kCopies; ++j) top = fmaxf(top, ml_s[j * kPad + rr].x);
+#pragma unroll
+        for (int j = 0; j < 2 * kCopies; ++j) {
+          const float2 ml = ml_s[j * kPad + rr];
+          sum = fmaf(ml.y, ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - top), sum);
+        }
+        const float by = (m == -INFINITY ? 0.f : ex2_approx(m - top)) * share(sum);
+        if (s == 0 && copy == 0 && mine) finish_row(row, r, top, sum);
+#pragma unroll 1
+        for (int c = 0; ok && c < D; c += J) {
+          if (busy) {
+#pragma unroll 1
+            for (int c2 = 0; c2 < J; c2 += 16) {
+              uint32_t o[16];
+              tmem_ld16(to + c + c2, o);
+              tmem_wait_ld();
+#pragma unroll
+              for (int e = 0; e < 16; e += 4)      // a stream without a tile has nothing in O
+                *quad(tid, (c2 + e) / 4) = done > 0 ? make_float4(__uint_as_float(o[e]) * by * vfull, __uint_as_float(o[e + 1]) * by * vfull,
+                                                                  __uint_as_float(o[e + 2]) * by * vfull, __uint_as_float(o[e + 3]) * by * vfull)
+                                                    : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+          }
+          meet();
+          if (!ok) break;
+#pragma unroll 1
+          for (int e = tid; e < it.rows * kQuads; e += 32 * kSoftmaxWarps) {
+            const int i = e / kQuads, q = e % kQuads;
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int j = 0; j < 2 * kCopies; ++j) {
+              const float4 o = *quad(j * kPad + i, q);
+              v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
+            }
+            const Row to_row = row_of(a, it, i);
+            v = checked(v, to_row.end, c + 4 * q);
+            if (whole) store4(reinterpret_cast<T *>(p.out) + to_row.n * p.out_stride[0] + to_row.h * p.out_stride[1] + c + 4 * q, v);
+            else *reinterpret_cast<float4 *>(a.part_o + (slot + i) * D + c + 4 * q) = v;
+          }
+          if (c + J < D) meet();      // the buffer is read
+        }
+        if (!ok) break;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_joined);
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar_o_free + 8 * s);
+    }
+    if (a.split && tid == 0) a.joins[blockIdx.x] = join;
+  }
+
+  if (!ok) flags |= DS_DEV_TIMEOUT;
+  if (flags && p.status) atomicOr(p.status, flags);
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kMmaWarp) {
+    tc_fence_after();
+    tmem_dealloc(tmem, kTmemCols);
+  }
+}
+
+size_t workspace_of(const Shape &h) { return h.tiles <= kWholeTiles || h.grid == 1 ? 0 : h.workspace(); }
+
+long long rows_per_head(const ds_paged_params &p) { return (long long)p.max_q * (p.Hq / p.Hkv); }
+int tile_rows(const ds_paged_params &p) {
+  const long long rows = rows_per_head(p);
+  return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
+}
+Shape shape_for(const ds_paged_params &p) { return shape_of(p, kKeys, tile_rows(p), kMinTiles, 1); }
+
+template <int D, bool kPair, int kCopies>
+int launch(const ds_paged8_params &p, cudaStream_t stream) {
+  using G = Geo<D, kPair>;
+  const Shape h = shape_for(p.a);
+  const Args8 a = args8_of(p, h, workspace_of(h));
+  static std::atomic<unsigned long long> allowed{0};
+  DS_CUDA_OK(allow_smem(attn_paged8_tc_kernel<D, kPair, kCopies>, G::kBytes, allowed));
+  DS_CUDA_OK(launch_kernel(attn_paged8_tc_kernel<D, kPair, kCopies>, dim3(h.grid), kThreads, G::kBytes, 0, false, stream, a));
+  note_launch(1);
+  return a.split ? launch_join<__nv_bfloat16, D>(a, h, stream) : (int)DS_OK;
+}
+
+template <int D>
+int launch_rows_of(const ds_paged8_params &p, cudaStream_t stream) {
+  switch (tile_rows(p.a)) {
+    case 32: return launch<D, false, 4>(p, stream);
+    case 64: return launch<D, false, 2>(p, stream);
+    case 128: return launch<D, false, 1>(p, stream);
+    default: return launch<D, true, 1>(p, stream);
+  }
+}
+
+}  // namespace
+
+bool attn_paged8_tc_counts_fit(const ds_paged_params &p) {
+  const PagedShape s = units_of(p, kKeys, tile_rows(p));
+  return paged_units_fit(s, longest_of(s));
+}
+
+size_t attn_paged8_tc_workspace_bytes(const ds_paged_params &p) { return workspace_of(shape_for(p)); }
+
+int launch_attn_paged8_tc(const ds_paged8_params &p, cudaStream_t stream) {
+  return p.a.D == 64 ? launch_rows_of<64>(p, stream) : launch_rows_of<128>(p, stream);
+}
+
+}  // namespace ds

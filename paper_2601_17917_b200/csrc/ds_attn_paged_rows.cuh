@@ -73,7 +73,7 @@ __device__ __forceinline__ void stream_keys(const typename Rows::Args &a, const 
   uint8_t *ring = smem + warp * L::kRing;
   const float scale2 = p.scale * kLog2e;
   Rows rows;
-  rows.begin(a, it, smem + L::kOffQ);
+  if constexpr (!Rows::kScaled) rows.begin(a, it, smem + L::kOffQ);
   constexpr int kStages = Rows::kStages, kChunks = Rows::kRowBytes / 16, kOps = Rows::kKeys * kChunks / 32;
   const int32_t *table = p.block_table + it.b * p.table_stride;
   const uint8_t *kbase = reinterpret_cast<const uint8_t *>(reinterpret_cast<const T *>(p.k_cache) + it.g * p.cache_stride[1]);
@@ -164,6 +164,7 @@ __device__ __forceinline__ void stream_keys(const typename Rows::Args &a, const 
     if (i < n_tiles) issue(i);
     cp_async_commit();
   }
+  if constexpr (Rows::kScaled) rows.begin(a, it, smem + L::kOffQ);      // queries through shared memory, behind the first keys
   for (int i = 0; i < n_tiles; ++i) {
     cp_async_wait<kStages - 2>();
     __syncwarp();      // stage i is there for the whole warp, and the warp is done with stage i - 1

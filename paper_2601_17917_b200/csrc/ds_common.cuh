@@ -144,6 +144,9 @@ int launch_kv8_read(const ds_kv8_read_params &p, cudaStream_t stream);
 int launch_attn_paged8(const ds_paged8_params &p, cudaStream_t stream);
 size_t attn_paged8_workspace_bytes(const ds_paged8_params &p);
 bool attn_paged8_counts_fit(const ds_paged8_params &p);
+bool attn_paged8_tc_counts_fit(const ds_paged_params &p);
+size_t attn_paged8_tc_workspace_bytes(const ds_paged_params &p);
+int launch_attn_paged8_tc(const ds_paged8_params &p, cudaStream_t stream);
 int launch_bounded_wait_selftest(uint32_t poll_limit, uint32_t *status, int32_t *report, cudaStream_t stream);
 void note_cuda_error(int code);  // remembered per host thread for ds_last_cuda_error
 int launch_attn_simt(const ds_attn_params &p, cudaStream_t stream);

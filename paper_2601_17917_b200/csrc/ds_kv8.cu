@@ -533,7 +533,7 @@ int launch_read(const ds_kv8_read_params &p, cudaStream_t stream) {
   ReadLaunch w;
   w.items = 2 * p.Hkv;
   // Rows of a CTA: what its threads hold at a time, fewer where there are few; then the heads are divided, too.
-  const long long rows = p.out_start ? p.N : (long long)p.B * p.N, enough = 4LL * sm_count();
+  const long long rows = p.out_start ? p.N : (long long)p.B * p.N, enough = 3LL * sm_count();
   const int at_a_time = kThreads / (p.D / 8);
   w.rows = at_a_time < kReadRows ? at_a_time : kReadRows;      // kThreads / (D / 8) is at least 8
   while (w.rows > 1 && rows / w.rows < enough) w.rows = (w.rows + 1) / 2;

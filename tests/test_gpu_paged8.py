@@ -5,10 +5,13 @@ bits is rounded to 24 and then to the type), so bytes, scales and bf16 rows are 
 
 Attention: tolerances as in ``test_gpu_paged.py`` (an output is rounded once; scores, weights and sums count against
 spread = sum_t p_t |v_t|), with what is different here:
-* queries are fp16 with a power of two per row: exact for bf16, for fp32 two parts, the second rounded at 2^-11 of at most 2^-11 of the
-  value: 2^-22 reach; what fp16 drops below 2^-25 of a row scaled to 2^14: 2^-39 max|q| sum|k|;
-* weights are fp16, half a step 2^-11, for fp32 outputs two parts, 2^-22; what is dropped below 2^-25 of weights scaled by 2^10, of
-  values up to 448 times the largest scale's next power of two, at most 4 max|v|: n 2^-33 max|v| (the sum of weights is at least 1).
+* queries are scaled by a power of two per row.  bf16: exact in fp16, or as e4m3 plus e5m2 (rows scaled to 2^7) but for elements below
+  2^-6, whose e4m3 part is a multiple of 2^-9 and whose rest, at most 2^-10, is rounded to 3 bits, half a step 2^-14: 2^-21 max|q| sum|k|.
+  fp32: two fp16 parts, the second rounded at 2^-11 of at most 2^-11 of the value: 2^-22 reach; what fp16 drops below 2^-25 of a
+  row scaled to 2^14: 2^-39 max|q| sum|k|;
+* weights are fp16, half a step 2^-11, for fp32 outputs two parts, 2^-22; what is dropped below 2^-25 of weights scaled by 2^6 (fp32: 2^10),
+  of values up to 448 times the largest scale's next power of two, at most 4 max|v|: n 2^-29 (2^-33) max|v| (the sum of weights is at
+  least 1).
 """
 import copy
 import math
@@ -413,9 +416,9 @@ def compare8(out, lse, ref, dtype, D, n, q, scale, most_v, most_k, keep=None):
     if keep is not None:
         want, want_lse, spread, reach, got, got_lse, most_q = (x[keep] for x in (want, want_lse, spread, reach, got, got_lse, most_q))
     bf = dtype == BF
-    E = (D + 4) * U * reach + 2.0 ** -39 * abs(scale) * most_q * most_k + (0.0 if bf else 2.0 ** -22 * reach)
+    E = (D + 4) * U * reach + (2.0 ** -21 if bf else 2.0 ** -39) * abs(scale) * most_q * most_k + (0.0 if bf else 2.0 ** -22 * reach)
     weights = 2 * (2 * E + 2.0 ** -21 + (2.0 ** -11 if bf else 2.0 ** -22)) + 4 * (16 + math.sqrt(n)) * U
-    tol = (2.0 ** -8 if bf else U) * np.abs(want) + weights[..., None] * spread + n * 2.0 ** -33 * most_v
+    tol = (2.0 ** -8 if bf else U) * np.abs(want) + weights[..., None] * spread + n * (2.0 ** -29 if bf else 2.0 ** -33) * most_v
     assert np.isfinite(want).all()
     err = np.abs(got - want)
     assert (err <= tol).all(), (np.nanmax(err - tol), np.isnan(got).sum(), np.argwhere(~(err <= tol))[:4])
@@ -572,7 +575,7 @@ def test_equal_keys_give_the_plain_average_at_any_size(path):
     G = c.q.shape[1] // c.codes[0].shape[1]
     want, spread = (x.mean(0).repeat(G, 0) for x in (v, np.abs(v)))
     w = 2.0 ** -11 if c.dtype == BF else 2.0 ** -22
-    tol = (2.0 ** -8 if c.dtype == BF else U) * np.abs(want) + (2 * w + 4 * (16 + math.sqrt(n)) * U) * spread + n * 2.0 ** -33 * c.extremes()[0]
+    tol = (2.0 ** -8 if c.dtype == BF else U) * np.abs(want) + (2 * w + 4 * (16 + math.sqrt(n)) * U) * spread + n * (2.0 ** -29 if c.dtype == BF else 2.0 ** -33) * c.extremes()[0]
     assert (np.abs(f64(out[:rows]) - want) <= tol).all()
     assert torch.isfinite(lse[:rows]).all() and (lse[:rows] < -1e30).all()
 
