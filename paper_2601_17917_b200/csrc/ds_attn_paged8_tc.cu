@@ -41,7 +41,7 @@ using namespace paged;
 using namespace sm100;
 
 constexpr int kKeys = 128;
-constexpr int kSoftmaxWarps = 8, kMmaWarp = 8, kLoadWarp = 9, kConvertWarp = 12, kConvertWarps = 4;
+constexpr int kSoftmaxWarps = 8, kMmaWarp = 8, kLoadWarp = 10, kLoadWarps = 2, kConvertWarp = 12, kConvertWarps = 4;
 constexpr int kThreads = 32 * (kConvertWarp + kConvertWarps);
 constexpr int kMinTiles = 2;       // a range has at least so many key tiles
 constexpr int kWholeTiles = 2;     // items of at most so many key tiles are not split
@@ -53,7 +53,7 @@ template <int D, bool kPair>
 struct Geo {
   static constexpr int kTile = 128 * D;      // bytes of 128 e4m3 rows
   static constexpr int kRows = kPair ? 256 : 128;
-  static constexpr int kSlots = kPair ? 2 : 3;      // of the rings of K and of V; a loading warp each
+  static constexpr int kSlots = kPair ? 2 : 3;      // of the rings of K and of V
   static constexpr int kQPart = kRows * D;          // one part of the queries
   static constexpr int kOffK = 2 * kQPart;
   static constexpr int kOffV = kOffK + kSlots * kTile;
@@ -65,7 +65,7 @@ struct Geo {
   // k_full, k_empty, v_full, v_empty [kSlots], v16_full, v16_free [2], scale_ready, scale_free [kScaleRing], s_full, p_full, pv_done, o_free
   // [2], q_full, q_free, meet, joined
   static constexpr int kNumBars = 4 * kSlots + 4 + 2 * kScaleRing + 8 + 4;
-  static constexpr int kOffMisc = kOffBar + 8 * kNumBars;      // TMEM base, abort flag, NaN in V, references of the scales [kScaleRing]
+  static constexpr int kOffMisc = kOffBar + 8 * kNumBars;      // TMEM base, unused, NaN in V, references of the scales [kScaleRing]
   static constexpr int kOffScan = (kOffMisc + 12 + 4 * kScaleRing + 7) / 8 * 8;
   static constexpr int kBytes = kOffScan + 8 * (kThreads / 32 + 2) + 1024;      // slack: the base is aligned to 1024
   static constexpr int kJoinDims = D == 128 ? 64 : 32;                          // 256 rows of so many fp32 fit into the tiles of V
@@ -111,30 +111,26 @@ __device__ __forceinline__ uint64_t rows_desc(uint32_t addr, int row) {
 __host__ __device__ constexpr uint32_t idesc8(int n, bool a_e5m2) { return (1u << 4) | ((a_e5m2 ? 1u : 0u) << 7) | ((uint32_t)(n >> 3) << 17) | (8u << 24); }
 __host__ __device__ constexpr uint32_t idesc16(int n) { return (1u << 4) | (1u << 16) | ((uint32_t)(n >> 3) << 17) | (8u << 24); }
 
-// Bounded wait that sleeps between its polls: many warps of this kernel wait at a time, and polls take issue slots from the others.
-__device__ __forceinline__ bool mbar_wait_nap(uint32_t bar, uint32_t parity, volatile int *abort_flag) {
-  for (uint32_t it = 0; it < kSpinLimit; ++it) {
-    if (mbar_try_wait(bar, parity)) return true;
-    if (it > 128) __nanosleep(64);
-    if (it > 64 && *abort_flag) return false;
-  }
-  *abort_flag = 1;
-  return false;
+// Bounded wait in few instructions: what runs once per tile comes through the instruction caches at some four cycles each.
+__device__ __forceinline__ bool wait_parity(uint32_t bar, uint32_t parity) {
+  uint32_t left = kSpinLimit;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n"
+      "WAIT:\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "@p bra DONE;\n\t"
+      "sub.u32 %0, %0, 1;\n\t"
+      "setp.ne.u32 q, %0, 0;\n\t"
+      "@q bra WAIT;\n"
+      "DONE:\n\t}"
+      : "+r"(left) : "r"(bar), "r"(parity) : "memory");
+  return left != 0;
 }
-// Registers of a thread: the block's 512 x 128 at launch, for the eight softmax warps 168 and for the eight others 80.
-__device__ __forceinline__ void registers_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 168;"); }
-__device__ __forceinline__ void registers_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 80;"); }
 
 // Arrives at the barrier when this thread's copies so far are complete.
 __device__ __forceinline__ void arrive_when_copied(uint32_t bar) {
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ uint32_t mul_halves(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
-}
-
 // The keys of a tile that a row sees: [0, hi) without [hole, back).
 struct Seen {
   int hi, hole, back;
@@ -195,7 +191,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
                  bar_pv_done = bar_p_full + 16, bar_o_free = bar_pv_done + 16, bar_q_full = bar_o_free + 16, bar_q_free = bar_q_full + 8,
                  bar_meet = bar_q_free + 8, bar_joined = bar_meet + 8;
   volatile uint32_t *tmem_s = reinterpret_cast<volatile uint32_t *>(smem + G::kOffMisc);
-  volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + G::kOffMisc + 4);
   volatile int *v_nan = reinterpret_cast<volatile int *>(smem + G::kOffMisc + 8);      // some tile of V held NaN so far
   volatile uint32_t *vref_s = reinterpret_cast<volatile uint32_t *>(smem + G::kOffMisc + 12);      // biased exponents
   float *scale_s = reinterpret_cast<float *>(smem + G::kOffScale);
@@ -204,7 +199,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
   if (tid == 0) {
     for (int s = 0; s < S; ++s) {
       mbar_init(bar_k_full + 8 * s, 32);
-      mbar_init(bar_k_empty + 8 * s, 1);
+      mbar_init(bar_k_empty + 8 * s, kPair ? 2 : 1);
       mbar_init(bar_v_full + 8 * s, 32);
       mbar_init(bar_v_empty + 8 * s, kConvertWarps);
     }
@@ -214,17 +209,16 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
     }
     for (int s = 0; s < 2; ++s) {
       mbar_init(bar_v16_full + 8 * s, kConvertWarps);
-      mbar_init(bar_v16_free + 8 * s, 1);
+      mbar_init(bar_v16_free + 8 * s, kPair ? 2 : 1);
       mbar_init(bar_s_full + 8 * s, 1);
       mbar_init(bar_p_full + 8 * s, kSoftmaxWarps / 2);
       mbar_init(bar_pv_done + 8 * s, 1);
       mbar_init(bar_o_free + 8 * s, kSoftmaxWarps / 2);
     }
     mbar_init(bar_q_full, kConvertWarps);
-    mbar_init(bar_q_free, 1 + kSoftmaxWarps);
+    mbar_init(bar_q_free, 2 + kSoftmaxWarps);
     mbar_init(bar_meet, kSoftmaxWarps);
     mbar_init(bar_joined, kSoftmaxWarps);
-    *abort_flag = 0;
     *v_nan = 0;
     fence_barrier_init();
   }
@@ -240,10 +234,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
   const Item &it = walk.it;
   bool ok = true;
   // Every wait is the whole warp's.
-  auto wait = [&](uint32_t bar, int phase) { return __all_sync(0xffffffffu, mbar_wait_nap(bar, phase & 1, abort_flag)) != 0; };
+  auto wait = [&](uint32_t bar, int phase) { return __all_sync(0xffffffffu, wait_parity(bar, phase & 1)) != 0; };
 
   if (warp >= kConvertWarp) {
-    registers_down();
     // ============================ queries, V to fp16 ============================
     const int cw = warp - kConvertWarp, cid = tid - 32 * kConvertWarp;
     int g = 0;      // key tiles of the pieces before
@@ -254,16 +247,22 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
       {
         constexpr int E = D / 4, kLoads = E / 8;      // elements of a thread, 16 bytes at a time
         const int u = cid & 3;
+        const int r_end = (it.rows + 7) / 8 * 8;      // whole warps
+        uint4 next[kLoads];
+        auto load = [&](int r) {
+          const Row row = row_of(a, it, r < it.rows ? r : 0);
+          const T *src = reinterpret_cast<const T *>(p.q) + row.n * p.q_stride[0] + row.h * p.q_stride[1] + E * u;
+#pragma unroll
+          for (int i = 0; i < kLoads; ++i) next[i] = *reinterpret_cast<const uint4 *>(src + 8 * i);
+        };
+        if ((cid >> 2) < r_end) load(cid >> 2);
 #pragma unroll 1
-        for (int r = cid >> 2; r < (it.rows + 7) / 8 * 8; r += 8 * kConvertWarps) {      // whole warps
+        for (int r = cid >> 2; r < r_end; r += 8 * kConvertWarps) {
           uint4 w[kLoads];
           const bool there = r < it.rows;
-          {
-            const Row row = row_of(a, it, there ? r : 0);
-            const T *src = reinterpret_cast<const T *>(p.q) + row.n * p.q_stride[0] + row.h * p.q_stride[1] + E * u;
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) w[i] = *reinterpret_cast<const uint4 *>(src + 8 * i);
-          }
+          for (int i = 0; i < kLoads; ++i) w[i] = next[i];
+          if (r + 8 * kConvertWarps < r_end) load(r + 8 * kConvertWarps);
           const QueryScale q = query_scale<kLoads>(w, p.scale);
           if (there && u == 0) factor_s[r] = q.factor;
 #pragma unroll
@@ -317,7 +316,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
         // eight rows side by side, four chunks of each; rows r and r ^ 5 next to each other meet no bank twice, in either layout
         constexpr int kOps = D / 16;
         const int r8 = 32 * cw + ((lane >> 3) ^ (lane & 4 ? 5 : 0)), c4 = lane & 3;
-#pragma unroll 4
+#pragma unroll 2
         for (int o = 0; o < kOps; ++o) {
           const int r = r8 + 8 * (o & 3), c = c4 + 4 * (o >> 2);
           const uint4 w = *reinterpret_cast<const uint4 *>(from + row_at<D>(r, c));
@@ -354,19 +353,18 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
       }
     }
   } else if (warp >= kMmaWarp) {
-   registers_down();
    if (warp >= kLoadWarp) {
     // ============================ K, V, scales ============================
     constexpr int kChunks = D / 16, kPer = 32 / kChunks, kOps = 16 / kPer;      // chunks of a row, rows of an instruction
     const int lw = warp - kLoadWarp, ch = lane % kChunks;
     const long long row_bytes = p.cache_stride[2];
     int g = 0;      // key tiles of the pieces before
-    for (; ok && lw < S && walk.piece(a); g += walk.n_tiles, walk.next(a)) {
+    for (; ok && walk.piece(a); g += walk.n_tiles, walk.next(a)) {
       const int32_t *table = p.block_table + it.b * p.table_stride;
       const uint8_t *kbase = reinterpret_cast<const uint8_t *>(p.k_cache) + it.g * p.cache_stride[1];
       const uint8_t *vbase = reinterpret_cast<const uint8_t *>(p.v_cache) + it.g * p.cache_stride[1];
       const float *kscale = a.k_scale + it.g * a.scale_stride[1], *vscale = a.v_scale + it.g * a.scale_stride[1];
-      int i = (lw + S - g % S) % S;      // this warp's first tile of the piece
+      int i = (lw ^ g) & 1;      // this warp's first tile of the piece
       int pos[4], page[4];               // of keys lane + 32 j
       auto look_up = [&]() {
 #pragma unroll
@@ -376,8 +374,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
         }
       };
       look_up();
-      for (; i < walk.n_tiles; i += S) {
-        const int t = g + i;
+      for (; i < walk.n_tiles; i += kLoadWarps) {
+        const int t = g + i, slot_of_t = t % S;
         // Code that runs for every tile is kept short: five roles share the instruction caches, and with all loops of these copies
         // unrolled (24 KB) every role waited for its instructions (123 us instead of KK).
         long long at[4], scale_at[4];
@@ -398,10 +396,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
         }
 #pragma unroll 1
         for (int v = 0; ok && v < 2; ++v) {
-          ok = wait((v ? bar_v_empty : bar_k_empty) + 8 * lw, t / S + 1);
+          ok = wait((v ? bar_v_empty : bar_k_empty) + 8 * slot_of_t, t / S + 1);
           if (!ok) break;
           const uint8_t *base = (v ? vbase : kbase) + 16 * ch;
-          const uint32_t dst = sbase + (v ? G::kOffV : G::kOffK) + lw * G::kTile;
+          const uint32_t dst = sbase + (v ? G::kOffV : G::kOffK) + slot_of_t * G::kTile;
 #pragma unroll 1
           for (int jh = 0; jh < 8; ++jh) {
             const long long mine = jh < 4 ? (jh < 2 ? at[0] : at[1]) : jh < 6 ? at[2] : at[3];
@@ -418,7 +416,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
               }
             }
           }
-          arrive_when_copied((v ? bar_v_full : bar_k_full) + 8 * lw);
+          arrive_when_copied((v ? bar_v_full : bar_k_full) + 8 * slot_of_t);
           if (v == 0) {
             ok = wait(bar_sc_free + 8 * (t % kScaleRing), t / kScaleRing + 1);
             if (!ok) break;
@@ -430,66 +428,63 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
             }
           }
         }
-        i += S;
+        i += kLoadWarps;
         look_up();      // of this warp's next tile
-        i -= S;
+        i -= kLoadWarps;
       }
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
    } else {
-    // ============================ products ============================
-    const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
-    const uint64_t dq0 = rows_desc(sbase, D), dk0 = rows_desc(sbase + G::kOffK, D), dv0 = smem_desc(sbase + G::kOffV16, kHalfBytes, 1024);
-    int g = 0, n_pv[2] = {0, 0};      // key tiles of the pieces before; products P V of a stream
+    // ============================ products, a warp for each stream ============================
+    const int s = warp - kMmaWarp;
+    const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), ts = tm + kTmemS + s * 128, to = tm + kTmemO + s * 128;
+    const uint64_t dq = rows_desc(sbase + (kPair ? s * 128 * D : 0), D), dk0 = rows_desc(sbase + G::kOffK, D), dv0 = smem_desc(sbase + G::kOffV16, kHalfBytes, 1024);
+    int g = 0, n = 0;      // key tiles of the pieces before; steps of this stream
     for (int k = 0; ok && walk.piece(a); g += walk.n_tiles, walk.next(a), ++k) {
       const int steps = kPair ? 2 * walk.n_tiles : walk.n_tiles;
-      auto qk = [&](int u) {
-        const int s = u & 1, t = g + (kPair ? u >> 1 : u);
-        ok = wait(bar_k_full + 8 * (t % S), t / S);
-        if (!ok) return;
-        fence_proxy_async();
-        tc_fence_after();
-        const uint64_t dq = dq0 + (uint64_t)((kPair ? s * 128 * D : 0) >> 4), dk = dk0 + (uint64_t)(((t % S) * G::kTile) >> 4);
-        if (elect_one()) {
-#pragma unroll 1
-          for (int part = 0; part < 2; ++part)
-#pragma unroll 1
-            for (int ks = 0; ks < D / 32; ++ks)
-              umma_ss8(tm + kTmemS + s * 128, dq + ((part * G::kQPart + ks * 32) >> 4), dk + ((ks * 32) >> 4), idesc8(kKeys, part == 1),
-                       part > 0 || ks > 0);
-          umma_commit(bar_s_full + 8 * s);
-          if (!kPair || s == 1) umma_commit(bar_k_empty + 8 * (t % S));
-          if (u == steps - 1) umma_commit(bar_q_free);
-        }
-        __syncwarp();
-      };
       ok = wait(bar_q_full, k);
+      if (s >= steps && lane == 0) mbar_arrive(bar_q_free);      // nothing for this stream
 #pragma unroll 1
-      for (int u = -2; ok && u < steps; ++u) {
+      for (int u = s - 2; ok && u < steps; u += 2) {
         if (u >= 0) {
-          const int s = u & 1, t = g + (kPair ? u >> 1 : u), first = u < 2;
-          bool w = wait(bar_p_full + 8 * s, n_pv[s]) && wait(bar_v16_full + 8 * (t & 1), t / 2);
-          if (first && k > 0) w = w && wait(bar_o_free + 8 * s, k - 1);
-          ok = w;
+          const int t = g + (kPair ? u >> 1 : u);
+          ok = wait(bar_p_full + 8 * s, n) && wait(bar_v16_full + 8 * (t & 1), t / 2);
+          if (ok && u < 2 && k > 0) ok = wait(bar_o_free + 8 * s, k - 1);
           if (!ok) break;
-          n_pv[0] += 1 - s, n_pv[1] += s;
+          ++n;
           tc_fence_after();
-          const uint64_t dv = dv0 + (uint64_t)(((t & 1) * 2 * G::kTile) >> 4);
           if (elect_one()) {
-#pragma unroll 1
-            for (int ks = 0; ks < kKeys / 16; ++ks)
-              umma_ts(tm + kTmemO + s * 128, tm + kTmemS + s * 128 + ks * 8, dv + ((ks * 2048) >> 4), idesc16(D), !first || ks > 0);
-            if (!kPair || s == 1) umma_commit(bar_v16_free + 8 * (t & 1));
+            uint64_t dv = dv0 + (uint64_t)(((t & 1) * 2 * G::kTile) >> 4);
+#pragma unroll 4
+            for (int ks = 0; ks < kKeys / 16; ++ks, dv += 2048 >> 4) umma_ts(to, ts + ks * 8, dv, idesc16(D), u >= 2 || ks > 0);
+            umma_commit(bar_v16_free + 8 * (t & 1));
             umma_commit(bar_pv_done + 8 * s);
           }
           __syncwarp();
         }
-        if (u + 2 < steps) qk(u + 2);
+        if (u + 2 < steps) {
+          const int t = g + (kPair ? (u + 2) >> 1 : u + 2);
+          ok = wait(bar_k_full + 8 * (t % S), t / S);
+          if (!ok) break;
+          fence_proxy_async();
+          tc_fence_after();
+          if (elect_one()) {
+            const uint64_t dk = dk0 + (uint64_t)(((t % S) * G::kTile) >> 4);
+#pragma unroll
+            for (int part = 0; part < 2; ++part)
+#pragma unroll
+              for (int ks = 0; ks < D / 32; ++ks)
+                umma_ss8(ts, dq + ((part * G::kQPart + ks * 32) >> 4), dk + ((ks * 32) >> 4), idesc8(kKeys, part == 1), part > 0 || ks > 0);
+            umma_commit(bar_s_full + 8 * s);
+            umma_commit(bar_k_empty + 8 * (t % S));
+            if (u + 4 >= steps) umma_commit(bar_q_free);
+          }
+          __syncwarp();
+        }
       }
     }
    }
   } else {
-    registers_up();
     // ============================ softmax and epilogue ============================
     const int s = warp >> 2, tr = tid & 127;      // stream, tile row
     const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
@@ -525,101 +520,86 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
           const int drop = 127 + (int)vref - (int)vnow;
           float keep = vnow == vref ? 1.f : __uint_as_float(drop > 0 ? (uint32_t)drop << 23 : 0u);      // of O
           vref = vnow;
-          // kHeld keys at a time, whose scores stay in registers: their largest, then their weights.  The reference m of the scores moves only
-          // when a weight would pass it by 2^4, and O with it, and the weights of the tile's keys before: rarely.
-          constexpr int kHeld = kMine < 64 ? kMine : 64;
-          auto weigh = [&](auto every, int c0) {      // std::true_type: no key of the tile is hidden
-            constexpr bool kAll = decltype(every)::value;
-            uint32_t z[kHeld];
+          // ---- largest score of this copy's keys, 16 at a time in a short loop
+          float top = -INFINITY, top1 = -INFINITY;
+          uint32_t z[16];
+          float y[16];
+          auto scores = [&](int c) {      // rounded before the reference is taken off: equal keys stay equal
 #pragma unroll
-            for (int c = 0; c < kHeld; c += 32) tmem_ld32(ts + key0 + c0 + c, z + c);
-            const float *kc = ks + key0 + c0, *vc = vs + key0 + c0;
-            uint32_t bits[kHeld / 32];
+            for (int e = 0; e < 16; e += 4) {
+              const float4 f = *reinterpret_cast<const float4 *>(ks + c + e);
+              y[e] = __fmul_rn(__uint_as_float(z[e]), f.x), y[e + 1] = __fmul_rn(__uint_as_float(z[e + 1]), f.y);
+              y[e + 2] = __fmul_rn(__uint_as_float(z[e + 2]), f.z), y[e + 3] = __fmul_rn(__uint_as_float(z[e + 3]), f.w);
+            }
+          };
+          auto hide = [&](int c, float what) {
+            const uint32_t bits = seen.bits(c);
 #pragma unroll
-            for (int c = 0; c < kHeld / 32; ++c) bits[c] = kAll ? 0xffffffffu : seen.bits(key0 + c0 + 32 * c);
+            for (int e = 0; e < 16; ++e) y[e] = (bits >> e) & 1 ? y[e] : what;
+          };
+#pragma unroll 1
+          for (int c = key0; c < key0 + kMine; c += 16) {
+            tmem_ld16(ts + c, z);
             tmem_wait_ld();
-            float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            scores(c);
+            if (!all) hide(c, -INFINITY);
 #pragma unroll
-            for (int e = 0; e < kHeld; e += 4) {
-              const float4 f = *reinterpret_cast<const float4 *>(kc + e);
-              // rounded before the reference is taken off: equal keys stay equal
-              float y[4] = {__fmul_rn(__uint_as_float(z[e]), f.x), __fmul_rn(__uint_as_float(z[e + 1]), f.y),
-                            __fmul_rn(__uint_as_float(z[e + 2]), f.z), __fmul_rn(__uint_as_float(z[e + 3]), f.w)};
-#pragma unroll
-              for (int h = 0; h < 4; ++h) {
-                if (!kAll && !((bits[e / 32] >> ((e + h) & 31)) & 1)) y[h] = -INFINITY;
-                z[e + h] = __float_as_uint(y[h]);
-              }
-              tops[e / 4 & 1] = fmax3(tops[e / 4 & 1], y[0], y[1]), tops[2 + (e / 4 & 1)] = fmax3(tops[2 + (e / 4 & 1)], y[2], y[3]);
-            }
-            const float top = fmaxf(fmax3(tops[0], tops[1], tops[2]), tops[3]);
-            const bool over = mine && (m == -INFINITY ? top > m : (top - m) * steep > W::kLag);
-            if (__any_sync(0xffffffffu, over || keep != 1.f)) {
-              const float fall = !over ? 1.f : m == -INFINITY ? 0.f : ex2_approx((m - top) * steep);
-              if (over) m = top;
-              l *= fall;
-              keep *= fall;
-              if (done > 0) {
-                ok = wait(bar_pv_done + 8 * s, n - 1);
-                if (!ok) return;
-                tc_fence_after();
+            for (int e = 0; e < 16; e += 4) top = fmax3(top, y[e], y[e + 1]), top1 = fmax3(top1, y[e + 2], y[e + 3]);
+          }
+          top = fmaxf(top, top1);
+          // The reference m of the scores moves only when a weight would pass it by 2^kLag, and O with it: rarely.
+          const bool over = mine && (m == -INFINITY ? top > m : (top - m) * steep > W::kLag);
+          if (__any_sync(0xffffffffu, over || keep != 1.f)) {
+            const float fall = !over ? 1.f : m == -INFINITY ? 0.f : ex2_approx((m - top) * steep);
+            if (over) m = top;
+            l *= fall;
+            keep *= fall;
+            if (done > 0) {
+              ok = wait(bar_pv_done + 8 * s, n - 1);
+              if (!ok) break;
+              tc_fence_after();
 #pragma unroll 1
-                for (int c = 0; c < D; c += 16) {
-                  uint32_t o[16];
-                  tmem_ld16(to + c, o);
-                  tmem_wait_ld();
+              for (int c = 0; c < D; c += 16) {
+                tmem_ld16(to + c, z);
+                tmem_wait_ld();
 #pragma unroll
-                  for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * keep);
-                  tmem_st16(to + c, o);
-                }
+                for (int e = 0; e < 16; ++e) z[e] = __float_as_uint(__uint_as_float(z[e]) * keep);
+                tmem_st16(to + c, z);
               }
-              if (c0 > 0) {
-                tmem_wait_st();
-                const uint32_t f2x = pack_half(fall, fall);
-#pragma unroll 1
-                for (int c = 0; c < c0 / 2; c += 8) {
-                  uint32_t o[8];
-                  tmem_ld8(ts + (key0 / 2) + c, o);
-                  tmem_wait_ld();
-#pragma unroll
-                  for (int e = 0; e < 8; ++e) o[e] = mul_halves(o[e], f2x);
-                  tmem_st8(ts + (key0 / 2) + c, o);
-                }
-              }
-              keep = 1.f;
             }
-            const float ref = m == -INFINITY ? 0.f : m;      // nothing seen yet: exp(-inf) = 0
-            const F2 ref2 = f2(-ref, -ref), steep2 = f2(steep, steep);
-            F2 l2[2] = {0, 0};
+          }
+          // ---- weights
+          const float ref = m == -INFINITY ? 0.f : m;      // nothing seen yet: exp(-inf) = 0
+          const F2 ref2 = f2(-ref, -ref), steep2 = f2(steep, steep);
+          F2 l2[2] = {0, 0};
+#pragma unroll 1
+          for (int c = key0; c < key0 + kMine; c += 16) {
+            tmem_ld16(ts + c, z);
+            tmem_wait_ld();
+            scores(c);
+            if (!all) hide(c, -INFINITY);
 #pragma unroll
-            for (int e = 0; e < kHeld; e += 4) {
-              const ulonglong2 v = *reinterpret_cast<const ulonglong2 *>(vc + e);
+            for (int e = 0; e < 16; e += 4) {
+              const ulonglong2 v = *reinterpret_cast<const ulonglong2 *>(vs + c + e);
 #pragma unroll
               for (int h = 0; h < 4; h += 2) {
-                float2 q = f2_get(mul2(add2(f2(__uint_as_float(z[e + h]), __uint_as_float(z[e + h + 1])), ref2), steep2));
+                float2 q = f2_get(mul2(add2(f2(y[e + h], y[e + h + 1]), ref2), steep2));
                 q.x = ex2_approx(q.x), q.y = ex2_approx(q.y);
                 const F2 weight = f2(q.x, q.y);
                 l2[h / 2] = add2(l2[h / 2], weight);
-                float2 b = f2_get(mul2(weight, h ? v.y : v.x));
-                if (!kAll) {      // zero times a scale that is not finite
-                  if (!((bits[e / 32] >> ((e + h) & 31)) & 1)) b.x = 0.f;
-                  if (!((bits[e / 32] >> ((e + h + 1) & 31)) & 1)) b.y = 0.f;
-                }
-                z[(e + h) / 2] = pack_half(b.x, b.y);
+                const float2 b = f2_get(mul2(weight, h ? v.y : v.x));
+                y[e + h] = b.x, y[e + h + 1] = b.y;
               }
             }
-            const float2 sum = f2_get(add2(l2[0], l2[1]));
-            l += sum.x + sum.y;
-            // over scores that have been read, or are another copy's
+            if (!all) hide(c, 0.f);      // zero times a scale that is not finite
+            uint32_t w[8];
 #pragma unroll
-            for (int c = 0; c < kHeld / 2; c += 16) tmem_st16(ts + (key0 + c0) / 2 + c, z + c);
-          };
-#pragma unroll 1
-          for (int c0 = 0; ok && c0 < kMine; c0 += kHeld) {
-            if (all) weigh(std::true_type(), c0);
-            else weigh(std::false_type(), c0);
+            for (int e = 0; e < 8; ++e) w[e] = pack_half(y[2 * e], y[2 * e + 1]);
+            // over scores that have been read, or are another copy's: columns c / 2 .. c / 2 + 7 <= c + 15
+            tmem_st8(ts + c / 2, w);
           }
-          if (!ok) break;
+          const float2 sum2 = f2_get(add2(l2[0], l2[1]));
+          l += sum2.x + sum2.y;
           if constexpr (kCopies > 1) {      // no weight for the other copies' keys
             uint32_t z[16] = {};
 #pragma unroll
