@@ -283,7 +283,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
         __syncwarp();
         if (lane == 0) mbar_arrive(bar_q_full);
       }
-      if (!kPair && k > 0) ok = wait(bar_joined, k - 1);      // the sums of the piece before, which lie in the tiles' place
+      if (k > 0) ok = wait(bar_joined, k - 1);      // the sums of the piece before, which lie in the tiles' place
       // ---- V, tile by tile
       uint32_t vref = 27;      // biased exponent of the reference of V's scales: 2^-100
       for (int i = 0; ok && i < walk.n_tiles; ++i) {
@@ -439,11 +439,14 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
     const int s = warp - kMmaWarp;
     const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), ts = tm + kTmemS + s * 128, to = tm + kTmemO + s * 128;
     const uint64_t dq = rows_desc(sbase + (kPair ? s * 128 * D : 0), D), dk0 = rows_desc(sbase + G::kOffK, D), dv0 = smem_desc(sbase + G::kOffV16, kHalfBytes, 1024);
-    int g = 0, n = 0;      // key tiles of the pieces before; steps of this stream
+    int g = 0, n = 0, n0 = 0;      // key tiles of the pieces before; steps of this stream, of the first one
     for (int k = 0; ok && walk.piece(a); g += walk.n_tiles, walk.next(a), ++k) {
       const int steps = kPair ? 2 * walk.n_tiles : walk.n_tiles;
       ok = wait(bar_q_full, k);
       if (s >= steps && lane == 0) mbar_arrive(bar_q_free);      // nothing for this stream
+      // Half a step apart: the exponentials of one stream beside the products of the other.  (In step, they wait for each other's pipes.)
+      if (ok && s == 1 && s < steps) ok = wait(bar_p_full, n0);
+      n0 += (steps + 1) / 2;
 #pragma unroll 1
       for (int u = s - 2; ok && u < steps; u += 2) {
         if (u >= 0) {
@@ -638,46 +641,57 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
         if (!whole) a.part_ml[slot + r] = make_float2(top, sum);
         else if (p.lse) p.lse[row.n * p.Hq + row.h] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
       };
+      constexpr int J = G::kJoinDims, kQuads = J / 4;
+      auto quad = [&](int i, int q) { return reinterpret_cast<float4 *>(smem + G::kOffV16 + i * (4 * J)) + (q ^ (i & 7)); };
+      auto meet = [&]() {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_meet);
+        ok = wait(bar_meet, meets++);
+      };
+      // O times `by` of dimensions c .. to shared memory, in the place of V's tiles
+      auto put_down = [&](int c, float by) {
+#pragma unroll 1
+        for (int c2 = 0; c2 < J; c2 += 16) {
+          uint32_t o[16];
+          tmem_ld16(to + c + c2, o);
+          tmem_wait_ld();
+#pragma unroll
+          for (int e = 0; e < 16; e += 4)
+            *quad(tid, (c2 + e) / 4) = make_float4(__uint_as_float(o[e]) * by, __uint_as_float(o[e + 1]) * by, __uint_as_float(o[e + 2]) * by,
+                                                  __uint_as_float(o[e + 3]) * by);
+        }
+      };
+      auto put_out = [&](const Row &row, int r, int d, float4 v) {
+        v = checked(v, row.end, d);
+        if (whole) store4(reinterpret_cast<T *>(p.out) + row.n * p.out_stride[0] + row.h * p.out_stride[1] + d, v);
+        else *reinterpret_cast<float4 *>(a.part_o + (slot + r) * D + d) = v;
+      };
       if constexpr (kPair) {
+        // rows are a warp's own; through shared memory, so that neighbouring lanes write neighbouring elements (a row to a thread took 8000
+        // cycles)
+        meet();      // all products have been waited for: V's tiles are free
+        if (!ok) break;
         nan = *v_nan != 0;
         if (busy) {
-          const float by = share(l);
-#pragma unroll 1
-          for (int c = 0; c < D; c += 32) {
-            uint32_t o[32];
-            tmem_ld32(to + c, o);
-            tmem_wait_ld();
-            if (!mine) continue;
-#pragma unroll
-            for (int e = 0; e < 32; e += 8) {
-              float4 v[2];
-#pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                const uint32_t *q = o + e + 4 * h;
-                v[h] = checked(make_float4(__uint_as_float(q[0]) * by * vfull, __uint_as_float(q[1]) * by * vfull,
-                                           __uint_as_float(q[2]) * by * vfull, __uint_as_float(q[3]) * by * vfull), end, c + e + 4 * h);
-              }
-              if (whole) {
-                *reinterpret_cast<uint4 *>(reinterpret_cast<T *>(p.out) + row.n * p.out_stride[0] + row.h * p.out_stride[1] + c + e) =
-                    make_uint4(pack_bf16(v[0].x, v[0].y), pack_bf16(v[0].z, v[0].w), pack_bf16(v[1].x, v[1].y), pack_bf16(v[1].z, v[1].w));
-              } else {
-                float4 *dst = reinterpret_cast<float4 *>(a.part_o + (slot + r) * D + c + e);
-                dst[0] = v[0], dst[1] = v[1];
-              }
-            }
-          }
+          const float by = share(l) * vfull;
           if (mine) finish_row(row, r, m, l);
+#pragma unroll 1
+          for (int c = 0; c < D; c += J) {
+            put_down(c, by);
+            __syncwarp();
+#pragma unroll 1
+            for (int e = lane; e < 32 * kQuads; e += 32) {
+              const int i = 32 * warp + e / kQuads, q = e % kQuads;
+              if (i < it.rows) put_out(row_of(a, it, i), i, c + 4 * q, *quad(i, q));
+            }
+            __syncwarp();
+          }
         }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_joined);
       } else {
         // ---- join the streams and copies of a row: each brings its O to the row's reference and writes it down, and they are added up
-        constexpr int J = G::kJoinDims, kQuads = J / 4;
         float2 *ml_s = reinterpret_cast<float2 *>(smem + G::kOffMl);
-        auto quad = [&](int i, int q) { return reinterpret_cast<float4 *>(smem + G::kOffV16 + i * (4 * J)) + (q ^ (i & 7)); };
-        auto meet = [&]() {
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bar_meet);
-          ok = wait(bar_meet, meets++);
-        };
         ml_s[tid] = make_float2(m, l);
         meet();      // all products have been waited for, too: V's tiles are free
         if (!ok) break;
@@ -691,22 +705,15 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
           const float2 ml = ml_s[j * kPad + rr];
           sum = fmaf(ml.y, ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - top), sum);
         }
-        const float by = (m == -INFINITY ? 0.f : ex2_approx(m - top)) * share(sum);
+        const float by = (m == -INFINITY ? 0.f : ex2_approx(m - top)) * share(sum) * vfull;
         if (s == 0 && copy == 0 && mine) finish_row(row, r, top, sum);
 #pragma unroll 1
         for (int c = 0; ok && c < D; c += J) {
-          if (busy) {
+          if (busy && done > 0) {
+            put_down(c, by);
+          } else if (busy) {      // a stream without a tile has nothing in O
 #pragma unroll 1
-            for (int c2 = 0; c2 < J; c2 += 16) {
-              uint32_t o[16];
-              tmem_ld16(to + c + c2, o);
-              tmem_wait_ld();
-#pragma unroll
-              for (int e = 0; e < 16; e += 4)      // a stream without a tile has nothing in O
-                *quad(tid, (c2 + e) / 4) = done > 0 ? make_float4(__uint_as_float(o[e]) * by * vfull, __uint_as_float(o[e + 1]) * by * vfull,
-                                                                  __uint_as_float(o[e + 2]) * by * vfull, __uint_as_float(o[e + 3]) * by * vfull)
-                                                    : make_float4(0.f, 0.f, 0.f, 0.f);
-            }
+            for (int q = 0; q < kQuads; ++q) *quad(tid, q) = make_float4(0.f, 0.f, 0.f, 0.f);
           }
           meet();
           if (!ok) break;
@@ -719,10 +726,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
               const float4 o = *quad(j * kPad + i, q);
               v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
             }
-            const Row to_row = row_of(a, it, i);
-            v = checked(v, to_row.end, c + 4 * q);
-            if (whole) store4(reinterpret_cast<T *>(p.out) + to_row.n * p.out_stride[0] + to_row.h * p.out_stride[1] + c + 4 * q, v);
-            else *reinterpret_cast<float4 *>(a.part_o + (slot + i) * D + c + 4 * q) = v;
+            put_out(row_of(a, it, i), i, c + 4 * q, v);
           }
           if (c + J < D) meet();      // the buffer is read
         }
