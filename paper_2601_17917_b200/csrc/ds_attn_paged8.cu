@@ -5,9 +5,9 @@
 // instruction, which holds every e4m3 value.
 //
 // K: a lane's four bytes of an ldmatrix are four neighbouring dimensions of a key, two and two of which stand where the
-// product has dimensions 2q, 2q + 1 and 2q + 8, 2q + 9: the queries are laid out in the same order.  V: transposed, a lane's four
-// bytes are two neighbouring dimensions of two neighbouring keys; a byte permutation makes them two fragments, of even and of odd
-// dimensions, and the output is put back in order where it is written.
+// product has dimensions 2q, 2q + 1 and 2q + 8, 2q + 9: the queries are laid out in the same order.  V: transposed as bytes, a lane's four
+// are four neighbouring keys of a dimension, two and two of which stand where the product has keys 2q, 2q + 1 and 2q + 8, 2q + 9; K's rows
+// are taken in the order that puts the weights of these keys there.
 //
 // Queries enter as fp16 too: a row is scaled by a power of two that puts its largest element into [2^14, 2^15), and 11 bits hold bf16's 8
 // down to 2^-31 of that.  fp32 queries are two such parts (22 bits).  The scale of K and the row's factor multiply the score, the scale of V
@@ -30,6 +30,12 @@ __device__ __forceinline__ void mma_half(float (&d)[4], uint32_t a0, uint32_t a1
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// Two 16 x 16 matrices of bytes, transposed: lane 4i + q gets rows 4q .. 4q + 3 of column i and of column i + 8, of either.
+__device__ __forceinline__ void ldmatrix2_trans_bytes(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m16n16.x2.trans.shared.b8 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+
 template <typename T_, int D_, int NB>
 struct ByteRows {
   using T = T_;
@@ -46,7 +52,7 @@ struct ByteRows {
   static constexpr int kQBytes = kOffFactor + kRows * 4;
   static constexpr int kGroups = NB * kParts <= 2 ? 2 : 1;      // 16s of keys at a time
   static constexpr int kCtas = NB == 1 ? (D == 64 ? 4 : 3) : 2, kStages = 2;
-  float o[NB][D / 16][4];      // dimensions 16 j + 2 (lane / 4) (+ 1), rows 2q, 2q + 1
+  float o[NB][D / 16][4];      // dimensions 16 j + lane / 4 (+ 8), rows 2q, 2q + 1
   float m[NB][2], l[NB][2], factor[NB][2];
   int end[NB][2];
   uint32_t qf[kQRegs ? kBlocks : 1][kQRegs ? D / 16 : 1][2];
@@ -132,6 +138,9 @@ struct ByteRows {
     vinv = __uint_as_float((254u + W::kLog2 - e) << 23);
   }
 
+  // The key of 16 that stands in row i of half h of a product: a lane of the second product has four neighbouring keys of V.
+  static __device__ __forceinline__ int key_at(int i, int h) { return 4 * (i >> 1) + (i & 1) + 2 * h; }
+
   // Makes vref the power of two at or above the largest finite scale of V of the stage.
   __device__ __forceinline__ void raise(float mine) {
     const uint32_t b = __float_as_uint(mine) & 0x7fffffffu;
@@ -184,8 +193,8 @@ struct ByteRows {
       }
 #pragma unroll
       for (int g = 0; g < kGroups; ++g) {
-        uint32_t w[4];      // keys 0-7 and 8-15 of dimensions 32 c .. + 15, the same of + 16 .. + 31
-        ldmatrix4(ks + chunk_at<kRowBytes>(16 * (g0 + g) + (lane & 15), 2 * c + (lane >> 4)), w);
+        uint32_t w[4];      // keys key_at(.., 0) and key_at(.., 1) of dimensions 32 c .. + 15, the same of + 16 .. + 31
+        ldmatrix4(ks + chunk_at<kRowBytes>(16 * (g0 + g) + key_at(lane & 7, (lane >> 3) & 1), 2 * c + (lane >> 4)), w);
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
           const uint32_t a0 = halves_lo(w[2 * k]), a1 = halves_lo(w[2 * k + 1]), a2 = halves_hi(w[2 * k]), a3 = halves_hi(w[2 * k + 1]);
@@ -203,7 +212,7 @@ struct ByteRows {
     for (int g = 0; g < kGroups; ++g)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int key = 16 * (g0 + g) + 8 * h + (lane >> 2);
+        const int key = 16 * (g0 + g) + key_at(lane >> 2, h);
         const float kscale = scales[key];
         vscale[g][h] = scales[32 + key] * vinv;
 #pragma unroll
@@ -212,13 +221,13 @@ struct ByteRows {
           for (int e = 0; e < 2; ++e) s[nb][g][2 * h + e] = __fmul_rn(s[nb][g][2 * h + e], factor[nb][e] * kscale);
       }
     const bool partial = !paged_all_visible(a.s, it.q, x + 16 * g0, 16 * kGroups);
-    uint32_t seen[NB] = {};      // only with partial: bit 4g + 2h + e: key 16g + 8h + lane / 4, row 2q + e
+    uint32_t seen[NB] = {};      // only with partial: bit 4g + 2h + e: key 16g + key_at(lane / 4, h), row 2q + e
     if (partial) {
 #pragma unroll
       for (int g = 0; g < kGroups; ++g)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const int pos = paged_key(it.q, x + 16 * (g0 + g) + 8 * h + (lane >> 2));
+          const int pos = paged_key(it.q, x + 16 * (g0 + g) + key_at(lane >> 2, h));
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -256,7 +265,7 @@ struct ByteRows {
           for (int j = 0; j < D / 16; ++j) o[nb][j][e] *= keep, o[nb][j][2 + e] *= keep;
         }
     }
-    uint32_t w[NB][kGroups][kParts][2];      // keys 0-7, 8-15: the weights (their parts), rows 2q and 2q + 1
+    uint32_t w[NB][kGroups][kParts][2];      // keys key_at(.., 0 and 1): the weights (their parts), rows 2q and 2q + 1
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       // nothing seen yet: weights exp(-inf) = 0
@@ -293,13 +302,11 @@ struct ByteRows {
     for (int c = 0; c < D / 32; ++c)
 #pragma unroll
       for (int g = 0; g < kGroups; ++g) {
-        uint32_t v[4];      // dimensions 32 c .. + 15 of keys 0-7 and 8-15, the same of + 16 .. + 31
-        ldmatrix4_trans(vs + chunk_at<kRowBytes>(16 * (g0 + g) + (lane & 15), 2 * c + (lane >> 4)), v);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = __byte_perm(v[k], 0, 0x3120);
+        uint32_t v[4];      // keys 4q .. 4q + 3 of dimensions 32 c + lane / 4, + 8, + 16, + 24
+        ldmatrix2_trans_bytes(vs + chunk_at<kRowBytes>(16 * (g0 + g) + (lane & 15), 2 * c + (lane >> 4)), v);
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          const uint32_t a0 = halves_lo(v[2 * k]), a1 = halves_hi(v[2 * k]), a2 = halves_lo(v[2 * k + 1]), a3 = halves_hi(v[2 * k + 1]);
+          const uint32_t a0 = halves_lo(v[2 * k]), a1 = halves_lo(v[2 * k + 1]), a2 = halves_hi(v[2 * k]), a3 = halves_hi(v[2 * k + 1]);
 #pragma unroll
           for (int part = 0; part < kParts; ++part)
 #pragma unroll
@@ -319,7 +326,8 @@ struct ByteRows {
     if (!__any_sync(0xffffffffu, bad)) return;
 #pragma unroll 1
     for (int key = 0; key < 16 * kGroups; ++key) {
-      const int src = (key & 7) * 4 + (lane & 3), at = 4 * (key >> 4) + 2 * ((key >> 3) & 1);
+      // key_at(i, h) is this key
+      const int src = (((key >> 2) & 3) * 2 + (key & 1)) * 4 + (lane & 3), at = 4 * (key >> 4) + 2 * ((key >> 1) & 1);
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         const uint32_t vis = __shfl_sync(0xffffffffu, seen[nb], src) >> at;
@@ -327,7 +335,7 @@ struct ByteRows {
         for (int j = 0; j < D / 16; ++j)
 #pragma unroll
           for (int odd = 0; odd < 2; ++odd) {
-            const uint8_t b = vbuf[chunk_at<kRowBytes>(16 * g0 + key, j) + 2 * (lane >> 2) + odd];
+            const uint8_t b = vbuf[chunk_at<kRowBytes>(16 * g0 + key, j) + (lane >> 2) + 8 * odd];
             if ((b & 0x7f) != 0x7f) continue;
             if (vis & 1) o[nb][j][2 * odd] = __uint_as_float(0x7fffffffu);
             if (vis & 2) o[nb][j][2 * odd + 1] = __uint_as_float(0x7fffffffu);
@@ -355,7 +363,7 @@ struct ByteRows {
         if (lane < 4) ml[r] = make_float2(m[nb][e], sum);
 #pragma unroll
         for (int j = 0; j < D / 16; ++j)
-          *reinterpret_cast<float2 *>(out + r * D + 16 * j + 2 * (lane >> 2)) = make_float2(o[nb][j][e] * down * vref, o[nb][j][2 + e] * down * vref);
+          out[r * D + 16 * j + (lane >> 2)] = o[nb][j][e] * down * vref, out[r * D + 16 * j + 8 + (lane >> 2)] = o[nb][j][2 + e] * down * vref;
       }
   }
 };
