@@ -36,22 +36,22 @@ __device__ __forceinline__ void ldmatrix2_trans_bytes(uint32_t addr, uint32_t (&
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
 
-template <typename T_, int D_, int NB>
+template <typename T_, int D_, int NB, int kKeys_ = 32>
 struct ByteRows {
   using T = T_;
   using Cache = uint8_t;
   using Args = Args8;
   static constexpr bool kScaled = true;
   using W = Weights8<!std::is_same<T, float>::value>;
-  static constexpr int D = D_, kRows = 8 * NB, kRowBytes = D, kKeys = 32;
+  static constexpr int D = D_, kRows = 8 * NB, kRowBytes = D, kKeys = kKeys_;
   static constexpr int kParts = std::is_same<T, float>::value ? 2 : 1;      // of a query, of a weight
   static constexpr int kBlocks = kParts * NB;                                // of 8 rows of queries
   static constexpr bool kQRegs = kBlocks <= 2;
   static constexpr int kQRowBytes = 2 * D;
   static constexpr int kOffFactor = kBlocks * 8 * kQRowBytes;
-  static constexpr int kQBytes = kOffFactor + kRows * 4;
-  static constexpr int kGroups = NB * kParts <= 2 ? 2 : 1;      // 16s of keys at a time
-  static constexpr int kCtas = NB == 1 ? (D == 64 ? 4 : 3) : 2, kStages = 2;
+  static constexpr int kQSmem = kOffFactor + kRows * 4, kQBytes = kQRegs ? 0 : kQSmem;      // for a moment in the ring, or beside it
+  static constexpr int kGroups = NB * kParts <= 2 && kKeys == 32 ? 2 : 1;      // 16s of keys at a time
+  static constexpr int kCtas = NB == 1 ? (D == 64 || kKeys == 16 ? 4 : 3) : 2, kStages = kKeys == 16 ? 3 : 2;
   float o[NB][D / 16][4];      // dimensions 16 j + lane / 4 (+ 8), rows 2q, 2q + 1
   float m[NB][2], l[NB][2], factor[NB][2];
   int end[NB][2];
@@ -129,6 +129,7 @@ struct ByteRows {
         end[nb][e] = r < it.rows ? row_of(a, it, r).end : 0;
       }
     }
+    if constexpr (kQRegs) __syncthreads();      // warp 0 loads keys there next
     set_vref(27);      // 2^-100
   }
 
@@ -159,12 +160,12 @@ struct ByteRows {
         for (int k = 0; k < 4; ++k) o[nb][j][k] *= keep;
   }
 
-  // 32 keys from x on; K, V and their scales (behind V: 32 of K, 32 of V) as loaded, V is scratch afterwards.
+  // kKeys keys from x on; K, V and their scales (behind V: of K, of V) as loaded, V is scratch afterwards.
   __device__ __forceinline__ void step(const Args8 &a, const Item &it, uint8_t *kbuf, uint8_t *vbuf, int x, float) {
     const float *scales = reinterpret_cast<const float *>(vbuf + kKeys * kRowBytes);
-    raise(scales[32 + (threadIdx.x & 31)]);
+    raise(scales[kKeys + threadIdx.x % kKeys]);
 #pragma unroll
-    for (int g = 0; g < 2; g += kGroups) keys16(a, it, kbuf, vbuf, scales, x, g);
+    for (int g = 0; g < kKeys / 16; g += kGroups) keys16(a, it, kbuf, vbuf, scales, x, g);
   }
 
   // Groups g .. g + kGroups - 1 of 16 keys.
@@ -214,7 +215,7 @@ struct ByteRows {
       for (int h = 0; h < 2; ++h) {
         const int key = 16 * (g0 + g) + key_at(lane >> 2, h);
         const float kscale = scales[key];
-        vscale[g][h] = scales[32 + key] * vinv;
+        vscale[g][h] = scales[kKeys + key] * vinv;
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -381,6 +382,16 @@ auto with_rows(const ds_paged_params &p, F f) {
   return rows <= 8 ? f(ByteRows<float, 128, 1>()) : f(ByteRows<float, 128, 2>());
 }
 
+// As with_rows; with 8 rows of 128 dimensions, items that get CTAs or clusters of their own load 16 keys a stage and run four CTAs
+// an SM: they are short, and start sooner (7.7 -> 7.3 us for one request, 19.4 -> 18.0 for 16 of 8 heads).  Ranges are better off
+// with 32 (186 against 205 us for 32 x 32 heads, 39 against 42 for one request of 131072 rows).
+template <class F>
+auto with_rows_at_length(const ds_paged_params &p, F f) {
+  using Short = ByteRows<__nv_bfloat16, 128, 1, 16>;
+  if (p.dtype == DS_BF16 && p.D == 128 && (long long)p.max_q * (p.Hq / p.Hkv) <= 8 && shape_for<Short>(p).cluster) return f(Short());
+  return with_rows(p, f);
+}
+
 // Rows per KV head from which the kernel with tcgen05 tiles takes over.
 constexpr int kTensorTileRows = 33;
 bool wide(const ds_paged_params &p) { return p.dtype == DS_BF16 && (long long)p.max_q * (p.Hq / p.Hkv) >= kTensorTileRows; }
@@ -399,12 +410,12 @@ bool attn_paged8_counts_fit(const ds_paged8_params &p) {
 size_t attn_paged8_workspace_bytes(const ds_paged8_params &p) {
   if (p.a.B == 0 || p.a.N == 0) return 0;
   if (wide(p.a)) return attn_paged8_tc_workspace_bytes(p.a);
-  return with_rows(p.a, [&](auto rows) { return rows_workspace_of(shape_for<decltype(rows)>(p.a)); });
+  return with_rows_at_length(p.a, [&](auto rows) { return rows_workspace_of(shape_for<decltype(rows)>(p.a)); });
 }
 
 int launch_attn_paged8(const ds_paged8_params &p, cudaStream_t stream) {
   if (wide(p.a)) return launch_attn_paged8_tc(p, stream);
-  return with_rows(p.a, [&](auto rows) {
+  return with_rows_at_length(p.a, [&](auto rows) {
     return launch_rows<decltype(rows)>(p.a, stream, [&](Args8 &a) { set_scales(p, a); });
   });
 }

@@ -97,26 +97,30 @@ __device__ __forceinline__ void stream_keys(const typename Rows::Args &a, const 
       if constexpr (Rows::kScaled) scale_at = ok * a.scale_stride[0] + fast_div(slot, a.scale_div) * a.scale_stride[2];
     }
     if constexpr (Rows::kScaled) {      // a lane per key; of a key that is not there, zero
-      static_assert(Rows::kKeys == 32 && kChunks <= 8, "");
-      cp_async4(dst + 2 * L::kSub + 4 * lane, kscale + scale_at, pos >= 0);
-      cp_async4(dst + 2 * L::kSub + 128 + 4 * lane, vscale + scale_at, pos >= 0);
+      static_assert((Rows::kKeys == 32 || Rows::kKeys == 16) && kChunks <= 8, "");
+      if constexpr (Rows::kKeys == 32) {
+        cp_async4(dst + 2 * L::kSub + 4 * lane, kscale + scale_at, pos >= 0);
+        cp_async4(dst + 2 * L::kSub + 128 + 4 * lane, vscale + scale_at, pos >= 0);
+      } else {
+        cp_async4(dst + 2 * L::kSub + 4 * lane, (lane < 16 ? kscale : vscale) + scale_at, pos >= 0);
+      }
       // 16 keys that lie evenly (in one page) need one address
       const long long at_lo = __shfl_sync(0xffffffffu, at, 0), at_hi = __shfl_sync(0xffffffffu, at, 16);
       const uint32_t even = __ballot_sync(0xffffffffu, at >= 0 && at == (lane < 16 ? at_lo : at_hi) + (lane & 15) * row_bytes);
       const int ch = lane % kChunks;
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
+      for (int half = 0; half < Rows::kKeys / 16; ++half) {
         if (((even >> (16 * half)) & 0xffffu) == 0xffffu) {
           long long from = (half ? at_hi : at_lo) + (lane / kChunks) * row_bytes + 16 * ch;
 #pragma unroll
-          for (int j = 0; j < kOps / 2; ++j, from += (32 / kChunks) * row_bytes) {
+          for (int j = 0; j < kChunks / 2; ++j, from += (32 / kChunks) * row_bytes) {
             const uint32_t to = dst + chunk_at<Rows::kRowBytes>(16 * half + j * (32 / kChunks) + lane / kChunks, ch);
             cp_async16(to, kbase + from, true);
             cp_async16(to + L::kSub, vbase + from, true);
           }
         } else {
 #pragma unroll
-          for (int j = 0; j < kOps / 2; ++j) {
+          for (int j = 0; j < kChunks / 2; ++j) {
             const int r = 16 * half + j * (32 / kChunks) + lane / kChunks;
             const long long off = __shfl_sync(0xffffffffu, at, r);
             const bool there = off >= 0;
@@ -164,7 +168,10 @@ __device__ __forceinline__ void stream_keys(const typename Rows::Args &a, const 
     if (i < n_tiles) issue(i);
     cp_async_commit();
   }
-  if constexpr (Rows::kScaled) rows.begin(a, it, smem + L::kOffQ);      // queries through shared memory, behind the first keys
+  if constexpr (Rows::kScaled) {      // queries through shared memory (the stage that is loaded last, or beside the ring), behind the first keys
+    static_assert(Rows::kQBytes > 0 || Rows::kQSmem <= L::kStage, "");
+    rows.begin(a, it, smem + (Rows::kQBytes ? L::kOffQ : (kStages - 1) * L::kStage));
+  }
   for (int i = 0; i < n_tiles; ++i) {
     cp_async_wait<kStages - 2>();
     __syncwarp();      // stage i is there for the whole warp, and the warp is done with stage i - 1
