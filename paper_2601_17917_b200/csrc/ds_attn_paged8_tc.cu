@@ -43,7 +43,7 @@ using namespace sm100;
 constexpr int kKeys = 128;
 constexpr int kSoftmaxWarps = 8, kMmaWarp = 8, kLoadWarp = 10, kLoadWarps = 2, kConvertWarp = 12, kConvertWarps = 4;
 constexpr int kThreads = 32 * (kConvertWarp + kConvertWarps);
-constexpr int kMinTiles = 2;       // a range has at least so many key tiles
+constexpr int kMinTiles = 2;       // a range has at least so many key tiles, where items are split
 constexpr int kWholeTiles = 2;     // items of at most so many key tiles are not split
 constexpr uint32_t kTmemS = 0, kTmemO = 256, kTmemCols = 512;      // S (2 x 128), O (2 x 128); P over S
 constexpr int kHalfBytes = 128 * 128;      // 128 keys of 64 dimensions in fp16: a swizzled half of a tile of D = 128
@@ -61,16 +61,19 @@ struct Geo {
   static constexpr int kOffScale = kOffV16 + 2 * 2 * kTile;               // [kScaleRing][2][128]
   static constexpr int kOffFactor = kOffScale + kScaleRing * 1024;        // [kRows]
   static constexpr int kOffMl = kOffFactor + kRows * 4;                   // [256]
-  static constexpr int kOffBar = kOffMl + (kPair ? 0 : 256 * 8);
+  static constexpr int kOffTo = kOffMl + (kPair ? 0 : 256 * 8);           // [kRows]
+  static constexpr int kOffBar = kOffTo + kRows * 8;
   // k_full, k_empty, v_full, v_empty [kSlots], v16_full, v16_free [2], scale_ready, scale_free [kScaleRing], s_full, p_full, pv_done, o_free
   // [2], q_full, q_free, meet, joined
   static constexpr int kNumBars = 4 * kSlots + 4 + 2 * kScaleRing + 8 + 4;
   static constexpr int kOffMisc = kOffBar + 8 * kNumBars;      // TMEM base, unused, NaN in V, references of the scales [kScaleRing]
   static constexpr int kOffScan = (kOffMisc + 12 + 4 * kScaleRing + 7) / 8 * 8;
-  static constexpr int kBytes = kOffScan + 8 * (kThreads / 32 + 2) + 1024;      // slack: the base is aligned to 1024
-  static constexpr int kJoinDims = D == 128 ? 64 : 32;                          // 256 rows of so many fp32 fit into the tiles of V
+  // Sums on their way out, [256][kOutDims] fp32.  Of pairs in a place of their own: a stream need not wait for the other's last products.
+  static constexpr int kOutDims = kPair ? 16 : D == 128 ? 64 : 32;
+  static constexpr int kOffOut = kPair ? (kOffScan + 8 * (kThreads / 32 + 2) + 127) / 128 * 128 : kOffV16;
+  static constexpr int kBytes = (kPair ? kOffOut + 256 * kOutDims * 4 : kOffScan + 8 * (kThreads / 32 + 2)) + 1024;      // slack: the base is aligned to 1024
   static_assert(kBytes <= 227 * 1024, "shared memory");
-  static_assert(256 * kJoinDims * 4 <= 4 * kTile, "sums to be joined");
+  static_assert(kPair || 256 * kOutDims * 4 <= 4 * kTile, "sums to be joined");
 };
 
 // Byte offset of 16-byte chunk `c` of row `r` of e4m3 values: the 128-byte swizzle for rows of 128 bytes, the 64-byte one for 64.
@@ -230,7 +233,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
   dependent_sync();
   uint32_t flags = 0;
   Walk walk;
-  walk.find<kThreads>(a, kMinTiles, reinterpret_cast<long long *>(smem + G::kOffScan), flags);
+  walk.find<kThreads>(a, a.split ? kMinTiles : 1, reinterpret_cast<long long *>(smem + G::kOffScan), flags);
   const Item &it = walk.it;
   bool ok = true;
   // Every wait is the whole warp's.
@@ -283,7 +286,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
         __syncwarp();
         if (lane == 0) mbar_arrive(bar_q_full);
       }
-      if (k > 0) ok = wait(bar_joined, k - 1);      // the sums of the piece before, which lie in the tiles' place
+      if (!kPair && k > 0) ok = wait(bar_joined, k - 1);      // the sums of the piece before, which lie in the tiles' place
       // ---- V, tile by tile
       uint32_t vref = 27;      // biased exponent of the reference of V's scales: 2^-100
       for (int i = 0; ok && i < walk.n_tiles; ++i) {
@@ -632,23 +635,22 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
       const float vfull = __uint_as_float(vref << 23);
       // O times this is a share of the output, or of the part's sums: O vref by the reference's weight, over the sum of weights or shrunk
       auto share = [&](float sum) { return whole ? (sum == 0.f ? 0.f : 1.f / (W::kOne * sum)) : a.shrink / W::kOne; };
-      // to be called when all products of the piece, of both streams, are done: the tiles that they read have then been looked through
+      // to be called when the stream's products are done (all of the piece, where a row has two): the tiles that they read have then been
+      // looked through
       bool nan = false;
-      auto checked = [&](float4 v, int end, int d) {
-        return __builtin_expect(nan, 0) ? with_nan(v, nan_elements(a, walk.it, x0, n_keys, end, d)) : v;
-      };
+      auto checked = [&](float4 v, int end, int d) { return with_nan(v, nan_elements(a, walk.it, x0, n_keys, end, d)); };
       auto finish_row = [&](const Row &row, int r, float top, float sum) {
         if (!whole) a.part_ml[slot + r] = make_float2(top, sum);
         else if (p.lse) p.lse[row.n * p.Hq + row.h] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
       };
-      constexpr int J = G::kJoinDims, kQuads = J / 4;
-      auto quad = [&](int i, int q) { return reinterpret_cast<float4 *>(smem + G::kOffV16 + i * (4 * J)) + (q ^ (i & 7)); };
+      constexpr int J = G::kOutDims, kQuads = J / 4;
+      auto quad = [&](int i, int q) { return reinterpret_cast<float4 *>(smem + G::kOffOut + i * (4 * J)) + (q ^ (kQuads == 4 ? (i >> 1) & 3 : i & 7)); };
       auto meet = [&]() {
         __syncwarp();
         if (lane == 0) mbar_arrive(bar_meet);
         ok = wait(bar_meet, meets++);
       };
-      // O times `by` of dimensions c .. to shared memory, in the place of V's tiles
+      // O times `by` of dimensions c .. to shared memory
       auto put_down = [&](int c, float by) {
 #pragma unroll 1
         for (int c2 = 0; c2 < J; c2 += 16) {
@@ -661,16 +663,18 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
                                                   __uint_as_float(o[e + 3]) * by);
         }
       };
-      auto put_out = [&](const Row &row, int r, int d, float4 v) {
-        v = checked(v, row.end, d);
-        if (whole) store4(reinterpret_cast<T *>(p.out) + row.n * p.out_stride[0] + row.h * p.out_stride[1] + d, v);
-        else *reinterpret_cast<float4 *>(a.part_o + (slot + r) * D + d) = v;
+      // Where the elements of a row go: looked up, as working it out for every four of them was half of the epilogue.
+      long long *to_s = reinterpret_cast<long long *>(smem + G::kOffTo);
+      if (mine && (kPair || (s == 0 && copy == 0)))      // (the piece before is written out: its sums were, before this one's products)
+        to_s[r] = whole ? row.n * p.out_stride[0] + row.h * p.out_stride[1] : (slot + r) * D;
+      auto put_out = [&](int r, int d, float4 v) {
+        if (__builtin_expect(nan, 0)) v = checked(v, row_of(a, walk.it, r).end, d);
+        if (whole) store4(reinterpret_cast<T *>(p.out) + to_s[r] + d, v);
+        else *reinterpret_cast<float4 *>(a.part_o + to_s[r] + d) = v;
       };
       if constexpr (kPair) {
         // rows are a warp's own; through shared memory, so that neighbouring lanes write neighbouring elements (a row to a thread took 8000
         // cycles)
-        meet();      // all products have been waited for: V's tiles are free
-        if (!ok) break;
         nan = *v_nan != 0;
         if (busy) {
           const float by = share(l) * vfull;
@@ -680,15 +684,19 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
             put_down(c, by);
             __syncwarp();
 #pragma unroll 1
-            for (int e = lane; e < 32 * kQuads; e += 32) {
-              const int i = 32 * warp + e / kQuads, q = e % kQuads;
-              if (i < it.rows) put_out(row_of(a, it, i), i, c + 4 * q, *quad(i, q));
+            for (int e = lane; e < 32 * kQuads; e += 128) {
+              float4 v[4];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) v[j] = *quad(32 * warp + (e + 32 * j) / kQuads, e % kQuads);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const int i = 32 * warp + (e + 32 * j) / kQuads;
+                if (i < it.rows) put_out(i, c + 4 * (e % kQuads), v[j]);
+              }
             }
             __syncwarp();
           }
         }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar_joined);
       } else {
         // ---- join the streams and copies of a row: each brings its O to the row's reference and writes it down, and they are added up
         float2 *ml_s = reinterpret_cast<float2 *>(smem + G::kOffMl);
@@ -726,7 +734,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
               const float4 o = *quad(j * kPad + i, q);
               v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
             }
-            put_out(row_of(a, it, i), i, c + 4 * q, v);
+            put_out(i, c + 4 * q, v);
           }
           if (c + J < D) meet();      // the buffer is read
         }
@@ -758,7 +766,10 @@ int tile_rows(const ds_paged_params &p) {
   const long long rows = rows_per_head(p);
   return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
 }
-Shape shape_for(const ds_paged_params &p) { return shape_of(p, kKeys, tile_rows(p), kMinTiles, 1); }
+Shape shape_for(const ds_paged_params &p) {
+  const int rows = tile_rows(p);
+  return shape_of(p, kKeys, rows, longest_of(units_of(p, kKeys, rows)).tiles <= kWholeTiles ? 1 : kMinTiles, 1);
+}
 
 template <int D, bool kPair, int kCopies>
 int launch(const ds_paged8_params &p, cudaStream_t stream) {
