@@ -392,14 +392,23 @@ auto with_rows_at_length(const ds_paged_params &p, F f) {
   return with_rows(p, f);
 }
 
-// Rows per KV head from which the kernel with tcgen05 tiles takes over.
+// Rows per KV head from which the kernel with tcgen05 tiles takes over (27 rows: 61 against 68 us; 40: 119 against 84, both 8 x 32 heads
+// x 2000 keys).
 constexpr int kTensorTileRows = 33;
-bool wide(const ds_paged_params &p) { return p.dtype == DS_BF16 && (long long)p.max_q * (p.Hq / p.Hkv) >= kTensorTileRows; }
+bool many_rows(const ds_paged_params &p) { return p.dtype == DS_BF16 && (long long)p.max_q * (p.Hq / p.Hkv) >= kTensorTileRows; }
+// But not for a few short items, which the clusters of the other are done with before a CTA of 200 KB is under way (4 KV heads of 224
+// rows x 1000 keys: 18 against 25 us; at four tiles of 128 keys to a CTA the two are level).
+bool wide(const ds_paged_params &p) {
+  if (!many_rows(p)) return false;
+  using T = __nv_bfloat16;
+  const Shape h = p.D == 64 ? shape_for<ByteRows<T, 64, 4>>(p) : shape_for<ByteRows<T, 128, 4>>(p);
+  return !(h.cluster && 4 * h.items <= 2 * sm_count() && h.tiles <= 3 * h.cluster);
+}
 
 }  // namespace
 
 bool attn_paged8_counts_fit(const ds_paged8_params &p) {
-  if (wide(p.a)) return attn_paged8_tc_counts_fit(p.a);
+  if (many_rows(p.a)) return attn_paged8_tc_counts_fit(p.a);
   return with_rows(p.a, [&](auto engine) {
     using Rows = decltype(engine);
     const PagedShape s = units_of(p.a, Layout<Rows>::kTile, Rows::kRows);

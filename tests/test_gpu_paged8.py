@@ -500,6 +500,9 @@ PATHS = {
     "100 rows": (BF, 128, 8, 2, [3000, 70], [25, 1], 1000),
     "200 rows": (BF, 64, 8, 2, [500, 70], [50, 1], 1000),
     "many rows of many sequences": (BF, 128, 8, 4, [600] * 36, [20] * 36, 1000),
+    "40 rows, items that are not split": (BF, 128, 8, 4, [200, 70] * 12, [10, 20] * 12, 0),
+    "100 rows, items that are not split": (BF, 64, 8, 2, [200, 100] * 10, [25, 1] * 10, 0),
+    "200 rows, items that are not split": (BF, 128, 8, 2, [250, 1] * 10, [50, 50] * 10, 0),
     "fp32 clusters": (F32, 128, 2, 2, [300, 70], [1, 1], 0),
     "fp32 clusters, 16 rows": (F32, 64, 8, 2, [300, 70], [4, 1], 0),
     "fp32 ranges, 40 rows": (F32, 64, 8, 2, [3000, 70], [10, 1], 1000),
@@ -642,7 +645,7 @@ def test_bad_pages_lengths_and_rows_are_flagged_and_reach_no_other_sequence(path
     mine = slice(int(c.starts[1]), int(c.starts[2]))
     for entry in (-5, 10 ** 6, c.codes[0].shape[0], -2 ** 31, 2 ** 31 - 1):
         t = c.table.clone()
-        t[1, 2] = entry
+        t[1, min(2, (c.lens[1] - 1) // c.ps)] = entry
         out, lse, _ = c.run(table=t, status=flag)
         out[mine], lse[mine] = want[mine], want_lse[mine]      # whatever page is read in its place, the others are as they were
         assert torch.equal(out, want) and torch.equal(lse, want_lse)
@@ -725,7 +728,8 @@ def test_refusals_of_the_binding():
 
 # ------------------------------------------------------------------------------------------------ graphs, streams, a serving loop
 @pytest.mark.parametrize("dtype,D,G,n,lens", [(BF, 128, 4, 1, [2000, 300, 77]), (BF, 128, 1, 1, [3000] * 30), (BF, 128, 4, 16, [2000, 300, 77]),
-                                              (BF, 64, 4, 16, [9000, 300, 77]), (F32, 64, 2, 2, [900, 5000, 1])])
+                                              (BF, 64, 4, 16, [9000, 300, 77]),
+                                              (BF, 128, 4, 16, [200, 30] * 12), (F32, 64, 2, 2, [900, 5000, 1])])
 def test_a_captured_call_reads_lengths_rows_and_tables_at_replay(dtype, D, G, n, lens):
     """Captured once with the longest lengths, replayed with others, which put the work on the CTAs differently."""
     B = len(lens)
