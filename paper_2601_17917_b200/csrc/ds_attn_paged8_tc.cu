@@ -12,20 +12,24 @@
 //   kPair      rows 0 .. 127 and 128 .. 255 of an item, over the same key tiles
 //   otherwise  the same rows, the even and the odd key tiles, joined when the item ends.  Up to 64 rows stand in the tile kCopies
 //              times: each copy weighs 1 / kCopies of the keys and has zeros for the others.
-// Step u of a piece is stream u % 2, key tile u (kPair: u / 2).  The products go out in the order QK0 QK1 PV0 QK2 PV1 ..; they execute
-// in order, so a stream's S may be written once the product that reads its P has been issued.
+// Step u of a piece is stream u % 2, key tile u (kPair: u / 2).  A stream's products go out in the order QK0 PV0 QK2 PV2 ..; they execute
+// in order, so S may be written once the product that reads the P in its place has been issued.  The second stream starts half a step
+// later (82 -> 80 us): its exponentials run beside the first one's products.
 //
 // Warps:
 //   0-7    softmax and epilogue, thread = tile row = TMEM lane, four warps a stream
-//   8      issues the products
-//   9-11   load, each the tiles of one slot of the rings: 16-byte asynchronous copies of K (in the swizzle of the products) and V from
-//          wherever the page table says, and the scales
+//   8-9    issue the products, a warp for each stream
+//   10-11  load, every other tile each: 16-byte asynchronous copies of K (in the swizzle of the products) and V from wherever the page
+//          table says, and the scales
 //   12-15  at the start of a piece the queries, four threads a row; then V to fp16, 32 keys each
-// (One set of four warps that loaded and converted took 5500 cycles a tile, most of them in its own instructions: 120 us where this takes
-// KK.)
+// (One set of four warps that loaded and converted took 5500 cycles a tile, most of them in its own instructions: 120 us where this
+// takes 80.)
 //
-// Bound by HBM while a key tile's 32 KB (1430 cycles of an SM's share) hide its products (256 + 256 cycles) and exponentials, which 128
-// rows do: 1024 cycles; beyond, by the exponentials.
+// A key tile's 32 KB are 1430 cycles of an SM's share of HBM; its products 256 (e4m3, two parts) + 256 cycles and its exponentials 1024, for 128
+// rows.  Measured, 16 sequences x 4 heads of 224 rows x 1500 .. 4128 keys: 80 us, where the bf16 cache takes 73; a step of a stream takes
+// 4800 cycles, 1300 for the maximum, 3100 for the weights of 128 keys, which is the latency of TMEM loads and exponentials with two softmax
+// warps a scheduler (issue slots 36 % in use, tensor pipe 17 %, exponentials 16 %).  Tried and not kept: scores held in
+// registers between the two passes and register splits between the roles (no faster), TMEM loads a step ahead (80.3 against 79.9 us).
 //
 // Every wait is bounded; on expiry the kernel raises DS_DEV_TIMEOUT, drains and frees TMEM.
 #include <type_traits>
@@ -66,7 +70,7 @@ struct Geo {
   // k_full, k_empty, v_full, v_empty [kSlots], v16_full, v16_free [2], scale_ready, scale_free [kScaleRing], s_full, p_full, pv_done, o_free
   // [2], q_full, q_free, meet, joined
   static constexpr int kNumBars = 4 * kSlots + 4 + 2 * kScaleRing + 8 + 4;
-  static constexpr int kOffMisc = kOffBar + 8 * kNumBars;      // TMEM base, unused, NaN in V, references of the scales [kScaleRing]
+  static constexpr int kOffMisc = kOffBar + 8 * kNumBars;      // TMEM base (8), NaN in V, references of the scales [kScaleRing]
   static constexpr int kOffScan = (kOffMisc + 12 + 4 * kScaleRing + 7) / 8 * 8;
   // Sums on their way out, [256][kOutDims] fp32.  Of pairs in a place of their own: a stream need not wait for the other's last products.
   static constexpr int kOutDims = kPair ? 16 : D == 128 ? 64 : 32;
@@ -380,7 +384,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
       for (; i < walk.n_tiles; i += kLoadWarps) {
         const int t = g + i, slot_of_t = t % S;
         // Code that runs for every tile is kept short: five roles share the instruction caches, and with all loops of these copies
-        // unrolled (24 KB) every role waited for its instructions (123 us instead of KK).
+        // unrolled (24 KB) every role waited for its instructions (123 us, 93 with short loops).
         long long at[4], scale_at[4];
         uint32_t even = 0;      // bit 2 j + half: 16 keys that lie evenly (in one page) need one address
 #pragma unroll

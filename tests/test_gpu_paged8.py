@@ -726,6 +726,28 @@ def test_refusals_of_the_binding():
             read(**bad)
 
 
+@every_path
+@pytest.mark.parametrize("junk", [math.nan, math.inf, -math.inf])
+def test_a_query_that_is_not_finite_is_its_own_output_only(path, junk):
+    c = path_case(path, seed=12)
+    clean, clean_lse, _ = c.run(causal=False)
+    row, head = int(c.starts[1]) - 1, c.q.shape[1] - 1
+    c.q[row, head, 5] = junk
+    out, lse, _ = c.run(causal=False)
+    assert torch.isnan(out[row, head]).all() and torch.isnan(lse[row, head])
+    out[row, head], lse[row, head] = clean[row, head], clean_lse[row, head]
+    assert torch.equal(out, clean) and torch.equal(lse, clean_lse)
+
+
+@every_path
+def test_outputs_in_the_place_of_the_queries(path):
+    c = path_case(path, seed=13)
+    want, _, scale = c.run()
+    q = c.q.to(DEV)
+    ds.ds_attn_paged8(q, *(x.to(DEV) for x in (*c.codes, *c.scales, c.table)), i32(c.lens), scale, i32(c.starts), max_q=max(c.counts), out=q)
+    assert torch.equal(q[:c.N], want) and torch.equal(q[c.N:].cpu(), c.q[c.N:])
+
+
 # ------------------------------------------------------------------------------------------------ graphs, streams, a serving loop
 @pytest.mark.parametrize("dtype,D,G,n,lens", [(BF, 128, 4, 1, [2000, 300, 77]), (BF, 128, 1, 1, [3000] * 30), (BF, 128, 4, 16, [2000, 300, 77]),
                                               (BF, 64, 4, 16, [9000, 300, 77]),
