@@ -7,8 +7,9 @@
 // of K or V and belongs to L lanes: they find the largest magnitude of the run, settle the exponent, and quantise; the run is read a
 // second time (from the caches close by) where it is longer than the lanes' registers hold.  Runs of more than 4 KB get a CTA per
 // item instead, whose threads stage runs in shared memory by asynchronous copies, two ahead, and quantise them from there.
-// Measured: one row each of 64 requests 3.4 us, the floor of a launch and of the dependent loads; 32 x 32 heads x 17 .. 2048 rows in blocks of 64, 830 MB, 176 - 184
-// us = 4.5 - 4.7 TB/s: a run's stores wait for all of its loads, the exchange of its maximum, and two runs ahead cover that in part.
+// Measured: one row each of 64 requests 3.5 - 3.9 us, the floor of a launch and of the dependent loads; 32 x 32 heads x 17 .. 2048 rows in blocks
+// of 64, 830 MB, 154 us = 5.4 TB/s of a copy's 6.55, seven tenths of the issue slots in use (184 before a thread's chunks stood at equal
+// steps and full runs were told apart: addresses and conditions were most of the instructions).
 // Reading.  A thread per row and 8 dimensions, four heads' loads in flight; 500 MB in 87 us = 5.7 TB/s.
 //
 // The power of two is found in the exponent bits: the smallest 2^e with a <= 448 2^e = 1.75 2^(e + 8) has a's exponent less 8, one
@@ -301,29 +302,29 @@ __global__ void __launch_bounds__(kThreads, 4) kv8_write_wide_kernel(const __gri
   uint32_t flags = check_sequences(p, launch.bound);
   const int item0 = blockIdx.y * launch.per_cta, item_end = min(launch.items, item0 + launch.per_cta);
   const int chunks = (int)launch.chunk_div.d;
+  // A thread has the same chunk of every at_a_time-th row, at equal steps: with chunks dealt out one after the other the addresses were
+  // most of the kernel's instructions.  (Up to chunks - 1 threads have none.)
+  const int row0 = fast_div(tid, launch.chunk_div), ch = (tid - row0 * chunks) * E, at_a_time = kThreads / chunks;
+  const long long src_step = at_a_time * p.kv_stride[0], code_step = at_a_time * p.cache_stride[2];
   RunWalk walk(p, launch);
   Run run;
   int turn = 0;
   while (walk.next(p, launch, run, flags)) {
-    const int total = run.count * chunks, n_keep = min(kWideKeep, (total - tid + kThreads - 1) / kThreads);
-    long long src_at[kWideKeep], code_at[kWideKeep];      // of this thread's chunks, from the run's first row
-#pragma unroll
-    for (int i = 0; i < kWideKeep; ++i) {
-      const int c = tid + i * kThreads, row = fast_div(c, launch.chunk_div), ch = (c - row * chunks) * E;
-      src_at[i] = row * p.kv_stride[0] + ch;
-      code_at[i] = row * p.cache_stride[2] + ch;
-    }
-    auto src_of = [&](int item) {
-      return reinterpret_cast<const T *>(item & 1 ? p.v : p.k) + run.row * p.kv_stride[0] + (item >> 1) * p.kv_stride[1];
-    };
+    const int n_mine = row0 < at_a_time ? max(0, (run.count - row0 + at_a_time - 1) / at_a_time) : 0, n_keep = min(kWideKeep, n_mine);
+    const bool full = __all_sync(0xffffffffu, n_mine == kWideKeep);      // nothing to ask for every chunk
+    const long long src_at = ((long long)run.row + row0) * p.kv_stride[0] + ch;
+    auto src_of = [&](int item) { return reinterpret_cast<const T *>(item & 1 ? p.v : p.k) + src_at + (item >> 1) * p.kv_stride[1]; };
     auto stage_of = [&](int item) { return ring + (item % (kAhead + 1)) * (kWideKeep * kThreads) + tid; };
     auto load = [&](int item) {
       if (item < item_end) {
         const T *src = src_of(item);
         uint4 *to = stage_of(item);
+        if (full) {
 #pragma unroll
-        for (int i = 0; i < kWideKeep; ++i)
-          if (i < n_keep) copy16(to + i * kThreads, src + src_at[i]);
+          for (int i = 0; i < kWideKeep; ++i, src += src_step) copy16(to + i * kThreads, src);
+        } else {
+          for (int i = 0; i < n_keep; ++i, src += src_step) copy16(to + i * kThreads, src);
+        }
       }
       copies_end();
     };
@@ -334,21 +335,22 @@ __global__ void __launch_bounds__(kThreads, 4) kv8_write_wide_kernel(const __gri
       const T *src = src_of(item);
       const int h = item >> 1;
       uint8_t *code = reinterpret_cast<uint8_t *>(item & 1 ? p.v_cache : p.k_cache) + run.code + h * p.cache_stride[1];
+      uint8_t *mine_at = code + row0 * p.cache_stride[2] + ch;
       float *scale = (item & 1 ? p.v_scale : p.k_scale) + run.scale + h * p.scale_stride[1];
       const float s0 = run.held > 0 ? *scale : 0.f;
       load(item + kAhead);
       copies_wait<kAhead>();
       const uint4 *mine = stage_of(item);
-      auto at = [&](int c) {
-        const int row = fast_div(c, launch.chunk_div);
-        return src + row * p.kv_stride[0] + (c - row * chunks) * E;
-      };
       auto peak = [&](bool finite) {
         uint32_t top = 0;
+        if (full) {
 #pragma unroll
-        for (int i = 0; i < kWideKeep; ++i)
-          if (i < n_keep) top = peak_of<T>(mine[i * kThreads], top, finite);
-        for (int c = tid + kWideKeep * kThreads; c < total; c += kThreads) top = peak_of<T>(*reinterpret_cast<const uint4 *>(at(c)), top, finite);
+          for (int i = 0; i < kWideKeep; ++i) top = peak_of<T>(mine[i * kThreads], top, finite);
+        } else {
+#pragma unroll 1
+          for (int i = 0; i < n_keep; ++i) top = peak_of<T>(mine[i * kThreads], top, finite);
+        }
+        for (int i = kWideKeep; i < n_mine; ++i) top = peak_of<T>(*reinterpret_cast<const uint4 *>(src + i * src_step), top, finite);
         top = __reduce_max_sync(0xffffffffu, top);
         if (lane == 0) top_s[turn][warp] = top;
         turn ^= 1;
@@ -361,13 +363,16 @@ __global__ void __launch_bounds__(kThreads, 4) kv8_write_wide_kernel(const __gri
       const bool plain = top <= kMostBits;
       if (!plain) top = peak(true);
       const Scale now = scale_of(top, run.held, s0);
+      if (full && plain) {
 #pragma unroll
-      for (int i = 0; i < kWideKeep; ++i)
-        if (i < n_keep) store_codes<T>(code + code_at[i], mine[i * kThreads], now.by, plain);
-      for (int c = tid + kWideKeep * kThreads; c < total; c += kThreads) {
-        const int row = fast_div(c, launch.chunk_div);
-        store_codes<T>(code + row * p.cache_stride[2] + (c - row * chunks) * E, *reinterpret_cast<const uint4 *>(at(c)), now.by, plain);
+        for (int i = 0; i < kWideKeep; ++i, mine_at += code_step) store_codes<T>(mine_at, mine[i * kThreads], now.by, true);
+      } else {
+#pragma unroll 1
+        for (int i = 0; i < n_keep; ++i, mine_at += code_step) store_codes<T>(mine_at, mine[i * kThreads], now.by, plain);
       }
+#pragma unroll 1
+      for (int i = kWideKeep; i < n_mine; ++i, mine_at += code_step)
+        store_codes<T>(mine_at, *reinterpret_cast<const uint4 *>(src + i * src_step), now.by, plain);
       const bool same = run.held > 0 && __float_as_uint(s0) == now.bits;
       if (run.held > 0 && !same) rescale(code - run.held * p.cache_stride[2], p.cache_stride[2], run.held, p.D, s0 * now.by, tid, kThreads);
       if (tid == 0 && !same) *scale = __uint_as_float(now.bits);
