@@ -311,7 +311,7 @@ __global__ void __launch_bounds__(kThreads, 4) kv8_write_wide_kernel(const __gri
   int turn = 0;
   while (walk.next(p, launch, run, flags)) {
     const int n_mine = row0 < at_a_time ? max(0, (run.count - row0 + at_a_time - 1) / at_a_time) : 0, n_keep = min(kWideKeep, n_mine);
-    const bool full = __all_sync(0xffffffffu, n_mine == kWideKeep);      // nothing to ask for every chunk
+    const bool full = __all_sync(0xffffffffu, n_keep == kWideKeep);      // nothing to ask for every chunk
     const long long src_at = ((long long)run.row + row0) * p.kv_stride[0] + ch;
     auto src_of = [&](int item) { return reinterpret_cast<const T *>(item & 1 ? p.v : p.k) + src_at + (item >> 1) * p.kv_stride[1]; };
     auto stage_of = [&](int item) { return ring + (item % (kAhead + 1)) * (kWideKeep * kThreads) + tid; };
