@@ -8,7 +8,7 @@
 // second time (from the caches close by) where it is longer than the lanes' registers hold.  Runs of more than 4 KB get a CTA per
 // item instead, whose threads stage runs in shared memory by asynchronous copies, two ahead, and quantise them from there.
 // Measured: one row each of 64 requests 3.5 - 3.9 us, the floor of a launch and of the dependent loads; 32 x 32 heads x 17 .. 2048 rows in blocks
-// of 64, 830 MB, 154 us = 5.4 TB/s of a copy's 6.55, seven tenths of the issue slots in use (184 before a thread's chunks stood at equal
+// of 64, 830 MB, 149 - 154 us = 5.4 - 5.6 TB/s of a copy's 6.55, seven tenths of the issue slots in use (184 before a thread's chunks stood at equal
 // steps and full runs were told apart: addresses and conditions were most of the instructions).
 // Reading.  A thread per row and 8 dimensions, four heads' loads in flight; 500 MB in 87 us = 5.7 TB/s.
 //
