@@ -11,12 +11,12 @@
 //
 // Queries enter as fp16 too: a row is scaled by a power of two that puts its largest element into [2^14, 2^15), and 11 bits hold bf16's 8
 // down to 2^-31 of that.  fp32 queries are two such parts (22 bits).  The scale of K and the row's factor multiply the score, the scale of V
-// the weight, relative to the largest that the warp has met (vref, a power of two).  The weights are fp16: that of the reference of the
-// exponents is 2^6, and they may pass it up to 2^14, which keeps 11 bits down to 2^-20 of it and drops what is below 2^-31: a weight's
-// rounding, 2^-11, is an eighth of the output's in bf16.  For fp32 outputs the reference is 2^10 and the weights are two such parts.
+// the weight, with a power of two for each row (Weights8): the largest weight that the row sees stands at 2^5 .. 2^14, which keeps 11 bits down
+// to 2^-19 of it and drops what is below 2^-30: a weight's rounding, 2^-11, is an eighth of the output's in bf16.  For fp32 outputs it stands
+// at 2^9 .. 2^14 and the weights are two such parts.
 //
 // Measured: 32 x 32 heads at length, 1.08 GB, 183 - 186 us (5.9 TB/s, nine tenths of a plain copy; 188 with V transposed in pairs and
-// permuted); the issue slots are half in use, a third of them for conversions.  8 x 32 heads of 32 rows x 1024 .. 2080 keys 61 us, which is the
+// permuted); the issue slots are half in use, a third of them for conversions.  8 x 32 heads of 32 rows x 1024 .. 2080 keys 66 us, which is the
 // chain score -> weight -> product in eight warps an SM (issue slots 36 %, tensor pipe 25 %); equal ranges 75, 16 rows to an item with 12 warps
 // 65, tcgen05 tiles, three quarters empty, 68.  Products of e4m3 (m16n8k32) for the scores, twice the rate, need two of them for the
 // queries' bits and as many conversions of V: 189 -> 206 us.
@@ -59,11 +59,10 @@ struct ByteRows {
   static constexpr int kGroups = NB * kParts <= 2 && kKeys == 32 ? 2 : 1;      // 16s of keys at a time
   static constexpr int kCtas = NB == 1 ? (D == 64 || kKeys == 16 ? 4 : 3) : 2, kStages = kKeys == 16 ? 3 : 2;
   float o[NB][D / 16][4];      // dimensions 16 j + lane / 4 (+ 8), rows 2q, 2q + 1
-  float m[NB][2], l[NB][2], factor[NB][2];
+  float m[NB][2], l[NB][2], e[NB][2], factor[kQRegs ? NB : 1][2];      // (more factors stay where the queries are)
   int end[NB][2];
   uint32_t qf[kQRegs ? kBlocks : 1][kQRegs ? D / 16 : 1][2];
   uint32_t q_smem;
-  float vref, vinv;
 
   __device__ void begin(const Args8 &a, const Item &it, uint8_t *q_buf) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -129,49 +128,65 @@ struct ByteRows {
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[nb][j][e] = 0.f;
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int r = 8 * nb + 2 * (lane & 3) + e;
-        m[nb][e] = -INFINITY, l[nb][e] = 0.f, factor[nb][e] = factor_s[r];
-        end[nb][e] = r < it.rows ? row_of(a, it, r).end : 0;
+      for (int y = 0; y < 2; ++y) {
+        const int r = 8 * nb + 2 * (lane & 3) + y;
+        m[nb][y] = -INFINITY, l[nb][y] = 0.f, e[nb][y] = 0.f;
+        if constexpr (kQRegs) factor[nb][y] = factor_s[r];
+        end[nb][y] = r < it.rows ? row_of(a, it, r).end : 0;
       }
     }
     if constexpr (kQRegs) __syncthreads();      // warp 0 loads keys there next
-    set_vref(27);      // 2^-100
   }
 
-  // vref = 2^(e - 127), vinv = the reference's weight / vref
-  __device__ __forceinline__ void set_vref(uint32_t e) {
-    vref = __uint_as_float(e << 23);
-    vinv = __uint_as_float((254u + W::kLog2 - e) << 23);
+  // Of this lane's rows.
+  __device__ __forceinline__ float2 factors(int nb) const {
+    if constexpr (kQRegs) return make_float2(factor[nb][0], factor[nb][1]);
+    float2 f;
+    asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(f.x), "=f"(f.y) : "r"(q_smem + kOffFactor + (8 * nb + 2 * (threadIdx.x & 3)) * 4));
+    return f;
   }
 
   // The key of 16 that stands in row i of half h of a product: a lane of the second product has four neighbouring keys of V.
   static __device__ __forceinline__ int key_at(int i, int h) { return 4 * (i >> 1) + (i & 1) + 2 * h; }
 
-  // Makes vref the power of two at or above the largest finite scale of V of the stage.
-  __device__ __forceinline__ void raise(float mine) {
-    const uint32_t b = __float_as_uint(mine) & 0x7fffffffu;
-    const bool more = b < 0x7f800000u && b > __float_as_uint(vref);
-    if (!__any_sync(0xffffffffu, more)) return;
-    const uint32_t top = __reduce_max_sync(0xffffffffu, more ? b : 0u);
-    const uint32_t e = min((top + 0x7fffffu) >> 23, 254u);
-    const int fall = 127 + (int)(__float_as_uint(vref) >> 23) - (int)e;
-    const float keep = __uint_as_float(fall > 0 ? (uint32_t)fall << 23 : 0u);
-    set_vref(e);
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-      for (int j = 0; j < D / 16; ++j)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) o[nb][j][k] *= keep;
-  }
-
   // kKeys keys from x on; K, V and their scales (behind V: of K, of V) as loaded, V is scratch afterwards.
   __device__ __forceinline__ void step(const Args8 &a, const Item &it, uint8_t *kbuf, uint8_t *vbuf, int x, float) {
     const float *scales = reinterpret_cast<const float *>(vbuf + kKeys * kRowBytes);
-    raise(scales[kKeys + threadIdx.x % kKeys]);
-#pragma unroll
+#pragma unroll 1
     for (int g = 0; g < kKeys / 16; g += kGroups) keys16(a, it, kbuf, vbuf, scales, x, g);
+  }
+
+  // The rows' references to the largest score so far, if `scores`, and the exponents of their weights.  s, top and vscale: scores of this
+  // lane's keys, the largest of them, their scales of V.  (Short rather than quick: it is run a few times in an item, and instructions that
+  // are fetched for the first time cost most of it.)
+  __device__ __forceinline__ void move_references(bool scores, const float (&s)[NB][kGroups][4], const float (&top)[NB][2], const float (&vscale)[kGroups][2]) {
+    float lv[kGroups][2];
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) lv[g][h] = log_scale(vscale[g][h]);
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const float old = m[nb][y];
+        float t = scores ? fmaxf(old, top[nb][y]) : old;
+#pragma unroll
+        for (int off = 4; off < 32; off <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, off));
+        const float moved = old == t ? e[nb][y] : e[nb][y] + (t - old), start = fminf(moved, W::kMost);
+        l[nb][y] *= old == t ? 1.f : ex2_approx(old - t);
+        float most = -INFINITY;
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) most = fmaxf(most, (s[nb][g][2 * h + y] - t) + (start + lv[g][h]));
+#pragma unroll
+        for (int off = 4; off < 32; off <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, off));
+        const float fresh = exponent_of_weights<W>(start, most, old != t), keep = ex2_approx(fresh - moved);
+        m[nb][y] = t, e[nb][y] = fresh;
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) o[nb][j][y] *= keep, o[nb][j][2 + y] *= keep;
+      }
   }
 
   // Groups g .. g + kGroups - 1 of 16 keys.
@@ -214,18 +229,21 @@ struct ByteRows {
         }
       }
     }
-    float vscale[kGroups][2];
+    float vscale[kGroups][2], vmost = 0.f;
 #pragma unroll
     for (int g = 0; g < kGroups; ++g)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int key = 16 * (g0 + g) + key_at(lane >> 2, h);
         const float kscale = scales[key];
-        vscale[g][h] = scales[kKeys + key] * vinv;
+        vscale[g][h] = scales[kKeys + key];
+        vmost = fmaxf(vmost, fabsf(vscale[g][h]));
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) s[nb][g][2 * h + e] = __fmul_rn(s[nb][g][2 * h + e], factor[nb][e] * kscale);
+        for (int nb = 0; nb < NB; ++nb) {
+          const float2 f = factors(nb);
+          s[nb][g][2 * h] = __fmul_rn(s[nb][g][2 * h], f.x * kscale);
+          s[nb][g][2 * h + 1] = __fmul_rn(s[nb][g][2 * h + 1], f.y * kscale);
+        }
       }
     const bool partial = !paged_all_visible(a.s, it.q, x + 16 * g0, 16 * kGroups);
     uint32_t seen[NB] = {};      // only with partial: bit 4g + 2h + e: key 16g + key_at(lane / 4, h), row 2q + e
@@ -244,39 +262,28 @@ struct ByteRows {
             }
         }
     }
-    // The reference of the exponents moves only when a weight would pass 2^14 (the result is the same): no maximum is
-    // exchanged until some lane finds such a score.
-    bool over = false;
+    // The references move only when a weight would pass 2^14 (the result is the same): no maximum is exchanged until some lane finds
+    // such a score, or that its largest score with the largest scale of its keys might be one.
+    bool over = false, heavy = false;
     float top[NB][2];
+    const float lmost = lg2_approx(vmost);
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        top[nb][e] = fmaxf(s[nb][0][e], s[nb][0][2 + e]);
+      for (int y = 0; y < 2; ++y) {
+        top[nb][y] = fmaxf(s[nb][0][y], s[nb][0][2 + y]);
 #pragma unroll
-        for (int g = 1; g < kGroups; ++g) top[nb][e] = fmaxf(top[nb][e], fmaxf(s[nb][g][e], s[nb][g][2 + e]));
-        over |= top[nb][e] > m[nb][e] + W::kLag;
+        for (int g = 1; g < kGroups; ++g) top[nb][y] = fmaxf(top[nb][y], fmaxf(s[nb][g][y], s[nb][g][2 + y]));
+        const float rise = top[nb][y] - m[nb][y];
+        over |= rise > W::kLag, heavy |= rise + (e[nb][y] + lmost) > W::kTop;
       }
-    if (__any_sync(0xffffffffu, over)) {
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          float t = fmaxf(m[nb][e], top[nb][e]);
-#pragma unroll
-          for (int off = 4; off < 32; off <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, off));
-          const float keep = m[nb][e] == t ? 1.f : ex2_approx(m[nb][e] - t);
-          m[nb][e] = t;
-          l[nb][e] *= keep;
-#pragma unroll
-          for (int j = 0; j < D / 16; ++j) o[nb][j][e] *= keep, o[nb][j][2 + e] *= keep;
-        }
-    }
+    if (__any_sync(0xffffffffu, over || heavy)) move_references(__any_sync(0xffffffffu, over), s, top, vscale);
     uint32_t w[NB][kGroups][kParts][2];      // keys key_at(.., 0 and 1): the weights (their parts), rows 2q and 2q + 1
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       // nothing seen yet: weights exp(-inf) = 0
       const float ref0 = m[nb][0] == -INFINITY ? 0.f : m[nb][0], ref1 = m[nb][1] == -INFINITY ? 0.f : m[nb][1];
+      const float up0 = power_of_two(e[nb][0] + W::kBias), up1 = power_of_two(e[nb][1] + W::kBias);
 #pragma unroll
       for (int g = 0; g < kGroups; ++g)
 #pragma unroll
@@ -284,7 +291,7 @@ struct ByteRows {
           const float p0 = ex2_approx(s[nb][g][2 * h] - ref0), p1 = ex2_approx(s[nb][g][2 * h + 1] - ref1);
           l[nb][0] += p0;
           l[nb][1] += p1;
-          float w0 = p0 * vscale[g][h], w1 = p1 * vscale[g][h];
+          float w0 = (p0 * up0) * (vscale[g][h] * kUnbiased), w1 = (p1 * up1) * (vscale[g][h] * kUnbiased);
           if (partial) {      // zero times a scale that is not finite
             if (!((seen[nb] >> (4 * g + 2 * h)) & 1)) w0 = 0.f;
             if (!((seen[nb] >> (4 * g + 2 * h + 1)) & 1)) w1 = 0.f;
@@ -357,20 +364,20 @@ struct ByteRows {
   // The warp's sums to shared memory: out[kRows][D], ml[kRows].
   __device__ void finish(const Args8 &a, const Item &it, float *out, float2 *ml) {
     const int lane = threadIdx.x & 31;
-    const float down = a.shrink / W::kOne;
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int r = 8 * nb + 2 * (lane & 3) + e;
-        float sum = l[nb][e];
+      for (int y = 0; y < 2; ++y) {
+        const int r = 8 * nb + 2 * (lane & 3) + y;
+        float sum = l[nb][y];
 #pragma unroll
         for (int off = 4; off < 32; off <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
         if (r >= it.rows) continue;
-        if (lane < 4) ml[r] = make_float2(m[nb][e], sum);
+        if (lane < 4) ml[r] = make_float2(m[nb][y], sum);
+        const float down = power_of_two(-e[nb][y]);
 #pragma unroll
         for (int j = 0; j < D / 16; ++j)
-          out[r * D + 16 * j + (lane >> 2)] = o[nb][j][e] * down * vref, out[r * D + 16 * j + 8 + (lane >> 2)] = o[nb][j][2 + e] * down * vref;
+          out[r * D + 16 * j + (lane >> 2)] = o[nb][j][y] * a.shrink * down, out[r * D + 16 * j + 8 + (lane >> 2)] = o[nb][j][2 + y] * a.shrink * down;
       }
   }
 };

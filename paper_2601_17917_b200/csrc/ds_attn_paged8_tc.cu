@@ -5,7 +5,7 @@
 // sum of an e4m3 value (rounded to the nearest 4 bits) and an e5m2 one: what is left of 8 bits is at most 8 of their units, which 3 bits
 // hold.  So two products of 8-bit operands, in one accumulator, are exact in the queries down to 2^-14 of the row's largest element and
 // within 2^-21 of it below.  O += P V takes fp16: four warps turn the e4m3 values of a tile into fp16, which holds them all, in the layout
-// of the product; weights are fp16 with V's scale in them, as in the kernel for few rows.  (P in 8-bit halves would drop what lies below
+// of the product; weights are fp16 with V's scale in them and a power of two for each row, as in the kernel for few rows (Weights8).  (P in 8-bit halves would drop what lies below
 // 2^-22 of the largest weight, a per cent of the sum in a long cache.)
 //
 // Two streams of 128 tile rows each, with a warpgroup, S and O of their own, keep the tensor pipe and the exponentials busy at once:
@@ -62,15 +62,15 @@ struct Geo {
   static constexpr int kOffK = 2 * kQPart;
   static constexpr int kOffV = kOffK + kSlots * kTile;
   static constexpr int kOffV16 = kOffV + kSlots * kTile;                  // [2] tiles in fp16; at the end of an item sums to be joined
-  static constexpr int kOffScale = kOffV16 + 2 * 2 * kTile;               // [kScaleRing][2][128]
-  static constexpr int kOffFactor = kOffScale + kScaleRing * 1024;        // [kRows]
+  static constexpr int kOffScale = kOffV16 + 2 * 2 * kTile;               // [kScaleRing][3][128]: K's, V's, logarithms of V's where they are asked for
+  static constexpr int kOffFactor = kOffScale + kScaleRing * 1536;        // [kRows]
   static constexpr int kOffMl = kOffFactor + kRows * 4;                   // [256]
   static constexpr int kOffTo = kOffMl + (kPair ? 0 : 256 * 8);           // [kRows]
   static constexpr int kOffBar = kOffTo + kRows * 8;
   // k_full, k_empty, v_full, v_empty [kSlots], v16_full, v16_free [2], scale_ready, scale_free [kScaleRing], s_full, p_full, pv_done, o_free
   // [2], q_full, q_free, meet, joined
   static constexpr int kNumBars = 4 * kSlots + 4 + 2 * kScaleRing + 8 + 4;
-  static constexpr int kOffMisc = kOffBar + 8 * kNumBars;      // TMEM base (8), NaN in V, references of the scales [kScaleRing]
+  static constexpr int kOffMisc = kOffBar + 8 * kNumBars;      // TMEM base (8), NaN in V, sizes of V's scales [kScaleRing]
   static constexpr int kOffScan = (kOffMisc + 12 + 4 * kScaleRing + 7) / 8 * 8;
   // Sums on their way out, [256][kOutDims] fp32.  Of pairs in a place of their own: a stream need not wait for the other's last products.
   static constexpr int kOutDims = kPair ? 16 : D == 128 ? 64 : 32;
@@ -178,6 +178,32 @@ __device__ __forceinline__ float4 with_nan(float4 v, uint32_t bytes) {
   return v;
 }
 
+// The largest weight times scale of V, log 2, of the n keys from c on that a row sees: scores at ts, factors ks, the scales' logarithms behind
+// them.  (Not inlined: the loop around it is short.)
+__device__ __noinline__ float heaviest(uint32_t ts, const float *ks, int c, int n, const Seen seen, float ref, float steep) {
+  float most[2] = {-INFINITY, -INFINITY};
+  const F2 ref2 = f2(-ref, -ref), steep2 = f2(steep, steep);
+#pragma unroll 1
+  for (const int end = c + n; c < end; c += 16) {
+    uint32_t z[16];
+    tmem_ld16(ts + c, z);
+    tmem_wait_ld();
+    const uint32_t bits = seen.bits(c);
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      const float4 k = *reinterpret_cast<const float4 *>(ks + c + i);
+      const ulonglong2 v = *reinterpret_cast<const ulonglong2 *>(ks + 256 + c + i);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const F2 y = f2(__fmul_rn(__uint_as_float(z[i + 2 * h]), h ? k.z : k.x), __fmul_rn(__uint_as_float(z[i + 2 * h + 1]), h ? k.w : k.y));
+        const float2 w = f2_get(fma2(add2(y, ref2), steep2, h ? v.y : v.x));
+        most[h] = fmax3(most[h], (bits >> (i + 2 * h)) & 1 ? w.x : -INFINITY, (bits >> (i + 2 * h + 1)) & 1 ? w.y : -INFINITY);
+      }
+    }
+  }
+  return fmaxf(most[0], most[1]);
+}
+
 template <int D, bool kPair, int kCopies>
 __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __grid_constant__ Args8 a) {
   using G = Geo<D, kPair>;
@@ -199,7 +225,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
                  bar_meet = bar_q_free + 8, bar_joined = bar_meet + 8;
   volatile uint32_t *tmem_s = reinterpret_cast<volatile uint32_t *>(smem + G::kOffMisc);
   volatile int *v_nan = reinterpret_cast<volatile int *>(smem + G::kOffMisc + 8);      // some tile of V held NaN so far
-  volatile uint32_t *vref_s = reinterpret_cast<volatile uint32_t *>(smem + G::kOffMisc + 12);      // biased exponents
+  // of the largest finite scale of V of a tile, its biased exponent, rounded up; kMixed: not every row sees every key, or some scale is
+  // below a quarter of that
+  volatile uint32_t *vsize_s = reinterpret_cast<volatile uint32_t *>(smem + G::kOffMisc + 12);
+  constexpr uint32_t kMixed = 256;
   float *scale_s = reinterpret_cast<float *>(smem + G::kOffScale);
   float *factor_s = reinterpret_cast<float *>(smem + G::kOffFactor);
 
@@ -292,27 +321,28 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
       }
       if (!kPair && k > 0) ok = wait(bar_joined, k - 1);      // the sums of the piece before, which lie in the tiles' place
       // ---- V, tile by tile
-      uint32_t vref = 27;      // biased exponent of the reference of V's scales: 2^-100
       for (int i = 0; ok && i < walk.n_tiles; ++i) {
         const int t = g + i;
         ok = wait(bar_v_full + 8 * (t % S), t / S);
         if (!ok) break;
         if (cw == 0) {
-          // the scales of V relative to the power of two at or above the largest finite one so far, times the reference's weight
-          float *vs = scale_s + (t % kScaleRing) * 256 + 128 + lane;
-          float v[4];
-          uint32_t big = 0;
+          // the scales as the products take them, and how large V's are
+          float *vs = scale_s + (t % kScaleRing) * 384 + 128 + lane;
+          uint32_t most = 0, least = ~0u;
+          float size[4];
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
-            v[c] = vs[32 * c];
-            const uint32_t b = __float_as_uint(v[c]) & 0x7fffffffu;
-            big = max(big, b < 0x7f800000u ? b : 0u);
+            const float v = vs[32 * c];
+            const uint32_t b = __float_as_uint(v) & 0x7fffffffu;
+            most = max(most, b < 0x7f800000u ? b : 0u), least = min(least, b);
+            size[c] = v;
+            vs[32 * c] = v * kUnbiased, vs[32 * c - 128] *= 0x1p-24f;      // a product of queries and K is below 2^24
           }
-          vref = max(vref, min((__reduce_max_sync(0xffffffffu, big) + 0x7fffffu) >> 23, 254u));
-          const float vinv = __uint_as_float((254u + W::kLog2 - vref) << 23);
-#pragma unroll
-          for (int c = 0; c < 4; ++c) vs[32 * c] = v[c] * vinv, vs[32 * c - 128] *= 0x1p-24f;      // a product of queries and K is below 2^24
-          if (lane == 0) vref_s[t % kScaleRing] = vref;
+          most = (__reduce_max_sync(0xffffffffu, most) + 0x7fffffu) >> 23, least = __reduce_min_sync(0xffffffffu, least) >> 23;
+          const bool mixed = least + 2 < most || !paged_all_visible(a.s, it.q, (walk.tile0 + i) * kKeys, kKeys);
+          if (mixed)
+            for (int c = 0; c < 4; ++c) vs[32 * c + 128] = log_scale(size[c]);
+          if (lane == 0) vsize_s[t % kScaleRing] = most | (mixed ? kMixed : 0u);
           __syncwarp();
           if (lane == 0) mbar_arrive(bar_sc_ready + 8 * (t % kScaleRing));
         }
@@ -427,7 +457,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
           if (v == 0) {
             ok = wait(bar_sc_free + 8 * (t % kScaleRing), t / kScaleRing + 1);
             if (!ok) break;
-            const uint32_t sc = sbase + G::kOffScale + (t % kScaleRing) * 1024 + 4 * lane;
+            const uint32_t sc = sbase + G::kOffScale + (t % kScaleRing) * 1536 + 4 * lane;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
               cp_async4(sc + 128 * j, kscale + (scale_at[j] >= 0 ? scale_at[j] : 0), scale_at[j] >= 0);
@@ -513,7 +543,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
       __syncwarp();
       if (lane == 0) mbar_arrive(bar_q_free);
       float m = -INFINITY, l = 0.f;      // m: the largest score before its factor
-      uint32_t vref = 27;                // biased exponent of the reference of V's scales
+      float e = 0.f;                     // of the row's weights
       const int steps = kPair ? 2 * walk.n_tiles : walk.n_tiles;
       int done = 0;
       for (int u = s; u < steps; u += 2, ++n, ++done) {
@@ -523,23 +553,18 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
         if (!ok) break;
         tc_fence_after();
         if (busy) {
-          const float *ks = scale_s + (t % kScaleRing) * 256, *vs = ks + 128;
+          const float *ks = scale_s + (t % kScaleRing) * 384, *vs = ks + 128;
           const Seen seen = seen_keys(a.s, it.q, x, end);
-          // V's scales are relative to a reference that may have risen
-          const uint32_t vnow = vref_s[t % kScaleRing];
-          const int drop = 127 + (int)vref - (int)vnow;
-          float keep = vnow == vref ? 1.f : __uint_as_float(drop > 0 ? (uint32_t)drop << 23 : 0u);      // of O
-          vref = vnow;
           // ---- largest score of this copy's keys, 16 at a time in a short loop
           float top = -INFINITY, top1 = -INFINITY;
           uint32_t z[16];
           float y[16];
           auto scores = [&](int c) {      // rounded before the reference is taken off: equal keys stay equal
 #pragma unroll
-            for (int e = 0; e < 16; e += 4) {
-              const float4 f = *reinterpret_cast<const float4 *>(ks + c + e);
-              y[e] = __fmul_rn(__uint_as_float(z[e]), f.x), y[e + 1] = __fmul_rn(__uint_as_float(z[e + 1]), f.y);
-              y[e + 2] = __fmul_rn(__uint_as_float(z[e + 2]), f.z), y[e + 3] = __fmul_rn(__uint_as_float(z[e + 3]), f.w);
+            for (int i = 0; i < 16; i += 4) {
+              const float4 f = *reinterpret_cast<const float4 *>(ks + c + i);
+              y[i] = __fmul_rn(__uint_as_float(z[i]), f.x), y[i + 1] = __fmul_rn(__uint_as_float(z[i + 1]), f.y);
+              y[i + 2] = __fmul_rn(__uint_as_float(z[i + 2]), f.z), y[i + 3] = __fmul_rn(__uint_as_float(z[i + 3]), f.w);
             }
           };
           auto hide = [&](int c, float what) {
@@ -557,14 +582,21 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
             for (int e = 0; e < 16; e += 4) top = fmax3(top, y[e], y[e + 1]), top1 = fmax3(top1, y[e + 2], y[e + 3]);
           }
           top = fmaxf(top, top1);
-          // The reference m of the scores moves only when a weight would pass it by 2^kLag, and O with it: rarely.
-          const bool over = mine && (m == -INFINITY ? top > m : (top - m) * steep > W::kLag);
-          if (__any_sync(0xffffffffu, over || keep != 1.f)) {
-            const float fall = !over ? 1.f : m == -INFINITY ? 0.f : ex2_approx((m - top) * steep);
-            if (over) m = top;
-            l *= fall;
-            keep *= fall;
-            if (done > 0) {
+          // The references of the row's scores and weights move only when one would pass its limit, and O with them: rarely.
+          const uint32_t size = vsize_s[t % kScaleRing];
+          const float now = mine && (m == -INFINITY ? top > m : (top - m) * steep > W::kLag) ? top : m;
+          const float moved = now == m ? e : e + (now - m) * steep, start = fminf(moved, W::kMost);
+          // the largest weight: at most this, with the tile's largest scale, whoever sees it
+          float most = mine ? (top - now) * steep + (start + (float)((int)(size & 255u) - 127)) : -INFINITY;
+          const bool over = now != m || most > W::kTop;
+          if (__any_sync(0xffffffffu, over)) {
+            // Where that is too much, and the tile is mixed, the row's own keys are gone through.
+            if ((size & kMixed) && __any_sync(0xffffffffu, most > W::kLog2)) most = start + heaviest(ts, ks, key0, kMine, seen, now, steep);
+            const float fresh = exponent_of_weights<W>(start, most, now != m);
+            if (now != m) l *= m == -INFINITY ? 0.f : ex2_approx((m - now) * steep);
+            const float keep = ex2_approx(fresh - moved);
+            m = now, e = fresh;
+            if (done > 0 && __any_sync(0xffffffffu, keep != 1.f)) {
               ok = wait(bar_pv_done + 8 * s, n - 1);
               if (!ok) break;
               tc_fence_after();
@@ -573,7 +605,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
                 tmem_ld16(to + c, z);
                 tmem_wait_ld();
 #pragma unroll
-                for (int e = 0; e < 16; ++e) z[e] = __float_as_uint(__uint_as_float(z[e]) * keep);
+                for (int i = 0; i < 16; ++i) z[i] = __float_as_uint(__uint_as_float(z[i]) * keep);
                 tmem_st16(to + c, z);
               }
             }
@@ -581,6 +613,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
           // ---- weights
           const float ref = m == -INFINITY ? 0.f : m;      // nothing seen yet: exp(-inf) = 0
           const F2 ref2 = f2(-ref, -ref), steep2 = f2(steep, steep);
+          const float up = power_of_two(e + W::kBias);
+          const F2 up2 = f2(up, up);
           F2 l2[2] = {0, 0};
 #pragma unroll 1
           for (int c = key0; c < key0 + kMine; c += 16) {
@@ -597,7 +631,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
                 q.x = ex2_approx(q.x), q.y = ex2_approx(q.y);
                 const F2 weight = f2(q.x, q.y);
                 l2[h / 2] = add2(l2[h / 2], weight);
-                const float2 b = f2_get(mul2(weight, h ? v.y : v.x));
+                const float2 b = f2_get(mul2(mul2(weight, up2), h ? v.y : v.x));
                 y[e + h] = b.x, y[e + h + 1] = b.y;
               }
             }
@@ -636,9 +670,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
       const bool whole = walk.whole();
       const int x0 = walk.tile0 * kKeys, n_keys = walk.n_tiles * kKeys;
       const long long slot = (long long)paged_slot(blockIdx.x, walk.first) * a.part_rows;
-      const float vfull = __uint_as_float(vref << 23);
-      // O times this is a share of the output, or of the part's sums: O vref by the reference's weight, over the sum of weights or shrunk
-      auto share = [&](float sum) { return whole ? (sum == 0.f ? 0.f : 1.f / (W::kOne * sum)) : a.shrink / W::kOne; };
+      const float down = power_of_two(-e);
+      // O times this, and down, is a share of the output, or of the part's sums: over the sum of weights or shrunk
+      auto share = [&](float sum) { return whole ? (sum == 0.f ? 0.f : 1.f / sum) : a.shrink; };
       // to be called when the stream's products are done (all of the piece, where a row has two): the tiles that they read have then been
       // looked through
       bool nan = false;
@@ -681,7 +715,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
         // cycles)
         nan = *v_nan != 0;
         if (busy) {
-          const float by = share(l) * vfull;
+          const float by = share(l) * down;
           if (mine) finish_row(row, r, m, l);
 #pragma unroll 1
           for (int c = 0; c < D; c += J) {
@@ -717,7 +751,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
           const float2 ml = ml_s[j * kPad + rr];
           sum = fmaf(ml.y, ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - top), sum);
         }
-        const float by = (m == -INFINITY ? 0.f : ex2_approx(m - top)) * share(sum) * vfull;
+        const float by = (m == -INFINITY ? 0.f : ex2_approx(m - top)) * share(sum) * down;
         if (s == 0 && copy == 0 && mine) finish_row(row, r, top, sum);
 #pragma unroll 1
         for (int c = 0; ok && c < D; c += J) {

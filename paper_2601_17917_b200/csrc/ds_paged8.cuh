@@ -12,14 +12,37 @@ struct Args8 : Params {
   FastDiv scale_div;      // by rows of a block
 };
 
-// Weights in fp16: that of the reference of the exponents is 2^kLog2, and weights may pass it by 2^kLag before the reference moves (2^14
-// together).  What falls below 2^-25 is dropped, 2^-(25 + kLog2) of the reference's weight.  bf16 outputs take a wide range for the
-// lag: moving the reference costs the tcgen05 kernel as much as a tile.
+// Weights in fp16.  A weight is p |vs| 2^e: p = exp(score - reference), vs the scale of V, and e, a whole number for each query row, such
+// that the largest p |vs| of the keys that the row sees stands near 2^kLog2.  The reference moves when p would pass 2^kLag, e with it or when a
+// weight would pass 2^kTop: by the scales that the row itself sees, whatever is hidden from it.  What falls below 2^-25 is dropped.  bf16
+// outputs take a wide range for the lag: moving either costs the tcgen05 kernel as much as a tile.
+// p 2^e stays a normal number for every vs of 2^-96 .. 2^128 with 2^kBias taken out of vs; e is at most kMost, and at least kLeast, which no
+// finite vs passes 2^kTop with.
 template <bool kBf16>
 struct Weights8 {
-  static constexpr int kLog2 = kBf16 ? 6 : 10;
-  static constexpr float kOne = (float)(1 << kLog2), kLag = (float)(14 - kLog2);
+  static constexpr float kLog2 = kBf16 ? 6.f : 10.f, kTop = 14.f, kLag = kTop - kLog2;
+  static constexpr float kMost = 102.f, kLeast = -126.f;
+  static constexpr int kBias = 16;
 };
+constexpr float kUnbiased = 0x1p-16f;      // 2^-kBias
+// The exponent of a row's weights, from the one that would leave its sums as they are and the largest weight, log 2, under that; with room for
+// more where the row's reference has moved.
+template <class W>
+__device__ __forceinline__ float exponent_of_weights(float e, float largest, bool moved) {
+  return fmaxf(floorf(largest > (moved ? W::kLog2 : W::kTop) ? e + (W::kLog2 - largest) : e), W::kLeast);
+}
+// 2^e of a whole number, from the low bits of a sum.
+__device__ __forceinline__ float power_of_two(float e) { return __uint_as_float(__float_as_uint(e + (0x1p23f + 127.f)) << 23); }
+__device__ __forceinline__ float lg2_approx(float x) {
+  float y;
+  asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// log2 |vs|, of what is not finite that of zero: it is NaN in the output whatever e is.
+__device__ __forceinline__ float log_scale(float vs) {
+  const float x = fabsf(vs);
+  return x < INFINITY ? lg2_approx(x) : -INFINITY;
+}
 
 __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
   uint32_t r;

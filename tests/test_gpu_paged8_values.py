@@ -1,0 +1,81 @@
+"""The 8-bit paged cache where values lie far apart or next to a border of the type.
+
+Scales of V: a weight enters its product as a 16-bit float, relative to the largest weight times scale that the query itself sees, which
+stands at 2^3 .. 2^14 (fp32 outputs 2^9 .. 2^14, two parts).  So a term is off by half a step, 2^-11 (2^-22) of itself, or by 2^-25 of
+those units, 2^-28 (2^-34) of the largest, where it is too small for that."""
+import copy
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged8 as oracle8
+from test_gpu_paged import BF, DEV, F32, U, f64
+from test_gpu_paged8 import PATHS, Case8, every_path
+
+pytestmark = pytest.mark.gpu
+
+
+def tokens(path, seed, at_least=4, **kw):
+    """A case with a scale for every token; its first sequence has at_least new rows."""
+    dtype, D, Hq, Hkv, lens, counts, room = PATHS[path]
+    return Case8(lens, [max(at_least, counts[0]), *counts[1:]], Hq, Hkv, D, 16, 1, dtype, seed=seed, room=room, **kw)
+
+
+def with_scale(c, t, by):
+    d = copy.copy(c)
+    d.scales = [x.clone() for x in c.scales]
+    page, off = d.place(0, t)
+    d.scales[1][page, :, off] *= by
+    return d
+
+
+@every_path
+@pytest.mark.parametrize("by", [2.0 ** 40, -2.0 ** 12, 2.0 ** 110])
+def test_large_values_of_a_hidden_row_leave_the_other_queries_as_they_are(path, by):
+    """The last new row, and rows at and outside a window's edge, with a scale of V far above the others."""
+    c = tokens(path, 3)
+    n, count = c.lens[0], c.counts[0]
+    clean, clean_lse, scale = c.run()
+    d = with_scale(c, n - 1, by)
+    out, lse, _ = d.run()
+    assert torch.equal(out[:count - 1], clean[:count - 1]) and torch.equal(out[count:], clean[count:]) and torch.equal(lse, clean_lse)
+    keep = np.zeros(c.N, dtype=bool)
+    keep[count - 1] = True
+    d.compare(out, lse, d.reference(scale), scale, keep)
+    edge = n - count + 1 - 5                     # window 5: of all queries the first alone sees this row
+    clean, clean_lse, _ = c.run(window=5)
+    out, lse, _ = with_scale(c, edge, by).run(window=5)
+    assert torch.equal(out[1:], clean[1:]) and torch.equal(lse, clean_lse)
+    out, lse, _ = with_scale(c, edge - 1, by).run(window=5)
+    assert torch.equal(out, clean) and torch.equal(lse, clean_lse)
+
+
+def weight_error(dtype, E, n):
+    bf = dtype == BF
+    return 2 * (2 * E + 2.0 ** -21 + (2.0 ** -11 if bf else 2.0 ** -22)) + 4 * (16 + math.sqrt(n)) * U
+
+
+@every_path
+def test_a_large_value_of_small_weight_does_not_take_the_others_bits(path):
+    """A row with 2^30 times the scale of V and weights near 2^-45: the largest terms are the others'."""
+    c = tokens(path, 5, 1)
+    D, rows = c.D, c.counts[0]
+    c.q = (c.q.float().abs() + 0.1).to(c.dtype)
+    page, off = c.place(0, 7)
+    c.codes[0][page, :, off] = 0xfe                                        # -448 each
+    c.scales[0][page, :, off] = 45 * math.log(2) * math.sqrt(D) / (0.9 * D * 448)
+    c.scales[1][page, :, off] = 0.01 * 2.0 ** 30
+    out, lse, scale = c.run(causal=False)
+    want, want_lse, spread, reach = (x[:rows] for x in c.reference(scale, causal=False))
+    k, v = c.values()
+    by_scale = [v, c.scales[1].abs().double().to(DEV)[..., None].expand(*c.codes[1].shape)]
+    most = oracle8.attn_paged(c.q[:c.N].double().to(DEV), k, by_scale[1], c.table, c.lens, c.starts, scale, False)[0][:rows]
+    q = f64(c.q)[:rows]
+    most_k = float(torch.where(torch.isfinite(k), k.abs(), 0.0).sum(-1).max())
+    bf, n = c.dtype == BF, max(c.lens)
+    E = (D + 4) * U * reach + (2.0 ** -21 if bf else 2.0 ** -39) * scale * np.abs(q).max(-1) * most_k + (0.0 if bf else 2.0 ** -22 * reach)
+    tol = (2.0 ** -8 if bf else U) * np.abs(want) + weight_error(c.dtype, E, n)[..., None] * spread + n * 448 * (2.0 ** -28 if bf else 2.0 ** -34) * most
+    err = np.abs(f64(out)[:rows] - want)
+    assert (err <= tol).all(), (err - tol).max()
