@@ -13,7 +13,8 @@
 // down to 2^-31 of that.  fp32 queries are two such parts (22 bits).  The scale of K and the row's factor multiply the score, the scale of V
 // the weight, with a power of two for each row (Weights8): the largest weight that the row sees stands at 2^5 .. 2^14, which keeps 11 bits down
 // to 2^-19 of it and drops what is below 2^-30: a weight's rounding, 2^-11, is an eighth of the output's in bf16.  For fp32 outputs it stands
-// at 2^9 .. 2^14 and the weights are two such parts.
+// at 2^9 .. 2^14 and the weights are two such parts, the second times 2^11 against V 2^-11: fp16's smallest steps would otherwise end it
+// at 2^-12 of the largest.  22 bits down to 2^-23 of the largest, nothing below 2^-45.
 //
 // Measured: 32 x 32 heads at length, 1.08 GB, 183 - 186 us (5.9 TB/s, nine tenths of a plain copy; 188 with V transposed in pairs and
 // permuted); the issue slots are half in use, a third of them for conversions.  8 x 32 heads of 32 rows x 1024 .. 2080 keys 66 us, which is the
@@ -299,7 +300,7 @@ struct ByteRows {
           w[nb][g][0][h] = pack_half(w0, w1);
           if constexpr (kParts == 2) {
             const float2 f = halves_f32(w[nb][g][0][h]);
-            w[nb][g][1][h] = pack_half(isfinite(f.x) ? w0 - f.x : 0.f, isfinite(f.y) ? w1 - f.y : 0.f);
+            w[nb][g][1][h] = pack_half(isfinite(f.x) ? (w0 - f.x) * 0x1p11f : 0.f, isfinite(f.y) ? (w1 - f.y) * 0x1p11f : 0.f);
           }
         }
     }
@@ -322,9 +323,12 @@ struct ByteRows {
         for (int k = 0; k < 2; ++k) {
           const uint32_t a0 = halves_lo(v[2 * k]), a1 = halves_lo(v[2 * k + 1]), a2 = halves_hi(v[2 * k]), a3 = halves_hi(v[2 * k + 1]);
 #pragma unroll
-          for (int part = 0; part < kParts; ++part)
+          for (int nb = 0; nb < NB; ++nb) mma_half(o[nb][2 * c + k], a0, a1, a2, a3, w[nb][g][0][0], w[nb][g][0][1]);
+          if constexpr (kParts == 2) {      // V 2^-11, which fp16 holds too: e4m3 values are multiples of 2^-9
+            const uint32_t s0 = mul_halves(a0, 0x10001000u), s1 = mul_halves(a1, 0x10001000u), s2 = mul_halves(a2, 0x10001000u), s3 = mul_halves(a3, 0x10001000u);
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) mma_half(o[nb][2 * c + k], a0, a1, a2, a3, w[nb][g][part][0], w[nb][g][part][1]);
+            for (int nb = 0; nb < NB; ++nb) mma_half(o[nb][2 * c + k], s0, s1, s2, s3, w[nb][g][1][0], w[nb][g][1][1]);
+          }
         }
       }
   }

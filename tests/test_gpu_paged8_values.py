@@ -1,8 +1,8 @@
 """The 8-bit paged cache where values lie far apart or next to a border of the type.
 
 Scales of V: a weight enters its product as a 16-bit float, relative to the largest weight times scale that the query itself sees, which
-stands at 2^3 .. 2^14 (fp32 outputs 2^9 .. 2^14, two parts).  So a term is off by half a step, 2^-11 (2^-22) of itself, or by 2^-25 of
-those units, 2^-28 (2^-34) of the largest, where it is too small for that."""
+stands at 2^3 .. 2^14 (fp32 outputs 2^9 .. 2^14, two parts, the second times 2^11).  So a term is off by half a step, 2^-11 (2^-22) of
+itself, or by 2^-25 of those units (2^-36), 2^-28 (2^-45) of the largest, where it is too small for that."""
 import copy
 import math
 
@@ -76,6 +76,34 @@ def test_a_large_value_of_small_weight_does_not_take_the_others_bits(path):
     most_k = float(torch.where(torch.isfinite(k), k.abs(), 0.0).sum(-1).max())
     bf, n = c.dtype == BF, max(c.lens)
     E = (D + 4) * U * reach + (2.0 ** -21 if bf else 2.0 ** -39) * scale * np.abs(q).max(-1) * most_k + (0.0 if bf else 2.0 ** -22 * reach)
-    tol = (2.0 ** -8 if bf else U) * np.abs(want) + weight_error(c.dtype, E, n)[..., None] * spread + n * 448 * (2.0 ** -28 if bf else 2.0 ** -34) * most
+    tol = (2.0 ** -8 if bf else U) * np.abs(want) + weight_error(c.dtype, E, n)[..., None] * spread + n * 448 * (2.0 ** -28 if bf else 2.0 ** -45) * most
     err = np.abs(f64(out)[:rows] - want)
     assert (err <= tol).all(), (err - tol).max()
+
+
+@every_path
+@pytest.mark.parametrize("below", [16, 24, 38])
+def test_scales_far_below_the_largest(path, below):
+    """In the upper half of the dimensions one row alone has values, under a scale of V 2^-below times the others'; weights near 1 / n."""
+    bf = PATHS[path][0] == BF
+    if bf and below > 24:
+        pytest.skip("a bf16 output's weights end at 2^-28")
+    c = tokens(path, 6, 1, sharp=0.02)
+    D, rows, n = c.D, c.counts[0], c.lens[0]
+    t = torch.arange(n)
+    page, off = c.place(0, t)
+    c.codes[1][page, :, off, D // 2:] = 0
+    c.scales[1][page, :, off] = 0.01
+    page, off = c.place(0, n // 2)
+    c.codes[1][page, :, off, D // 2:] = 0x7e                               # 448
+    c.scales[1][page, :, off] = 0.01 * 2.0 ** -below
+    out, lse, scale = c.run(causal=False)
+    want, _, spread, reach = (x[:rows] for x in c.reference(scale, causal=False))
+    assert (reach < 0.3).all()                                             # so that a weight is at most e^0.6 < 2 times another
+    q = f64(c.q)[:rows]
+    k = c.values()[0]
+    most_k = float(torch.where(torch.isfinite(k), k.abs(), 0.0).sum(-1).max())
+    E = (D + 4) * U * reach + (2.0 ** -21 if bf else 2.0 ** -39) * scale * np.abs(q).max(-1) * most_k + (0.0 if bf else 2.0 ** -22 * reach)
+    rel = (2.0 ** -8 if bf else U) + weight_error(c.dtype, E, n) + 2 * 2.0 ** (below - (28 if bf else 45))
+    err = np.abs(f64(out)[:rows] - want)[..., D // 2:]
+    assert (err <= rel[..., None] * np.abs(want[..., D // 2:])).all(), (err / np.abs(want[..., D // 2:])).max()
