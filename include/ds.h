@@ -615,7 +615,7 @@ DS_API int ds_attn_paged(const ds_paged_params *p, void *stream);
  *     a  = largest |x| of the call's finite values in the block
  *     2^e with e the smallest integer >= -126 for which a <= 448 * 2^e, and
  *          2^e >= |s| where the block holds rows from before the call (before kv_len[b] - n_b) and its scale has |s| <= 2^127
- *     the new rows become  RN(x / 2^e), the rows from before  RN(value * s / 2^e)  unless s = 2^e;  the scale becomes 2^e
+ *     the new rows become  RN(x / 2^e), the rows from before  RN(value * s / 2^e)  unless s = 2^e (448 beyond it);  the scale becomes 2^e
  * with RN to the nearest e4m3 value, ties to even.  The division by a power of two is exact, so that there is one
  * rounding, and rows from before change only where they fall below 2^-6 of the new scale.  Infinities and NaN are held as
  * NaN, as are rows from before under an infinite or NaN scale; |x| > 1.875 * 2^127 is held as that (what it would be rounded to

@@ -30,6 +30,13 @@ __device__ __forceinline__ uint32_t halves_hi(uint32_t w) {
 }
 __device__ __forceinline__ float2 halves_f32(uint32_t h) { return __half22float2(*reinterpret_cast<const __half2 *>(&h)); }
 
+// The product cut off at 24 bits, its last bit set if that lost something: rounding it to two bits fewer or less gives the product
+// rounded once.  The product must be 2^-100 or more in magnitude, or zero; what passes the largest value becomes that value.
+__device__ __forceinline__ float mul_to_odd(float a, float b) {
+  const float r = __fmul_rz(a, b), rest = fmaf(a, b, -r);
+  return rest > 0.f || rest < 0.f ? __uint_as_float(__float_as_uint(r) | 1u) : r;
+}
+
 // Whether one of a word's four bytes is NaN.
 __device__ __forceinline__ bool any_nan_e4m3(uint32_t w) { return __vcmpeq4(w & 0x7f7f7f7fu, 0x7f7f7f7fu) != 0; }
 

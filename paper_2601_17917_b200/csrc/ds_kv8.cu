@@ -158,8 +158,13 @@ __device__ __forceinline__ void store_codes(uint8_t *to, const uint4 &w, float b
   if constexpr (E == 8) *reinterpret_cast<uint2 *>(to) = make_uint2(pack_e4m3x4(f[0], f[1], f[2], f[3]), pack_e4m3x4(f[4], f[5], f[6], f[7]));
   else *reinterpret_cast<uint32_t *>(to) = pack_e4m3x4(f[0], f[1], f[2], f[3]);
 }
-// Rows under the scale s0 that come under another: lane u of n.
-__device__ __forceinline__ void rescale(uint8_t *rows, long long row_bytes, int held, int D, float f, int u, int n) {
+// Rows under the scale s0 that come under another: lane u of n.  The quotient of the scales is exact; beyond 2^60 and below 2^-60 of
+// it every value but zero is the largest or zero.
+__device__ __forceinline__ void rescale(uint8_t *rows, long long row_bytes, int held, int D, float s0, uint32_t now_bits, int u, int n) {
+  const bool small = fabsf(s0) < 0x1p-100f;
+  const uint32_t b = __float_as_uint(small ? s0 * 0x1p40f : s0), exponent = (b >> 23) & 255u;
+  const int power = max(-60, min(60, (int)exponent - (small ? 40 : 0) - (int)(now_bits >> 23)));
+  const float f = exponent == 255u ? __uint_as_float(0x7fffffffu) : s0 == 0.f ? s0 : __uint_as_float((b & 0x807fffffu) | (uint32_t)(127 + power) << 23);
   for (int c = u; c < held * (D / 16); c += n) {
     uint4 *at = reinterpret_cast<uint4 *>(rows + c / (D / 16) * row_bytes + c % (D / 16) * 16);
     const uint4 w = *at;
@@ -167,7 +172,7 @@ __device__ __forceinline__ void rescale(uint8_t *rows, long long row_bytes, int 
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       const float2 lo = halves_f32(halves_lo(x[k])), hi = halves_f32(halves_hi(x[k]));
-      x[k] = pack_e4m3x4(scaled(lo.x * f, 1.f), scaled(lo.y * f, 1.f), scaled(hi.x * f, 1.f), scaled(hi.y * f, 1.f));
+      x[k] = pack_e4m3x4(mul_to_odd(lo.x, f), mul_to_odd(lo.y, f), mul_to_odd(hi.x, f), mul_to_odd(hi.y, f));
     }
     *at = make_uint4(x[0], x[1], x[2], x[3]);
   }
@@ -207,7 +212,7 @@ __device__ __forceinline__ void write_run(uint4 *buf, const T *src, long long sr
   }
   if (count > 0) {
     const bool same = held > 0 && __float_as_uint(s0) == now.bits;
-    if (held > 0 && !same) rescale(before, code_row, held, D, s0 * now.by, u, L);
+    if (held > 0 && !same) rescale(before, code_row, held, D, s0, now.bits, u, L);
     if (u == 0 && !same) *scale = __uint_as_float(now.bits);
   }
   __syncwarp();
@@ -374,7 +379,7 @@ __global__ void __launch_bounds__(kThreads, 4) kv8_write_wide_kernel(const __gri
       for (int i = kWideKeep; i < n_mine; ++i, mine_at += code_step)
         store_codes<T>(mine_at, *reinterpret_cast<const uint4 *>(src + i * src_step), now.by, plain);
       const bool same = run.held > 0 && __float_as_uint(s0) == now.bits;
-      if (run.held > 0 && !same) rescale(code - run.held * p.cache_stride[2], p.cache_stride[2], run.held, p.D, s0 * now.by, tid, kThreads);
+      if (run.held > 0 && !same) rescale(code - run.held * p.cache_stride[2], p.cache_stride[2], run.held, p.D, s0, now.bits, tid, kThreads);
       if (tid == 0 && !same) *scale = __uint_as_float(now.bits);
     }
   }

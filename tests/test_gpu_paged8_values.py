@@ -12,7 +12,7 @@ import torch
 
 from oracle import paged8 as oracle8
 from test_gpu_paged import BF, DEV, F32, U, f64
-from test_gpu_paged8 import PATHS, Case8, every_path
+from test_gpu_paged8 import PATHS, Case8, Pool, every_path
 
 pytestmark = pytest.mark.gpu
 
@@ -107,3 +107,51 @@ def test_scales_far_below_the_largest(path, below):
     rel = (2.0 ** -8 if bf else U) + weight_error(c.dtype, E, n) + 2 * 2.0 ** (below - (28 if bf else 45))
     err = np.abs(f64(out)[:rows] - want)[..., D // 2:]
     assert (err <= rel[..., None] * np.abs(want[..., D // 2:])).all(), (err / np.abs(want[..., D // 2:])).max()
+
+
+# ------------------------------------------------------------------------------------------------ one rounding
+def near_ties(n, ties, low, high, seed):
+    """n pairs of an e4m3 byte and an fp32 scale in (low, high] whose product lies within 2^-24 of a tie, or on it."""
+    rng = np.random.default_rng(seed)
+    codes, scales = [], []
+    while len(codes) < n:
+        c, tie = int(rng.integers(1, 0x7f)), float(rng.choice(ties))
+        s = np.float32(tie / oracle8.E4M3[c])
+        if low < s <= high:
+            codes.append(c | (0x80 if rng.random() < 0.5 else 0))
+            scales.append(s)
+    return np.array(codes, np.uint8), np.array(scales, np.float32)
+
+
+def test_rows_held_under_foreign_scales_are_rounded_once():
+    """Scales in (1/2, 1] become 1: products next to the border between two e4m3 values."""
+    B = 400
+    p = Pool([7] * B, [1] * B, 1, 32, 8, 8, seed=2)
+    mid = (oracle8.E4M3[1:0x7f] + oracle8.E4M3[:0x7e]) / 2
+    for i in range(2):
+        codes, scales = near_ties(B, mid, 0.5, 1.0, seed=i)
+        codes[0], scales[0] = 0x09, 0.6111111
+        assert oracle8.E4M3[codes[0]] == 0.017578125
+        pages = p.table[:, 0].long()
+        p.codes[i][pages, 0, :, ::2] = torch.from_numpy(codes)[:, None, None].expand(B, 8, 16)
+        p.scales[i][pages, 0, 0] = torch.from_numpy(scales)
+    for dtype in (BF, F32):
+        p.check(torch.zeros(p.N + 3, 2, 32, dtype=dtype))
+
+
+@pytest.mark.parametrize("s", [1.5 * 2.0 ** 127, -1.0000001 * 2.0 ** 127, 2.0 ** 127, 2.0 ** -149, -1.7 * 2.0 ** -130])
+@pytest.mark.parametrize("new", [0.0, 1.0, 2.0 ** 100, 2.0 ** 127])
+def test_rows_held_under_the_largest_and_smallest_scales(s, new):
+    """Every byte, rescaled from s to what the new row needs: beyond 448 the largest, far below nothing."""
+    p = Pool([8], [1], 1, 256, 16, 16)
+    page = p.table[0, 0].long()
+    for i in range(2):
+        p.codes[i][page] = torch.arange(256, dtype=torch.int32).to(torch.uint8)
+        p.scales[i][page] = s
+    p.check(torch.full((4, 2, 256), new, dtype=F32))
+    long = Pool([8], [40], 1, 256, 64, 64)                                 # the kernel for long runs
+    page = long.table[0, 0].long()
+    for i in range(2):
+        long.codes[i][page] = torch.arange(256, dtype=torch.int32).to(torch.uint8)
+        long.scales[i][page] = s
+    long.check(torch.full((43, 2, 256), new, dtype=F32))
