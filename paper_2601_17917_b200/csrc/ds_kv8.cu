@@ -396,6 +396,31 @@ struct ReadLaunch {
 };
 constexpr int kReadRows = 32;
 
+// Eight values times a scale of any bits, each rounded once: the products are cut off at 24 bits, to odd; small ones by way of 64 bits, as
+// what is cut off has to be a number.  (Scales of ds_kv8_write do not come here.)
+__device__ __noinline__ void store_any_scale(__nv_bfloat16 *to, uint32_t lo, uint32_t hi, float s) {
+  __nv_bfloat162 v[4];
+  if (fabsf(s) >= 0x1p-90f || s != s) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float2 a = halves_f32(e & 1 ? halves_hi(e < 2 ? lo : hi) : halves_lo(e < 2 ? lo : hi));
+      v[e] = __floats2bfloat162_rn(mul_to_odd(a.x, s), mul_to_odd(a.y, s));
+    }
+  } else {
+    auto small = [&](float a) {
+      const double x = (double)a * (double)s;
+      const float r = __double2float_rz(x);
+      return (double)r != x ? __uint_as_float(__float_as_uint(r) | 1u) : r;
+    };
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float2 a = halves_f32(e & 1 ? halves_hi(e < 2 ? lo : hi) : halves_lo(e < 2 ? lo : hi));
+      v[e] = __floats2bfloat162_rn(small(a.x), small(a.y));
+    }
+  }
+  *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(v);
+}
+
 template <typename T>
 __device__ __forceinline__ void store_values(T *to, const uint2 &w, float s) {
   const float2 a0 = halves_f32(halves_lo(w.x)), a1 = halves_f32(halves_hi(w.x)), a2 = halves_f32(halves_lo(w.y)), a3 = halves_f32(halves_hi(w.y));
@@ -403,6 +428,10 @@ __device__ __forceinline__ void store_values(T *to, const uint2 &w, float s) {
     reinterpret_cast<float4 *>(to)[0] = make_float4(a0.x * s, a0.y * s, a1.x * s, a1.y * s);
     reinterpret_cast<float4 *>(to)[1] = make_float4(a2.x * s, a2.y * s, a3.x * s, a3.y * s);
   } else {
+    const uint32_t b = __float_as_uint(s) & 0x7fffffffu;
+    // a power of two, as ds_kv8_write's are, and no product too small for fp32: exact; or nothing but zeros, whose scale is the smallest
+    const bool exact = (b & 0x7fffffu) == 0 && (b >= (127u - 90u) << 23 || ((w.x | w.y) & 0x7f7f7f7fu) == 0);
+    if (__builtin_expect(!exact, 0)) return store_any_scale(to, w.x, w.y, s);
     const __nv_bfloat162 v[4] = {__floats2bfloat162_rn(a0.x * s, a0.y * s), __floats2bfloat162_rn(a1.x * s, a1.y * s),
                                  __floats2bfloat162_rn(a2.x * s, a2.y * s), __floats2bfloat162_rn(a3.x * s, a3.y * s)};
     *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(v);

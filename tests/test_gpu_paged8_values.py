@@ -12,7 +12,7 @@ import torch
 
 from oracle import paged8 as oracle8
 from test_gpu_paged import BF, DEV, F32, U, f64
-from test_gpu_paged8 import PATHS, Case8, Pool, every_path
+from test_gpu_paged8 import PATHS, Case8, Pool, every_path, read_back
 
 pytestmark = pytest.mark.gpu
 
@@ -155,3 +155,37 @@ def test_rows_held_under_the_largest_and_smallest_scales(s, new):
         long.codes[i][page] = torch.arange(256, dtype=torch.int32).to(torch.uint8)
         long.scales[i][page] = s
     long.check(torch.full((43, 2, 256), new, dtype=F32))
+
+
+def nearest_bf16(x):
+    """float64 -> the nearest bf16 value, ties to even; beyond the largest infinite."""
+    unit = np.exp2(np.maximum(np.frexp(x)[1], -125) - 8.0)
+    y = np.rint(x / unit) * unit
+    return np.where(np.abs(y) >= 2.0 ** 128, np.sign(y) * np.inf, y)
+
+
+@pytest.mark.parametrize("shift", [0, 60, 115, -100, -118, -125, -130])
+def test_rows_read_back_in_bf16_are_rounded_once(shift):
+    """Products next to the border between two bf16 values, ordinary ones and some that are next to the type's ends."""
+    n = 600
+    rng = np.random.default_rng(7)
+    ties = (256 + rng.integers(0, 256, 4000) + 0.5) * 2.0 ** (shift - 8)   # halfway between neighbours of 8 bits
+    if shift < -110:
+        ties = (rng.integers(1, 256, 4000) + 0.5) * 2.0 ** -133            # of the smallest
+        if shift < -118:
+            ties = ties + rng.choice([-1, 1], 4000) * 2.0 ** (-149 if shift == -125 else -153)
+    p = Pool([n], [0], 1, 16, 8, 1)
+    t = np.arange(n)
+    page, off = p.table[0].long()[torch.from_numpy(t // 8)], torch.from_numpy(t % 8)
+    want = []
+    for i in range(2):
+        codes, scales = near_ties(n, ties, 2.0 ** -149, 3e38, seed=i)
+        if shift == 0:
+            codes[0], scales[0] = 0x09, 58.444443
+        p.codes[i][page, 0, off] = torch.from_numpy(codes)[:, None].expand(n, 16)
+        p.scales[i][page, 0, off] = torch.from_numpy(scales)
+        want.append(nearest_bf16(oracle8.E4M3[codes] * scales.astype(np.float64)))
+    out, _ = read_back(p, [c.to(DEV) for c in p.codes], [s.to(DEV) for s in p.scales], BF)
+    for i in range(2):
+        got = f64(out[i])[:, 0]
+        assert np.array_equal(got, np.repeat(want[i][:, None], 16, 1)), np.argwhere(got[:, 0] != want[i])[:4]
