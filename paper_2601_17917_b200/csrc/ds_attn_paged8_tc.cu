@@ -66,11 +66,12 @@ struct Geo {
   static constexpr int kOffFactor = kOffScale + kScaleRing * 1536;        // [kRows]
   static constexpr int kOffMl = kOffFactor + kRows * 4;                   // [256]
   static constexpr int kOffTo = kOffMl + (kPair ? 0 : 256 * 8);           // [kRows]
-  static constexpr int kOffBar = kOffTo + kRows * 8;
+  static constexpr int kOffNan = kOffTo + kRows * 8;                      // [kRows][D / 32]: outputs that V makes NaN
+  static constexpr int kOffBar = kOffNan + kRows * D / 8;
   // k_full, k_empty, v_full, v_empty [kSlots], v16_full, v16_free [2], scale_ready, scale_free [kScaleRing], s_full, p_full, pv_done, o_free
   // [2], q_full, q_free, meet, joined
   static constexpr int kNumBars = 4 * kSlots + 4 + 2 * kScaleRing + 8 + 4;
-  static constexpr int kOffMisc = kOffBar + 8 * kNumBars;      // TMEM base (8), NaN in V, sizes of V's scales [kScaleRing]
+  static constexpr int kOffMisc = kOffBar + 8 * kNumBars;      // TMEM base (8), piece with NaN in V, sizes of V's scales [kScaleRing]
   static constexpr int kOffScan = (kOffMisc + 12 + 4 * kScaleRing + 7) / 8 * 8;
   // Sums on their way out, [256][kOutDims] fp32.  Of pairs in a place of their own: a stream need not wait for the other's last products.
   static constexpr int kOutDims = kPair ? 16 : D == 128 ? 64 : 32;
@@ -152,29 +153,33 @@ __device__ __forceinline__ Seen seen_keys(const PagedShape &s, const PagedSeq &q
   return {end - t, paged_max(s.sinks - t, 0), paged_max(end - s.window, 0) - t};
 }
 
-// V's NaN are zeros in the product.  Where there were any, the n keys from x on are gone through for those that the row sees: bit e
-// of the result: element d + e, of four, is NaN.
-__device__ __noinline__ uint32_t nan_elements(const Args8 &a, const Item it, int x, int n, int end, int d) {
-  const ds_paged_params &p = a.p;
-  const int32_t *table = p.block_table + it.b * p.table_stride;
-  const uint8_t *base = reinterpret_cast<const uint8_t *>(p.v_cache) + it.g * p.cache_stride[1] + d;
-  uint32_t found = 0;
-#pragma unroll 1
-  for (int i = 0; i < n; ++i) {
-    const int t = paged_key(it.q, x + i);
-    if (!paged_visible(a.s, t, end)) continue;
-    const int j = fast_div(t, a.page_div), page = paged_clamp_page(table[j], p.n_pages);
-    found |= __vcmpeq4(*reinterpret_cast<const uint32_t *>(base + page * p.cache_stride[0] + (t - j * p.page_size) * p.cache_stride[2]) & 0x7f7f7f7fu,
-                       0x7f7f7f7fu);
-  }
-  return found;
+// V's NaN are zeros in the product of a tile that not every row sees whole; what they make of the rows' outputs is noted here, a bit for
+// each dimension: which bytes of a chunk of 16 dimensions are NaN,
+__device__ __forceinline__ uint32_t nan_bits(const uint4 &w) {
+  const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+  uint32_t bits = 0;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) bits |= (((__vcmpeq4(x[e] & 0x7f7f7f7fu, 0x7f7f7f7fu) & 0x01010101u) * 0x01020408u) >> 24) << (4 * e);
+  return bits;
 }
-__device__ __forceinline__ float4 with_nan(float4 v, uint32_t bytes) {
+// the rows of an item that see cache row t, which follow one another,
+struct RowRange {
+  int lo, hi;
+};
+__device__ __forceinline__ RowRange rows_that_see(const PagedShape &s, const Item &it, int t) {
+  if (t < 0) return {0, 0};
+  const long long last_seen = s.window > 0 && t >= s.sinks ? (long long)t + s.window : 0x7fffffffffffll;      // ends beyond t and up to this see it
+  if (!s.causal) return {0, it.q.len > t && it.q.len <= last_seen ? it.rows : 0};
+  auto queries = [&](long long i) { return (int)min(max(i, 0ll), (long long)it.q.count) * s.G - it.row0; };      // rows of those before i
+  return {max(queries((long long)t + 1 - it.q.end_min), 0), min(queries(last_seen - it.q.end_min + 1), it.rows)};
+}
+// and the outputs.
+__device__ __forceinline__ float4 with_nan(float4 v, uint32_t bits) {
   const float nan = __uint_as_float(0x7fffffffu);
-  if (bytes & 0xffu) v.x = nan;
-  if (bytes & 0xff00u) v.y = nan;
-  if (bytes & 0xff0000u) v.z = nan;
-  if (bytes & 0xff000000u) v.w = nan;
+  if (bits & 1u) v.x = nan;
+  if (bits & 2u) v.y = nan;
+  if (bits & 4u) v.z = nan;
+  if (bits & 8u) v.w = nan;
   return v;
 }
 
@@ -224,7 +229,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
                  bar_pv_done = bar_p_full + 16, bar_o_free = bar_pv_done + 16, bar_q_full = bar_o_free + 16, bar_q_free = bar_q_full + 8,
                  bar_meet = bar_q_free + 8, bar_joined = bar_meet + 8;
   volatile uint32_t *tmem_s = reinterpret_cast<volatile uint32_t *>(smem + G::kOffMisc);
-  volatile int *v_nan = reinterpret_cast<volatile int *>(smem + G::kOffMisc + 8);      // some tile of V held NaN so far
+  volatile int *v_nan = reinterpret_cast<volatile int *>(smem + G::kOffMisc + 8);      // the last piece, from 1 on, in which kOffNan has something
   // of the largest finite scale of V of a tile, its biased exponent, rounded up; kMixed: not every row sees every key, or some scale is
   // below a quarter of that
   volatile uint32_t *vsize_s = reinterpret_cast<volatile uint32_t *>(smem + G::kOffMisc + 12);
@@ -258,6 +263,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
     *v_nan = 0;
     fence_barrier_init();
   }
+  uint32_t *nan_s = reinterpret_cast<uint32_t *>(smem + G::kOffNan);
+  for (int i = tid; i < G::kRows * D / 32; i += kThreads) nan_s[i] = 0;
   if (warp == kMmaWarp) tmem_alloc(sbase + G::kOffMisc, kTmemCols);
   tc_fence_before();
   __syncthreads();
@@ -361,8 +368,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
           *reinterpret_cast<uint4 *>(to + half_at(r, 2 * c + 1)) = make_uint4(halves_lo(w.z), halves_hi(w.z), halves_lo(w.w), halves_hi(w.w));
         }
         if (!paged_all_visible(a.s, it.q, (walk.tile0 + i) * kKeys, kKeys)) {
-          // Keys that some rows see and others do not: a weight of zero times NaN would be NaN.  NaN becomes zero here, and the epilogue
-          // is told to look for it.  (Where every row sees every key, the product does what it should.)
+          // Keys that some rows see and others do not: a weight of zero times NaN would be NaN.  NaN becomes zero here, and the outputs of
+          // the rows that see it are noted.  (Where every row sees every key, the product does what it should.)
           bool nan = false;
 #pragma unroll 1
           for (int o = 0; o < kOps; ++o) {
@@ -379,7 +386,21 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
               *h = v & ~(((v & 0x7c00u) == 0x7c00u ? 0xffffu : 0u) | ((v & 0x7c000000u) == 0x7c000000u ? 0xffff0000u : 0u));
             }
           }
-          if (nan) *v_nan = 1;
+          if (__any_sync(0xffffffffu, nan)) {
+            if (k > 0) ok = wait(bar_o_free, k - 1) && wait(bar_o_free + 8, k - 1);      // the piece before is written out
+            if (!ok) break;
+#pragma unroll 1
+            for (int o = 0; o < kOps; ++o) {
+              const int r = r8 + 8 * (o & 3), c = c4 + 4 * (o >> 2);
+              const uint32_t bits = nan_bits(*reinterpret_cast<const uint4 *>(from + row_at<D>(r, c)));
+              if (bits == 0) continue;
+              const RowRange rows = rows_that_see(a.s, it, paged_key(it.q, (walk.tile0 + i) * kKeys + r));
+#pragma unroll 1
+              for (int row = rows.lo; row < rows.hi; ++row) atomicOr(nan_s + row * (D / 32) + c / 2, bits << (16 * (c & 1)));
+            }
+            *v_nan = k + 1;
+            __syncwarp();
+          }
         }
         fence_proxy_async();
         __syncwarp();
@@ -668,15 +689,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
         tc_fence_after();
       }
       const bool whole = walk.whole();
-      const int x0 = walk.tile0 * kKeys, n_keys = walk.n_tiles * kKeys;
       const long long slot = (long long)paged_slot(blockIdx.x, walk.first) * a.part_rows;
       const float down = power_of_two(-e);
       // O times this, and down, is a share of the output, or of the part's sums: over the sum of weights or shrunk
       auto share = [&](float sum) { return whole ? (sum == 0.f ? 0.f : 1.f / sum) : a.shrink; };
-      // to be called when the stream's products are done (all of the piece, where a row has two): the tiles that they read have then been
-      // looked through
-      bool nan = false;
-      auto checked = [&](float4 v, int end, int d) { return with_nan(v, nan_elements(a, walk.it, x0, n_keys, end, d)); };
+      bool nan = false;      // known when the stream's products are done (all of the piece, where a row has two): their tiles have been looked through
       auto finish_row = [&](const Row &row, int r, float top, float sum) {
         if (!whole) a.part_ml[slot + r] = make_float2(top, sum);
         else if (p.lse) p.lse[row.n * p.Hq + row.h] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
@@ -706,14 +723,14 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
       if (mine && (kPair || (s == 0 && copy == 0)))      // (the piece before is written out: its sums were, before this one's products)
         to_s[r] = whole ? row.n * p.out_stride[0] + row.h * p.out_stride[1] : (slot + r) * D;
       auto put_out = [&](int r, int d, float4 v) {
-        if (__builtin_expect(nan, 0)) v = checked(v, row_of(a, walk.it, r).end, d);
+        if (__builtin_expect(nan, 0)) v = with_nan(v, nan_s[r * (D / 32) + d / 32] >> (d & 31));
         if (whole) store4(reinterpret_cast<T *>(p.out) + to_s[r] + d, v);
         else *reinterpret_cast<float4 *>(a.part_o + to_s[r] + d) = v;
       };
       if constexpr (kPair) {
         // rows are a warp's own; through shared memory, so that neighbouring lanes write neighbouring elements (a row to a thread took 8000
         // cycles)
-        nan = *v_nan != 0;
+        nan = *v_nan == k + 1;
         if (busy) {
           const float by = share(l) * down;
           if (mine) finish_row(row, r, m, l);
@@ -734,6 +751,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
             }
             __syncwarp();
           }
+          if (__builtin_expect(nan, 0)) {
+            for (int i = 0; i < D / 32; ++i) nan_s[(32 * warp + lane) * (D / 32) + i] = 0;
+          }
         }
       } else {
         // ---- join the streams and copies of a row: each brings its O to the row's reference and writes it down, and they are added up
@@ -741,7 +761,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
         ml_s[tid] = make_float2(m, l);
         meet();      // all products have been waited for, too: V's tiles are free
         if (!ok) break;
-        nan = *v_nan != 0;
+        nan = *v_nan == k + 1;
         const int rr = tr % kPad;
         float top = -INFINITY, sum = 0.f;
 #pragma unroll
@@ -777,6 +797,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
           if (c + J < D) meet();      // the buffer is read
         }
         if (!ok) break;
+        if (__builtin_expect(nan, 0)) {
+          meet();      // every row is written
+          if (!ok) break;
+          for (int i = tid; i < G::kRows * D / 32; i += 32 * kSoftmaxWarps) nan_s[i] = 0;
+        }
         __syncwarp();
         if (lane == 0) mbar_arrive(bar_joined);
       }

@@ -189,3 +189,42 @@ def test_rows_read_back_in_bf16_are_rounded_once(shift):
     for i in range(2):
         got = f64(out[i])[:, 0]
         assert np.array_equal(got, np.repeat(want[i][:, None], 16, 1)), np.argwhere(got[:, 0] != want[i])[:4]
+
+
+# ------------------------------------------------------------------------------------------------ NaN in partly visible tiles
+@pytest.mark.parametrize("D,Hq,count", [(128, 2, 20), (64, 4, 20), (128, 4, 60), (64, 8, 30)])
+@pytest.mark.parametrize("kw", [dict(), dict(causal=False, window=900), dict(window=300, sinks=4)])
+@pytest.mark.parametrize("workspace", [True, False])
+def test_nan_in_one_sequence_costs_the_others_nothing(D, Hq, count, kw, workspace):
+    """NaN in V at the edge of what the first sequence's queries see, long sequences behind it in the same CTAs: status 0, their outputs
+    as they were, and in the first sequence NaN where the formula has it."""
+    n, lens = 330, [330, 40000, 333, 20000, 7, 331]
+    counts = [count, count, count, count, 3, count]
+    c = Case8(lens, counts, Hq, 1, D, 64, 1, BF, seed=count)
+    ws = None if workspace else torch.empty(0, dtype=torch.uint8, device=DEV)
+    clean, clean_lse, _ = c.run(workspace=ws, **kw)
+    d = copy.copy(c)
+    d.codes = [x.clone() for x in c.codes]
+    marks = {t: slice(j, None, 7 + j) for j, t in enumerate((n - 1, n - 2, n - 9, n - count, 3, 40))}
+    for b in (0, 2):
+        for t, dims in marks.items():
+            page, off = d.place(b, t)
+            d.codes[1][page, :, off, dims] = 0x7f
+    out, lse, _ = d.run(workspace=ws, **kw)
+    want, want_lse = clean.clone(), clean_lse
+    for b in (0, 2):
+        for i in range(count):
+            end = lens[b] - count + 1 + i if kw.get("causal", True) else lens[b]
+            for t, dims in marks.items():
+                if t < end and ("window" not in kw or t < kw.get("sinks", 0) or t >= end - kw["window"]):
+                    want[int(c.starts[b]) + i, :, dims] = math.nan
+    assert torch.isnan(want).any() and torch.equal(torch.isnan(out), torch.isnan(want))
+    assert torch.equal(out.nan_to_num(9.0), want.nan_to_num(9.0)) and torch.equal(lse, want_lse)
+
+
+def test_a_whole_prompt_of_nan_ends():
+    """Every byte of V NaN, hundreds of rows: each row that sees a key is NaN, within the kernel's limits of waiting."""
+    c = Case8([1500, 9], [1500, 9], 4, 1, 128, 16, 16, BF, seed=2)
+    c.codes[1].fill_(0xff)
+    out, lse, _ = c.run(window=700)
+    assert torch.isnan(out).all() and torch.isfinite(lse).all()
