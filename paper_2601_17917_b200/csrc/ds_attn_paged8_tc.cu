@@ -69,8 +69,8 @@ struct Geo {
   static constexpr int kOffNan = kOffTo + kRows * 8;                      // [kRows][D / 32]: outputs that V makes NaN
   static constexpr int kOffBar = kOffNan + kRows * D / 8;
   // k_full, k_empty, v_full, v_empty [kSlots], v16_full, v16_free [2], scale_ready, scale_free [kScaleRing], s_full, p_full, pv_done, o_free
-  // [2], q_full, q_free, meet, joined
-  static constexpr int kNumBars = 4 * kSlots + 4 + 2 * kScaleRing + 8 + 4;
+  // [2], q_full, q_free, meet, joined, begun
+  static constexpr int kNumBars = 4 * kSlots + 4 + 2 * kScaleRing + 8 + 5;
   static constexpr int kOffMisc = kOffBar + 8 * kNumBars;      // TMEM base (8), piece with NaN in V, sizes of V's scales [kScaleRing]
   static constexpr int kOffScan = (kOffMisc + 12 + 4 * kScaleRing + 7) / 8 * 8;
   // Sums on their way out, [256][kOutDims] fp32.  Of pairs in a place of their own: a stream need not wait for the other's last products.
@@ -227,7 +227,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
                  bar_v16_full = bar_v_empty + 8 * S, bar_v16_free = bar_v16_full + 16, bar_sc_ready = bar_v16_free + 16,
                  bar_sc_free = bar_sc_ready + 8 * kScaleRing, bar_s_full = bar_sc_free + 8 * kScaleRing, bar_p_full = bar_s_full + 16,
                  bar_pv_done = bar_p_full + 16, bar_o_free = bar_pv_done + 16, bar_q_full = bar_o_free + 16, bar_q_free = bar_q_full + 8,
-                 bar_meet = bar_q_free + 8, bar_joined = bar_meet + 8;
+                 bar_meet = bar_q_free + 8, bar_joined = bar_meet + 8, bar_begun = bar_joined + 8;
   volatile uint32_t *tmem_s = reinterpret_cast<volatile uint32_t *>(smem + G::kOffMisc);
   volatile int *v_nan = reinterpret_cast<volatile int *>(smem + G::kOffMisc + 8);      // the last piece, from 1 on, in which kOffNan has something
   // of the largest finite scale of V of a tile, its biased exponent, rounded up; kMixed: not every row sees every key, or some scale is
@@ -260,6 +260,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
     mbar_init(bar_q_free, 2 + kSoftmaxWarps);
     mbar_init(bar_meet, kSoftmaxWarps);
     mbar_init(bar_joined, kSoftmaxWarps);
+    mbar_init(bar_begun, kSoftmaxWarps / 2);
     *v_nan = 0;
     fence_barrier_init();
   }
@@ -497,14 +498,15 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
     const int s = warp - kMmaWarp;
     const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), ts = tm + kTmemS + s * 128, to = tm + kTmemO + s * 128;
     const uint64_t dq = rows_desc(sbase + (kPair ? s * 128 * D : 0), D), dk0 = rows_desc(sbase + G::kOffK, D), dv0 = smem_desc(sbase + G::kOffV16, kHalfBytes, 1024);
-    int g = 0, n = 0, n0 = 0;      // key tiles of the pieces before; steps of this stream, of the first one
+    int g = 0, n = 0;      // key tiles of the pieces before; steps of this stream
     for (int k = 0; ok && walk.piece(a); g += walk.n_tiles, walk.next(a), ++k) {
       const int steps = kPair ? 2 * walk.n_tiles : walk.n_tiles;
       ok = wait(bar_q_full, k);
       if (s >= steps && lane == 0) mbar_arrive(bar_q_free);      // nothing for this stream
       // Half a step apart: the exponentials of one stream beside the products of the other.  (In step, they wait for each other's pipes.)
-      if (ok && s == 1 && s < steps) ok = wait(bar_p_full, n0);
-      n0 += (steps + 1) / 2;
+      // bar_begun, a phase a piece, as the first stream's steps may pass two while this warp waits for one: the next piece's phase needs its
+      // bar_q_free, which this warp's last product arrives at.
+      if (ok && s == 1 && s < steps) ok = wait(bar_begun, k);
 #pragma unroll 1
       for (int u = s - 2; ok && u < steps; u += 2) {
         if (u >= 0) {
@@ -677,6 +679,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
         __syncwarp();
         if (lane == 0) {
           mbar_arrive(bar_p_full + 8 * s);
+          if (u == 0) mbar_arrive(bar_begun);
           mbar_arrive(bar_sc_free + 8 * (t % kScaleRing));
         }
       }

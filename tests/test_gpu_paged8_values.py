@@ -228,3 +228,19 @@ def test_a_whole_prompt_of_nan_ends():
     c.codes[1].fill_(0xff)
     out, lse, _ = c.run(window=700)
     assert torch.isnan(out).all() and torch.isfinite(lse).all()
+
+
+# ------------------------------------------------------------------------------------------------ items of many and of few rows in turn
+@pytest.mark.parametrize("D,Hq,most", [(128, 2, 128), (64, 4, 64), (128, 8, 25), (64, 2, 30)])
+@pytest.mark.parametrize("workspace", [True, False])
+def test_items_of_many_rows_and_of_few_behind_each_other(D, Hq, most, workspace):
+    """256, 100 or 60 rows, then 1 to 4, over 1 to 3 tiles, several items to a CTA: the streams of a CTA end and begin at different times."""
+    B = 330
+    counts = [most if b % 2 == 0 else 1 for b in range(B)]
+    lens = [(150, 40, 260, 390, 120)[b % 5] + b % 7 for b in range(B)]
+    c = Case8(lens, counts, Hq, 1, D, 16, 16, BF, seed=most)
+    ws = None if workspace else torch.empty(0, dtype=torch.uint8, device=DEV)
+    out, lse = c.check(workspace=ws)
+    for _ in range(5):
+        again, lse2, _ = c.run(workspace=ws)
+        assert torch.equal(out, again) and torch.equal(lse, lse2)
