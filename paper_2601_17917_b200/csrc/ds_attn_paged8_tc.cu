@@ -12,9 +12,10 @@
 //   kPair      rows 0 .. 127 and 128 .. 255 of an item, over the same key tiles
 //   otherwise  the same rows, the even and the odd key tiles, joined when the item ends.  Up to 64 rows stand in the tile kCopies
 //              times: each copy weighs 1 / kCopies of the keys and has zeros for the others.
-// Step u of a piece is stream u % 2, key tile u (kPair: u / 2).  A stream's products go out in the order QK0 PV0 QK2 PV2 ..; they execute
-// in order, so S may be written once the product that reads the P in its place has been issued.  The second stream starts half a step
-// later (82 -> 80 us): its exponentials run beside the first one's products.
+// Step u of a piece is stream u % 2, key tile u (kPair: u / 2).  A stream's products go out in the order QK0 PV0 QK2 PV2 ..; S is written
+// again when the product that reads the P in its place is done (waited for: products of different kinds and shapes need not execute in the
+// order of their issue; 82.5 -> 83.4 us).  The second stream starts half a step later (82 -> 80 us): its exponentials run beside the first
+// one's products.
 //
 // Warps:
 //   0-7    softmax and epilogue, thread = tile row = TMEM lane, four warps a stream
@@ -527,7 +528,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
         }
         if (u + 2 < steps) {
           const int t = g + (kPair ? (u + 2) >> 1 : u + 2);
-          ok = wait(bar_k_full + 8 * (t % S), t / S);
+          ok = wait(bar_k_full + 8 * (t % S), t / S) && (u < 0 || wait(bar_pv_done + 8 * s, n - 1));
           if (!ok) break;
           fence_proxy_async();
           tc_fence_after();
