@@ -72,7 +72,7 @@ struct Geo {
   // k_full, k_empty, v_full, v_empty [kSlots], v16_full, v16_free [2], scale_ready, scale_free [kScaleRing], s_full, p_full, pv_done, o_free
   // [2], q_full, q_free, meet, joined, begun
   static constexpr int kNumBars = 4 * kSlots + 4 + 2 * kScaleRing + 8 + 5;
-  static constexpr int kOffMisc = kOffBar + 8 * kNumBars;      // TMEM base (8), piece with NaN in V, sizes of V's scales [kScaleRing]
+  static constexpr int kOffMisc = kOffBar + 8 * kNumBars;      // TMEM base, whether a wait has run out, piece with NaN in V, sizes of V's scales [kScaleRing]
   static constexpr int kOffScan = (kOffMisc + 12 + 4 * kScaleRing + 7) / 8 * 8;
   // Sums on their way out, [256][kOutDims] fp32.  Of pairs in a place of their own: a stream need not wait for the other's last products.
   static constexpr int kOutDims = kPair ? 16 : D == 128 ? 64 : 32;
@@ -120,20 +120,24 @@ __device__ __forceinline__ uint64_t rows_desc(uint32_t addr, int row) {
 __host__ __device__ constexpr uint32_t idesc8(int n, bool a_e5m2) { return (1u << 4) | ((a_e5m2 ? 1u : 0u) << 7) | ((uint32_t)(n >> 3) << 17) | (8u << 24); }
 __host__ __device__ constexpr uint32_t idesc16(int n) { return (1u << 4) | (1u << 16) | ((uint32_t)(n >> 3) << 17) | (8u << 24); }
 
-// Bounded wait in few instructions: what runs once per tile comes through the instruction caches at some four cycles each.
-__device__ __forceinline__ bool wait_parity(uint32_t bar, uint32_t parity) {
-  uint32_t left = kSpinLimit;
+// Bounded wait in few instructions: what runs once per tile comes through the instruction caches at some four cycles each.  The word at
+// `gave_up` is 0, or kSpinLimit when another role's wait has run out: then this one ends, too.
+__device__ __forceinline__ bool wait_parity(uint32_t bar, uint32_t parity, uint32_t gave_up) {
+  int left = kSpinLimit;
   asm volatile(
-      "{\n\t.reg .pred p, q;\n"
+      "{\n\t.reg .pred p, q;\n\t"
+      ".reg .b32 f;\n"
       "WAIT:\n\t"
       "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
       "@p bra DONE;\n\t"
-      "sub.u32 %0, %0, 1;\n\t"
-      "setp.ne.u32 q, %0, 0;\n\t"
+      "ld.volatile.shared.u32 f, [%3];\n\t"
+      "sub.s32 %0, %0, 1;\n\t"
+      "sub.s32 %0, %0, f;\n\t"
+      "setp.gt.s32 q, %0, 0;\n\t"
       "@q bra WAIT;\n"
       "DONE:\n\t}"
-      : "+r"(left) : "r"(bar), "r"(parity) : "memory");
-  return left != 0;
+      : "+r"(left) : "r"(bar), "r"(parity), "r"(gave_up) : "memory");
+  return left > 0;
 }
 
 // Arrives at the barrier when this thread's copies so far are complete.
@@ -229,7 +233,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
                  bar_sc_free = bar_sc_ready + 8 * kScaleRing, bar_s_full = bar_sc_free + 8 * kScaleRing, bar_p_full = bar_s_full + 16,
                  bar_pv_done = bar_p_full + 16, bar_o_free = bar_pv_done + 16, bar_q_full = bar_o_free + 16, bar_q_free = bar_q_full + 8,
                  bar_meet = bar_q_free + 8, bar_joined = bar_meet + 8, bar_begun = bar_joined + 8;
-  volatile uint32_t *tmem_s = reinterpret_cast<volatile uint32_t *>(smem + G::kOffMisc);
+  volatile uint32_t *tmem_s = reinterpret_cast<volatile uint32_t *>(smem + G::kOffMisc), *gave_up = tmem_s + 1;
   volatile int *v_nan = reinterpret_cast<volatile int *>(smem + G::kOffMisc + 8);      // the last piece, from 1 on, in which kOffNan has something
   // of the largest finite scale of V of a tile, its biased exponent, rounded up; kMixed: not every row sees every key, or some scale is
   // below a quarter of that
@@ -262,7 +266,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
     mbar_init(bar_meet, kSoftmaxWarps);
     mbar_init(bar_joined, kSoftmaxWarps);
     mbar_init(bar_begun, kSoftmaxWarps / 2);
-    *v_nan = 0;
+    *v_nan = 0, *gave_up = 0;
     fence_barrier_init();
   }
   uint32_t *nan_s = reinterpret_cast<uint32_t *>(smem + G::kOffNan);
@@ -279,7 +283,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
   const Item &it = walk.it;
   bool ok = true;
   // Every wait is the whole warp's.
-  auto wait = [&](uint32_t bar, int phase) { return __all_sync(0xffffffffu, wait_parity(bar, phase & 1)) != 0; };
+  auto wait = [&](uint32_t bar, int phase) {
+    const bool there = __all_sync(0xffffffffu, wait_parity(bar, phase & 1, sbase + G::kOffMisc + 4));
+    if (!there) *gave_up = kSpinLimit;
+    return there;
+  };
 
   if (warp >= kConvertWarp) {
     // ============================ queries, V to fp16 ============================
