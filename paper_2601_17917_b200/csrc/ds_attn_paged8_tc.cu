@@ -10,8 +10,8 @@
 //
 // Two streams of 128 tile rows each, with a warpgroup, S and O of their own, keep the tensor pipe and the exponentials busy at once:
 //   kPair      rows 0 .. 127 and 128 .. 255 of an item, over the same key tiles
-//   otherwise  the same rows, the even and the odd key tiles, joined when the item ends.  Up to 64 rows stand in the tile kCopies
-//              times: each copy weighs 1 / kCopies of the keys and has zeros for the others.
+//   otherwise  the same rows, the even and the odd key tiles, joined when the item ends.  Up to 64 rows stand in the tile twice (kCopies):
+//              each copy weighs half of the keys and has zeros for the others.
 // Step u of a piece is stream u % 2, key tile u (kPair: u / 2).  A stream's products go out in the order QK0 PV0 QK2 PV2 ..; S is written
 // again when the product that reads the P in its place is done (waited for: products of different kinds and shapes need not execute in the
 // order of their issue; 82.5 -> 83.4 us).  The second stream starts half a step later (82 -> 80 us): its exponentials run beside the first
@@ -839,7 +839,7 @@ size_t workspace_of(const Shape &h) { return h.tiles <= kWholeTiles || h.grid ==
 long long rows_per_head(const ds_paged_params &p) { return (long long)p.max_q * (p.Hq / p.Hkv); }
 int tile_rows(const ds_paged_params &p) {
   const long long rows = rows_per_head(p);
-  return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
+  return rows <= 64 ? 64 : rows <= 128 ? 128 : 256;      // (fewer than 33 are the other kernel's)
 }
 Shape shape_for(const ds_paged_params &p) {
   const int rows = tile_rows(p);
@@ -861,7 +861,6 @@ int launch(const ds_paged8_params &p, cudaStream_t stream) {
 template <int D>
 int launch_rows_of(const ds_paged8_params &p, cudaStream_t stream) {
   switch (tile_rows(p.a)) {
-    case 32: return launch<D, false, 4>(p, stream);
     case 64: return launch<D, false, 2>(p, stream);
     case 128: return launch<D, false, 1>(p, stream);
     default: return launch<D, true, 1>(p, stream);

@@ -81,13 +81,10 @@ def test_a_large_value_of_small_weight_does_not_take_the_others_bits(path):
     assert (err <= tol).all(), (err - tol).max()
 
 
-@every_path
-@pytest.mark.parametrize("below", [16, 24, 38])
+@pytest.mark.parametrize("path,below", [(p, b) for p in PATHS for b in ((16, 24) if PATHS[p][0] == BF else (16, 24, 38))])
 def test_scales_far_below_the_largest(path, below):
     """In the upper half of the dimensions one row alone has values, under a scale of V 2^-below times the others'; weights near 1 / n."""
     bf = PATHS[path][0] == BF
-    if bf and below > 24:
-        pytest.skip("a bf16 output's weights end at 2^-28")
     c = tokens(path, 6, 1, sharp=0.02)
     D, rows, n = c.D, c.counts[0], c.lens[0]
     t = torch.arange(n)
@@ -244,3 +241,10 @@ def test_items_of_many_rows_and_of_few_behind_each_other(D, Hq, most, workspace)
     for _ in range(5):
         again, lse2, _ = c.run(workspace=ws)
         assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
+# ------------------------------------------------------------------------------------------------ long prompts
+@pytest.mark.parametrize("dtype,D,Hq,Hkv", [(BF, 128, 2, 2), (BF, 64, 4, 1), (F32, 64, 2, 1)])
+@pytest.mark.parametrize("kw", [dict(), dict(causal=False), dict(window=150, sinks=5)])
+def test_prompts_of_hundreds_of_rows(dtype, D, Hq, Hkv, kw):
+    Case8([700, 513, 1000], [700, 513, 300], Hq, Hkv, D, 16, 16, dtype, seed=D).check(**kw)
