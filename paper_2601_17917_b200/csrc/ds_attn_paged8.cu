@@ -11,10 +11,10 @@
 //
 // Queries enter as fp16 too: a row is scaled by a power of two that puts its largest element into [2^14, 2^15), and 11 bits hold bf16's 8
 // down to 2^-31 of that.  fp32 queries are two such parts (22 bits).  The scale of K and the row's factor multiply the score, the scale of V
-// the weight, with a power of two for each row (Weights8): the largest weight that the row sees stands at 2^5 .. 2^14, which keeps 11 bits down
-// to 2^-19 of it and drops what is below 2^-30: a weight's rounding, 2^-11, is an eighth of the output's in bf16.  For fp32 outputs it stands
-// at 2^9 .. 2^14 and the weights are two such parts, the second times 2^11 against V 2^-11: fp16's smallest steps would otherwise end it
-// at 2^-12 of the largest.  22 bits down to 2^-23 of the largest, nothing below 2^-45.
+// the weight, with a power of two for each row (Weights8): the largest weight that the row sees stands at 2^6 .. 2^15, which keeps 11 bits down
+// to 2^-20 of it and drops what is below 2^-31: a weight's rounding, 2^-11, is an eighth of the output's in bf16.  For fp32 outputs it stands
+// at 2^10 .. 2^15 and the weights are two such parts, the second times 2^11 against V 2^-11: fp16's smallest steps would otherwise end it
+// at 2^-12 of the largest.  22 bits down to 2^-24 of the largest, nothing below 2^-46.
 //
 // Measured: 32 x 32 heads at length, 1.08 GB, 183 - 186 us (5.9 TB/s, nine tenths of a plain copy; 188 with V transposed in pairs and
 // permuted); the issue slots are half in use, a third of them for conversions.  8 x 32 heads of 32 rows x 1024 .. 2080 keys 66 us, which is the
@@ -263,7 +263,7 @@ struct ByteRows {
             }
         }
     }
-    // The references move only when a weight would pass 2^14 (the result is the same): no maximum is exchanged until some lane finds
+    // The references move only when a weight would pass 2^kTop (the result is the same): no maximum is exchanged until some lane finds
     // such a score, or that its largest score with the largest scale of its keys might be one.
     bool over = false, heavy = false;
     float top[NB][2];

@@ -235,10 +235,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
                  bar_meet = bar_q_free + 8, bar_joined = bar_meet + 8, bar_begun = bar_joined + 8;
   volatile uint32_t *tmem_s = reinterpret_cast<volatile uint32_t *>(smem + G::kOffMisc), *gave_up = tmem_s + 1;
   volatile int *v_nan = reinterpret_cast<volatile int *>(smem + G::kOffMisc + 8);      // the last piece, from 1 on, in which kOffNan has something
-  // of the largest finite scale of V of a tile, its biased exponent, rounded up; kMixed: not every row sees every key, or some scale is
-  // below a quarter of that
+  // of the largest finite scale of V of a tile, its biased exponent, rounded up; of the smallest, rounded down, times 256; kPartial: not every
+  // row sees every key; kMixed: that, or some scale is below an eighth of the largest
   volatile uint32_t *vsize_s = reinterpret_cast<volatile uint32_t *>(smem + G::kOffMisc + 12);
-  constexpr uint32_t kMixed = 256;
+  constexpr uint32_t kPartial = 1u << 16, kMixed = 1u << 17;
+  constexpr float kShort = 3.f;      // the largest weight of a row is not to stand below 2^kShort
   float *scale_s = reinterpret_cast<float *>(smem + G::kOffScale);
   float *factor_s = reinterpret_cast<float *>(smem + G::kOffFactor);
 
@@ -345,21 +346,23 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
         if (cw == 0) {
           // the scales as the products take them, and how large V's are
           float *vs = scale_s + (t % kScaleRing) * 384 + 128 + lane;
-          uint32_t most = 0, least = ~0u;
+          const bool partial = !paged_all_visible(a.s, it.q, (walk.tile0 + i) * kKeys, kKeys);
+          uint32_t most = 0, least = 0x7fffffffu;
           float size[4];
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
             const float v = vs[32 * c];
             const uint32_t b = __float_as_uint(v) & 0x7fffffffu;
-            most = max(most, b < 0x7f800000u ? b : 0u), least = min(least, b);
+            most = max(most, b < 0x7f800000u ? b : 0u);
+            if (!partial || paged_key(it.q, (walk.tile0 + i) * kKeys + 32 * c + lane) >= 0) least = min(least, b);
             size[c] = v;
             vs[32 * c] = v * kUnbiased, vs[32 * c - 128] *= 0x1p-24f;      // a product of queries and K is below 2^24
           }
           most = (__reduce_max_sync(0xffffffffu, most) + 0x7fffffu) >> 23, least = __reduce_min_sync(0xffffffffu, least) >> 23;
-          const bool mixed = least + 2 < most || !paged_all_visible(a.s, it.q, (walk.tile0 + i) * kKeys, kKeys);
+          const bool mixed = least + 3 < most || partial;
           if (mixed)
             for (int c = 0; c < 4; ++c) vs[32 * c + 128] = log_scale(size[c]);
-          if (lane == 0) vsize_s[t % kScaleRing] = most | (mixed ? kMixed : 0u);
+          if (lane == 0) vsize_s[t % kScaleRing] = most | least << 8 | (partial ? kPartial : 0u) | (mixed ? kMixed : 0u);
           __syncwarp();
           if (lane == 0) mbar_arrive(bar_sc_ready + 8 * (t % kScaleRing));
         }
@@ -616,17 +619,28 @@ __global__ void __launch_bounds__(kThreads, 1) attn_paged8_tc_kernel(const __gri
           top = fmaxf(top, top1);
           // The references of the row's scores and weights move only when one would pass its limit, and O with them: rarely.
           const uint32_t size = vsize_s[t % kScaleRing];
-          const float now = mine && (m == -INFINITY ? top > m : (top - m) * steep > W::kLag) ? top : m;
-          const float moved = now == m ? e : e + (now - m) * steep, start = fminf(moved, W::kMost);
+          const float v_most = (float)((int)(size & 255u) - 127), v_least = (float)((int)(size >> 8 & 255u) - 127);
+          const bool first = m == -INFINITY;
+          const float rise = (top - m) * steep;
+          // the reference of the scores moves with the largest weight, too, where that is the row's own whatever the key
+          const float now = mine && (first ? top > m : rise > W::kLag || (!(size & kPartial) && rise > 0.f && rise + (e + v_most) > W::kTop)) ? top : m;
+          const float start = first ? W::kMost : e;
           // the largest weight: at most this, with the tile's largest scale, whoever sees it
-          float most = mine ? (top - now) * steep + (start + (float)((int)(size & 255u) - 127)) : -INFINITY;
+          float most = mine ? (top - now) * steep + (start + v_most) : -INFINITY;
           const bool over = now != m || most > W::kTop;
           if (__any_sync(0xffffffffu, over)) {
-            // Where that is too much, and the tile is mixed, the row's own keys are gone through.
-            if ((size & kMixed) && __any_sync(0xffffffffu, most > W::kLog2)) most = start + heaviest(ts, ks, key0, kMine, seen, now, steep);
-            const float fresh = exponent_of_weights<W>(start, most, now != m);
-            if (now != m) l *= m == -INFINITY ? 0.f : ex2_approx((m - now) * steep);
-            const float keep = ex2_approx(fresh - moved);
+            // Where that and the smallest scale do not settle it, and the tile is mixed, the row's own keys are gone through.
+            const bool settled = !(most > W::kTop) && (now == m || (!first && e + v_least >= kShort));
+            if ((size & kMixed) && __any_sync(0xffffffffu, !settled)) {
+              const float exact = start + heaviest(ts, ks, key0, kMine, seen, now, steep);
+              if (!settled) most = exact;
+            }
+            const float fall = now == m ? 0.f : first ? -INFINITY : (m - now) * steep;      // of sums under an unchanged e
+            float fresh = e;
+            if (most > W::kTop || (now != m && (first || most < kShort)))
+              fresh = fmaxf(floorf(fminf(start + (W::kLog2 - most), fminf(e - fall, W::kMost))), W::kLeast);
+            if (now != m) l *= ex2_approx(fall);
+            const float keep = ex2_approx(fall + (fresh - e));
             m = now, e = fresh;
             if (done > 0 && __any_sync(0xffffffffu, keep != 1.f)) {
               ok = wait(bar_pv_done + 8 * s, n - 1);

@@ -20,7 +20,7 @@ struct Args8 : Params {
 // finite vs passes 2^kTop with.
 template <bool kBf16>
 struct Weights8 {
-  static constexpr float kLog2 = kBf16 ? 6.f : 10.f, kTop = 14.f, kLag = kTop - kLog2;
+  static constexpr float kLog2 = kBf16 ? 7.f : 11.f, kTop = 15.f, kLag = kTop - kLog2;
   static constexpr float kMost = 102.f, kLeast = -126.f;
   static constexpr int kBias = 16;
 };

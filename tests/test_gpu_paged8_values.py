@@ -1,7 +1,7 @@
 """The 8-bit paged cache where values lie far apart or next to a border of the type.
 
 Scales of V: a weight enters its product as a 16-bit float, relative to the largest weight times scale that the query itself sees, which
-stands at 2^3 .. 2^14 (fp32 outputs 2^9 .. 2^14, two parts, the second times 2^11).  So a term is off by half a step, 2^-11 (2^-22) of
+stands at 2^3 .. 2^15 (fp32 outputs 2^9 .. 2^15, two parts, the second times 2^11).  So a term is off by half a step, 2^-11 (2^-22) of
 itself, or by 2^-25 of those units (2^-36), 2^-28 (2^-45) of the largest, where it is too small for that."""
 import copy
 import math
