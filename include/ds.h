@@ -700,6 +700,7 @@ DS_API int ds_kv8_read(const ds_kv8_read_params *p, void *stream);
  * A query with an infinity or NaN in it has NaN for output.  V enters relative to the largest weight times |scale of V| among the rows that the
  * query sees: a value counts with all bits while its own is at least 2^-17 (DS_F32: 2^-23) of that, and not at all below 2^-28 (2^-45);
  * scales of V below 2^-96, scales of K below 2^-102, queries below 2^-85 and outputs below 2^-117 times the bound of the lengths lose bits.
+ * A query's elements times |scale| are to stay below 2^108, and below 2^140 over the scales of K: scores beyond that are not defined.
  * In addition DS_ERR_INVALID_ARG: page_size not a multiple of scale_block, scale_block < 1, a NULL or misaligned scale pointer, a
  * negative scale stride; DS_ERR_UNSUPPORTED: scale_block > 65536. */
 typedef struct {

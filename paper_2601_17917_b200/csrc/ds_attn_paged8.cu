@@ -16,10 +16,10 @@
 // at 2^10 .. 2^15 and the weights are two such parts, the second times 2^11 against V 2^-11: fp16's smallest steps would otherwise end it
 // at 2^-12 of the largest.  22 bits down to 2^-24 of the largest, nothing below 2^-46.
 //
-// Measured: 32 x 32 heads at length, 1.08 GB, 183 - 186 us (5.9 TB/s, nine tenths of a plain copy; 188 with V transposed in pairs and
-// permuted); the issue slots are half in use, a third of them for conversions.  8 x 32 heads of 32 rows x 1024 .. 2080 keys 66 us, which is the
-// chain score -> weight -> product in eight warps an SM (issue slots 36 %, tensor pipe 25 %); equal ranges 75, 16 rows to an item with 12 warps
-// 65, tcgen05 tiles, three quarters empty, 68.  Products of e4m3 (m16n8k32) for the scores, twice the rate, need two of them for the
+// Measured: 32 x 32 heads at length, 1.08 GB, 176 - 189 us by box (5.7 to 6.2 TB/s, nine tenths of a plain copy; 2 us more with V transposed
+// in pairs and permuted); the issue slots are half in use, a third of them for conversions.  8 x 32 heads of 32 rows x 1024 .. 2080 keys 66 us, which is the
+// chain score -> weight -> product in eight warps an SM (issue slots 40 %, tensor pipe 24 %); equal ranges, 16 rows to an item with 12 warps and
+// tcgen05 tiles, three quarters empty, were slower (75, 65 and 68 when this took 61).  Products of e4m3 (m16n8k32) for the scores, twice the rate, need two of them for the
 // queries' bits and as many conversions of V: 189 -> 206 us.
 #include <type_traits>
 
@@ -409,12 +409,12 @@ auto with_rows_at_length(const ds_paged_params &p, F f) {
   return with_rows(p, f);
 }
 
-// Rows per KV head from which the kernel with tcgen05 tiles takes over (27 rows: 61 against 68 us; 40: 119 against 84, both 8 x 32 heads
+// Rows per KV head from which the kernel with tcgen05 tiles takes over (27 rows: 70 against 90 us; 40: 127 against 93, both 8 x 32 heads
 // x 2000 keys).
 constexpr int kTensorTileRows = 33;
 bool many_rows(const ds_paged_params &p) { return p.dtype == DS_BF16 && (long long)p.max_q * (p.Hq / p.Hkv) >= kTensorTileRows; }
 // But not for a few short items, which the clusters of the other are done with before a CTA of 200 KB is under way (4 KV heads of 224
-// rows x 1000 keys: 18 against 25 us; at four tiles of 128 keys to a CTA the two are level).
+// rows x 1000 keys: 23 against 33 us; at four tiles of 128 keys to a CTA the two are level).
 bool wide(const ds_paged_params &p) {
   if (!many_rows(p)) return false;
   using T = __nv_bfloat16;

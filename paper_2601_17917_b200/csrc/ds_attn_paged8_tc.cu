@@ -24,13 +24,14 @@
 //          table says, and the scales
 //   12-15  at the start of a piece the queries, four threads a row; then V to fp16, 32 keys each
 // (One set of four warps that loaded and converted took 5500 cycles a tile, most of them in its own instructions: 120 us where this
-// takes 80.)
+// took 80.)
 //
 // A key tile's 32 KB are 1430 cycles of an SM's share of HBM; its products 256 (e4m3, two parts) + 256 cycles and its exponentials 1024, for 128
-// rows.  Measured, 16 sequences x 4 heads of 224 rows x 1500 .. 4128 keys: 80 us, where the bf16 cache takes 73; a step of a stream takes
-// 4800 cycles, 1300 for the maximum, 3100 for the weights of 128 keys, which is the latency of TMEM loads and exponentials with two softmax
-// warps a scheduler (issue slots 36 % in use, tensor pipe 17 %, exponentials 16 %).  Tried and not kept: scores held in
-// registers between the two passes and register splits between the roles (no faster), TMEM loads a step ahead (80.3 against 79.9 us).
+// rows.  Measured, 16 sequences x 4 heads of 224 rows x 1500 .. 4128 keys: 84 us, where the bf16 cache takes 73 (91 with scales for every
+// token); a step of a stream takes some 5000 cycles, a quarter of them for the maximum, the most for the weights of 128 keys, which is the
+// latency of TMEM loads and exponentials with two softmax warps a scheduler (issue slots 32 % in use, tensor pipe 13 %, exponentials 12 % in a
+// small case).  Tried and not kept: scores held in registers between the two passes and register splits between the roles (no faster), TMEM
+// loads a step ahead (80.3 against 79.9 us).
 //
 // Every wait is bounded; on expiry the kernel raises DS_DEV_TIMEOUT, drains and frees TMEM.
 #include <type_traits>
