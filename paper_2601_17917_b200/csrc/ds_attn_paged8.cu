@@ -143,7 +143,7 @@ struct ByteRows {
   __device__ __forceinline__ float2 factors(int nb) const {
     if constexpr (kQRegs) return make_float2(factor[nb][0], factor[nb][1]);
     float2 f;
-    asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(f.x), "=f"(f.y) : "r"(q_smem + kOffFactor + (8 * nb + 2 * (threadIdx.x & 3)) * 4));
+    asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(f.x), "=f"(f.y) : "r"(q_smem + kOffFactor + (8 * nb + 2 * (threadIdx.x & 3)) * 4) : "memory");
     return f;
   }
 
